@@ -307,6 +307,106 @@ int sffn_lopa_m_step(const float* W, const float* P, int H, int D, int32_t* g_id
                      float* row_best, void* stream);
 int sffn_lopa_residual(const float* W, const int32_t* g_idx, const int8_t* g_sign, int H, int D, float* A, void* stream);
 
+/* ---- training -------------------------------------------------------------------------------------------------
+ * The same FFN with its gradients, and the optimiser step of its weights.  These calls take no handle: what a call
+ * needs is in its arguments, and the caller owns every buffer, the workspace too.  They are ordinary stream work:
+ * nothing is read before the work queued earlier on `stream` has finished (weights included, so a forward pass may
+ * follow the step that wrote them) -- but the inference calls above may start reading weights early, so put a stream
+ * or event synchronisation between sffn_adamw_step and the next sparse_ffn_forward on the same weights.
+ * `status` (device int32, zeroed by the caller once) receives SFFN_ERR_TIMEOUT if a bounded wait inside a kernel runs
+ * out; it is never cleared by the library.  Results are bitwise the same on every call with the same inputs.
+ *
+ * T tokens, x [T, D], weights as above (W_down transposed, [H, D]):
+ *     z = x W_g^T + b_g,   u = x W_up^T,   h = A(z) . A_3(u),   y = h W_down.
+ * A (`act`) and A_3 (`act_up`; SFFN_ACT_NONE = Eq. 1) may each be any entry of sffn_act here: a dense model before it
+ * is cast (Sec. 3.3) trains through the same call with SFFN_ACT_SILU.
+ * Gradients, from dy = dL/dy and the z and u that the forward call stored:
+ *     dh = dy W_down^T,  dz = dh . A_3(u) . A'(z),  du = dh . A(z) . A_3'(u),
+ *     dx = dz W_g + du W_up,  dW_g = dz^T x,  dW_up = du^T x,  dW_down = h^T dy,  db_g = sum_t dz_t
+ * with A'(z) = 0 for z <= 0 where A is RELU, SQRELU or RSPLUS (a neuron fires when z > 0).
+ *
+ * Types: x, dy, weights, y, z, u, dx and the weight gradients are all of `dtype`; b_g and db_g fp32.  With bf16 each
+ * product's operands are bf16 with fp32 sums; h, dz and du enter the products rounded to bf16 (one rounding, as the
+ * outputs have; db_g is summed before it).  With fp32 the large products take every operand as three bf16 terms
+ * (24 bits; six products), small ones run in fp32 FMAs.  Finite operands are assumed, as above; fp32 operands larger
+ * than 3.38e38 do not fit bf16 terms.
+ * Rows: D a multiple of 16 bytes; x, dy, y, dx [T, D] and z, u [T, H] have row strides `ld_*` in elements, a multiple
+ * of 16 bytes and at least the width; H may be any number (columns of z and u past H are neither read nor written).
+ * T = 0 is a call like any other: gradients of the weights come out as zeros. */
+typedef struct {
+  int32_t T, D, H;            /* tokens, model width, hidden width                                                */
+  int32_t dtype, act, act_up; /* sffn_dtype, sffn_act, sffn_act                                                   */
+  const void* x;              /* [T, D]                                                                           */
+  int64_t ld_x;
+  const void *W_g, *W_up, *W_down; /* [H, D]                                                                      */
+  const float* b_g;           /* [H] or NULL; only the forward call reads it                                      */
+  void *z, *u;                /* [T, H]: forward: written, or both NULL (nothing is saved); backward: read        */
+  int64_t ld_hidden;          /* of z and u                                                                       */
+  void* workspace;            /* 256-byte aligned                                                                 */
+  size_t workspace_bytes;
+  int32_t* status;
+} sffn_train_call;
+
+/* What a backward call writes; any of them may be NULL (not wanted), and its products are then left out. */
+typedef struct {
+  void* dx;                        /* [T, D] */
+  int64_t ld_dx;
+  void *dW_g, *dW_up, *dW_down;    /* [H, D] */
+  float* db_g;                     /* [H]    */
+} sffn_train_grads;
+
+/* Bytes of workspace of a forward (backward = 0) or backward (1) call. */
+int sffn_train_workspace_bytes(int T, int D, int H, int dtype, int backward, size_t* bytes);
+int gated_ffn_forward(const sffn_train_call* call, void* y, int64_t ld_y, void* stream);
+int gated_ffn_backward(const sffn_train_call* call, const void* dy, int64_t ld_dy, const sffn_train_grads* grads,
+                       void* stream);
+
+/* norm = sqrt(sum of g^2 over all entries of n tensors), one fp32 word on the device.  Squares are summed in fp32
+ * within a thread (an entry beyond 1.8e19 gives infinity) and in fp64 beyond.  `workspace`: SFFN_GRAD_NORM_WORKSPACE
+ * bytes, 16-byte aligned, zeroed by the caller once and not shared by calls that may overlap; n is not limited. */
+#define SFFN_GRAD_NORM_WORKSPACE 16384
+typedef struct {
+  const void* data;
+  int64_t n;       /* entries, 0 or more */
+  int32_t dtype;   /* sffn_dtype */
+} sffn_tensor;
+int sffn_grad_norm(const sffn_tensor* tensors, int n, float* norm, void* workspace, size_t workspace_bytes, void* stream);
+
+/* One AdamW step over n tensors, in place:
+ *     g' = g min(1, max_norm / (grad_norm + 1e-6))                     (grad_norm given; else g' = g)
+ *     m = beta1 m + (1 - beta1) g',   v = beta2 v + (1 - beta2) g'^2
+ *     p = p (1 - lr weight_decay) - lr / (1 - beta1^step) m / (sqrt(v / (1 - beta2^step)) + eps)
+ * in fp32.  grad_norm is a device word, as sffn_grad_norm leaves it; where it is not finite the whole step is left out
+ * (parameters and moments keep their bits), without the host having to look.
+ * p: fp32 or bf16; g: fp32 or bf16; master (bf16 p only, or NULL): fp32 copy of p that takes the step, p = bf16(master).
+ * Moments with state_bits 32: m, v fp32.  With state_bits 8: m int8, v uint8 codes and one fp32 scale of each for every
+ * 256 consecutive entries (the last group may be shorter; ceil(n / 256) scales),
+ *     m = m_scale sign(c) (c / 127)^2,  v = v_scale (c / 255)^4,
+ * the scale being the group's largest |m| (v), the code the nearest one in (|m| / scale)^(1/2), (v / scale)^(1/4), up on a tie;
+ * a v that is not zero keeps a code of at least 1, as it divides m; a group whose largest value is below 2^-100 is
+ * stored as zeros.  Pointers need the alignment of their type only; 16 bytes are faster. */
+typedef struct {
+  void* p;
+  const void* g;
+  float* master;
+  void *m, *v;
+  float *m_scale, *v_scale;   /* state_bits 8 */
+  int64_t n;
+  int32_t p_dtype, g_dtype, state_bits;
+  double lr, weight_decay;
+} sffn_adamw_tensor;
+typedef struct {
+  double beta1, beta2, eps;
+  int64_t step;              /* 1, 2, ... : the number of this step */
+  const float* grad_norm;    /* device, or NULL */
+  double max_norm;           /* read where grad_norm is given; infinity: no clipping, only the test for finite */
+} sffn_adamw_config;
+int sffn_adamw_step(const sffn_adamw_tensor* tensors, int n, const sffn_adamw_config* config, void* stream);
+
+/* The values that the 8-bit moments of n tensors stand for, as fp32: m_out[i], v_out[i] (device, entries as tensors[i].n;
+ * either array of pointers may be NULL). */
+int sffn_adamw_state_values(const sffn_adamw_tensor* tensors, int n, float* const* m_out, float* const* v_out, void* stream);
+
 /* Static string for a status code. */
 const char* sffn_status_string(int status);
 

@@ -16,3 +16,13 @@ from .binding import (  # noqa: F401
     test_set_knob,
 )
 from .lopa import g_diagonal, g_tiled, touched_bytes, dense_bytes, lopa_approximation  # noqa: F401
+from .training import (  # noqa: F401
+    GatedFFNFunction,
+    adamw_state,
+    adamw_state_values,
+    adamw_step,
+    gated_ffn_backward,
+    gated_ffn_forward,
+    grad_norm,
+    training_status,
+)

@@ -289,6 +289,7 @@ int check_call(const sffn_handle* h, const void* x, int B, const sffn_gate* g, c
 // The CUDA error behind the calling thread's last SFFN_ERR_CUDA (sffn_last_cuda_error).
 thread_local cudaError_t g_last_cuda_error = cudaSuccess;
 thread_local int g_last_cuda_line = 0;
+thread_local const char* g_last_cuda_file = "api.cu";
 
 #define SFFN_CUDA(expr)               \
   do {                                \
@@ -296,6 +297,7 @@ thread_local int g_last_cuda_line = 0;
     if (e_ != cudaSuccess) {          \
       g_last_cuda_error = e_;         \
       g_last_cuda_line = __LINE__;    \
+      g_last_cuda_file = "api.cu";    \
       return SFFN_ERR_CUDA;           \
     }                                 \
   } while (0)
@@ -765,11 +767,20 @@ const void* mapped_device_pointer(const void* host) {
 
 }  // namespace
 
+namespace sffn {
+// The same for calls that live in another source file.
+void note_cuda_error(cudaError_t e, const char* file, int line) {
+  g_last_cuda_error = e;
+  g_last_cuda_file = file;
+  g_last_cuda_line = line;
+}
+}  // namespace sffn
+
 extern "C" {
 
 const char* sffn_last_cuda_error(void) {
   static thread_local char text[96];
-  snprintf(text, sizeof(text), "%s (api.cu:%d)", cudaGetErrorName(g_last_cuda_error), g_last_cuda_line);
+  snprintf(text, sizeof(text), "%s (%s:%d)", cudaGetErrorName(g_last_cuda_error), g_last_cuda_file, g_last_cuda_line);
   return g_last_cuda_error == cudaSuccess ? "cudaSuccess" : text;
 }
 
