@@ -20,6 +20,7 @@ namespace {
     }                                                     \
   } while (0)
 
+constexpr double kSplitProducts = 1e9;  // T D H
 constexpr int kMaxRows = 1 << 22;  // tokens, and neurons: the kernels' grids and tensor maps have room for so many
 
 inline bool aligned(const void* p, uintptr_t a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) == 0; }
@@ -36,8 +37,16 @@ int sm_count(int* n) {
   return SFFN_OK;
 }
 
+// Which kernels serve a call: tensor cores for bf16, and for fp32 from the size on at which splitting every operand into three
+// terms and multiplying them six times is faster than fp32 FMAs.
+bool on_tensor_cores(int T, int D, int H, int dtype) { return dtype == SFFN_BF16 || (double)T * D * H >= kSplitProducts; }
+
 struct TrainLayout {
-  size_t h, dz, du, db, total;
+  bool umma, split;         // split: operands in three bf16 terms
+  int64_t ld_h, ld_d;       // rows of hidden values, and of the terms of D-wide operands
+  int64_t limb_h, limb_t, limb_w;  // elements between the terms of hidden values, of x and dy, of a weight
+  size_t counters, partial, h, dz, du, db, x, dy, w[3], total;
+  int lines;
 };
 TrainLayout train_layout(int T, int D, int H, int dtype, bool backward) {
   TrainLayout L{};
@@ -47,16 +56,71 @@ TrainLayout train_layout(int T, int D, int H, int dtype, bool backward) {
     off += up256(bytes);
     return o;
   };
-  const size_t hidden = (size_t)T * hidden_ld(H) * element(dtype);
+  L.umma = on_tensor_cores(T, D, H, dtype);
+  L.split = L.umma && dtype == SFFN_F32;
+  L.ld_h = hidden_ld(H);
+  L.ld_d = hidden_ld(D);
+  L.limb_h = T * L.ld_h;
+  L.limb_t = T * L.ld_d;
+  L.limb_w = H * L.ld_d;
+  if (L.umma) {
+    L.counters = take(sffn::kTrainCounterBytes);
+    L.partial = take(sffn::kTrainPartialBytes);
+  }
+  const size_t hidden = (size_t)T * L.ld_h * (L.split ? 6 : element(dtype));
   L.h = take(hidden);
+  L.lines = L.umma ? sffn::train_umma_lines(T) : sffn::train_simt_lines(T);
   if (backward) {
     L.dz = take(hidden);
     L.du = take(hidden);
-    L.db = take((size_t)sffn::train_simt_lines(T) * hidden_ld(H) * 4);
+    L.db = take((size_t)L.lines * L.ld_h * 4);
+  }
+  if (L.split) {
+    L.x = take((size_t)L.limb_t * 6);
+    if (backward) L.dy = take((size_t)L.limb_t * 6);
+    for (size_t& w : L.w) w = take((size_t)L.limb_w * 6);
   }
   L.total = off > 256 ? off : 256;
   return L;
 }
+
+// The products of one call, on the kernels that serve it.
+struct Products {
+  const sffn_train_call* c;
+  TrainLayout L;
+  char* ws;
+  cudaStream_t s;
+
+  Products(const sffn_train_call* call, bool backward, cudaStream_t stream) : c(call), s(stream) {
+    L = train_layout(c->T, c->D, c->H, c->dtype, backward);
+    ws = static_cast<char*>(c->workspace);
+  }
+  void* hidden(size_t at) const { return ws + at; }
+  cudaError_t begin() const { return L.umma ? cudaMemsetAsync(ws + L.counters, 0, sffn::kTrainCounterBytes, s) : cudaSuccess; }
+  // An operand as the products take it: itself, or its terms, which `at` receives.
+  cudaError_t split(const void* in, int64_t ld, int rows, size_t at, int64_t limb) const {
+    if (!L.split) return cudaSuccess;
+    return sffn::launch_train_split(static_cast<const float*>(in), ld, rows, c->D, reinterpret_cast<__nv_bfloat16*>(ws + at), L.ld_d, limb, s);
+  }
+  sffn::TrainOperand operand(const void* in, int64_t ld, size_t at) const {
+    return L.split ? sffn::TrainOperand{ws + at, L.ld_d} : sffn::TrainOperand{in, ld};
+  }
+  cudaError_t run(sffn::TrainGemm& g, const int64_t* limb_a, const int64_t* limb_b) const {
+    g.epi.limb = L.limb_h;
+    if (!L.umma) return sffn::launch_train_simt(g, c->dtype, s);
+    sffn::TrainUmma t{};
+    t.g = g;
+    t.f32 = L.split;
+    for (int i = 0; i < 3; ++i) {
+      t.limb_a[i] = limb_a[i];
+      t.limb_b[i] = limb_b[i];
+    }
+    t.partial = reinterpret_cast<float*>(ws + L.partial);
+    t.counters = reinterpret_cast<uint32_t*>(ws + L.counters);
+    t.status = c->status;
+    return sffn::launch_train_umma(t, s);
+  }
+};
 
 int check_shape(int T, int D, int H, int dtype) {
   if (T < 0 || D <= 0 || H <= 0 || !storage_type(dtype)) return SFFN_ERR_INVALID_ARG;
@@ -113,35 +177,39 @@ int gated_ffn_forward(const sffn_train_call* c, void* y, int64_t ld_y, void* str
   if (!y) return SFFN_ERR_INVALID_ARG;
   rc = check_rows(y, ld_y, c->D, element(c->dtype));
   if (rc != SFFN_OK) return rc;
-  const cudaStream_t s = static_cast<cudaStream_t>(stream);
-  char* ws = static_cast<char*>(c->workspace);
-  const TrainLayout L = train_layout(c->T, c->D, c->H, c->dtype, false);
-  const int64_t ld_h = hidden_ld(c->H);
+  const Products p(c, false, static_cast<cudaStream_t>(stream));
+  const TrainLayout& L = p.L;
+  const int64_t tokens[3] = {L.limb_t, L.limb_t, L.limb_t}, weights[3] = {L.limb_w, L.limb_w, L.limb_w}, hidden[3] = {L.limb_h, L.limb_h, L.limb_h};
+  SFFN_CUDA(p.begin());
+  SFFN_CUDA(p.split(c->x, c->ld_x, c->T, L.x, L.limb_t));
+  SFFN_CUDA(p.split(c->W_g, c->D, c->H, L.w[0], L.limb_w));
+  SFFN_CUDA(p.split(c->W_up, c->D, c->H, L.w[1], L.limb_w));
+  SFFN_CUDA(p.split(c->W_down, c->D, c->H, L.w[2], L.limb_w));
 
   sffn::TrainGemm up{};
   up.M = c->T; up.N = c->H; up.K = c->D;
   up.parts = 2; up.batch = 1;
-  up.a[0] = {c->x, c->ld_x};
-  up.b[0] = {c->W_g, c->D};
-  up.b[1] = {c->W_up, c->D};
+  up.a[0] = p.operand(c->x, c->ld_x, L.x);
+  up.b[0] = p.operand(c->W_g, c->D, L.w[0]);
+  up.b[1] = p.operand(c->W_up, c->D, L.w[1]);
   up.a_major_k = up.b_major_k = true;
   up.epilogue = sffn::kEpiGateUp;
   sffn::TrainEpilogue& e = up.epi;
   e.M = c->T; e.N = c->H; e.act = c->act; e.act_up = c->act_up;
   e.bias = c->b_g; e.z = c->z; e.u = c->u; e.ld_zu = c->ld_hidden;
-  e.h = ws + L.h; e.ld_h = ld_h;
-  SFFN_CUDA(sffn::launch_train_simt(up, c->dtype, s));
+  e.h = p.hidden(L.h); e.ld_h = L.ld_h;
+  SFFN_CUDA(p.run(up, tokens, weights));
 
   sffn::TrainGemm down{};
   down.M = c->T; down.N = c->D; down.K = c->H;
   down.parts = down.batch = 1;
-  down.a[0] = {ws + L.h, ld_h};
-  down.b[0] = {c->W_down, c->D};
+  down.a[0] = {p.hidden(L.h), L.ld_h};
+  down.b[0] = p.operand(c->W_down, c->D, L.w[2]);
   down.a_major_k = true; down.b_major_k = false;
   down.epilogue = sffn::kEpiStore;
   down.epi.M = c->T; down.epi.N = c->D;
   down.epi.out[0] = y; down.epi.ld_out = ld_y;
-  SFFN_CUDA(sffn::launch_train_simt(down, c->dtype, s));
+  SFFN_CUDA(p.run(down, hidden, weights));
   return SFFN_OK;
 }
 
@@ -166,57 +234,67 @@ int gated_ffn_backward(const sffn_train_call* c, const void* dy, int64_t ld_dy, 
     rc = check_rows(g->dx, g->ld_dx, c->D, esz);
     if (rc != SFFN_OK) return rc;
   }
-  char* ws = static_cast<char*>(c->workspace);
-  const TrainLayout L = train_layout(c->T, c->D, c->H, c->dtype, true);
-  const int64_t ld_h = hidden_ld(c->H);
-  void* const hidden[3] = {ws + L.dz, ws + L.du, ws + L.h};
-  float* const lines = reinterpret_cast<float*>(ws + L.db);
+  const Products p(c, true, s);
+  const TrainLayout& L = p.L;
+  const bool want_dz = g->dx || g->dW_g, want_du = g->dx || g->dW_up, want_dh = want_dz || want_du || g->db_g;
+  if (!want_dh && !g->dW_down) return SFFN_OK;
+  const int64_t tokens[3] = {L.limb_t, L.limb_t, L.limb_t}, weights[3] = {L.limb_w, L.limb_w, L.limb_w}, hidden[3] = {L.limb_h, L.limb_h, L.limb_h};
+  void* const values[3] = {p.hidden(L.dz), p.hidden(L.du), p.hidden(L.h)};
+  float* const lines = reinterpret_cast<float*>(p.ws + L.db);
+  SFFN_CUDA(p.begin());
+  SFFN_CUDA(p.split(dy, ld_dy, c->T, L.dy, L.limb_t));
+  SFFN_CUDA(p.split(c->W_down, c->D, c->H, L.w[2], L.limb_w));
+  if (g->dW_g || g->dW_up) SFFN_CUDA(p.split(c->x, c->ld_x, c->T, L.x, L.limb_t));
+  if (g->dx) {
+    SFFN_CUDA(p.split(c->W_g, c->D, c->H, L.w[0], L.limb_w));
+    SFFN_CUDA(p.split(c->W_up, c->D, c->H, L.w[1], L.limb_w));
+  }
 
   sffn::TrainGemm dh{};
   dh.M = c->T; dh.N = c->H; dh.K = c->D;
   dh.parts = dh.batch = 1;
-  dh.a[0] = {dy, ld_dy};
-  dh.b[0] = {c->W_down, c->D};
+  dh.a[0] = p.operand(dy, ld_dy, L.dy);
+  dh.b[0] = p.operand(c->W_down, c->D, L.w[2]);
   dh.a_major_k = dh.b_major_k = true;
   dh.epilogue = sffn::kEpiHidden;
   sffn::TrainEpilogue& e = dh.epi;
   e.M = c->T; e.N = c->H; e.act = c->act; e.act_up = c->act_up;
-  e.z = c->z; e.u = c->u; e.ld_zu = c->ld_hidden; e.ld_h = ld_h;
-  e.dz = g->dx || g->dW_g ? hidden[0] : nullptr;
-  e.du = g->dx || g->dW_up ? hidden[1] : nullptr;
-  e.h = g->dW_down ? hidden[2] : nullptr;
+  e.z = c->z; e.u = c->u; e.ld_zu = c->ld_hidden; e.ld_h = L.ld_h;
+  e.dz = want_dz ? values[0] : nullptr;
+  e.du = want_du ? values[1] : nullptr;
+  e.h = g->dW_down ? values[2] : nullptr;
   e.db = g->db_g ? lines : nullptr;
-  if (e.dz || e.du || e.h || e.db) SFFN_CUDA(sffn::launch_train_simt(dh, c->dtype, s));
-  if (g->db_g) SFFN_CUDA(sffn::launch_train_column_sums(lines, sffn::train_simt_lines(c->T), ld_h, c->H, g->db_g, s));
+  SFFN_CUDA(p.run(dh, tokens, weights));
+  if (g->db_g) SFFN_CUDA(sffn::launch_train_column_sums(lines, L.lines, L.ld_h, c->H, g->db_g, s));
 
   if (g->dx) {
     sffn::TrainGemm dx{};
     dx.M = c->T; dx.N = c->D; dx.K = c->H;
     dx.parts = 2; dx.batch = 1;
-    dx.a[0] = {hidden[0], ld_h};
-    dx.a[1] = {hidden[1], ld_h};
-    dx.b[0] = {c->W_g, c->D};
-    dx.b[1] = {c->W_up, c->D};
+    dx.a[0] = {values[0], L.ld_h};
+    dx.a[1] = {values[1], L.ld_h};
+    dx.b[0] = p.operand(c->W_g, c->D, L.w[0]);
+    dx.b[1] = p.operand(c->W_up, c->D, L.w[1]);
     dx.a_major_k = true; dx.b_major_k = false;
     dx.epilogue = sffn::kEpiStore;
     dx.epi.M = c->T; dx.epi.N = c->D;
     dx.epi.out[0] = g->dx; dx.epi.ld_out = g->ld_dx;
-    SFFN_CUDA(sffn::launch_train_simt(dx, c->dtype, s));
+    SFFN_CUDA(p.run(dx, hidden, weights));
   }
   sffn::TrainGemm dw{};
   dw.M = c->H; dw.N = c->D; dw.K = c->T;
   dw.parts = 1;
   for (int i = 0; i < 3; ++i) {
     if (!dW[i]) continue;
-    dw.a[dw.batch] = {hidden[i], ld_h};
-    dw.b[dw.batch] = i < 2 ? sffn::TrainOperand{c->x, c->ld_x} : sffn::TrainOperand{dy, ld_dy};
+    dw.a[dw.batch] = {values[i], L.ld_h};
+    dw.b[dw.batch] = i < 2 ? p.operand(c->x, c->ld_x, L.x) : p.operand(dy, ld_dy, L.dy);
     dw.epi.out[dw.batch++] = dW[i];
   }
   if (dw.batch == 0) return SFFN_OK;
   dw.a_major_k = dw.b_major_k = false;
   dw.epilogue = sffn::kEpiStore;
   dw.epi.M = c->H; dw.epi.N = c->D; dw.epi.ld_out = c->D;
-  SFFN_CUDA(sffn::launch_train_simt(dw, c->dtype, s));
+  SFFN_CUDA(p.run(dw, hidden, tokens));
   return SFFN_OK;
 }
 

@@ -34,6 +34,7 @@ struct TrainEpilogue {
   int64_t ld_zu;
   void *h, *dz, *du;       // workspace [M, ld_h], NULL where not wanted
   int64_t ld_h;
+  int64_t limb;            // tensor-core kernels, fp32 storage: h, dz, du are three bf16 matrices, so many elements apart
   float* db;               // [lines, ld_h] partial sums of dz, NULL where not wanted
 };
 
@@ -78,5 +79,24 @@ int train_simt_lines(int M);   // lines of partial sums that kHidden leaves in `
 cudaError_t launch_train_simt(const TrainGemm& g, int dtype, cudaStream_t s);
 // db_g[j] = sum over `lines` lines of partial sums, in order; 0 for no line.
 cudaError_t launch_train_column_sums(const float* partial, int lines, int64_t ld, int N, float* out, cudaStream_t s);
+
+// Tensor-core kernels (train_umma.cu).  Operands are bf16 matrices or, for fp32 storage, three bf16 matrices each (`limb`
+// elements apart) that add up to it; all on 16 bytes, rows a multiple of 16 bytes apart.
+struct TrainUmma {
+  TrainGemm g;
+  bool f32;                // storage type of the outputs, and three terms an operand
+  int64_t limb_a[3], limb_b[3];
+  float* partial;          // room for the pieces of tiles that several pairs of CTAs share (train_umma_partial_bytes)
+  uint32_t* counters;      // train_umma_counter_bytes of zeros; zeros again after the launch
+  int32_t* status;
+};
+constexpr int kTrainUmmaPairs = 80;    // pairs of CTAs at most
+constexpr size_t kTrainPieceBytes = 256 * 256 * 4;
+constexpr size_t kTrainPartialBytes = 2 * kTrainUmmaPairs * kTrainPieceBytes;
+constexpr size_t kTrainCounterBytes = kTrainUmmaPairs * 16 * 4;
+int train_umma_lines(int M);
+cudaError_t launch_train_umma(const TrainUmma& t, cudaStream_t s);
+// out[l][r][c], l = 0, 1, 2: the bf16 terms of in[r][c]; `ld_out` elements between rows, `limb` between terms.
+cudaError_t launch_train_split(const float* in, int64_t ld_in, int rows, int cols, __nv_bfloat16* out, int64_t ld_out, int64_t limb, cudaStream_t s);
 
 }  // namespace sffn
