@@ -226,6 +226,40 @@ struct Raw16 {
   }
 };
 
+// Activations of sixteen values, the choice made once: inside the loops it would be made, and its code be there, sixteen times.
+template <bool FAST>
+__device__ __forceinline__ void act16(int act, const float* t, float* v) {
+  if (act == kActNone) {
+#pragma unroll
+    for (int i = 0; i < 16; ++i) v[i] = t[i];
+  } else if (act == kActRelu) {
+#pragma unroll
+    for (int i = 0; i < 16; ++i) v[i] = train_act<FAST>(kActRelu, t[i]);
+  } else if (act == kActSqRelu) {
+#pragma unroll
+    for (int i = 0; i < 16; ++i) v[i] = train_act<FAST>(kActSqRelu, t[i]);
+  } else if (act == kActRsPlus) {
+#pragma unroll
+    for (int i = 0; i < 16; ++i) v[i] = train_act<FAST>(kActRsPlus, t[i]);
+  } else {
+#pragma unroll
+    for (int i = 0; i < 16; ++i) v[i] = train_act<FAST>(kActSilu, t[i]);
+  }
+}
+template <bool FAST, int ACT, typename Raw>
+__device__ __forceinline__ void slope16_of(const Raw& t, float* v, float* d) {
+#pragma unroll
+  for (int i = 0; i < 16; ++i) train_act_slope<FAST>(ACT, t.get(i), v[i], d[i]);
+}
+template <bool FAST, typename Raw>
+__device__ __forceinline__ void slope16(int act, const Raw& t, float* v, float* d) {
+  if (act == kActNone) slope16_of<FAST, kActNone>(t, v, d);
+  else if (act == kActRelu) slope16_of<FAST, kActRelu>(t, v, d);
+  else if (act == kActSqRelu) slope16_of<FAST, kActSqRelu>(t, v, d);
+  else if (act == kActRsPlus) slope16_of<FAST, kActRsPlus>(t, v, d);
+  else slope16_of<FAST, kActSilu>(t, v, d);
+}
+
 // Sums of sixteen columns over the lanes of a warp: lanes 2 i and 2 i + 1 get column i's (in halves of what is left, five
 // exchanges deep, sixteen shuffles).
 __device__ __forceinline__ float column_sum(float* v, int lane) {
@@ -365,7 +399,6 @@ __global__ void __launch_bounds__(kThreads, 1) train_umma_kernel(const __grid_co
     const bool wide_own = EPI != kEpiStore && (e.ld_h & 15) == 0;
     int b = 0, b_phase = 0;
     bool ok = true;
-    float acc[PROMOTE ? 16 * kChunks : 1];
     Walk walk(p, pairs, pair);
     Item it;
     while (ok && walk.step(p, it)) {
@@ -373,43 +406,47 @@ __global__ void __launch_bounds__(kThreads, 1) train_umma_kernel(const __grid_co
       const int m = at.m * kRows + rank * 128 + 32 * quad + lane;
       const int n0 = at.n * p.tile_cols + (EPI == kEpiGateUp ? 64 : 128) * half;  // first output column of this warp
       const bool row = m < e.M;
+      // This item's sums, in tensor memory: as the MMAs left them, or added up over the runs and put back where the last run was.
       uint32_t tacc = 0;
       if constexpr (PROMOTE) {
-        for (int u = it.u0; u < it.u1; u = min(it.u1, u + p.run_units)) {
+        float acc[16 * kChunks];
+        for (int u = it.u0; u < it.u1;) {
+          const int end = min(it.u1, u + p.run_units);
           ok = __all_sync(0xffffffffu, mbar_wait(acc_full + 8 * b, b_phase, abort_flag, p.status, p.budget));
           if (!ok) break;
           fence_after();
+          tacc = tmem + lanes + b * kCols;
           const bool first = u == it.u0;
 #pragma unroll
           for (int c = 0; c < kChunks; ++c) {
             float v[16];
-            tmem_ld16(tmem + lanes + b * kCols + column(c), v);
+            tmem_ld16(tacc + column(c), v);
             tmem_arrived(v);
 #pragma unroll
             for (int i = 0; i < 16; ++i) acc[16 * c + i] = first ? v[i] : acc[16 * c + i] + v[i];
           }
-          fence_before();
-          __syncwarp();
-          if (lane == 0) mbar_arrive_cluster(empty0 + 8 * b);
-          b ^= 1;
-          if (b == 0) b_phase ^= 1;
+          u = end;
+          if (u < it.u1) {
+            fence_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive_cluster(empty0 + 8 * b);
+            b ^= 1;
+            if (b == 0) b_phase ^= 1;
+          }
         }
         if (!ok) break;
+#pragma unroll
+        for (int c = 0; c < kChunks; ++c) tmem_st16(tacc + column(c), acc + 16 * c);
+        tmem_stored();
       } else {
         ok = __all_sync(0xffffffffu, mbar_wait(acc_full + 8 * b, b_phase, abort_flag, p.status, p.budget));
         if (!ok) break;
         fence_after();
         tacc = tmem + lanes + b * kCols;
       }
-      // sixteen of this item's own sums
       auto own = [&](int c, float* v) {
-        if constexpr (PROMOTE) {
-#pragma unroll
-          for (int i = 0; i < 16; ++i) v[i] = acc[16 * c + i];
-        } else {
-          tmem_ld16(tacc + column(c), v);
-          tmem_arrived(v);
-        }
+        tmem_ld16(tacc + column(c), v);
+        tmem_arrived(v);
       };
       // A tile that several pairs share: this warp's part of it is 16 KB of every piece.
       int pieces = 1, mine = 0, first_pair = 0;
@@ -426,7 +463,7 @@ __global__ void __launch_bounds__(kThreads, 1) train_umma_kernel(const __grid_co
         mine = pair - first_pair;
         // a pair's first piece and its second (the one that begins its tile) have places of their own
         float4* out = reinterpret_cast<float4*>(p.partial + (size_t)(2 * pair + (it.u0 == 0 && walk.share(pair) < lo ? 1 : 0)) * (kTrainPieceBytes / 4) + region);
-#pragma unroll
+#pragma unroll 2
         for (int c = 0; c < kChunks; ++c) {
           float v[16];
           own(c, v);
@@ -453,6 +490,7 @@ __global__ void __launch_bounds__(kThreads, 1) train_umma_kernel(const __grid_co
 #pragma unroll
         for (int i = 0; i < 16; ++i) v[i] = 0.f;
         const long long lo = (long long)(it.tile - p.whole) * p.units;
+#pragma unroll 1
         for (int q = 0; q < pieces; ++q) {
           const int from = first_pair + q;
           const float4* in = reinterpret_cast<const float4*>(p.partial + (size_t)(2 * from + (q > 0 || walk.share(from) == lo ? 0 : 1)) * (kTrainPieceBytes / 4) + region);
@@ -467,7 +505,7 @@ __global__ void __launch_bounds__(kThreads, 1) train_umma_kernel(const __grid_co
         if constexpr (EPI == kEpiStore) {
           void* out = e.out[at.batch];
           const bool wide = wide_user && (reinterpret_cast<uintptr_t>(out) & 31) == 0;
-#pragma unroll
+#pragma unroll 2
           for (int c = 0; c < kOut; ++c) {
             const int n = n0 + 16 * c;
             float v[16];
@@ -475,7 +513,7 @@ __global__ void __launch_bounds__(kThreads, 1) train_umma_kernel(const __grid_co
             if (row && n < e.N) store16<F32>(out, m * e.ld_out + n, v, min(16, e.N - n), wide);
           }
         } else if constexpr (EPI == kEpiGateUp) {
-#pragma unroll
+#pragma unroll 1
           for (int c = 0; c < kOut; ++c) {
             const int n = n0 + 16 * c;
             float z[16], u[16];
@@ -492,8 +530,10 @@ __global__ void __launch_bounds__(kThreads, 1) train_umma_kernel(const __grid_co
                 store16<F32>(e.z, m * e.ld_zu + n, z, left, wide_user);
                 store16<F32>(e.u, m * e.ld_zu + n, u, left, wide_user);
               }
+              act16<!F32>(e.act, z, z);
+              act16<!F32>(e.act_up, u, u);
 #pragma unroll
-              for (int i = 0; i < 16; ++i) z[i] = train_act<!F32>(e.act, z[i]) * train_act<!F32>(e.act_up, u[i]);
+              for (int i = 0; i < 16; ++i) z[i] *= u[i];
               const int room = (int)min((int64_t)16, e.ld_h - n);
               if constexpr (F32) store16_limbs(e.h, m * e.ld_h + n, e.limb, z, room, wide_own);
               else store16<false>(e.h, m * e.ld_h + n, z, room, wide_own);
@@ -506,53 +546,48 @@ __global__ void __launch_bounds__(kThreads, 1) train_umma_kernel(const __grid_co
             rz.load(e.z, m * e.ld_zu + n, left, wide_user);
             ru.load(e.u, m * e.ld_zu + n, left, wide_user);
           };
+          auto store = [&](void* to, int64_t at_h, float* v, int room) {
+            if (!to || room <= 0) return;
+            if constexpr (F32) store16_limbs(to, at_h, e.limb, v, room, wide_own);
+            else store16<false>(to, at_h, v, room, wide_own);
+          };
           fetch(0);
-#pragma unroll
+#pragma unroll 1
           for (int c = 0; c < kOut; ++c) {
             const int n = n0 + 16 * c, room = row ? (int)min((int64_t)16, e.ld_h - n) : 0;
-            float dz[16], du[16], h[16];
-            sums(c, dz);
+            const int64_t at_h = m * e.ld_h + n;
+            float dh[16], a[16], da[16], bv[16], db[16];
+            slope16<!F32>(e.act, rz, a, da);
+            slope16<!F32>(e.act_up, ru, bv, db);
+            if (c + 1 < kOut) fetch(c + 1);
+            sums(c, dh);
 #pragma unroll
             for (int i = 0; i < 16; ++i) {
-              float a, da, bv, db;
-              train_act_slope<!F32>(e.act, rz.get(i), a, da);
-              train_act_slope<!F32>(e.act_up, ru.get(i), bv, db);
-              h[i] = a * bv;
-              du[i] = dz[i] * a * db;
-              dz[i] = dz[i] * bv * da;
+              db[i] *= dh[i] * a[i];   // du
+              da[i] *= dh[i] * bv[i];  // dz
+              a[i] *= bv[i];           // h
             }
-            if (c + 1 < kOut) fetch(c + 1);
-            if (room > 0) {
-              if constexpr (F32) {
-                if (e.h) store16_limbs(e.h, m * e.ld_h + n, e.limb, h, room, wide_own);
-                if (e.du) store16_limbs(e.du, m * e.ld_h + n, e.limb, du, room, wide_own);
-              } else {
-                if (e.h) store16<false>(e.h, m * e.ld_h + n, h, room, wide_own);
-                if (e.du) store16<false>(e.du, m * e.ld_h + n, du, room, wide_own);
-                if (e.dz) store16<false>(e.dz, m * e.ld_h + n, dz, room, wide_own);
-              }
-            }
-            if (F32 && e.dz && room > 0) {
-              float copy[16];
-#pragma unroll
-              for (int i = 0; i < 16; ++i) copy[i] = dz[i];
-              store16_limbs(e.dz, m * e.ld_h + n, e.limb, copy, room, wide_own);
-            }
+            store(e.h, at_h, a, room);
+            store(e.du, at_h, db, room);
+            float sum = 0.f;
             if (e.db) {
-              const float sum = column_sum(dz, lane);
+#pragma unroll
+              for (int i = 0; i < 16; ++i) dh[i] = da[i];
+              sum = column_sum(dh, lane);
+            }
+            store(e.dz, at_h, da, room);
+            if (e.db) {
               const int line = at.m * (kRows / 32) + rank * 4 + quad, n_of = n + (lane >> 1);
               if (!(lane & 1) && n_of < e.N && line * 32 < e.M) e.db[line * e.ld_h + n_of] = sum;
             }
           }
         }
       }
-      if constexpr (!PROMOTE) {
-        fence_before();
-        __syncwarp();
-        if (lane == 0) mbar_arrive_cluster(empty0 + 8 * b);
-        b ^= 1;
-        if (b == 0) b_phase ^= 1;
-      }
+      fence_before();
+      __syncwarp();
+      if (lane == 0) mbar_arrive_cluster(empty0 + 8 * b);
+      b ^= 1;
+      if (b == 0) b_phase ^= 1;
     }
   }
 
