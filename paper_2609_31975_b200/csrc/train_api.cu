@@ -20,7 +20,7 @@ namespace {
     }                                                     \
   } while (0)
 
-constexpr double kSplitProducts = 1e9;  // T D H
+constexpr double kSplitProducts = 1e8;  // T D H
 constexpr int kMaxRows = 1 << 22;  // tokens, and neurons: the kernels' grids and tensor maps have room for so many
 
 inline bool aligned(const void* p, uintptr_t a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) == 0; }
@@ -105,9 +105,11 @@ struct Products {
   sffn::TrainOperand operand(const void* in, int64_t ld, size_t at) const {
     return L.split ? sffn::TrainOperand{ws + at, L.ld_d} : sffn::TrainOperand{in, ld};
   }
-  cudaError_t run(sffn::TrainGemm& g, const int64_t* limb_a, const int64_t* limb_b) const {
+  cudaError_t run(sffn::TrainGemm& g, const int64_t* limb_a, const int64_t* limb_b, int* lines = nullptr) const {
+    int unused = 0;
     g.epi.limb = L.limb_h;
-    if (!L.umma) return sffn::launch_train_simt(g, c->dtype, s);
+    if (!L.umma) return sffn::launch_train_simt(g, lines ? lines : &unused, s);
+    if (lines) *lines = L.lines;
     sffn::TrainUmma t{};
     t.g = g;
     t.f32 = L.split;
@@ -264,8 +266,9 @@ int gated_ffn_backward(const sffn_train_call* c, const void* dy, int64_t ld_dy, 
   e.du = want_du ? values[1] : nullptr;
   e.h = g->dW_down ? values[2] : nullptr;
   e.db = g->db_g ? lines : nullptr;
-  SFFN_CUDA(p.run(dh, tokens, weights));
-  if (g->db_g) SFFN_CUDA(sffn::launch_train_column_sums(lines, L.lines, L.ld_h, c->H, g->db_g, s));
+  int n_lines = 0;
+  SFFN_CUDA(p.run(dh, tokens, weights, &n_lines));
+  if (g->db_g) SFFN_CUDA(sffn::launch_train_column_sums(lines, n_lines, L.ld_h, c->H, g->db_g, s));
 
   if (g->dx) {
     sffn::TrainGemm dx{};

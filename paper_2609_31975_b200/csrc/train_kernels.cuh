@@ -74,9 +74,10 @@ __device__ __forceinline__ void train_act_slope(int act, float t, float& value, 
   slope = keep ? fmaf(t * s, 1.f - s, s) : 0.f;
 }
 
-// CUDA-core kernels (train_simt.cu): fp32 FMAs on fp32 or bf16 operands, any size.
-int train_simt_lines(int M);   // lines of partial sums that kHidden leaves in `db`
-cudaError_t launch_train_simt(const TrainGemm& g, int dtype, cudaStream_t s);
+// Small products in fp32 FMAs (train_simt.cu), fp32 operands.  *lines: of partial sums that kHidden leaves in `db`, at most
+// train_simt_lines(M).
+int train_simt_lines(int M);
+cudaError_t launch_train_simt(const TrainGemm& g, int* lines, cudaStream_t s);
 // db_g[j] = sum over `lines` lines of partial sums, in order; 0 for no line.
 cudaError_t launch_train_column_sums(const float* partial, int lines, int64_t ld, int N, float* out, cudaStream_t s);
 

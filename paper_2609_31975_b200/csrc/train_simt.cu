@@ -1,134 +1,269 @@
-// Products of the training calls on the CUDA cores: fp32 FMAs, operands fp32 or bf16, any size and either order of the
-// operands in memory.  One CTA owns a 64 x 64 tile, a thread 4 x 4 of it.
+// Products of small training calls in fp32 FMAs (fp32 storage; larger calls split their operands for the tensor cores).
+//
+// A CTA owns a 32 x 64 tile of C, or z and u of 32 tokens x 32 neurons; a thread 2 x 4 of it.  Pieces of 32 k go through
+// registers into [k][m] and [k][n] arrays, whichever way an operand lies in memory, the next piece under way while one is
+// multiplied.  Such a call has few tiles and is bound by latency, so K is cut among up to eight CTAs of a cluster: each
+// leaves its sums in shared memory and takes a share of the tile's rows, which it adds up over all of them, in order.
 #include "train_kernels.cuh"
 
 namespace sffn {
 namespace {
 
-constexpr int kTile = 64, kDepth = 16, kThreads = 256;
+constexpr int kRows = 32, kCols = 64, kDepth = 32, kThreads = 256;
+constexpr int kMaxSplit = 8;
 
-__device__ __forceinline__ float value_of(float v) { return v; }
-__device__ __forceinline__ float value_of(__nv_bfloat16 v) { return __bfloat162float(v); }
-__device__ __forceinline__ void put(float* p, float v) { *p = v; }
-__device__ __forceinline__ void put(__nv_bfloat16* p, float v) { *p = __float2bfloat16(v); }
+// A thread's share of a [kDepth][N] piece: N / 32 times four values, consecutive in memory.
+template <int N>
+struct Piece {
+  static constexpr int kQuads = N * kDepth / 4 / kThreads;
+  float4 v[kQuads];
 
-// A [kDepth][kTile] piece of an operand, zeros outside of it.
-template <typename T>
-__device__ __forceinline__ void fetch(float (*s)[kTile + 4], const TrainOperand& o, bool major_k, int row0, int rows, int k0, int K) {
-  const T* p = static_cast<const T*>(o.data);
-  for (int i = threadIdx.x; i < kTile * kDepth; i += kThreads) {
-    const int r = major_k ? i / kDepth : i % kTile, k = major_k ? i % kDepth : i / kTile;
-    float v = 0.f;
-    if (row0 + r < rows && k0 + k < K) v = value_of(p[major_k ? (int64_t)(row0 + r) * o.ld + k0 + k : (int64_t)(k0 + k) * o.ld + row0 + r]);
-    s[k][r] = v;
+  // rows are a multiple of 16 bytes apart; along an axis that ends inside a quad what lies beyond is not looked at
+  __device__ __forceinline__ void fetch(const TrainOperand& o, bool major_k, int row0, int rows, int k0, int k1) {
+    const float* p = static_cast<const float*>(o.data);
+#pragma unroll
+    for (int q = 0; q < kQuads; ++q) {
+      const int i = threadIdx.x + q * kThreads;
+      const int r = major_k ? i / (kDepth / 4) : i % (N / 4) * 4, k = major_k ? i % (kDepth / 4) * 4 : i / (N / 4);
+      const int line = major_k ? row0 + r : k0 + k, at = major_k ? k0 + k : row0 + r, lines = major_k ? rows : k1, end = major_k ? k1 : rows;
+      float4 f = make_float4(0.f, 0.f, 0.f, 0.f);
+      if (line < lines && at < end) {
+        const float* s = p + line * o.ld + at;
+        if (at + 4 <= end) {
+          f = *reinterpret_cast<const float4*>(s);
+        } else {
+          f.x = s[0];
+          if (at + 1 < end) f.y = s[1];
+          if (at + 2 < end) f.z = s[2];
+        }
+      }
+      v[q] = f;
+    }
+  }
+  __device__ __forceinline__ void store(float (*s)[N + 4], bool major_k) const {
+#pragma unroll
+    for (int q = 0; q < kQuads; ++q) {
+      const int i = threadIdx.x + q * kThreads;
+      if (major_k) {
+        const int r = i / (kDepth / 4), k = i % (kDepth / 4) * 4;
+        s[k][r] = v[q].x; s[k + 1][r] = v[q].y; s[k + 2][r] = v[q].z; s[k + 3][r] = v[q].w;
+      } else {
+        *reinterpret_cast<float4*>(&s[i / (N / 4)][i % (N / 4) * 4]) = v[q];
+      }
+    }
+  }
+};
+
+__device__ __forceinline__ void cluster_meet() {
+  asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+__device__ __forceinline__ float4 remote_quad(const float* local, int rank) {
+  uint32_t a = static_cast<uint32_t>(__cvta_generic_to_shared(local)), r;
+  asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(rank));
+  float4 v;
+  asm volatile("ld.shared::cluster.v4.f32 {%0,%1,%2,%3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(r) : "memory");
+  return v;
+}
+
+// Four values of a row, the first n of them: rows may end, and start, anywhere in a user's matrix of odd width.
+__device__ __forceinline__ void put4(void* base, int64_t at, const float* v, int n) {
+  float* p = static_cast<float*>(base) + at;
+  if (n == 4) {
+    *reinterpret_cast<float4*>(p) = make_float4(v[0], v[1], v[2], v[3]);
+  } else {
+    for (int i = 0; i < n; ++i) p[i] = v[i];
+  }
+}
+__device__ __forceinline__ void get4(const void* base, int64_t at, float* v, int n) {
+  const float* p = static_cast<const float*>(base) + at;
+  if (n == 4) {
+    const float4 f = *reinterpret_cast<const float4*>(p);
+    v[0] = f.x; v[1] = f.y; v[2] = f.z; v[3] = f.w;
+  } else {
+    for (int i = 0; i < 4; ++i) v[i] = i < n ? p[i] : 0.f;
   }
 }
 
-template <typename T, int EPI>
-__global__ void __launch_bounds__(kThreads) train_simt_kernel(const __grid_constant__ TrainGemm g) {
-  constexpr int kSums = EPI == kEpiGateUp ? 2 : 1;
-  constexpr bool kFast = sizeof(T) == 2;
-  __shared__ float sa[kDepth][kTile + 4], sb[kSums][kDepth][kTile + 4];
-  __shared__ float column[EPI == kEpiHidden ? 16 : 1][kTile];
+// A cluster of `splits` CTAs for each tile, tiles along N first, then along M, then of the batch.
+template <int EPI>
+__global__ void __launch_bounds__(kThreads) train_simt_kernel(const __grid_constant__ TrainGemm g, int splits) {
+  constexpr bool kDual = EPI == kEpiGateUp;
+  constexpr int kNeurons = kDual ? kCols / 2 : kCols;  // output columns of a tile
+  __shared__ __align__(16) float pool[kDepth * (kRows + 4 + kCols + 4)];
+  float(*const sa)[kRows + 4] = reinterpret_cast<float(*)[kRows + 4]>(pool);
+  float(*const sb)[kCols + 4] = reinterpret_cast<float(*)[kCols + 4]>(pool + kDepth * (kRows + 4));  // kDual: columns of W_g, then of W_up
+  __shared__ __align__(16) float tile[kRows][kCols + 4];
+  pdl_launch_dependents();
+  pdl_wait();
   const int tx = threadIdx.x & 15, ty = threadIdx.x >> 4;
-  const int m0 = blockIdx.y * kTile, n0 = blockIdx.x * kTile, z = blockIdx.z;
-  float acc[kSums][4][4] = {};
-  const int parts = EPI == kEpiGateUp ? 1 : g.parts;
-  for (int part = 0; part < parts; ++part) {
-    const int at = g.batch > 1 ? z : part;
-    for (int k0 = 0; k0 < g.K; k0 += kDepth) {
-      fetch<T>(sa, g.a[at], g.a_major_k, m0, g.M, k0, g.K);
+  const int m_tiles = (g.M + kRows - 1) / kRows, n_tiles = (g.N + kNeurons - 1) / kNeurons;
+  const int at_tile = blockIdx.x / splits, split = blockIdx.x - at_tile * splits, at_row = at_tile / n_tiles, z = at_row / m_tiles;
+  const int m0 = (at_row - z * m_tiles) * kRows, n0 = (at_tile - at_row * n_tiles) * kNeurons;
+  // K of all parts in a row, in pieces
+  const int parts = kDual ? 1 : g.parts, per = (g.K + kDepth - 1) / kDepth, pieces = parts * per;
+  const int first = (int)((long long)pieces * split / splits), last = (int)((long long)pieces * (split + 1) / splits);
+  float acc[2][4] = {};
+  Piece<kRows> pa;
+  Piece<kDual ? kNeurons : kCols> pb;
+  Piece<kDual ? kNeurons : kRows> pu;  // kDual: of W_up
+  auto fetch = [&](int i) {
+    const int part = i / per, k0 = (i - part * per) * kDepth, at = g.batch > 1 ? z : part;
+    pa.fetch(g.a[kDual ? 0 : at], g.a_major_k, m0, g.M, k0, g.K);
+    pb.fetch(g.b[kDual ? 0 : at], g.b_major_k, n0, g.N, k0, g.K);
+    if constexpr (kDual) pu.fetch(g.b[1], g.b_major_k, n0, g.N, k0, g.K);
+  };
+  auto store = [&]() {
+    pa.store(sa, g.a_major_k);
+    if constexpr (kDual) {  // always K-major
 #pragma unroll
-      for (int q = 0; q < kSums; ++q) fetch<T>(sb[q], g.b[kSums > 1 ? q : at], g.b_major_k, n0, g.N, k0, g.K);
-      __syncthreads();
-#pragma unroll
-      for (int k = 0; k < kDepth; ++k) {
-        const float4 a = *reinterpret_cast<const float4*>(&sa[k][4 * ty]);
-        const float av[4] = {a.x, a.y, a.z, a.w};
-#pragma unroll
-        for (int q = 0; q < kSums; ++q) {
-          const float4 b = *reinterpret_cast<const float4*>(&sb[q][k][4 * tx]);
-          const float bv[4] = {b.x, b.y, b.z, b.w};
-#pragma unroll
-          for (int i = 0; i < 4; ++i)
-#pragma unroll
-            for (int j = 0; j < 4; ++j) acc[q][i][j] = fmaf(av[i], bv[j], acc[q][i][j]);
-        }
+      for (int q = 0; q < Piece<kNeurons>::kQuads; ++q) {
+        const int i = threadIdx.x + q * kThreads, r = i / (kDepth / 4), k = i % (kDepth / 4) * 4;
+        sb[k][r] = pb.v[q].x; sb[k + 1][r] = pb.v[q].y; sb[k + 2][r] = pb.v[q].z; sb[k + 3][r] = pb.v[q].w;
+        sb[k][kNeurons + r] = pu.v[q].x; sb[k + 1][kNeurons + r] = pu.v[q].y; sb[k + 2][kNeurons + r] = pu.v[q].z; sb[k + 3][kNeurons + r] = pu.v[q].w;
       }
-      __syncthreads();
+    } else {
+      pb.store(sb, g.b_major_k);
     }
+  };
+  if (first < last) fetch(first);
+  for (int i = first; i < last; ++i) {
+    store();
+    __syncthreads();
+    if (i + 1 < last) fetch(i + 1);
+#pragma unroll 8
+    for (int k = 0; k < kDepth; ++k) {
+      const float2 a = *reinterpret_cast<const float2*>(&sa[k][2 * ty]);
+      const float4 b = *reinterpret_cast<const float4*>(&sb[k][4 * tx]);
+      acc[0][0] = fmaf(a.x, b.x, acc[0][0]); acc[0][1] = fmaf(a.x, b.y, acc[0][1]); acc[0][2] = fmaf(a.x, b.z, acc[0][2]); acc[0][3] = fmaf(a.x, b.w, acc[0][3]);
+      acc[1][0] = fmaf(a.y, b.x, acc[1][0]); acc[1][1] = fmaf(a.y, b.y, acc[1][1]); acc[1][2] = fmaf(a.y, b.z, acc[1][2]); acc[1][3] = fmaf(a.y, b.w, acc[1][3]);
+    }
+    __syncthreads();
   }
+#pragma unroll
+  for (int i = 0; i < 2; ++i) *reinterpret_cast<float4*>(&tile[2 * ty + i][4 * tx]) = make_float4(acc[i][0], acc[i][1], acc[i][2], acc[i][3]);
+  if (splits > 1) cluster_meet();
+  else __syncthreads();
+
+  // This CTA's rows of the tile, four columns a thread.
   const TrainEpilogue& e = g.epi;
-  float down[4] = {};
+  const int rows = kRows / splits, r0 = split * rows;
+  auto sums = [&](int r, int c, float* v) {
+    if (splits == 1) {
+      const float4 f = *reinterpret_cast<const float4*>(&tile[r][c]);
+      v[0] = f.x; v[1] = f.y; v[2] = f.z; v[3] = f.w;
+      return;
+    }
+    v[0] = v[1] = v[2] = v[3] = 0.f;
+    for (int s = 0; s < splits; ++s) {
+      const float4 f = remote_quad(&tile[r][c], s);
+      v[0] += f.x; v[1] += f.y; v[2] += f.z; v[3] += f.w;
+    }
+  };
+  float* const down = pool;  // kHidden: [rows][kCols] of dz
+  static_assert(kRows * kCols <= kDepth * (kRows + 4 + kCols + 4), "dz of a tile fits the operands' arrays");
+  for (int i = threadIdx.x; i < rows * (kNeurons / 4); i += kThreads) {
+    const int r = i / (kNeurons / 4), c = i % (kNeurons / 4) * 4, m = m0 + r0 + r, n = n0 + c;
+    const int left = m < g.M ? min(4, g.N - n) : 0;
+    float v[4];
+    sums(r0 + r, c, v);
+    if constexpr (EPI == kEpiStore) {
+      if (left > 0) put4(e.out[z], m * e.ld_out + n, v, left);
+    } else if constexpr (EPI == kEpiGateUp) {
+      float u[4], h[4];
+      sums(r0 + r, kNeurons + c, u);
+      if (left <= 0) continue;
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const int m = m0 + 4 * ty + i;
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      const int n = n0 + 4 * tx + j;
-      if (m >= g.M || n >= g.N) continue;
-      if (EPI == kEpiStore) {
-        put(static_cast<T*>(e.out[z]) + m * e.ld_out + n, acc[0][i][j]);
-      } else if (EPI == kEpiGateUp) {
-        const float zv = acc[0][i][j] + (e.bias ? e.bias[n] : 0.f), uv = acc[kSums - 1][i][j];
-        if (e.z) {
-          put(static_cast<T*>(e.z) + m * e.ld_zu + n, zv);
-          put(static_cast<T*>(e.u) + m * e.ld_zu + n, uv);
-        }
-        put(static_cast<T*>(e.h) + m * e.ld_h + n, train_act<kFast>(e.act, zv) * train_act<kFast>(e.act_up, uv));
-      } else {
-        const float zv = value_of(static_cast<const T*>(e.z)[m * e.ld_zu + n]), uv = value_of(static_cast<const T*>(e.u)[m * e.ld_zu + n]);
-        float a, da, b, db;
-        train_act_slope<kFast>(e.act, zv, a, da);
-        train_act_slope<kFast>(e.act_up, uv, b, db);
-        const float dz = acc[0][i][j] * b * da, du = acc[0][i][j] * a * db;
-        if (e.dz) put(static_cast<T*>(e.dz) + m * e.ld_h + n, dz);
-        if (e.du) put(static_cast<T*>(e.du) + m * e.ld_h + n, du);
-        if (e.h) put(static_cast<T*>(e.h) + m * e.ld_h + n, a * b);
-        down[j] += dz;
+      for (int j = 0; j < 4; ++j) {
+        if (e.bias && j < left) v[j] += e.bias[n + j];
+        h[j] = train_act<false>(e.act, v[j]) * train_act<false>(e.act_up, u[j]);
       }
+      if (e.z) {
+        put4(e.z, m * e.ld_zu + n, v, left);
+        put4(e.u, m * e.ld_zu + n, u, left);
+      }
+      put4(e.h, m * e.ld_h + n, h, left);
+    } else {
+      float zv[4], uv[4], h[4], du[4];
+      get4(e.z, m * e.ld_zu + n, zv, left);
+      get4(e.u, m * e.ld_zu + n, uv, left);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        float a, da, b, db;
+        train_act_slope<false>(e.act, zv[j], a, da);
+        train_act_slope<false>(e.act_up, uv[j], b, db);
+        h[j] = a * b;
+        du[j] = v[j] * a * db;
+        v[j] = v[j] * b * da;
+      }
+      if (left > 0) {
+        if (e.dz) put4(e.dz, m * e.ld_h + n, v, left);
+        if (e.du) put4(e.du, m * e.ld_h + n, du, left);
+        if (e.h) put4(e.h, m * e.ld_h + n, h, left);
+      }
+#pragma unroll
+      for (int j = 0; j < 4; ++j) down[r * kCols + c + j] = j < left ? v[j] : 0.f;
     }
   }
   if (EPI == kEpiHidden && e.db) {
-#pragma unroll
-    for (int j = 0; j < 4; ++j) column[ty][4 * tx + j] = down[j];
     __syncthreads();
-    if (threadIdx.x < kTile && n0 + threadIdx.x < g.N) {
+    if (threadIdx.x < kCols && n0 + threadIdx.x < g.N) {
       float sum = 0.f;
-      for (int r = 0; r < 16; ++r) sum += column[r][threadIdx.x];
-      e.db[blockIdx.y * e.ld_h + n0 + threadIdx.x] = sum;
+      for (int r = 0; r < rows; ++r) sum += down[r * kCols + threadIdx.x];
+      e.db[((int64_t)(m0 / kRows) * splits + split) * e.ld_h + n0 + threadIdx.x] = sum;
     }
+  }
+  if (splits > 1) cluster_meet();  // nobody leaves while its sums may still be read
+}
+
+// One column a lane, eight runs of lines a CTA.
+__global__ void __launch_bounds__(256) train_column_sums_kernel(const float* partial, int lines, int64_t ld, int N, float* out) {
+  __shared__ float run[8][32];
+  pdl_launch_dependents();
+  pdl_wait();
+  const int lane = threadIdx.x & 31, part = threadIdx.x >> 5, n = blockIdx.x * 32 + lane;
+  float sum = 0.f;
+  if (n < N) {
+    const int first = lines * part / 8, last = lines * (part + 1) / 8;
+#pragma unroll 8
+    for (int l = first; l < last; ++l) sum += partial[l * ld + n];
+  }
+  run[part][lane] = sum;
+  __syncthreads();
+  if (part == 0 && n < N) {
+    sum = run[0][lane];
+    for (int q = 1; q < 8; ++q) sum += run[q][lane];
+    out[n] = sum;
   }
 }
 
-__global__ void __launch_bounds__(256) column_sums_kernel(const float* partial, int lines, int64_t ld, int N, float* out) {
-  const int n = blockIdx.x * 256 + threadIdx.x;
-  if (n >= N) return;
-  float sum = 0.f;
-  for (int l = 0; l < lines; ++l) sum += partial[l * ld + n];
-  out[n] = sum;
-}
-
-template <typename T>
-cudaError_t launch(const TrainGemm& g, cudaStream_t s) {
-  const dim3 grid((g.N + kTile - 1) / kTile, (g.M + kTile - 1) / kTile, g.batch > 1 ? g.batch : 1);
-  if (g.epilogue == kEpiStore) train_simt_kernel<T, kEpiStore><<<grid, kThreads, 0, s>>>(g);
-  else if (g.epilogue == kEpiGateUp) train_simt_kernel<T, kEpiGateUp><<<grid, kThreads, 0, s>>>(g);
-  else train_simt_kernel<T, kEpiHidden><<<grid, kThreads, 0, s>>>(g);
-  return cudaGetLastError();
+// CTAs that share a tile's K: as long as all run at once, and each has two pieces.
+int splits_for(const TrainGemm& g) {
+  const int neurons = g.epilogue == kEpiGateUp ? kCols / 2 : kCols;
+  const long long tiles = (long long)((g.M + kRows - 1) / kRows) * ((g.N + neurons - 1) / neurons) * g.batch;
+  const int pieces = (g.epilogue == kEpiGateUp ? 1 : g.parts) * ((g.K + kDepth - 1) / kDepth);
+  int s = 1;
+  while (s < kMaxSplit && tiles * s * 2 <= 2 * 148 && pieces >= 4 * s) s *= 2;
+  return s;
 }
 
 }  // namespace
 
-int train_simt_lines(int M) { return (M + kTile - 1) / kTile; }
+int train_simt_lines(int M) { return (M + kRows - 1) / kRows * kMaxSplit; }
 
-cudaError_t launch_train_simt(const TrainGemm& g, int dtype, cudaStream_t s) {
-  return dtype == SFFN_BF16 ? launch<__nv_bfloat16>(g, s) : launch<float>(g, s);
+cudaError_t launch_train_simt(const TrainGemm& g, int* lines, cudaStream_t s) {
+  const int neurons = g.epilogue == kEpiGateUp ? kCols / 2 : kCols, splits = splits_for(g);
+  const int m_tiles = (g.M + kRows - 1) / kRows;
+  const long long ctas = (long long)splits * ((g.N + neurons - 1) / neurons) * m_tiles * g.batch;
+  if (ctas > 0x7fffffff) return cudaErrorInvalidValue;
+  const dim3 grid((unsigned)ctas);
+  *lines = m_tiles * splits;
+  if (g.epilogue == kEpiStore) return launch_clusters(splits, train_simt_kernel<kEpiStore>, grid, dim3(kThreads), 0, s, g, splits);
+  if (g.epilogue == kEpiGateUp) return launch_clusters(splits, train_simt_kernel<kEpiGateUp>, grid, dim3(kThreads), 0, s, g, splits);
+  return launch_clusters(splits, train_simt_kernel<kEpiHidden>, grid, dim3(kThreads), 0, s, g, splits);
 }
 
 cudaError_t launch_train_column_sums(const float* partial, int lines, int64_t ld, int N, float* out, cudaStream_t s) {
-  column_sums_kernel<<<(N + 255) / 256, 256, 0, s>>>(partial, lines, ld, N, out);
-  return cudaGetLastError();
+  return launch_pdl(train_column_sums_kernel, dim3((N + 31) / 32), dim3(256), 0, s, partial, lines, ld, N, out);
 }
 
 }  // namespace sffn
