@@ -384,7 +384,7 @@ int sffn_grad_norm(const sffn_tensor* tensors, int n, float* norm, void* workspa
  *     m = m_scale sign(c) (c / 127)^2,  v = v_scale (c / 255)^4,
  * the scale being the group's largest |m| (v), the code the nearest one in (|m| / scale)^(1/2), (v / scale)^(1/4), up on a tie;
  * a v that is not zero keeps a code of at least 1, as it divides m; a group whose largest value is below 2^-100 is
- * stored as zeros.  Pointers need the alignment of their type only; 16 bytes are faster. */
+ * stored as zeros.  Pointers need the alignment of their type only; 32 bytes are faster. */
 typedef struct {
   void* p;
   const void* g;

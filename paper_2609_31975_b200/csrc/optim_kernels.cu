@@ -28,8 +28,8 @@ __device__ __forceinline__ void advance(const List& list, uint32_t piece, int& e
 // ---- norm ------------------------------------------------------------------------------------------------------------
 
 constexpr int kNormThreads = 512;
-constexpr int kNormLoads = 4;                         // 16-byte loads of a lane in flight
-constexpr int kNormPiece = 32 * 16 * kNormLoads;      // bytes of a warp's piece
+constexpr int kNormLoads = 4;                         // 32-byte loads of a lane in flight
+constexpr int kNormPiece = 32 * 32 * kNormLoads;      // bytes of a warp's piece
 constexpr int kNormMaxGrid = 1024;
 static_assert(256 + 8 * kNormMaxGrid + 16 <= SFFN_GRAD_NORM_WORKSPACE, "partial sums fit");
 
@@ -49,21 +49,30 @@ struct NormList {
   NormEntry e[N];
 };
 
-__device__ __forceinline__ float sum_squares(const uint4& v, bool bf16, float acc) {
+__device__ __forceinline__ float sum_squares(const uint32_t* w, bool bf16, float acc) {
+  float2 a = make_float2(acc, 0.f), b = make_float2(0.f, 0.f);
   if (bf16) {
-    float f[8];
-    Elem<__nv_bfloat16>::unpack(v, f);
-    float2 a = make_float2(acc, 0.f);
 #pragma unroll
-    for (int i = 0; i < 8; i += 2) a = fma2(make_float2(f[i], f[i + 1]), make_float2(f[i], f[i + 1]), a);
-    return a.x + a.y;
+    for (int i = 0; i < 8; ++i) {
+      const float2 f = make_float2(__uint_as_float(w[i] << 16), __uint_as_float(w[i] & 0xffff0000u));
+      if (i & 1) b = fma2(f, f, b);
+      else a = fma2(f, f, a);
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const float2 f = make_float2(__uint_as_float(w[2 * i]), __uint_as_float(w[2 * i + 1]));
+      if (i & 1) b = fma2(f, f, b);
+      else a = fma2(f, f, a);
+    }
   }
-  float f[4];
-  Elem<float>::unpack(v, f);
-  float2 a = make_float2(acc, 0.f);
-  a = fma2(make_float2(f[0], f[1]), make_float2(f[0], f[1]), a);
-  a = fma2(make_float2(f[2], f[3]), make_float2(f[2], f[3]), a);
-  return a.x + a.y;
+  return (a.x + a.y) + (b.x + b.y);
+}
+__device__ __forceinline__ void ld32(const void* p, uint32_t* w) {  // 32 bytes
+  asm volatile("ld.global.v8.b32 {%0,%1,%2,%3,%4,%5,%6,%7}, [%8];"
+               : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]), "=r"(w[4]), "=r"(w[5]), "=r"(w[6]), "=r"(w[7])
+               : "l"(p)
+               : "memory");
 }
 
 template <int N>
@@ -72,6 +81,8 @@ __global__ void __launch_bounds__(kNormThreads) grad_norm_kernel(const __grid_co
   __shared__ bool last_cta;
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const uint32_t warps = gridDim.x * (kNormThreads / 32);
+  pdl_launch_dependents();
+  pdl_wait();
   float acc[kNormLoads] = {};
   double total = 0.0;
   int e = 0, since = 0;
@@ -83,20 +94,20 @@ __global__ void __launch_bounds__(kNormThreads) grad_norm_kernel(const __grid_co
     const long long first = (long long)(piece - t.begin) * (kNormPiece / esz);
     const char* p = static_cast<const char*>(t.data) + first * esz;
     const long long left = t.n - first;
-    if (left >= kNormPiece / esz && (reinterpret_cast<uintptr_t>(p) & 15u) == 0) {
-      uint4 v[kNormLoads];
+    if (left >= kNormPiece / esz && (reinterpret_cast<uintptr_t>(p) & 31u) == 0) {
+      uint32_t v[kNormLoads][8];
 #pragma unroll
-      for (int i = 0; i < kNormLoads; ++i) v[i] = ld_stream16(p + (i * 32 + lane) * 16);
+      for (int i = 0; i < kNormLoads; ++i) ld32(p + (i * 32 + lane) * 32, v[i]);
 #pragma unroll
       for (int i = 0; i < kNormLoads; ++i) acc[i] = sum_squares(v[i], bf16, acc[i]);
-    } else {  // a tensor's end, or one that does not start on 16 bytes
+    } else {  // a tensor's end, or one that does not start on 32 bytes
       const int count = (int)(left < kNormPiece / esz ? left : kNormPiece / esz);
       for (int i = lane; i < count; i += 32) {
         const float g = bf16 ? __bfloat162float(reinterpret_cast<const __nv_bfloat16*>(p)[i]) : reinterpret_cast<const float*>(p)[i];
         acc[0] = fmaf(g, g, acc[0]);
       }
     }
-    if (++since == 32) {  // short runs in 32 bits, their sums in 64
+    if (++since == 16) {  // short runs in 32 bits, their sums in 64
 #pragma unroll
       for (int i = 0; i < kNormLoads; ++i) { total += (double)acc[i]; acc[i] = 0.f; }
       since = 0;
@@ -163,8 +174,7 @@ cudaError_t norm_launches(const sffn_tensor* t, int n, float* norm, void* worksp
     const long long want = (pieces + kNormThreads / 32 - 1) / (kNormThreads / 32);
     int grid = 4 * sm_count < kNormMaxGrid ? 4 * sm_count : kNormMaxGrid;
     if (want < grid) grid = want > 0 ? (int)want : 1;
-    grad_norm_kernel<N><<<grid, kNormThreads, 0, s>>>(list);
-    const cudaError_t e = cudaGetLastError();
+    const cudaError_t e = launch_pdl(grad_norm_kernel<N>, dim3(grid), dim3(kNormThreads), 0, s, list);
     if (e != cudaSuccess) return e;
     first = false;
   } while (at < n);
@@ -197,36 +207,97 @@ struct StepList {
   StepEntry e[N];
 };
 
-__device__ __forceinline__ float sqrt_approx(float x) {
+// Pairs of fp32 in one register pair, each half as in the scalar operation -- but the compiler may fuse a product and the sum it
+// goes into, which it does not do across halves taken apart (add_apart).
+typedef unsigned long long f2;
+__device__ __forceinline__ f2 mul2(f2 a, f2 b) {
+  f2 d;
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
+  return d;
+}
+__device__ __forceinline__ f2 both(float v) { return pack2(v, v); }
+__device__ __forceinline__ void halves(f2 v, float& lo, float& hi) { asm("mov.b64 {%0, %1}, %2;" : "=f"(lo), "=f"(hi) : "l"(v)); }
+__device__ __forceinline__ float low(f2 v) { float a, b; halves(v, a, b); return a; }
+__device__ __forceinline__ float high(f2 v) { float a, b; halves(v, a, b); return b; }
+
+__device__ __forceinline__ f2 add_apart(f2 a, f2 b) { return pack2(__fadd_rn(low(a), low(b)), __fadd_rn(high(a), high(b))); }
+
+__device__ __forceinline__ float sqrt_approx(float x) {  // what is below 2^-126 counts as zero
   float r;
-  asm("sqrt.approx.f32 %0, %1;" : "=f"(r) : "f"(x));
+  asm("sqrt.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
+  return r;
+}
+__device__ __forceinline__ float rcp_approx(float x) {
+  float r;
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
+  return r;
+}
+__device__ __forceinline__ float max_nan(float a, float b) {
+  float r;
+  asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
   return r;
 }
 
-// The number of edges (k + 1/2)^2, k < 127, at or below q: a square root that may be off by its last bits, then the edges
-// themselves (exact in 32 bits) decide.
-__device__ __forceinline__ int code_of_square(float q) {
-  float c = fminf(floorf(sqrt_approx(q) + 0.5f), 127.f);
-  const float up = fmaf(c, c, c) + 0.25f, down = fmaf(c, c, -c) + 0.25f;  // c <= 127: exact
-  if (q >= up) c += 1.f;
-  else if (q < down) c -= 1.f;
-  return (int)fminf(fmaxf(c, 0.f), 127.f);
+constexpr float kMagic = 12582912.f;   // 1.5 2^23: a small number added to it is rounded to an integer, in its low bits
+constexpr float kMargin = 2e-4f;       // how far a square root of at most 255 is certainly not off
+
+// Codes: the number of edges (k + 1/2)^2 (for v: the rounded square of that) at or below q.  The approximate root, made a
+// little too small, is rounded to an integer c that the code is never below and at most one above; whether q reaches the edge above
+// c is then seen in numbers that fp32 holds exactly: q - c^2 >= c + 1/4.  Left in the low bits of *r, with the sign of m.
+__device__ __forceinline__ void code_squares(f2 m, f2 q, uint32_t* r) {
+  float q0, q1, m0, m1;
+  halves(q, q0, q1);
+  halves(m, m0, m1);
+  const f2 s = add2_b64(pack2(sqrt_approx(q0), sqrt_approx(q1)), both(-kMargin));
+  const f2 n = add2_b64(s, both(kMagic));
+  const f2 c = add2_b64(n, both(-kMagic));
+  const f2 minus = mul2(c, both(-1.f));
+  const f2 over = fma2_b64(minus, c, q), edge = add2_b64(c, both(0.25f));
+  int c0 = __float_as_int(low(n)) - __float_as_int(kMagic), c1 = __float_as_int(high(n)) - __float_as_int(kMagic);
+  if (low(over) >= low(edge)) ++c0;
+  if (high(over) >= high(edge)) ++c1;
+  r[0] = m0 < 0.f ? -c0 : c0;
+  r[1] = m1 < 0.f ? -c1 : c1;
 }
-// The same with edges (k + 1/2)^4, k < 255, each the rounded square of an exact (k + 1/2)^2.
-__device__ __forceinline__ int code_of_fourth(float q) {
-  float c = fminf(floorf(sqrt_approx(sqrt_approx(q)) + 0.5f), 255.f);
-  float up = fmaf(c, c, c) + 0.25f, down = fmaf(c, c, -c) + 0.25f;
-  up = __fmul_rn(up, up);
-  down = __fmul_rn(down, down);
-  if (q >= up) c += 1.f;
-  else if (q < down) c -= 1.f;
-  return (int)fminf(fmaxf(c, 0.f), 255.f);
+// `half_root`: an approximate square root of q.
+__device__ __forceinline__ void code_fourths(f2 v, f2 q, f2 half_root, uint32_t* r) {
+  float v0, v1;
+  halves(v, v0, v1);
+  const f2 s = add2_b64(pack2(sqrt_approx(low(half_root)), sqrt_approx(high(half_root))), both(-kMargin));
+  const f2 n = add2_b64(s, both(kMagic));
+  const f2 c = add2_b64(n, both(-kMagic));
+  const f2 t = fma2_b64(c, c, add2_b64(c, both(0.25f)));  // (c + 1/2)^2, exact
+  const f2 edge = mul2(t, t);
+  int c0 = __float_as_int(low(n)) - __float_as_int(kMagic), c1 = __float_as_int(high(n)) - __float_as_int(kMagic);
+  if (low(q) >= low(edge)) ++c0;
+  if (high(q) >= high(edge)) ++c1;
+  r[0] = max(c0, v0 > 0.f ? 1 : 0);  // what is not zero stays so: it divides
+  r[1] = max(c1, v1 > 0.f ? 1 : 0);
 }
 
 __device__ __forceinline__ float code_m(int c, float unit) { return __fmul_rn((float)(c * abs(c)), unit); }
 __device__ __forceinline__ float code_v(int c, float unit) {
   const float t = (float)(c * c);
   return __fmul_rn(__fmul_rn(t, t), unit);
+}
+// Four codes of a word, without integer conversions: the byte (m: + 128) goes under the exponent of 2^23.
+__device__ __forceinline__ void codes_m(uint32_t w, f2 unit, f2* v) {
+  w ^= 0x80808080u;
+  const f2 bias = both(-8388736.f);
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    const f2 c = add2_b64(pack2(__uint_as_float(__byte_perm(w, 0x4b000000u, i ? 0x7442 : 0x7440)), __uint_as_float(__byte_perm(w, 0x4b000000u, i ? 0x7443 : 0x7441))), bias);
+    v[i] = mul2(mul2(c, pack2(fabsf(low(c)), fabsf(high(c)))), unit);
+  }
+}
+__device__ __forceinline__ void codes_v(uint32_t w, f2 unit, f2* v) {
+  const f2 bias = both(-8388608.f);
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    const f2 c = add2_b64(pack2(__uint_as_float(__byte_perm(w, 0x4b000000u, i ? 0x7442 : 0x7440)), __uint_as_float(__byte_perm(w, 0x4b000000u, i ? 0x7443 : 0x7441))), bias);
+    const f2 t = mul2(c, c);
+    v[i] = mul2(mul2(t, t), unit);
+  }
 }
 __device__ __forceinline__ float unit_m(float scale) { return __fmul_rn(scale, (float)(1.0 / (127.0 * 127.0))); }
 __device__ __forceinline__ float unit_v(float scale) { return __fmul_rn(scale, (float)(1.0 / (255.0 * 255.0 * 255.0 * 255.0))); }
@@ -242,43 +313,180 @@ __device__ __forceinline__ float warp_most(float mine) {  // values >= 0 order l
   return __uint_as_float(__reduce_max_sync(0xffffffffu, __float_as_uint(mine) & 0x7fffffffu));
 }
 
-__device__ __forceinline__ void load8_f32(const float* p, uint4* raw) {
-  raw[0] = *reinterpret_cast<const uint4*>(p);
-  raw[1] = *reinterpret_cast<const uint4*>(p + 4);
+__device__ __forceinline__ void st32(void* p, const f2* v) {
+  asm volatile("st.global.v4.b64 [%0], {%1,%2,%3,%4};" ::"l"(p), "l"(v[0]), "l"(v[1]), "l"(v[2]), "l"(v[3]) : "memory");
 }
-__device__ __forceinline__ void floats_of(const uint4* raw, bool bf16, float* f) {
-  if (bf16) {
-    Elem<__nv_bfloat16>::unpack(raw[0], f);
+__device__ __forceinline__ void ld16(const void* p, uint32_t* w) {
+  asm volatile("ld.global.v4.b32 {%0,%1,%2,%3}, [%4];" : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]) : "l"(p) : "memory");
+}
+__device__ __forceinline__ void pairs_of(const uint32_t* w, bool bf16, f2* f) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+    f[i] = bf16 ? pack2(__uint_as_float(w[i] << 16), __uint_as_float(w[i] & 0xffff0000u)) : pack2(__uint_as_float(w[2 * i]), __uint_as_float(w[2 * i + 1]));
+}
+__device__ __forceinline__ uint32_t two_bf16(f2 v) {
+  const __nv_bfloat162 b = __floats2bfloat162_rn(low(v), high(v));
+  return *reinterpret_cast<const uint32_t*>(&b);
+}
+
+// Eight entries of a lane as four pairs.  Entry j of a lane: 8 lane + j where vectors are used (WIDE), 32 j + lane otherwise.
+// CODES: the moments are held in codes.
+template <bool CODES, bool WIDE, typename List>
+__device__ __forceinline__ void step_group(const List& c, const StepEntry& t, uint32_t group, float coef, int lane) {
+  const uint32_t kind = t.kind;
+  const long long first = (long long)group * kGroup;
+  const bool p_bf16 = kind & kPBf16, g_bf16 = kind & kGBf16, master = kind & kMaster;
+  const int left = WIDE ? kGroup : (int)min((long long)kGroup, t.n - first);
+  f2 w[4], g[4], m[4], v[4];
+  float sm = 0.f, sv = 0.f;
+  if (CODES) {
+    sm = t.m_scale[group];
+    sv = t.v_scale[group];
+  }
+  if constexpr (WIDE) {
+    const long long at = first + lane * kPer;
+    uint32_t rw[8], rg[8], rm[8], rv[8];
+    // every load is under way before the first value is looked at
+    if (master) ld32(t.master + at, rw);
+    else if (p_bf16) ld16(static_cast<const __nv_bfloat16*>(t.p) + at, rw);
+    else ld32(static_cast<const float*>(t.p) + at, rw);
+    if (g_bf16) ld16(static_cast<const __nv_bfloat16*>(t.g) + at, rg);
+    else ld32(static_cast<const float*>(t.g) + at, rg);
+    if constexpr (CODES) {
+      const uint2 a = *reinterpret_cast<const uint2*>(static_cast<const int8_t*>(t.m) + at);
+      const uint2 b = *reinterpret_cast<const uint2*>(static_cast<const uint8_t*>(t.v) + at);
+      rm[0] = a.x; rm[1] = a.y;
+      rv[0] = b.x; rv[1] = b.y;
+    } else {
+      ld32(static_cast<const float*>(t.m) + at, rm);
+      ld32(static_cast<const float*>(t.v) + at, rv);
+    }
+    pairs_of(rw, p_bf16 && !master, w);
+    pairs_of(rg, g_bf16, g);
+    if constexpr (CODES) {
+      const f2 um = both(unit_m(sm)), uv = both(unit_v(sv));
+      codes_m(rm[0], um, m); codes_m(rm[1], um, m + 2);
+      codes_v(rv[0], uv, v); codes_v(rv[1], uv, v + 2);
+    } else {
+      pairs_of(rm, false, m);
+      pairs_of(rv, false, v);
+    }
   } else {
-    Elem<float>::unpack(raw[0], f);
-    Elem<float>::unpack(raw[1], f + 4);
+    const float um = unit_m(sm), uv = unit_v(sv);
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      float e[4][2];
+#pragma unroll
+      for (int j = 0; j < 2; ++j) {
+        const int i = 32 * (2 * q + j) + lane;
+        const long long at = first + i;
+        e[0][j] = e[1][j] = e[2][j] = e[3][j] = 0.f;
+        if (i >= left) continue;
+        e[0][j] = master ? t.master[at] : p_bf16 ? __bfloat162float(static_cast<const __nv_bfloat16*>(t.p)[at]) : static_cast<const float*>(t.p)[at];
+        e[1][j] = g_bf16 ? __bfloat162float(static_cast<const __nv_bfloat16*>(t.g)[at]) : static_cast<const float*>(t.g)[at];
+        e[2][j] = CODES ? code_m(static_cast<const int8_t*>(t.m)[at], um) : static_cast<const float*>(t.m)[at];
+        e[3][j] = CODES ? code_v(static_cast<const uint8_t*>(t.v)[at], uv) : static_cast<const float*>(t.v)[at];
+      }
+      w[q] = pack2(e[0][0], e[0][1]); g[q] = pack2(e[1][0], e[1][1]); m[q] = pack2(e[2][0], e[2][1]); v[q] = pack2(e[3][0], e[3][1]);
+    }
+  }
+  float most_m = 0.f, most_v = 0.f;
+  f2 root[4];
+#pragma unroll
+  for (int q = 0; q < 4; ++q) {
+    // products and sums of the moments are rounded one by one: codes do not depend on how an expression is contracted
+    g[q] = mul2(g[q], both(coef));
+    m[q] = add_apart(mul2(m[q], both(c.beta1)), mul2(g[q], both(c.one_beta1)));
+    v[q] = add_apart(mul2(v[q], both(c.beta2)), mul2(mul2(g[q], g[q]), both(c.one_beta2)));
+    root[q] = pack2(sqrt_approx(low(v[q])), sqrt_approx(high(v[q])));
+    const f2 below = fma2_b64(root[q], both(c.root_bc2), both(c.eps));
+    const f2 part = mul2(m[q], pack2(rcp_approx(low(below)), rcp_approx(high(below))));
+    w[q] = fma2_b64(part, both(-t.rate), mul2(w[q], both(t.decay)));
+    if (CODES) {  // entries past the end are zeros, of weight zero
+      most_m = max_nan(most_m, max_nan(fabsf(low(m[q])), fabsf(high(m[q]))));
+      most_v = max_nan(most_v, max_nan(low(v[q]), high(v[q])));
+    }
+  }
+  uint32_t cm[8], cv[8];
+  if constexpr (CODES) {
+    float im, iv;
+    sm = group_scale(warp_most(most_m), im);
+    sv = group_scale(warp_most(most_v), iv);
+    const float half = 65025.f * sqrt_approx(iv);  // sqrt(255^4 / scale)
+    const bool small = iv > 1.2379400392853803e27f;  // scale < 2^-90: roots of single values may have been taken for zeros
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      const f2 a = pack2(fabsf(low(m[q])), fabsf(high(m[q])));
+      code_squares(m[q], mul2(mul2(a, both(im)), both(16129.f)), cm + 2 * q);
+      const f2 b = mul2(mul2(v[q], both(iv)), both(4228250624.f));
+      root[q] = mul2(root[q], both(half));
+      if (small) root[q] = pack2(sqrt_approx(low(b)), sqrt_approx(high(b)));
+      code_fourths(v[q], b, root[q], cv + 2 * q);
+    }
+    if (im == 0.f) {
+#pragma unroll
+      for (int j = 0; j < 8; ++j) cm[j] = 0;
+    }
+    if (iv == 0.f) {
+#pragma unroll
+      for (int j = 0; j < 8; ++j) cv[j] = 0;
+    }
+    if (lane == 0) {
+      t.m_scale[group] = sm;
+      t.v_scale[group] = sv;
+    }
+  }
+  if constexpr (WIDE) {
+    const long long at = first + lane * kPer;
+    if (p_bf16) {
+      *reinterpret_cast<uint4*>(static_cast<__nv_bfloat16*>(t.p) + at) = make_uint4(two_bf16(w[0]), two_bf16(w[1]), two_bf16(w[2]), two_bf16(w[3]));
+      if (master) st32(t.master + at, w);
+    } else {
+      st32(static_cast<float*>(t.p) + at, w);
+    }
+    if constexpr (CODES) {
+      uint32_t a[2], b[2];
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        a[h] = __byte_perm(__byte_perm(cm[4 * h], cm[4 * h + 1], 0x0040), __byte_perm(cm[4 * h + 2], cm[4 * h + 3], 0x0040), 0x5410);
+        b[h] = __byte_perm(__byte_perm(cv[4 * h], cv[4 * h + 1], 0x0040), __byte_perm(cv[4 * h + 2], cv[4 * h + 3], 0x0040), 0x5410);
+      }
+      *reinterpret_cast<uint2*>(static_cast<int8_t*>(t.m) + at) = make_uint2(a[0], a[1]);
+      *reinterpret_cast<uint2*>(static_cast<uint8_t*>(t.v) + at) = make_uint2(b[0], b[1]);
+    } else {
+      st32(static_cast<float*>(t.m) + at, m);
+      st32(static_cast<float*>(t.v) + at, v);
+    }
+  } else {
+#pragma unroll
+    for (int j = 0; j < kPer; ++j) {
+      const int i = 32 * j + lane;
+      if (i >= left) continue;
+      const long long at = first + i;
+      const float wj = j & 1 ? high(w[j / 2]) : low(w[j / 2]);
+      if (p_bf16) {
+        static_cast<__nv_bfloat16*>(t.p)[at] = __float2bfloat16(wj);
+        if (master) t.master[at] = wj;
+      } else {
+        static_cast<float*>(t.p)[at] = wj;
+      }
+      if (CODES) {
+        static_cast<int8_t*>(t.m)[at] = (int8_t)cm[j];
+        static_cast<uint8_t*>(t.v)[at] = (uint8_t)cv[j];
+      } else {
+        static_cast<float*>(t.m)[at] = j & 1 ? high(m[j / 2]) : low(m[j / 2]);
+        static_cast<float*>(t.v)[at] = j & 1 ? high(v[j / 2]) : low(v[j / 2]);
+      }
+    }
   }
 }
-__device__ __forceinline__ void store8_f32(float* p, const float* f) {
-  *reinterpret_cast<float4*>(p) = make_float4(f[0], f[1], f[2], f[3]);
-  *reinterpret_cast<float4*>(p + 4) = make_float4(f[4], f[5], f[6], f[7]);
-}
-__device__ __forceinline__ uint32_t two_bf16(float lo, float hi) {
-  const __nv_bfloat162 v = __floats2bfloat162_rn(lo, hi);
-  return *reinterpret_cast<const uint32_t*>(&v);
-}
 
-// One step of one entry; the products and sums of the moments are rounded one by one, so that codes do not depend on
-// how an expression is contracted.
-template <typename List>
-__device__ __forceinline__ void step_entry(const List& c, const StepEntry& t, float coef, float g, float& w, float& m, float& v) {
-  g = __fmul_rn(g, coef);
-  m = __fadd_rn(__fmul_rn(m, c.beta1), __fmul_rn(g, c.one_beta1));
-  v = __fadd_rn(__fmul_rn(v, c.beta2), __fmul_rn(__fmul_rn(g, g), c.one_beta2));
-  const float denominator = fmaf(sqrt_approx(v), c.root_bc2, c.eps);
-  w = w * t.decay - __fdividef(m, denominator) * t.rate;
-}
-
-// Entry j of a lane: 8 lane + j where vectors are used, 32 j + lane otherwise.
 template <int N>
 __global__ void __launch_bounds__(kStepThreads) adamw_kernel(const __grid_constant__ StepList<N> list) {
   const int lane = threadIdx.x & 31;
   const uint32_t warps = gridDim.x * (kStepThreads / 32);
+  pdl_launch_dependents();
+  pdl_wait();
   float coef = 1.f;
   if (list.grad_norm) {
     const float norm = *list.grad_norm;
@@ -289,135 +497,14 @@ __global__ void __launch_bounds__(kStepThreads) adamw_kernel(const __grid_consta
   for (uint32_t piece = blockIdx.x * (kStepThreads / 32) + (threadIdx.x >> 5); piece < list.pieces; piece += warps) {
     advance(list, piece, e);
     const StepEntry& t = list.e[e];
-    const uint32_t kind = t.kind, group = piece - t.begin;
-    const long long first = (long long)group * kGroup;
-    const bool codes = kind & kCodes, p_bf16 = kind & kPBf16, g_bf16 = kind & kGBf16, master = kind & kMaster;
-    const bool wide = (kind & kWide) && t.n - first >= kGroup;
-    const int left = (int)min((long long)kGroup, t.n - first);
-    float w[kPer], g[kPer], m[kPer], v[kPer], sm = 0.f, sv = 0.f;
-    if (codes) {
-      sm = t.m_scale[group];
-      sv = t.v_scale[group];
-    }
-    if (wide) {
-      const long long at = first + lane * kPer;
-      uint4 rw[2], rg[2], rm[2], rv[2];
-      // every load is under way before the first value is looked at
-      if (master) load8_f32(t.master + at, rw);
-      else if (p_bf16) rw[0] = *reinterpret_cast<const uint4*>(static_cast<const __nv_bfloat16*>(t.p) + at);
-      else load8_f32(static_cast<const float*>(t.p) + at, rw);
-      if (g_bf16) rg[0] = ld_stream16(static_cast<const __nv_bfloat16*>(t.g) + at);
-      else {
-        rg[0] = ld_stream16(static_cast<const float*>(t.g) + at);
-        rg[1] = ld_stream16(static_cast<const float*>(t.g) + at + 4);
-      }
-      if (codes) {
-        const uint2 a = *reinterpret_cast<const uint2*>(static_cast<const int8_t*>(t.m) + at);
-        const uint2 b = *reinterpret_cast<const uint2*>(static_cast<const uint8_t*>(t.v) + at);
-        rm[0] = make_uint4(a.x, a.y, 0, 0);
-        rv[0] = make_uint4(b.x, b.y, 0, 0);
-      } else {
-        load8_f32(static_cast<const float*>(t.m) + at, rm);
-        load8_f32(static_cast<const float*>(t.v) + at, rv);
-      }
-      floats_of(rw, p_bf16 && !master, w);
-      floats_of(rg, g_bf16, g);
-      if (codes) {
-        const float um = unit_m(sm), uv = unit_v(sv);
-#pragma unroll
-        for (int j = 0; j < kPer; ++j) {
-          m[j] = code_m((int)(int8_t)((j < 4 ? rm[0].x : rm[0].y) >> (8 * (j & 3))), um);
-          v[j] = code_v((int)(uint8_t)((j < 4 ? rv[0].x : rv[0].y) >> (8 * (j & 3))), uv);
-        }
-      } else {
-        floats_of(rm, false, m);
-        floats_of(rv, false, v);
-      }
+    const uint32_t group = piece - t.begin;
+    const bool wide = (t.kind & kWide) && t.n - (long long)group * kGroup >= kGroup;
+    if (t.kind & kCodes) {
+      if (wide) step_group<true, true>(list, t, group, coef, lane);
+      else step_group<true, false>(list, t, group, coef, lane);
     } else {
-      const float um = unit_m(sm), uv = unit_v(sv);
-#pragma unroll
-      for (int j = 0; j < kPer; ++j) {
-        w[j] = g[j] = m[j] = v[j] = 0.f;
-        const int i = 32 * j + lane;
-        if (i >= left) continue;
-        const long long at = first + i;
-        w[j] = master ? t.master[at] : p_bf16 ? __bfloat162float(static_cast<const __nv_bfloat16*>(t.p)[at]) : static_cast<const float*>(t.p)[at];
-        g[j] = g_bf16 ? __bfloat162float(static_cast<const __nv_bfloat16*>(t.g)[at]) : static_cast<const float*>(t.g)[at];
-        m[j] = codes ? code_m(static_cast<const int8_t*>(t.m)[at], um) : static_cast<const float*>(t.m)[at];
-        v[j] = codes ? code_v(static_cast<const uint8_t*>(t.v)[at], uv) : static_cast<const float*>(t.v)[at];
-      }
-    }
-    float most_m = 0.f, most_v = 0.f;
-    uint32_t bits_m = 0, bits_v = 0;
-#pragma unroll
-    for (int j = 0; j < kPer; ++j) {
-      step_entry(list, t, coef, g[j], w[j], m[j], v[j]);
-      if (!wide && 32 * j + lane >= left) m[j] = v[j] = 0.f;
-      bits_m = max(bits_m, __float_as_uint(m[j]) & 0x7fffffffu);
-      bits_v = max(bits_v, __float_as_uint(v[j]) & 0x7fffffffu);
-    }
-    int8_t cm[kPer];
-    uint8_t cv[kPer];
-    if (codes) {
-      most_m = warp_most(__uint_as_float(bits_m));
-      most_v = warp_most(__uint_as_float(bits_v));
-      float im, iv;
-      sm = group_scale(most_m, im);
-      sv = group_scale(most_v, iv);
-#pragma unroll
-      for (int j = 0; j < kPer; ++j) {
-        const int a = code_of_square(__fmul_rn(__fmul_rn(fabsf(m[j]), im), 16129.f));
-        const int b = code_of_fourth(__fmul_rn(__fmul_rn(v[j], iv), 4228250624.f));
-        cm[j] = (int8_t)(im == 0.f ? 0 : m[j] < 0.f ? -a : a);
-        cv[j] = (uint8_t)(iv == 0.f ? 0 : v[j] > 0.f ? max(b, 1) : b);
-      }
-      if (lane == 0) {
-        t.m_scale[group] = sm;
-        t.v_scale[group] = sv;
-      }
-    }
-    if (wide) {
-      const long long at = first + lane * kPer;
-      if (p_bf16) {
-        *reinterpret_cast<uint4*>(static_cast<__nv_bfloat16*>(t.p) + at) =
-            make_uint4(two_bf16(w[0], w[1]), two_bf16(w[2], w[3]), two_bf16(w[4], w[5]), two_bf16(w[6], w[7]));
-        if (master) store8_f32(t.master + at, w);
-      } else {
-        store8_f32(static_cast<float*>(t.p) + at, w);
-      }
-      if (codes) {
-        uint32_t a[2] = {0, 0}, b[2] = {0, 0};
-#pragma unroll
-        for (int j = 0; j < kPer; ++j) {
-          a[j >> 2] |= (uint32_t)(uint8_t)cm[j] << (8 * (j & 3));
-          b[j >> 2] |= (uint32_t)cv[j] << (8 * (j & 3));
-        }
-        *reinterpret_cast<uint2*>(static_cast<int8_t*>(t.m) + at) = make_uint2(a[0], a[1]);
-        *reinterpret_cast<uint2*>(static_cast<uint8_t*>(t.v) + at) = make_uint2(b[0], b[1]);
-      } else {
-        store8_f32(static_cast<float*>(t.m) + at, m);
-        store8_f32(static_cast<float*>(t.v) + at, v);
-      }
-    } else {
-#pragma unroll
-      for (int j = 0; j < kPer; ++j) {
-        const int i = 32 * j + lane;
-        if (i >= left) continue;
-        const long long at = first + i;
-        if (p_bf16) {
-          static_cast<__nv_bfloat16*>(t.p)[at] = __float2bfloat16(w[j]);
-          if (master) t.master[at] = w[j];
-        } else {
-          static_cast<float*>(t.p)[at] = w[j];
-        }
-        if (codes) {
-          static_cast<int8_t*>(t.m)[at] = cm[j];
-          static_cast<uint8_t*>(t.v)[at] = cv[j];
-        } else {
-          static_cast<float*>(t.m)[at] = m[j];
-          static_cast<float*>(t.v)[at] = v[j];
-        }
-      }
+      if (wide) step_group<false, true>(list, t, group, coef, lane);
+      else step_group<false, false>(list, t, group, coef, lane);
     }
   }
 }
@@ -446,8 +533,7 @@ cudaError_t list_launches(List& list, Kernel kernel, int n, const sffn_adamw_ten
     if (err != cudaSuccess) return err;
     const long long want = (pieces + kStepThreads / 32 - 1) / (kStepThreads / 32);
     const long long room = (long long)(per_sm > 0 ? per_sm : 1) * sm_count;
-    kernel<<<(unsigned)(want < room ? want : room), kStepThreads, 0, s>>>(list);
-    err = cudaGetLastError();
+    err = launch_pdl(kernel, dim3((unsigned)(want < room ? want : room)), dim3(kStepThreads), 0, s, list);
     if (err != cudaSuccess) return err;
   }
   return cudaSuccess;
@@ -469,8 +555,10 @@ cudaError_t adamw_launches(const sffn_adamw_tensor* t, int n, const sffn_adamw_c
     const sffn_adamw_tensor& a = t[i];
     e.p = a.p; e.g = a.g; e.master = a.master; e.m = a.m; e.v = a.v; e.m_scale = a.m_scale; e.v_scale = a.v_scale; e.n = a.n;
     e.kind = (a.p_dtype == SFFN_BF16 ? kPBf16 : 0) | (a.g_dtype == SFFN_BF16 ? kGBf16 : 0) | (a.master ? kMaster : 0) | (a.state_bits == 8 ? kCodes : 0);
-    const uintptr_t sa = a.state_bits == 8 ? 8 : 16;
-    if (aligned_to(a.p, 16) && aligned_to(a.g, 16) && aligned_to(a.master, 16) && aligned_to(a.m, sa) && aligned_to(a.v, sa)) e.kind |= kWide;
+    const uintptr_t state = a.state_bits == 8 ? 8 : 32;
+    if (aligned_to(a.p, a.p_dtype == SFFN_BF16 ? 16 : 32) && aligned_to(a.g, a.g_dtype == SFFN_BF16 ? 16 : 32) && aligned_to(a.master, 32) &&
+        aligned_to(a.m, state) && aligned_to(a.v, state))
+      e.kind |= kWide;
     e.decay = (float)(1.0 - a.lr * a.weight_decay);
     e.rate = (float)(a.lr / bc1);
   });
@@ -497,6 +585,8 @@ template <int N>
 __global__ void __launch_bounds__(kStepThreads) adamw_values_kernel(const __grid_constant__ ValueList<N> list) {
   const int lane = threadIdx.x & 31;
   const uint32_t warps = gridDim.x * (kStepThreads / 32);
+  pdl_launch_dependents();
+  pdl_wait();
   int e = 0;
   for (uint32_t piece = blockIdx.x * (kStepThreads / 32) + (threadIdx.x >> 5); piece < list.pieces; piece += warps) {
     advance(list, piece, e);
@@ -505,20 +595,21 @@ __global__ void __launch_bounds__(kStepThreads) adamw_values_kernel(const __grid
     const long long first = (long long)group * kGroup;
     const int left = (int)min((long long)kGroup, t.n - first);
     const float um = t.m_out ? unit_m(t.m_scale[group]) : 0.f, uv = t.v_out ? unit_v(t.v_scale[group]) : 0.f;
-    if (t.wide && left == kGroup) {  // four entries of a lane in each half, so that a warp's stores are 512 bytes in a row
-#pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        const long long at = first + 128 * h + 4 * lane;
-        if (t.m_out) {
-          const uint32_t w = *reinterpret_cast<const uint32_t*>(t.m + at);
-          *reinterpret_cast<float4*>(t.m_out + at) = make_float4(code_m((int8_t)w, um), code_m((int8_t)(w >> 8), um),
-                                                                 code_m((int8_t)(w >> 16), um), code_m((int8_t)(w >> 24), um));
-        }
-        if (t.v_out) {
-          const uint32_t w = *reinterpret_cast<const uint32_t*>(t.v + at);
-          *reinterpret_cast<float4*>(t.v_out + at) = make_float4(code_v((uint8_t)w, uv), code_v((uint8_t)(w >> 8), uv),
-                                                                 code_v((uint8_t)(w >> 16), uv), code_v((uint8_t)(w >> 24), uv));
-        }
+    if (t.wide && left == kGroup) {
+      const long long at = first + lane * kPer;
+      uint2 a, b;
+      if (t.m_out) a = *reinterpret_cast<const uint2*>(t.m + at);
+      if (t.v_out) b = *reinterpret_cast<const uint2*>(t.v + at);
+      f2 f[4];
+      if (t.m_out) {
+        codes_m(a.x, both(um), f);
+        codes_m(a.y, both(um), f + 2);
+        st32(t.m_out + at, f);
+      }
+      if (t.v_out) {
+        codes_v(b.x, both(uv), f);
+        codes_v(b.y, both(uv), f + 2);
+        st32(t.v_out + at, f);
       }
     } else {
       for (int i = lane; i < left; i += 32) {
@@ -540,7 +631,7 @@ cudaError_t value_launches(const sffn_adamw_tensor* t, int n, float* const* m_ou
     e.m_out = m_out ? m_out[i] : nullptr;
     e.v_out = v_out ? v_out[i] : nullptr;
     e.n = t[i].n;
-    e.wide = aligned_to(e.m, 4) && aligned_to(e.v, 4) && aligned_to(e.m_out, 16) && aligned_to(e.v_out, 16);
+    e.wide = aligned_to(e.m, 8) && aligned_to(e.v, 8) && aligned_to(e.m_out, 32) && aligned_to(e.v_out, 32);
   });
 }
 
