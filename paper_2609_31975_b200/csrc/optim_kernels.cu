@@ -183,7 +183,7 @@ cudaError_t norm_launches(const sffn_tensor* t, int n, float* norm, void* worksp
 
 // ---- AdamW -----------------------------------------------------------------------------------------------------------
 
-constexpr int kStepThreads = 256;
+constexpr int kStepThreads = 128;
 
 // What a tensor's kinds of storage are, in one word.
 constexpr uint32_t kPBf16 = 1, kGBf16 = 2, kMaster = 4, kCodes = 8, kWide = 16;  // kWide: every pointer allows vector accesses
@@ -201,7 +201,7 @@ struct StepEntry {
 template <int N>
 struct StepList {
   int n;
-  uint32_t pieces;
+  uint32_t pieces, run;  // run: groups of a piece
   const float* grad_norm;
   float max_norm, beta1, one_beta1, beta2, one_beta2, root_bc2, eps;  // root_bc2: 1 / sqrt(1 - beta2^step)
   StepEntry e[N];
@@ -239,40 +239,26 @@ __device__ __forceinline__ float max_nan(float a, float b) {
 }
 
 constexpr float kMagic = 12582912.f;   // 1.5 2^23: a small number added to it is rounded to an integer, in its low bits
-constexpr float kMargin = 2e-4f;       // how far a square root of at most 255 is certainly not off
 
-// Codes: the number of edges (k + 1/2)^2 (for v: the rounded square of that) at or below q.  The approximate root, made a
-// little too small, is rounded to an integer c that the code is never below and at most one above; whether q reaches the edge above
-// c is then seen in numbers that fp32 holds exactly: q - c^2 >= c + 1/4.  Left in the low bits of *r, with the sign of m.
-__device__ __forceinline__ void code_squares(f2 m, f2 q, uint32_t* r) {
-  float q0, q1, m0, m1;
-  halves(q, q0, q1);
-  halves(m, m0, m1);
-  const f2 s = add2_b64(pack2(sqrt_approx(q0), sqrt_approx(q1)), both(-kMargin));
-  const f2 n = add2_b64(s, both(kMagic));
-  const f2 c = add2_b64(n, both(-kMagic));
-  const f2 minus = mul2(c, both(-1.f));
-  const f2 over = fma2_b64(minus, c, q), edge = add2_b64(c, both(0.25f));
-  int c0 = __float_as_int(low(n)) - __float_as_int(kMagic), c1 = __float_as_int(high(n)) - __float_as_int(kMagic);
-  if (low(over) >= low(edge)) ++c0;
-  if (high(over) >= high(edge)) ++c1;
-  r[0] = m0 < 0.f ? -c0 : c0;
-  r[1] = m1 < 0.f ? -c1 : c1;
+// Codes: the number of edges (k + 1/2)^2, k < 127 (for v: the rounded squares of those, k < 255) at or below q.  An approximate root
+// rounded to an integer is the code unless it lies within kNear of an edge.  That leaves one group in fifteen, where the edges
+// are asked: the root, made a little too small, is rounded to an integer c that the code is never below and at most one above, and
+// whether q reaches the edge above c is seen in numbers that fp32 holds exactly.
+// (Roots are off by at most 255 (5e-7 / 2 + 2e-7) = 1.2e-4: products and approximate roots of 2 to 5 roundings.)
+constexpr float kNear = 1.5e-4f, kMargin = 2e-4f;
+
+__device__ __forceinline__ uint32_t code_of_square(float m, float q) {
+  const float n = sqrt_approx(q) - kMargin + kMagic, c = n - kMagic;
+  int code = __float_as_int(n) - __float_as_int(kMagic);
+  if (fmaf(-c, c, q) >= c + 0.25f) ++code;
+  return m < 0.f ? -code : code;
 }
-// `half_root`: an approximate square root of q.
-__device__ __forceinline__ void code_fourths(f2 v, f2 q, f2 half_root, uint32_t* r) {
-  float v0, v1;
-  halves(v, v0, v1);
-  const f2 s = add2_b64(pack2(sqrt_approx(low(half_root)), sqrt_approx(high(half_root))), both(-kMargin));
-  const f2 n = add2_b64(s, both(kMagic));
-  const f2 c = add2_b64(n, both(-kMagic));
-  const f2 t = fma2_b64(c, c, add2_b64(c, both(0.25f)));  // (c + 1/2)^2, exact
-  const f2 edge = mul2(t, t);
-  int c0 = __float_as_int(low(n)) - __float_as_int(kMagic), c1 = __float_as_int(high(n)) - __float_as_int(kMagic);
-  if (low(q) >= low(edge)) ++c0;
-  if (high(q) >= high(edge)) ++c1;
-  r[0] = max(c0, v0 > 0.f ? 1 : 0);  // what is not zero stays so: it divides
-  r[1] = max(c1, v1 > 0.f ? 1 : 0);
+__device__ __forceinline__ uint32_t code_of_fourth(float v, float q) {
+  const float n = sqrt_approx(sqrt_approx(q)) - kMargin + kMagic, c = n - kMagic;
+  const float t = fmaf(c, c, c + 0.25f);  // (c + 1/2)^2, exact
+  int code = __float_as_int(n) - __float_as_int(kMagic);
+  if (q >= __fmul_rn(t, t)) ++code;
+  return max(code, v > 0.f ? 1 : 0);      // what is not zero stays so: it divides
 }
 
 __device__ __forceinline__ float code_m(int c, float unit) { return __fmul_rn((float)(c * abs(c)), unit); }
@@ -287,7 +273,7 @@ __device__ __forceinline__ void codes_m(uint32_t w, f2 unit, f2* v) {
 #pragma unroll
   for (int i = 0; i < 2; ++i) {
     const f2 c = add2_b64(pack2(__uint_as_float(__byte_perm(w, 0x4b000000u, i ? 0x7442 : 0x7440)), __uint_as_float(__byte_perm(w, 0x4b000000u, i ? 0x7443 : 0x7441))), bias);
-    v[i] = mul2(mul2(c, pack2(fabsf(low(c)), fabsf(high(c)))), unit);
+    v[i] = mul2(pack2(__fmul_rn(low(c), fabsf(low(c))), __fmul_rn(high(c), fabsf(high(c)))), unit);
   }
 }
 __device__ __forceinline__ void codes_v(uint32_t w, f2 unit, f2* v) {
@@ -332,64 +318,12 @@ __device__ __forceinline__ uint32_t two_bf16(f2 v) {
 // Eight entries of a lane as four pairs.  Entry j of a lane: 8 lane + j where vectors are used (WIDE), 32 j + lane otherwise.
 // CODES: the moments are held in codes.
 template <bool CODES, bool WIDE, typename List>
-__device__ __forceinline__ void step_group(const List& c, const StepEntry& t, uint32_t group, float coef, int lane) {
+__device__ __forceinline__ void finish_group(const List& c, const StepEntry& t, uint32_t group, float coef, int lane, f2* w, f2* g, f2* m, f2* v) {
   const uint32_t kind = t.kind;
   const long long first = (long long)group * kGroup;
-  const bool p_bf16 = kind & kPBf16, g_bf16 = kind & kGBf16, master = kind & kMaster;
+  const bool p_bf16 = kind & kPBf16, master = kind & kMaster;
   const int left = WIDE ? kGroup : (int)min((long long)kGroup, t.n - first);
-  f2 w[4], g[4], m[4], v[4];
-  float sm = 0.f, sv = 0.f;
-  if (CODES) {
-    sm = t.m_scale[group];
-    sv = t.v_scale[group];
-  }
-  if constexpr (WIDE) {
-    const long long at = first + lane * kPer;
-    uint32_t rw[8], rg[8], rm[8], rv[8];
-    // every load is under way before the first value is looked at
-    if (master) ld32(t.master + at, rw);
-    else if (p_bf16) ld16(static_cast<const __nv_bfloat16*>(t.p) + at, rw);
-    else ld32(static_cast<const float*>(t.p) + at, rw);
-    if (g_bf16) ld16(static_cast<const __nv_bfloat16*>(t.g) + at, rg);
-    else ld32(static_cast<const float*>(t.g) + at, rg);
-    if constexpr (CODES) {
-      const uint2 a = *reinterpret_cast<const uint2*>(static_cast<const int8_t*>(t.m) + at);
-      const uint2 b = *reinterpret_cast<const uint2*>(static_cast<const uint8_t*>(t.v) + at);
-      rm[0] = a.x; rm[1] = a.y;
-      rv[0] = b.x; rv[1] = b.y;
-    } else {
-      ld32(static_cast<const float*>(t.m) + at, rm);
-      ld32(static_cast<const float*>(t.v) + at, rv);
-    }
-    pairs_of(rw, p_bf16 && !master, w);
-    pairs_of(rg, g_bf16, g);
-    if constexpr (CODES) {
-      const f2 um = both(unit_m(sm)), uv = both(unit_v(sv));
-      codes_m(rm[0], um, m); codes_m(rm[1], um, m + 2);
-      codes_v(rv[0], uv, v); codes_v(rv[1], uv, v + 2);
-    } else {
-      pairs_of(rm, false, m);
-      pairs_of(rv, false, v);
-    }
-  } else {
-    const float um = unit_m(sm), uv = unit_v(sv);
-#pragma unroll
-    for (int q = 0; q < 4; ++q) {
-      float e[4][2];
-#pragma unroll
-      for (int j = 0; j < 2; ++j) {
-        const int i = 32 * (2 * q + j) + lane;
-        const long long at = first + i;
-        e[0][j] = e[1][j] = e[2][j] = e[3][j] = 0.f;
-        if (i >= left) continue;
-        e[0][j] = master ? t.master[at] : p_bf16 ? __bfloat162float(static_cast<const __nv_bfloat16*>(t.p)[at]) : static_cast<const float*>(t.p)[at];
-        e[1][j] = g_bf16 ? __bfloat162float(static_cast<const __nv_bfloat16*>(t.g)[at]) : static_cast<const float*>(t.g)[at];
-        e[2][j] = CODES ? code_m(static_cast<const int8_t*>(t.m)[at], um) : static_cast<const float*>(t.m)[at];
-        e[3][j] = CODES ? code_v(static_cast<const uint8_t*>(t.v)[at], uv) : static_cast<const float*>(t.v)[at];
-      }
-      w[q] = pack2(e[0][0], e[0][1]); g[q] = pack2(e[1][0], e[1][1]); m[q] = pack2(e[2][0], e[2][1]); v[q] = pack2(e[3][0], e[3][1]);
-    }
-  }
+  float sm, sv;
   float most_m = 0.f, most_v = 0.f;
   f2 root[4];
 #pragma unroll
@@ -413,15 +347,33 @@ __device__ __forceinline__ void step_group(const List& c, const StepEntry& t, ui
     sm = group_scale(warp_most(most_m), im);
     sv = group_scale(warp_most(most_v), iv);
     const float half = 65025.f * sqrt_approx(iv);  // sqrt(255^4 / scale)
-    const bool small = iv > 1.2379400392853803e27f;  // scale < 2^-90: roots of single values may have been taken for zeros
+    float near = 0.f;
 #pragma unroll
     for (int q = 0; q < 4; ++q) {
-      const f2 a = pack2(fabsf(low(m[q])), fabsf(high(m[q])));
-      code_squares(m[q], mul2(mul2(a, both(im)), both(16129.f)), cm + 2 * q);
+      float m0, m1;
+      halves(m[q], m0, m1);
+      const f2 a = mul2(pack2(__fmul_rn(fabsf(m0), im), __fmul_rn(fabsf(m1), im)), both(16129.f));
       const f2 b = mul2(mul2(v[q], both(iv)), both(4228250624.f));
-      root[q] = mul2(root[q], both(half));
-      if (small) root[q] = pack2(sqrt_approx(low(b)), sqrt_approx(high(b)));
-      code_fourths(v[q], b, root[q], cv + 2 * q);
+      const f2 hr = mul2(root[q], both(half));
+      const f2 sa = pack2(copysignf(sqrt_approx(low(a)), m0), copysignf(sqrt_approx(high(a)), m1));
+      const f2 big = mul2(b, both(8.507059e37f));  // 2^126: beyond one for every b that counts
+      const f2 sb = pack2(fmaxf(sqrt_approx(low(hr)), fminf(low(big), 0.6f)), fmaxf(sqrt_approx(high(hr)), fminf(high(big), 0.6f)));
+      const f2 na = add2_b64(sa, both(kMagic)), nb = add2_b64(sb, both(kMagic));
+      const f2 da = fma2_b64(add2_b64(na, both(-kMagic)), both(-1.f), sa), db = fma2_b64(add2_b64(nb, both(-kMagic)), both(-1.f), sb);
+      near = fmaxf(near, fmaxf(fabsf(low(da)), fabsf(high(da))));
+      near = fmaxf(near, fmaxf(fabsf(low(db)), fabsf(high(db))));
+      cm[2 * q] = __float_as_uint(low(na)); cm[2 * q + 1] = __float_as_uint(high(na));
+      cv[2 * q] = __float_as_uint(low(nb)); cv[2 * q + 1] = __float_as_uint(high(nb));
+    }
+    // The edges decide: a root near one, a scale below 2^-90 (single values may have counted as zeros when their roots were
+    // taken) or above one (quotients may have).
+    if (__any_sync(0xffffffffu, near > 0.5f - kNear) || iv > 1.2379400392853803e27f || sv > 1.f) {
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        const float mj = j & 1 ? high(m[j / 2]) : low(m[j / 2]), vj = j & 1 ? high(v[j / 2]) : low(v[j / 2]);
+        cm[j] = code_of_square(mj, __fmul_rn(__fmul_rn(fabsf(mj), im), 16129.f));
+        cv[j] = code_of_fourth(vj, __fmul_rn(__fmul_rn(vj, iv), 4228250624.f));
+      }
     }
     if (im == 0.f) {
 #pragma unroll
@@ -481,8 +433,101 @@ __device__ __forceinline__ void step_group(const List& c, const StepEntry& t, ui
   }
 }
 
-template <int N>
-__global__ void __launch_bounds__(kStepThreads) adamw_kernel(const __grid_constant__ StepList<N> list) {
+template <bool CODES, bool WIDE, typename List>
+__device__ __forceinline__ void step_group(const List& c, const StepEntry& t, uint32_t group, float coef, int lane) {
+  const uint32_t kind = t.kind;
+  const long long first = (long long)group * kGroup;
+  const bool p_bf16 = kind & kPBf16, g_bf16 = kind & kGBf16, master = kind & kMaster;
+  const int left = WIDE ? kGroup : (int)min((long long)kGroup, t.n - first);
+  f2 w[4], g[4], m[4], v[4];
+  float sm = 0.f, sv = 0.f;
+  if (CODES) {
+    sm = t.m_scale[group];
+    sv = t.v_scale[group];
+  }
+  if constexpr (WIDE) {
+    const long long at = first + lane * kPer;
+    uint32_t rw[8], rg[8], rm[8], rv[8];
+    // every load is under way before the first value is looked at
+    if (master) ld32(t.master + at, rw);
+    else if (p_bf16) ld16(static_cast<const __nv_bfloat16*>(t.p) + at, rw);
+    else ld32(static_cast<const float*>(t.p) + at, rw);
+    if (g_bf16) ld16(static_cast<const __nv_bfloat16*>(t.g) + at, rg);
+    else ld32(static_cast<const float*>(t.g) + at, rg);
+    if constexpr (CODES) {
+      const uint2 a = *reinterpret_cast<const uint2*>(static_cast<const int8_t*>(t.m) + at);
+      const uint2 b = *reinterpret_cast<const uint2*>(static_cast<const uint8_t*>(t.v) + at);
+      rm[0] = a.x; rm[1] = a.y;
+      rv[0] = b.x; rv[1] = b.y;
+    } else {
+      ld32(static_cast<const float*>(t.m) + at, rm);
+      ld32(static_cast<const float*>(t.v) + at, rv);
+    }
+    pairs_of(rw, p_bf16 && !master, w);
+    pairs_of(rg, g_bf16, g);
+    if constexpr (CODES) {
+      const f2 um = both(unit_m(sm)), uv = both(unit_v(sv));
+      codes_m(rm[0], um, m); codes_m(rm[1], um, m + 2);
+      codes_v(rv[0], uv, v); codes_v(rv[1], uv, v + 2);
+    } else {
+      pairs_of(rm, false, m);
+      pairs_of(rv, false, v);
+    }
+  } else {
+    const float um = unit_m(sm), uv = unit_v(sv);
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      float e[4][2];
+#pragma unroll
+      for (int j = 0; j < 2; ++j) {
+        const int i = 32 * (2 * q + j) + lane;
+        const long long at = first + i;
+        e[0][j] = e[1][j] = e[2][j] = e[3][j] = 0.f;
+        if (i >= left) continue;
+        e[0][j] = master ? t.master[at] : p_bf16 ? __bfloat162float(static_cast<const __nv_bfloat16*>(t.p)[at]) : static_cast<const float*>(t.p)[at];
+        e[1][j] = g_bf16 ? __bfloat162float(static_cast<const __nv_bfloat16*>(t.g)[at]) : static_cast<const float*>(t.g)[at];
+        e[2][j] = CODES ? code_m(static_cast<const int8_t*>(t.m)[at], um) : static_cast<const float*>(t.m)[at];
+        e[3][j] = CODES ? code_v(static_cast<const uint8_t*>(t.v)[at], uv) : static_cast<const float*>(t.v)[at];
+      }
+      w[q] = pack2(e[0][0], e[0][1]); g[q] = pack2(e[1][0], e[1][1]); m[q] = pack2(e[2][0], e[2][1]); v[q] = pack2(e[3][0], e[3][1]);
+    }
+  }
+  finish_group<CODES, WIDE>(c, t, group, coef, lane, w, g, m, v);
+}
+
+// bf16 parameters and gradients, moments in codes: a group's 24 bytes a lane.
+struct HalfGroup {
+  uint4 w, g;
+  uint2 m, v;
+  float sm, sv;
+  __device__ __forceinline__ void load(const StepEntry& t, uint32_t group, int lane) {
+    const long long at = (long long)group * kGroup + lane * kPer;
+    w = *reinterpret_cast<const uint4*>(static_cast<const __nv_bfloat16*>(t.p) + at);
+    g = ld_stream16(static_cast<const __nv_bfloat16*>(t.g) + at);
+    m = *reinterpret_cast<const uint2*>(static_cast<const int8_t*>(t.m) + at);
+    v = *reinterpret_cast<const uint2*>(static_cast<const uint8_t*>(t.v) + at);
+    sm = t.m_scale[group];
+    sv = t.v_scale[group];
+  }
+  template <typename List>
+  __device__ __forceinline__ void step(const List& c, const StepEntry& t, uint32_t group, float coef, int lane) const {
+    f2 pw[4], pg[4], pm[4], pv[4];
+    pairs_of(reinterpret_cast<const uint32_t*>(&w), true, pw);
+    pairs_of(reinterpret_cast<const uint32_t*>(&g), true, pg);
+    const f2 um = both(unit_m(sm)), uv = both(unit_v(sv));
+    codes_m(m.x, um, pm); codes_m(m.y, um, pm + 2);
+    codes_v(v.x, uv, pv); codes_v(v.y, uv, pv + 2);
+    finish_group<true, true>(c, t, group, coef, lane, pw, pg, pm, pv);
+  }
+};
+
+// What a launch's tensors have in common: moments in 32 bits; in codes; in codes, with bf16 parameters and gradients (and no copies).
+enum { kWords = 0, kAnyCodes = 1, kHalfCodes = 2 };
+
+// A warp's piece is `run` groups in a row.  The step of a group is some 550 instructions a warp, half of which wait for the
+// group's loads: kHalfCodes has the next group's under way meanwhile.
+template <int N, int WHAT>
+__global__ void __launch_bounds__(kStepThreads, WHAT == kHalfCodes ? 5 : 6) adamw_kernel(const __grid_constant__ StepList<N> list) {
   const int lane = threadIdx.x & 31;
   const uint32_t warps = gridDim.x * (kStepThreads / 32);
   pdl_launch_dependents();
@@ -497,28 +542,41 @@ __global__ void __launch_bounds__(kStepThreads) adamw_kernel(const __grid_consta
   for (uint32_t piece = blockIdx.x * (kStepThreads / 32) + (threadIdx.x >> 5); piece < list.pieces; piece += warps) {
     advance(list, piece, e);
     const StepEntry& t = list.e[e];
-    const uint32_t group = piece - t.begin;
-    const bool wide = (t.kind & kWide) && t.n - (long long)group * kGroup >= kGroup;
-    if (t.kind & kCodes) {
-      if (wide) step_group<true, true>(list, t, group, coef, lane);
-      else step_group<true, false>(list, t, group, coef, lane);
+    uint32_t group = (piece - t.begin) * list.run;
+    const uint32_t end = min(group + list.run, (uint32_t)((t.n + kGroup - 1) / kGroup));
+    const uint32_t wide_end = t.kind & kWide ? min(end, (uint32_t)(t.n / kGroup)) : group;
+    if constexpr (WHAT == kHalfCodes) {
+      HalfGroup now, next;
+      if (group < wide_end) now.load(t, group, lane);
+#pragma unroll 1
+      for (; group < wide_end; ++group) {
+        if (group + 1 < wide_end) next.load(t, group + 1, lane);
+        now.step(list, t, group, coef, lane);
+        now = next;
+      }
     } else {
-      if (wide) step_group<false, true>(list, t, group, coef, lane);
-      else step_group<false, false>(list, t, group, coef, lane);
+#pragma unroll 1
+      for (; group < wide_end; ++group) step_group<WHAT != kWords, true>(list, t, group, coef, lane);
     }
+#pragma unroll 1
+    for (; group < end; ++group) step_group<WHAT != kWords, false>(list, t, group, coef, lane);
   }
 }
 
 inline bool aligned_to(const void* p, uintptr_t a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) == 0; }
 
-// Launches a kernel over a list of tensors, at most N at a time: `fill` writes one tensor's entry.
-template <int N, typename List, typename Kernel, typename Fill>
-cudaError_t list_launches(List& list, Kernel kernel, int n, const sffn_adamw_tensor* t, int sm_count, cudaStream_t s, Fill fill) {
+inline int what_of(const sffn_adamw_tensor& t) {
+  return t.state_bits != 8 ? kWords : t.p_dtype == SFFN_BF16 && t.g_dtype == SFFN_BF16 && !t.master ? kHalfCodes : kAnyCodes;
+}
+
+// Launches a kernel over the tensors of a list that `mine` names, at most N at a time: `fill` writes one's entry.
+template <int N, typename List, typename Kernel, typename Mine, typename Fill>
+cudaError_t list_launches(List& list, Kernel kernel, int n, const sffn_adamw_tensor* t, int sm_count, cudaStream_t s, Mine mine, Fill fill) {
   for (int at = 0; at < n;) {
     list.n = 0;
     long long pieces = 0;
     for (; at < n && list.n < N; ++at) {
-      const long long own = (t[at].n + kGroup - 1) / kGroup;
+      const long long own = mine(t[at]) ? ((t[at].n + kGroup - 1) / kGroup + list.run - 1) / list.run : 0;
       if (own == 0) continue;
       if (pieces + own > 0xffffffffll - (1 << 20)) break;
       auto& e = list.e[list.n++];
@@ -539,6 +597,13 @@ cudaError_t list_launches(List& list, Kernel kernel, int n, const sffn_adamw_ten
   return cudaSuccess;
 }
 
+// Groups of a piece: `most` once every warp of the device has several such pieces.
+inline uint32_t run_of(const sffn_adamw_tensor* t, int n, int sm_count, uint32_t most) {
+  long long groups = 0;
+  for (int i = 0; i < n; ++i) groups += (t[i].n + kGroup - 1) / kGroup;
+  return groups > 256ll * most * sm_count ? most : 1;
+}
+
 template <int N>
 cudaError_t adamw_launches(const sffn_adamw_tensor* t, int n, const sffn_adamw_config& c, int sm_count, cudaStream_t s) {
   StepList<N> list;
@@ -551,7 +616,7 @@ cudaError_t adamw_launches(const sffn_adamw_tensor* t, int n, const sffn_adamw_c
   list.eps = (float)c.eps;
   const double bc1 = 1.0 - pow(c.beta1, (double)c.step), bc2 = 1.0 - pow(c.beta2, (double)c.step);
   list.root_bc2 = (float)(1.0 / sqrt(bc2));
-  return list_launches<N>(list, adamw_kernel<N>, n, t, sm_count, s, [&](StepEntry& e, int i) {
+  auto fill = [&](StepEntry& e, int i) {
     const sffn_adamw_tensor& a = t[i];
     e.p = a.p; e.g = a.g; e.master = a.master; e.m = a.m; e.v = a.v; e.m_scale = a.m_scale; e.v_scale = a.v_scale; e.n = a.n;
     e.kind = (a.p_dtype == SFFN_BF16 ? kPBf16 : 0) | (a.g_dtype == SFFN_BF16 ? kGBf16 : 0) | (a.master ? kMaster : 0) | (a.state_bits == 8 ? kCodes : 0);
@@ -561,7 +626,15 @@ cudaError_t adamw_launches(const sffn_adamw_tensor* t, int n, const sffn_adamw_c
       e.kind |= kWide;
     e.decay = (float)(1.0 - a.lr * a.weight_decay);
     e.rate = (float)(a.lr / bc1);
-  });
+  };
+  list.run = 1;
+  cudaError_t err = list_launches<N>(list, adamw_kernel<N, kWords>, n, t, sm_count, s, [](const sffn_adamw_tensor& a) { return what_of(a) == kWords; }, fill);
+  if (err != cudaSuccess) return err;
+  list.run = run_of(t, n, sm_count, 16);
+  err = list_launches<N>(list, adamw_kernel<N, kHalfCodes>, n, t, sm_count, s, [](const sffn_adamw_tensor& a) { return what_of(a) == kHalfCodes; }, fill);
+  if (err != cudaSuccess) return err;
+  list.run = 1;
+  return list_launches<N>(list, adamw_kernel<N, kAnyCodes>, n, t, sm_count, s, [](const sffn_adamw_tensor& a) { return what_of(a) == kAnyCodes; }, fill);
 }
 
 // ---- values of 8-bit moments -----------------------------------------------------------------------------------------
@@ -577,7 +650,7 @@ struct ValueEntry {
 template <int N>
 struct ValueList {
   int n;
-  uint32_t pieces;
+  uint32_t pieces, run;
   ValueEntry e[N];
 };
 
@@ -591,30 +664,39 @@ __global__ void __launch_bounds__(kStepThreads) adamw_values_kernel(const __grid
   for (uint32_t piece = blockIdx.x * (kStepThreads / 32) + (threadIdx.x >> 5); piece < list.pieces; piece += warps) {
     advance(list, piece, e);
     const ValueEntry& t = list.e[e];
-    const uint32_t group = piece - t.begin;
-    const long long first = (long long)group * kGroup;
-    const int left = (int)min((long long)kGroup, t.n - first);
-    const float um = t.m_out ? unit_m(t.m_scale[group]) : 0.f, uv = t.v_out ? unit_v(t.v_scale[group]) : 0.f;
-    if (t.wide && left == kGroup) {
-      const long long at = first + lane * kPer;
-      uint2 a, b;
-      if (t.m_out) a = *reinterpret_cast<const uint2*>(t.m + at);
-      if (t.v_out) b = *reinterpret_cast<const uint2*>(t.v + at);
-      f2 f[4];
-      if (t.m_out) {
-        codes_m(a.x, both(um), f);
-        codes_m(a.y, both(um), f + 2);
-        st32(t.m_out + at, f);
+    const uint32_t group0 = (piece - t.begin) * list.run;
+    const long long first = (long long)group0 * kGroup;
+    if (t.wide && list.run == 4 && t.n - first >= 4 * kGroup) {  // four groups, every load under way first
+      uint2 a[4], b[4];
+      float um[4], uv[4];
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        const long long at = first + q * kGroup + lane * kPer;
+        if (t.m_out) a[q] = __ldcs(reinterpret_cast<const uint2*>(t.m + at));
+        if (t.v_out) b[q] = __ldcs(reinterpret_cast<const uint2*>(t.v + at));
+        um[q] = t.m_out ? t.m_scale[group0 + q] : 0.f;
+        uv[q] = t.v_out ? t.v_scale[group0 + q] : 0.f;
       }
-      if (t.v_out) {
-        codes_v(b.x, both(uv), f);
-        codes_v(b.y, both(uv), f + 2);
-        st32(t.v_out + at, f);
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        const long long at = first + q * kGroup + lane * kPer;
+        f2 f[4];
+        if (t.m_out) {
+          codes_m(a[q].x, both(unit_m(um[q])), f);
+          codes_m(a[q].y, both(unit_m(um[q])), f + 2);
+          st32(t.m_out + at, f);
+        }
+        if (t.v_out) {
+          codes_v(b[q].x, both(unit_v(uv[q])), f);
+          codes_v(b[q].y, both(unit_v(uv[q])), f + 2);
+          st32(t.v_out + at, f);
+        }
       }
     } else {
-      for (int i = lane; i < left; i += 32) {
-        if (t.m_out) t.m_out[first + i] = code_m(t.m[first + i], um);
-        if (t.v_out) t.v_out[first + i] = code_v(t.v[first + i], uv);
+      const long long end = min(t.n, first + (long long)list.run * kGroup);
+      for (long long i = first + lane; i < end; i += 32) {
+        if (t.m_out) t.m_out[i] = code_m(t.m[i], unit_m(t.m_scale[i / kGroup]));
+        if (t.v_out) t.v_out[i] = code_v(t.v[i], unit_v(t.v_scale[i / kGroup]));
       }
     }
   }
@@ -623,7 +705,8 @@ __global__ void __launch_bounds__(kStepThreads) adamw_values_kernel(const __grid
 template <int N>
 cudaError_t value_launches(const sffn_adamw_tensor* t, int n, float* const* m_out, float* const* v_out, int sm_count, cudaStream_t s) {
   ValueList<N> list;
-  return list_launches<N>(list, adamw_values_kernel<N>, n, t, sm_count, s, [&](ValueEntry& e, int i) {
+  list.run = run_of(t, n, sm_count, 4);
+  return list_launches<N>(list, adamw_values_kernel<N>, n, t, sm_count, s, [](const sffn_adamw_tensor&) { return true; }, [&](ValueEntry& e, int i) {
     e.m = static_cast<const int8_t*>(t[i].m);
     e.v = static_cast<const uint8_t*>(t[i].v);
     e.m_scale = t[i].m_scale;
