@@ -92,9 +92,9 @@ struct TrainUmma {
   int32_t* status;
 };
 constexpr int kTrainUmmaPairs = 80;    // pairs of CTAs at most
-constexpr size_t kTrainPieceBytes = 256 * 256 * 4;
+constexpr size_t kTrainPieceBytes = 256 * 512 * 4;
 constexpr size_t kTrainPartialBytes = 2 * kTrainUmmaPairs * kTrainPieceBytes;
-constexpr size_t kTrainCounterBytes = kTrainUmmaPairs * 16 * 4;
+constexpr size_t kTrainCounterBytes = kTrainUmmaPairs * 32 * 4;
 int train_umma_lines(int M);
 cudaError_t launch_train_umma(const TrainUmma& t, cudaStream_t s);
 // out[l][r][c], l = 0, 1, 2: the bf16 terms of in[r][c]; `ld_out` elements between rows, `limb` between terms.

@@ -1,0 +1,213 @@
+// Shared by the tensor-core kernels of the training calls (train_umma.cu, train_umma_f32.cu): what a launch is given, how its
+// tiles are dealt to pairs of CTAs, and element-wise parts of the epilogues.
+#pragma once
+
+#include "tcgen05.cuh"
+#include "train_kernels.cuh"
+
+namespace sffn {
+
+constexpr int kPairRows = 256;               // rows of a pair's tile
+constexpr int kDeep = 64;                    // bf16 elements of one 128-byte swizzle row: a K block
+constexpr int kHalfBytes = 128 * kDeep * 2;  // 128 rows of a K block
+constexpr int kLimbBlocks = 4;               // fp32: K blocks of a run, which is six times as long
+constexpr int kLimbUnit = 6 * kLimbBlocks;
+constexpr int kRunBlocks = 8;                // dh: K blocks of a run
+
+constexpr int kCutBlocks = 16;               // K blocks that a pair's share of the cut tiles has at least
+
+struct UmmaParams {
+  TrainEpilogue epi;
+  int m_tiles, n_tiles, tiles;        // tiles = m_tiles * n_tiles * batch
+  int blocks;                         // K blocks of a part (fp32: rounded up to runs)
+  int units, unit_blocks, run_units;  // a tile's K in units (what is not cut), K blocks of a unit, units of a run
+  int whole;                          // tiles dealt whole; the others are cut along K
+  int batch, tile_cols;
+  int a_mn, b_mn;
+  float* partial;
+  size_t piece;                       // floats of a pair's piece of a tile
+  uint32_t* counters;
+  int32_t* status;
+  long long budget;
+};
+
+// One piece of work of a pair of CTAs: units [u0, u1) of a tile.
+struct Item {
+  int tile, u0, u1;
+};
+// A pair's items in order: its share of the tiles that are cut, then whole tiles.
+struct Walk {
+  int pairs, pair, cut, units, lo, hi, next;  // lo, hi: its units of all cut tiles in a row
+  __device__ __forceinline__ Walk(const UmmaParams& p, int pairs_, int pair_) {
+    pairs = pairs_; pair = pair_; units = p.units;
+    cut = p.tiles - p.whole;
+    lo = share(pair);
+    hi = share(pair + 1);
+    next = pair;
+  }
+  __device__ __forceinline__ int share(int q) const { return (int)((long long)cut * units * q / pairs); }
+  __device__ __forceinline__ bool step(const UmmaParams& p, Item& it) {
+    if (lo < hi) {
+      const int t = lo / units;
+      it.tile = p.whole + t;
+      it.u0 = lo - t * units;
+      it.u1 = min(units, hi - t * units);
+      lo = t * units + it.u1;
+      return true;
+    }
+    if (next >= p.whole) return false;
+    it.tile = next;
+    it.u0 = 0;
+    it.u1 = units;
+    next += pairs;
+    return true;
+  }
+};
+
+// Where a tile lies: groups of eight tile rows, column by column, so that what runs at one time shares rows and columns in L2.
+struct Place {
+  int batch, m, n;
+};
+__device__ __forceinline__ Place place_of(const UmmaParams& p, int tile) {
+  constexpr int kGroup = 8;
+  const int per = p.m_tiles * p.n_tiles;
+  Place at;
+  at.batch = tile / per;
+  tile -= at.batch * per;
+  const int group = tile / (kGroup * p.n_tiles), first = group * kGroup, rows = min(kGroup, p.m_tiles - first);
+  tile -= first * p.n_tiles;
+  at.m = first + tile % rows;
+  at.n = tile / rows;
+  return at;
+}
+
+// K block j of unit u: which part, which block of it, which terms.
+__device__ __forceinline__ void block_of(const UmmaParams& p, int u, int j, int& part, int& kb, int& la, int& lb) {
+  if (p.unit_blocks == 1) {
+    part = u >= p.blocks ? 1 : 0;
+    kb = u - part * p.blocks;
+    la = lb = 0;
+  } else {
+    const int first = u * kLimbBlocks;
+    part = first >= p.blocks ? 1 : 0;
+    kb = first - part * p.blocks + j % kLimbBlocks;
+    const int product = j / kLimbBlocks;  // (0,2) (2,0) (1,1) (0,1) (1,0) (0,0)
+    la = product == 1 ? 2 : product == 2 || product == 4 ? 1 : 0;
+    lb = product == 0 ? 2 : product == 2 || product == 3 ? 1 : 0;
+  }
+}
+
+// The pieces of a cut tile, in the order of K: consecutive pairs have one each, the first of them perhaps as its second piece.
+struct Cut {
+  int first, pieces;
+  long long lo;  // the tile's first unit among those of all cut tiles
+  __device__ __forceinline__ Cut(const UmmaParams& p, const Walk& w, const Item& it) {
+    lo = (long long)(it.tile - p.whole) * p.units;
+    const long long all = (long long)(p.tiles - p.whole) * p.units, hi = lo + p.units;
+    first = (int)(lo * w.pairs / all);
+    while (w.share(first + 1) <= lo) ++first;
+    while (first > 0 && w.share(first) > lo) --first;
+    int last = first;
+    while (w.share(last + 1) < hi) ++last;
+    pieces = last - first + 1;
+  }
+  // Where pair `q` keeps its piece of this tile.
+  __device__ __forceinline__ float* place(const UmmaParams& p, const Walk& w, int q) const {
+    return p.partial + (size_t)(2 * q + (w.share(q) < lo ? 1 : 0)) * p.piece;
+  }
+};
+__device__ __forceinline__ bool is_cut(const UmmaParams& p, const Item& it) { return it.u0 > 0 || it.u1 < p.units; }
+
+// One warp has stored its part of a piece; true for the warp that finds all the others there.  The counter is left at zero.
+__device__ __forceinline__ bool last_piece(uint32_t* counter, int pieces, int lane) {
+  __threadfence();
+  __syncwarp();
+  uint32_t before = 0;
+  if (lane == 0) before = atomicAdd(counter, 1u);
+  before = __shfl_sync(0xffffffffu, before, 0);
+  if (before != (uint32_t)(pieces - 1)) return false;
+  __threadfence();
+  if (lane == 0) *counter = 0;
+  return true;
+}
+// Sixteen columns of a warp's 32 rows in a piece: four rows of 512 bytes.
+__device__ __forceinline__ void put_piece(float* part, int chunk, int lane, const float* v) {
+  float4* out = reinterpret_cast<float4*>(part) + (size_t)chunk * 128 + lane;
+#pragma unroll
+  for (int q = 0; q < 4; ++q) __stcg(out + 32 * q, make_float4(v[4 * q], v[4 * q + 1], v[4 * q + 2], v[4 * q + 3]));
+}
+__device__ __forceinline__ void add_piece(const float* part, int chunk, int lane, float* v) {
+  const float4* in = reinterpret_cast<const float4*>(part) + (size_t)chunk * 128 + lane;
+#pragma unroll
+  for (int q = 0; q < 4; ++q) {
+    const float4 f = __ldcg(in + 32 * q);
+    v[4 * q] += f.x; v[4 * q + 1] += f.y; v[4 * q + 2] += f.z; v[4 * q + 3] += f.w;
+  }
+}
+
+__device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
+  const __nv_bfloat162 v = __floats2bfloat162_rn(lo, hi);
+  return *reinterpret_cast<const uint32_t*>(&v);
+}
+// Activations of sixteen values, the choice made once: inside the loops it would be made, and its code be there, sixteen times.
+template <bool FAST>
+__device__ __forceinline__ void act16(int act, const float* t, float* v) {
+  if (act == kActNone) {
+#pragma unroll
+    for (int i = 0; i < 16; ++i) v[i] = t[i];
+  } else if (act == kActRelu) {
+#pragma unroll
+    for (int i = 0; i < 16; ++i) v[i] = train_act<FAST>(kActRelu, t[i]);
+  } else if (act == kActSqRelu) {
+#pragma unroll
+    for (int i = 0; i < 16; ++i) v[i] = train_act<FAST>(kActSqRelu, t[i]);
+  } else if (act == kActRsPlus) {
+#pragma unroll
+    for (int i = 0; i < 16; ++i) v[i] = train_act<FAST>(kActRsPlus, t[i]);
+  } else {
+#pragma unroll
+    for (int i = 0; i < 16; ++i) v[i] = train_act<FAST>(kActSilu, t[i]);
+  }
+}
+template <bool FAST, int ACT, typename Raw>
+__device__ __forceinline__ void slope16_of(const Raw& t, float* v, float* d) {
+#pragma unroll
+  for (int i = 0; i < 16; ++i) train_act_slope<FAST>(ACT, t.get(i), v[i], d[i]);
+}
+template <bool FAST, typename Raw>
+__device__ __forceinline__ void slope16(int act, const Raw& t, float* v, float* d) {
+  if (act == kActNone) slope16_of<FAST, kActNone>(t, v, d);
+  else if (act == kActRelu) slope16_of<FAST, kActRelu>(t, v, d);
+  else if (act == kActSqRelu) slope16_of<FAST, kActSqRelu>(t, v, d);
+  else if (act == kActRsPlus) slope16_of<FAST, kActRsPlus>(t, v, d);
+  else slope16_of<FAST, kActSilu>(t, v, d);
+}
+
+// Sums of sixteen columns over the lanes of a warp: lanes 2 i and 2 i + 1 get column i's (in halves of what is left, five
+// exchanges deep, sixteen shuffles).
+__device__ __forceinline__ float column_sum(float* v, int lane) {
+#pragma unroll
+  for (int width = 8; width >= 1; width >>= 1) {
+    const bool upper = lane & (2 * width);
+#pragma unroll
+    for (int i = 0; i < width; ++i) {
+      const float send = upper ? v[i] : v[i + width], keep = upper ? v[i + width] : v[i];
+      v[i] = keep + __shfl_xor_sync(0xffffffffu, send, 2 * width);
+    }
+  }
+  return v[0] + __shfl_xor_sync(0xffffffffu, v[0], 1);
+}
+
+// ---- host ------------------------------------------------------------------------------------------------------------
+
+// `terms` bf16 matrices [rows, width], rows `ld` elements apart, in boxes of 64 elements x `box` rows, 128-byte swizzle.
+bool make_train_map(CUtensorMap* m, const void* base, int64_t width, int64_t rows, int64_t ld, int terms, int64_t limb, int box);
+// The maps of a product's operands, three of each (the last one repeated where there are fewer).
+bool make_operand_maps(const TrainUmma& t, CUtensorMap* a, CUtensorMap* b);
+// Fills in what follows from the product: tiles of `cols` columns, K in units, which tiles are cut for `pairs` pairs of CTAs
+// (returned: the pairs that have work).
+int plan_umma(const TrainUmma& t, int cols, UmmaParams& p, int pairs);
+
+cudaError_t launch_train_umma_f32(const TrainUmma& t, int pairs, cudaStream_t s);
+
+}  // namespace sffn

@@ -1,0 +1,442 @@
+// Products of the training calls in fp32 on the tensor cores: every operand is three bf16 terms (24 bits), a product the six of
+// the terms' products above 2^-27.
+//
+// Tiles, roles and cut tiles as in train_umma.cu.  The tensor cores truncate when they add onto an accumulator (a sum over K = 2688
+// comes out low by 1e-6 of its typical size): runs of 256 k get an accumulator of their own, products of the smallest terms
+// first, and the epilogue warps add the runs up in registers, rounding to nearest.
+#include "fused_kernel.cuh"
+#include "train_umma.cuh"
+
+namespace sffn {
+namespace {
+
+using namespace tc;
+
+constexpr int kCols = 256;
+constexpr int kStageBytes = 2 * kHalfBytes;
+constexpr int kStages = 6;
+constexpr int kThreads = 384;
+constexpr int kEpilogueWarps = 8;
+constexpr int kSmemBytes = kStages * kStageBytes + 1024 + 256;
+
+struct Maps {
+  CUtensorMap a[3], b[3];
+};
+
+__device__ __forceinline__ void st8(void* p, const uint32_t* w, bool wide) {  // 32 bytes
+  if (wide) {
+    asm volatile("st.global.v8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};" ::"l"(p), "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3]), "r"(w[4]), "r"(w[5]),
+                 "r"(w[6]), "r"(w[7])
+                 : "memory");
+  } else {
+    reinterpret_cast<uint4*>(p)[0] = make_uint4(w[0], w[1], w[2], w[3]);
+    reinterpret_cast<uint4*>(p)[1] = make_uint4(w[4], w[5], w[6], w[7]);
+  }
+}
+__device__ __forceinline__ void ld8(const void* p, uint32_t* w, bool wide) {
+  if (wide) {
+    asm volatile("ld.global.v8.b32 {%0,%1,%2,%3,%4,%5,%6,%7}, [%8];"
+                 : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]), "=r"(w[4]), "=r"(w[5]), "=r"(w[6]), "=r"(w[7])
+                 : "l"(p)
+                 : "memory");
+  } else {
+    const uint4 a = reinterpret_cast<const uint4*>(p)[0], b = reinterpret_cast<const uint4*>(p)[1];
+    w[0] = a.x; w[1] = a.y; w[2] = a.z; w[3] = a.w;
+    w[4] = b.x; w[5] = b.y; w[6] = b.z; w[7] = b.w;
+  }
+}
+
+// Stores the first n of sixteen values from element `at` on; `wide`: 32-byte accesses are aligned.
+__device__ __forceinline__ void store16(void* base, int64_t at, const float* v, int n, bool wide) {
+  float* p = static_cast<float*>(base) + at;
+  if (n == 16) {
+    st8(p, reinterpret_cast<const uint32_t*>(v), wide);
+    st8(p + 8, reinterpret_cast<const uint32_t*>(v) + 8, wide);
+  } else {
+#pragma unroll
+    for (int i = 0; i < 16; ++i)
+      if (i < n) p[i] = v[i];
+  }
+}
+// The three bf16 terms of the first n of sixteen values (in a workspace: n is 8 or 16).
+__device__ __forceinline__ void store16_limbs(void* base, int64_t at, int64_t limb, float* v, int n, bool wide) {
+#pragma unroll
+  for (int l = 0; l < 3; ++l) {
+    __nv_bfloat16* p = static_cast<__nv_bfloat16*>(base) + l * limb + at;
+    uint32_t w[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) w[i] = pack_bf16(v[2 * i], v[2 * i + 1]);
+    if (n == 16) st8(p, w, wide);
+    else *reinterpret_cast<uint4*>(p) = make_uint4(w[0], w[1], w[2], w[3]);
+    if (l < 2) {
+#pragma unroll
+      for (int i = 0; i < 16; ++i) v[i] -= __bfloat162float(__float2bfloat16(v[i]));
+    }
+  }
+}
+struct Raw16 {
+  float v[16];
+  __device__ __forceinline__ void load(const void* base, int64_t at, int n, bool wide) {
+    const float* p = static_cast<const float*>(base) + at;
+    if (n == 16) {
+      ld8(p, reinterpret_cast<uint32_t*>(v), wide);
+      ld8(p + 8, reinterpret_cast<uint32_t*>(v) + 8, wide);
+    } else {
+#pragma unroll
+      for (int i = 0; i < 16; ++i) v[i] = i < n ? p[i] : 0.f;
+    }
+  }
+  __device__ __forceinline__ float get(int i) const { return v[i]; }
+};
+
+template <int EPI>
+__global__ void __launch_bounds__(kThreads, 1) train_umma_f32_kernel(const __grid_constant__ UmmaParams p, const __grid_constant__ Maps maps) {
+  extern __shared__ uint8_t smem_raw[];
+  __shared__ int abort_word;
+  __shared__ uint32_t tmem_slot;
+  __shared__ __align__(8) uint64_t bars[2 * kStages + 4];
+  volatile int* const abort_flag = &abort_word;
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  const uint32_t ring = (smem_u32(smem_raw) + 1023u) & ~1023u;
+  const uint32_t full = smem_u32(bars), empty = full + 8 * kStages, acc_full = empty + 8 * kStages, acc_empty = acc_full + 16;
+  const int rank = (int)cluster_rank(), pair = (int)blockIdx.x >> 1, pairs = (int)gridDim.x >> 1;
+
+  if (tid == 0) {
+    for (int s = 0; s < kStages; ++s) {
+      mbar_init(full + 8 * s, 1);
+      mbar_init(empty + 8 * s, 1);
+    }
+    for (int b = 0; b < 2; ++b) {
+      mbar_init(acc_full + 8 * b, 1);
+      mbar_init(acc_empty + 8 * b, 2 * kEpilogueWarps);
+    }
+    abort_word = 0;
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  }
+  if (warp == 2) {
+    asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&tmem_slot)), "r"(512) : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
+  }
+  fence_before();
+  cluster_sync();
+  fence_after();
+  const uint32_t tmem = tmem_slot;
+  pdl_launch_dependents();
+  pdl_wait();
+
+  if (warp < 4) {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 64;");
+    Walk walk(p, pairs, pair);
+    Item it;
+    if (warp == 0 && lane == 0) {
+      int s = 0, phase = 0;
+      bool ok = true;
+      while (ok && walk.step(p, it)) {
+        const Place at = place_of(p, it.tile);
+        const int m0 = at.m * kPairRows + rank * 128;
+        const int n0 = at.n * p.tile_cols + (EPI == kEpiGateUp ? 0 : rank * 128);
+        for (int u = it.u0; ok && u < it.u1; ++u)
+          for (int j = 0; j < p.unit_blocks; ++j) {
+            ok = mbar_wait(empty + 8 * s, phase ^ 1, abort_flag, p.status, p.budget);
+            if (!ok) break;
+            int part, kb, la, lb;
+            block_of(p, u, j, part, kb, la, lb);
+            const int which = p.batch > 1 ? at.batch : part;
+            const CUtensorMap* ma = &maps.a[EPI == kEpiGateUp ? 0 : which];
+            const CUtensorMap* mb = &maps.b[EPI == kEpiGateUp ? rank : which];
+            const uint32_t bar = map_rank(full + 8 * s, 0), da = ring + s * kStageBytes, db = da + kHalfBytes;
+            if (rank == 0) mbar_expect_tx(full + 8 * s, 2 * kStageBytes);
+            const int k0 = kb * kDeep;
+            if (p.a_mn) {
+              tma_tile_3d(da, ma, m0, k0, la, bar);
+              tma_tile_3d(da + kHalfBytes / 2, ma, m0 + 64, k0, la, bar);
+            } else {
+              tma_tile_3d(da, ma, k0, m0, la, bar);
+            }
+            if (p.b_mn) {
+              tma_tile_3d(db, mb, n0, k0, lb, bar);
+              tma_tile_3d(db + kHalfBytes / 2, mb, n0 + 64, k0, lb, bar);
+            } else {
+              tma_tile_3d(db, mb, k0, n0, lb, bar);
+            }
+            if (++s == kStages) { s = 0; phase ^= 1; }
+          }
+      }
+    } else if (warp == 1 && lane == 0 && rank == 0) {
+      const uint32_t idesc = idesc_bf16(kPairRows, kCols, p.a_mn, p.b_mn);
+      const uint64_t a0 = p.a_mn ? desc_mn_major(ring, kHalfBytes / 2) : desc_k_major(ring);
+      const uint64_t b0 = p.b_mn ? desc_mn_major(ring + kHalfBytes, kHalfBytes / 2) : desc_k_major(ring + kHalfBytes);
+      const uint32_t a_step = p.a_mn ? 2048 >> 4 : 32 >> 4, b_step = p.b_mn ? 2048 >> 4 : 32 >> 4;  // sixteen k
+      int s = 0, phase = 0, b = 0, b_phase = 0;
+      bool ok = true;
+      while (ok && walk.step(p, it)) {
+        for (int u = it.u0; ok && u < it.u1;) {
+          const int end = min(it.u1, u + p.run_units);
+          ok = mbar_wait(acc_empty + 8 * b, b_phase ^ 1, abort_flag, p.status, p.budget);
+          if (!ok) break;
+          fence_after();
+          const uint32_t acc = tmem + b * kCols;
+          uint32_t more = 0;
+          for (int n = (end - u) * p.unit_blocks; n > 0; --n) {
+            ok = mbar_wait(full + 8 * s, phase, abort_flag, p.status, p.budget);
+            if (!ok) break;
+            fence_after();
+            const uint32_t off = (uint32_t)(s * kStageBytes) >> 4;
+#pragma unroll
+            for (int k = 0; k < kDeep / 16; ++k) {
+              umma_pair(acc, a0 + off + k * a_step, b0 + off + k * b_step, idesc, more);
+              more = 1;
+            }
+            commit_pair(empty + 8 * s);
+            if (++s == kStages) { s = 0; phase ^= 1; }
+          }
+          if (!ok) break;
+          commit_pair(acc_full + 8 * b);
+          b ^= 1;
+          if (b == 0) b_phase ^= 1;
+          u = end;
+        }
+      }
+    }
+  } else {
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 216;");
+    const TrainEpilogue& e = p.epi;
+    const int quad = warp & 3, half = (warp - 4) >> 2;
+    const uint32_t lanes = (uint32_t)(32 * quad) << 16;
+    constexpr int kChunks = 8;                                   // of sixteen columns, of a warp
+    constexpr int kOut = EPI == kEpiGateUp ? kChunks / 2 : kChunks;  // of sixteen output columns
+    // column (in the accumulator) of a chunk: kGateUp: a warp has z and u of 64 neurons, z's chunks first
+    auto column = [&](int c) { return EPI == kEpiGateUp ? (c < 4 ? 0 : 128) + 64 * half + 16 * (c & 3) : 128 * half + 16 * c; };
+    const uint32_t empty0 = map_rank(acc_empty, 0);
+    const uintptr_t wide_out = EPI == kEpiStore ? (uintptr_t)(e.ld_out * 4) : (uintptr_t)(e.ld_zu * 4) | reinterpret_cast<uintptr_t>(e.z) | reinterpret_cast<uintptr_t>(e.u);
+    const bool wide_user = (wide_out & 31) == 0;
+    const bool wide_own = EPI != kEpiStore && (e.ld_h & 15) == 0;
+    int b = 0, b_phase = 0;
+    bool ok = true;
+    Walk walk(p, pairs, pair);
+    Item it;
+    while (ok && walk.step(p, it)) {
+      const Place at = place_of(p, it.tile);
+      const int m = at.m * kPairRows + rank * 128 + 32 * quad + lane;
+      const int n0 = at.n * p.tile_cols + (EPI == kEpiGateUp ? 64 : 128) * half;  // first output column of this warp
+      const bool row = m < e.M;
+      // This item's sums, in tensor memory: as the MMAs left them, or added up over the runs and put back where the last run was.
+      uint32_t tacc = 0;
+      float acc[16 * kChunks];
+#pragma unroll
+      for (int i = 0; i < 16 * kChunks; ++i) acc[i] = 0.f;
+#pragma unroll 1
+      for (int u = it.u0; u < it.u1;) {
+        const int end = min(it.u1, u + p.run_units);
+        ok = __all_sync(0xffffffffu, mbar_wait(acc_full + 8 * b, b_phase, abort_flag, p.status, p.budget));
+        if (!ok) break;
+        fence_after();
+        tacc = tmem + lanes + b * kCols;
+#pragma unroll
+        for (int c = 0; c < kChunks; ++c) {
+          float v[16];
+          tmem_ld16(tacc + column(c), v);
+          tmem_arrived(v);
+#pragma unroll
+          for (int i = 0; i < 16; ++i) acc[16 * c + i] += v[i];
+        }
+        u = end;
+        if (u < it.u1) {
+          fence_before();
+          __syncwarp();
+          if (lane == 0) mbar_arrive_cluster(empty0 + 8 * b);
+          b ^= 1;
+          if (b == 0) b_phase ^= 1;
+        }
+      }
+      if (!ok) break;
+#pragma unroll
+      for (int c = 0; c < kChunks; ++c) tmem_st16(tacc + column(c), acc + 16 * c);
+      tmem_stored();
+      auto own = [&](int c, float* v) {
+        tmem_ld16(tacc + column(c), v);
+        tmem_arrived(v);
+      };
+      // A tile that several pairs share: this warp's part of it is 16 KB of every piece.
+      bool finish = true;
+      const bool cut = is_cut(p, it);
+      const size_t region = ((size_t)rank * kEpilogueWarps + (warp - 4)) * (16 * kChunks * 32);  // floats
+      if (cut) {
+        const Cut of(p, walk, it);
+        float* out = of.place(p, walk, pair) + region;
+#pragma unroll 2
+        for (int c = 0; c < kChunks; ++c) {
+          float v[16];
+          own(c, v);
+          put_piece(out, c, lane, v);
+        }
+        finish = last_piece(p.counters + (it.tile - p.whole) * 16 + rank * kEpilogueWarps + (warp - 4), of.pieces, lane);
+      }
+      auto sums = [&](int c, float* v) {
+        if (!cut) {
+          own(c, v);
+          return;
+        }
+#pragma unroll
+        for (int i = 0; i < 16; ++i) v[i] = 0.f;
+        const Cut of(p, walk, it);
+#pragma unroll 1
+        for (int q = of.first; q < of.first + of.pieces; ++q) add_piece(of.place(p, walk, q) + region, c, lane, v);
+      };
+      if (finish) {
+        if constexpr (EPI == kEpiStore) {
+          void* out = e.out[at.batch];
+          const bool wide = wide_user && (reinterpret_cast<uintptr_t>(out) & 31) == 0;
+#pragma unroll 2
+          for (int c = 0; c < kOut; ++c) {
+            const int n = n0 + 16 * c;
+            float v[16];
+            sums(c, v);
+            if (row && n < e.N) store16(out, m * e.ld_out + n, v, min(16, e.N - n), wide);
+          }
+        } else if constexpr (EPI == kEpiGateUp) {
+#pragma unroll 1
+          for (int c = 0; c < kOut; ++c) {
+            const int n = n0 + 16 * c;
+            float z[16], u[16];
+            sums(c, z);
+            sums(c + 4, u);
+            const int left = min(16, e.N - n);
+            if (e.bias) {
+              const float bias = lane < left ? e.bias[n + lane] : 0.f;
+#pragma unroll
+              for (int i = 0; i < 16; ++i) z[i] += __shfl_sync(0xffffffffu, bias, i);
+            }
+            if (row && left > 0) {
+              if (e.z) {
+                store16(e.z, m * e.ld_zu + n, z, left, wide_user);
+                store16(e.u, m * e.ld_zu + n, u, left, wide_user);
+              }
+              act16<false>(e.act, z, z);
+              act16<false>(e.act_up, u, u);
+#pragma unroll
+              for (int i = 0; i < 16; ++i) z[i] *= u[i];
+              const int room = (int)min((int64_t)16, e.ld_h - n);
+              store16_limbs(e.h, m * e.ld_h + n, e.limb, z, room, wide_own);
+            }
+          }
+        } else {
+          Raw16 rz, ru;
+          auto fetch = [&](int c) {
+            const int n = n0 + 16 * c, left = row ? min(16, e.N - n) : 0;
+            rz.load(e.z, m * e.ld_zu + n, left, wide_user);
+            ru.load(e.u, m * e.ld_zu + n, left, wide_user);
+          };
+          auto store = [&](void* to, int64_t at_h, float* v, int room) {
+            if (!to || room <= 0) return;
+            store16_limbs(to, at_h, e.limb, v, room, wide_own);
+          };
+          fetch(0);
+#pragma unroll 1
+          for (int c = 0; c < kOut; ++c) {
+            const int n = n0 + 16 * c, room = row ? (int)min((int64_t)16, e.ld_h - n) : 0;
+            const int64_t at_h = m * e.ld_h + n;
+            float dh[16], a[16], da[16], bv[16], db[16];
+            slope16<false>(e.act, rz, a, da);
+            slope16<false>(e.act_up, ru, bv, db);
+            if (c + 1 < kOut) fetch(c + 1);
+            sums(c, dh);
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+              db[i] *= dh[i] * a[i];   // du
+              da[i] *= dh[i] * bv[i];  // dz
+              a[i] *= bv[i];           // h
+            }
+            store(e.h, at_h, a, room);
+            store(e.du, at_h, db, room);
+            float sum = 0.f;
+            if (e.db) {
+#pragma unroll
+              for (int i = 0; i < 16; ++i) dh[i] = da[i];
+              sum = column_sum(dh, lane);
+            }
+            store(e.dz, at_h, da, room);
+            if (e.db) {
+              const int line = at.m * (kPairRows / 32) + rank * 4 + quad, n_of = n + (lane >> 1);
+              if (!(lane & 1) && n_of < e.N && line * 32 < e.M) e.db[line * e.ld_h + n_of] = sum;
+            }
+          }
+        }
+      }
+      fence_before();
+      __syncwarp();
+      if (lane == 0) mbar_arrive_cluster(empty0 + 8 * b);
+      b ^= 1;
+      if (b == 0) b_phase ^= 1;
+    }
+  }
+
+  // Everybody meets, then the allocating warps free tensor memory.  (After a wait that ran out, copies and MMAs may still be in
+  // flight: they end within microseconds, and shared memory and tensor memory are only given back after that.)
+  if (*abort_flag)
+    for (int i = 0; i < 50; ++i) __nanosleep(1000);
+  fence_before();
+  cluster_sync();
+  if (warp == 2) {
+    fence_after();
+    asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512) : "memory");
+  }
+}
+
+// The terms of fp32 values: eight a thread.
+__global__ void __launch_bounds__(256) train_split_kernel(const float* in, int64_t ld_in, int rows, int cols, __nv_bfloat16* out, int64_t ld_out, int64_t limb) {
+  pdl_launch_dependents();
+  pdl_wait();
+  const int per = (cols + 7) / 8;
+  const int64_t total = (int64_t)rows * per;
+  for (int64_t i = blockIdx.x * 256ll + threadIdx.x; i < total; i += gridDim.x * 256ll) {
+    const int64_t r = i / per;
+    const int c = (int)(i - r * per) * 8;
+    const float* p = in + r * ld_in + c;
+    float v[8];
+    const int n = min(8, cols - c);
+#pragma unroll
+    for (int q = 0; q < 2; ++q) {  // columns are a multiple of four
+      const float4 f = 4 * q < n ? *reinterpret_cast<const float4*>(p + 4 * q) : make_float4(0, 0, 0, 0);
+      v[4 * q] = f.x; v[4 * q + 1] = f.y; v[4 * q + 2] = f.z; v[4 * q + 3] = f.w;
+    }
+#pragma unroll
+    for (int l = 0; l < 3; ++l) {
+      uint32_t w[4];
+#pragma unroll
+      for (int q = 0; q < 4; ++q) w[q] = pack_bf16(v[2 * q], v[2 * q + 1]);
+      *reinterpret_cast<uint4*>(out + l * limb + r * ld_out + c) = make_uint4(w[0], w[1], w[2], w[3]);
+#pragma unroll
+      for (int q = 0; q < 8; ++q) v[q] -= __bfloat162float(__float2bfloat16(v[q]));
+    }
+  }
+}
+
+template <int EPI>
+cudaError_t launch_one(const UmmaParams& p, const Maps& maps, int pairs, cudaStream_t s) {
+  static unsigned long long configured = 0;
+  const cudaError_t e = allow_dynamic_smem(train_umma_f32_kernel<EPI>, kSmemBytes, configured);
+  if (e != cudaSuccess) return e;
+  return launch_clusters(2, train_umma_f32_kernel<EPI>, dim3(2 * pairs), dim3(kThreads), kSmemBytes, s, p, maps);
+}
+
+}  // namespace
+
+cudaError_t launch_train_split(const float* in, int64_t ld_in, int rows, int cols, __nv_bfloat16* out, int64_t ld_out, int64_t limb, cudaStream_t s) {
+  const int64_t total = (int64_t)rows * ((cols + 7) / 8);
+  const int64_t want = (total + 255) / 256;
+  return launch_pdl(train_split_kernel, dim3((unsigned)(want < 148 * 8 ? want : 148 * 8)), dim3(256), 0, s, in, ld_in, rows, cols, out, ld_out, limb);
+}
+
+cudaError_t launch_train_umma_f32(const TrainUmma& t, int pairs, cudaStream_t s) {
+  UmmaParams p{};
+  pairs = plan_umma(t, t.g.epilogue == kEpiGateUp ? kCols / 2 : kCols, p, pairs);
+  p.piece = (size_t)kPairRows * kCols;
+  Maps maps;
+  if (pairs <= 0 || !make_operand_maps(t, maps.a, maps.b)) return cudaErrorInvalidValue;
+  if (t.g.epilogue == kEpiStore) return launch_one<kEpiStore>(p, maps, pairs, s);
+  if (t.g.epilogue == kEpiGateUp) return launch_one<kEpiGateUp>(p, maps, pairs, s);
+  return launch_one<kEpiHidden>(p, maps, pairs, s);
+}
+
+}  // namespace sffn
