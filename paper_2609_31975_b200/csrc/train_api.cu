@@ -45,7 +45,7 @@ struct TrainLayout {
   bool umma, split;         // split: operands in three bf16 terms
   int64_t ld_h, ld_d;       // rows of hidden values, and of the terms of D-wide operands
   int64_t limb_h, limb_t, limb_w;  // elements between the terms of hidden values, of x and dy, of a weight
-  size_t counters, partial, h, dz, du, db, x, dy, w[3], total;
+  size_t partial, h, dz, du, db, x, dy, w[3], total;
   int lines;
 };
 TrainLayout train_layout(int T, int D, int H, int dtype, bool backward) {
@@ -64,7 +64,6 @@ TrainLayout train_layout(int T, int D, int H, int dtype, bool backward) {
   L.limb_t = T * L.ld_d;
   L.limb_w = H * L.ld_d;
   if (L.umma) {
-    L.counters = take(sffn::kTrainCounterBytes);
     L.partial = take(sffn::kTrainPartialBytes);
   }
   const size_t hidden = (size_t)T * L.ld_h * (L.split ? 6 : element(dtype));
@@ -96,7 +95,6 @@ struct Products {
     ws = static_cast<char*>(c->workspace);
   }
   void* hidden(size_t at) const { return ws + at; }
-  cudaError_t begin() const { return L.umma ? cudaMemsetAsync(ws + L.counters, 0, sffn::kTrainCounterBytes, s) : cudaSuccess; }
   // An operand as the products take it: itself, or its terms, which `at` receives.
   cudaError_t split(const void* in, int64_t ld, int rows, size_t at, int64_t limb) const {
     if (!L.split) return cudaSuccess;
@@ -118,7 +116,6 @@ struct Products {
       t.limb_b[i] = limb_b[i];
     }
     t.partial = reinterpret_cast<float*>(ws + L.partial);
-    t.counters = reinterpret_cast<uint32_t*>(ws + L.counters);
     t.status = c->status;
     return sffn::launch_train_umma(t, s);
   }
@@ -182,7 +179,6 @@ int gated_ffn_forward(const sffn_train_call* c, void* y, int64_t ld_y, void* str
   const Products p(c, false, static_cast<cudaStream_t>(stream));
   const TrainLayout& L = p.L;
   const int64_t tokens[3] = {L.limb_t, L.limb_t, L.limb_t}, weights[3] = {L.limb_w, L.limb_w, L.limb_w}, hidden[3] = {L.limb_h, L.limb_h, L.limb_h};
-  SFFN_CUDA(p.begin());
   SFFN_CUDA(p.split(c->x, c->ld_x, c->T, L.x, L.limb_t));
   SFFN_CUDA(p.split(c->W_g, c->D, c->H, L.w[0], L.limb_w));
   SFFN_CUDA(p.split(c->W_up, c->D, c->H, L.w[1], L.limb_w));
@@ -243,7 +239,6 @@ int gated_ffn_backward(const sffn_train_call* c, const void* dy, int64_t ld_dy, 
   const int64_t tokens[3] = {L.limb_t, L.limb_t, L.limb_t}, weights[3] = {L.limb_w, L.limb_w, L.limb_w}, hidden[3] = {L.limb_h, L.limb_h, L.limb_h};
   void* const values[3] = {p.hidden(L.dz), p.hidden(L.du), p.hidden(L.h)};
   float* const lines = reinterpret_cast<float*>(p.ws + L.db);
-  SFFN_CUDA(p.begin());
   SFFN_CUDA(p.split(dy, ld_dy, c->T, L.dy, L.limb_t));
   SFFN_CUDA(p.split(c->W_down, c->D, c->H, L.w[2], L.limb_w));
   if (g->dW_g || g->dW_up) SFFN_CUDA(p.split(c->x, c->ld_x, c->T, L.x, L.limb_t));

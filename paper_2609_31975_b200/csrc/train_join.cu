@@ -1,0 +1,167 @@
+// Tiles that the tensor-core kernels cut along K: adds up their pieces, in the order of K, and does the epilogue.
+//
+// A CTA has 32 rows x 64 output columns of a tile, or 8 rows where there are few such CTAs (kHidden sums 32 rows at a time), a thread
+// four columns of a row at a time; the loads of eight pieces are under way at once.  Bound by the pieces' bytes, which are still in L2, and by latency
+// where few tiles have many pieces.
+#include "train_umma.cuh"
+
+namespace sffn {
+namespace {
+
+constexpr int kJoinCols = 64;
+__host__ __device__ constexpr int join_threads(int epilogue) { return (epilogue == kEpiHidden ? 32 : 8) * kJoinCols / 4; }
+
+__device__ __forceinline__ void load4(const float* p, float* v, int n) {
+  if (n == 4) {
+    const float4 f = *reinterpret_cast<const float4*>(p);
+    v[0] = f.x; v[1] = f.y; v[2] = f.z; v[3] = f.w;
+  } else {
+    for (int i = 0; i < 4; ++i) v[i] = i < n ? p[i] : 0.f;
+  }
+}
+__device__ __forceinline__ void load4(const __nv_bfloat16* p, float* v, int n) {
+  if (n == 4) {
+    const uint2 w = *reinterpret_cast<const uint2*>(p);
+    v[0] = __uint_as_float(w.x << 16); v[1] = __uint_as_float(w.x & 0xffff0000u);
+    v[2] = __uint_as_float(w.y << 16); v[3] = __uint_as_float(w.y & 0xffff0000u);
+  } else {
+    for (int i = 0; i < 4; ++i) v[i] = i < n ? __bfloat162float(p[i]) : 0.f;
+  }
+}
+__device__ __forceinline__ void store4(float* p, const float* v, int n) {
+  if (n == 4) {
+    *reinterpret_cast<float4*>(p) = make_float4(v[0], v[1], v[2], v[3]);
+  } else {
+    for (int i = 0; i < n; ++i) p[i] = v[i];
+  }
+}
+__device__ __forceinline__ void store4(__nv_bfloat16* p, const float* v, int n) {
+  if (n == 4) {
+    *reinterpret_cast<uint2*>(p) = make_uint2(pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]));
+  } else {
+    for (int i = 0; i < n; ++i) p[i] = __float2bfloat16(v[i]);
+  }
+}
+// Four hidden values as the next products take them: bf16, or three bf16 terms.
+template <typename T>
+__device__ __forceinline__ void store_hidden(void* base, int64_t at, int64_t limb, const float* v, int n) {
+  if (!base) return;
+  __nv_bfloat16* p = static_cast<__nv_bfloat16*>(base) + at;
+  store4(p, v, n);
+  if constexpr (sizeof(T) == 4) {
+    float r[4] = {v[0], v[1], v[2], v[3]};
+#pragma unroll
+    for (int l = 1; l < 3; ++l) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) r[i] -= __bfloat162float(__float2bfloat16(r[i]));
+      store4(p + l * limb, r, n);
+    }
+  }
+}
+
+template <int EPI, typename T>
+__global__ void __launch_bounds__(join_threads(EPI)) train_join_kernel(const __grid_constant__ UmmaParams p, int pairs, int acc_cols, int rows) {
+  __shared__ float down[EPI == kEpiHidden ? 32 : 1][kJoinCols];
+  __shared__ const float* place[kTrainUmmaPairs];
+  constexpr bool kFast = sizeof(T) == 2;
+  pdl_launch_dependents();
+  const TrainEpilogue& e = p.epi;
+  const int across = (p.tile_cols + kJoinCols - 1) / kJoinCols, per = across * (kPairRows / rows);
+  const int t = blockIdx.x / per, in = blockIdx.x - t * per, r0 = in / across * rows, c0 = in % across * kJoinCols;
+  const Place at = place_of(p, p.whole + t);
+  const int m0 = at.m * kPairRows + r0, n0 = at.n * p.tile_cols + c0;
+  if (m0 >= e.M || n0 >= e.N) return;
+  // the pairs whose shares of the cut tiles overlap this one, and where their pieces are
+  const Walk walk(p, pairs, 0);
+  const long long lo = (long long)t * p.units, hi = lo + p.units, all = (long long)(p.tiles - p.whole) * p.units;
+  int first = (int)(lo * pairs / all);
+  while (walk.share(first + 1) <= lo) ++first;
+  while (first > 0 && walk.share(first) > lo) --first;
+  int pieces = 1;
+  while (walk.share(first + pieces) < hi) ++pieces;
+  if (threadIdx.x < pieces) place[threadIdx.x] = piece_of(p, walk, first + threadIdx.x, p.whole + t);
+  __syncthreads();
+  pdl_wait();
+
+  for (int r = threadIdx.x / (kJoinCols / 4); r < rows; r += join_threads(EPI) / (kJoinCols / 4)) {
+    const int c = threadIdx.x % (kJoinCols / 4) * 4, m = m0 + r, n = n0 + c;
+    const int left = m < e.M ? min(4, e.N - n) : 0;
+    float v[4] = {}, u[4] = {};
+    if (left > 0) {
+      const size_t off = (size_t)(r0 + r) * acc_cols + c0 + c;
+#pragma unroll 8
+      for (int q = 0; q < pieces; ++q) {
+        const float* piece = place[q] + off;
+        const float4 f = __ldcg(reinterpret_cast<const float4*>(piece));
+        v[0] += f.x; v[1] += f.y; v[2] += f.z; v[3] += f.w;
+        if constexpr (EPI == kEpiGateUp) {
+          const float4 g = __ldcg(reinterpret_cast<const float4*>(piece + 128));
+          u[0] += g.x; u[1] += g.y; u[2] += g.z; u[3] += g.w;
+        }
+      }
+    }
+    if constexpr (EPI == kEpiStore) {
+      if (left > 0) store4(static_cast<T*>(e.out[at.batch]) + m * e.ld_out + n, v, left);
+    } else if constexpr (EPI == kEpiGateUp) {
+      if (left <= 0) continue;
+      float h[4];
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        if (e.bias && j < left) v[j] += e.bias[n + j];
+        h[j] = train_act<kFast>(e.act, v[j]) * train_act<kFast>(e.act_up, u[j]);
+      }
+      if (e.z) {
+        store4(static_cast<T*>(e.z) + m * e.ld_zu + n, v, left);
+        store4(static_cast<T*>(e.u) + m * e.ld_zu + n, u, left);
+      }
+      store_hidden<T>(e.h, m * e.ld_h + n, e.limb, h, left);
+    } else {
+      float du[4] = {}, h[4];
+      if (left > 0) {
+        float zv[4];
+        load4(static_cast<const T*>(e.z) + m * e.ld_zu + n, zv, left);
+        load4(static_cast<const T*>(e.u) + m * e.ld_zu + n, u, left);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          float a, da, b, db;
+          train_act_slope<kFast>(e.act, zv[j], a, da);
+          train_act_slope<kFast>(e.act_up, u[j], b, db);
+          h[j] = a * b;
+          du[j] = v[j] * a * db;
+          v[j] = v[j] * b * da;
+        }
+        store_hidden<T>(e.dz, m * e.ld_h + n, e.limb, v, left);
+        store_hidden<T>(e.du, m * e.ld_h + n, e.limb, du, left);
+        store_hidden<T>(e.h, m * e.ld_h + n, e.limb, h, left);
+      }
+#pragma unroll
+      for (int j = 0; j < 4; ++j) down[r][c + j] = j < left ? v[j] : 0.f;
+    }
+  }
+  if (EPI == kEpiHidden && e.db) {
+    __syncthreads();
+    const int n = n0 + threadIdx.x;
+    if (threadIdx.x < kJoinCols && n < e.N) {
+      float sum = 0.f;
+#pragma unroll
+      for (int r = 0; r < 32; ++r) sum += down[r][threadIdx.x];
+      e.db[(int64_t)(m0 >> 5) * e.ld_h + n] = sum;
+    }
+  }
+}
+
+}  // namespace
+
+cudaError_t launch_train_join(const UmmaParams& p, int epilogue, bool f32, int pairs, cudaStream_t s) {
+  const int across = (p.tile_cols + kJoinCols - 1) / kJoinCols, cols = (int)(p.piece / kPairRows);
+  const int tiles = (p.tiles - p.whole) * across, rows = epilogue == kEpiHidden || tiles >= 148 ? 32 : 8;
+  const dim3 grid((unsigned)(tiles * (kPairRows / rows))), block(join_threads(epilogue));
+  if (epilogue == kEpiStore) return f32 ? launch_pdl(train_join_kernel<kEpiStore, float>, grid, block, 0, s, p, pairs, cols, rows)
+                                        : launch_pdl(train_join_kernel<kEpiStore, __nv_bfloat16>, grid, block, 0, s, p, pairs, cols, rows);
+  if (epilogue == kEpiGateUp) return f32 ? launch_pdl(train_join_kernel<kEpiGateUp, float>, grid, block, 0, s, p, pairs, cols, rows)
+                                         : launch_pdl(train_join_kernel<kEpiGateUp, __nv_bfloat16>, grid, block, 0, s, p, pairs, cols, rows);
+  return f32 ? launch_pdl(train_join_kernel<kEpiHidden, float>, grid, block, 0, s, p, pairs, cols, rows)
+             : launch_pdl(train_join_kernel<kEpiHidden, __nv_bfloat16>, grid, block, 0, s, p, pairs, cols, rows);
+}
+
+}  // namespace sffn

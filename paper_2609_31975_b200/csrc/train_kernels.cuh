@@ -87,14 +87,12 @@ struct TrainUmma {
   TrainGemm g;
   bool f32;                // storage type of the outputs, and three terms an operand
   int64_t limb_a[3], limb_b[3];
-  float* partial;          // room for the pieces of tiles that several pairs of CTAs share (train_umma_partial_bytes)
-  uint32_t* counters;      // train_umma_counter_bytes of zeros; zeros again after the launch
+  float* partial;          // room for the pieces of tiles that several pairs of CTAs share (kTrainPartialBytes)
   int32_t* status;
 };
 constexpr int kTrainUmmaPairs = 80;    // pairs of CTAs at most
 constexpr size_t kTrainPieceBytes = 256 * 512 * 4;
 constexpr size_t kTrainPartialBytes = 2 * kTrainUmmaPairs * kTrainPieceBytes;
-constexpr size_t kTrainCounterBytes = kTrainUmmaPairs * 32 * 4;
 int train_umma_lines(int M);
 cudaError_t launch_train_umma(const TrainUmma& t, cudaStream_t s);
 // out[l][r][c], l = 0, 1, 2: the bf16 terms of in[r][c]; `ld_out` elements between rows, `limb` between terms.

@@ -10,16 +10,16 @@
 //   kGateUp  z and u of 128 neurons, 256 columns: the even CTA's half of B is W_g, the odd one's W_up, so that z and u of a neuron are
 //            in the same lane of tensor memory, 128 columns apart.  Two accumulators: one tile's epilogue runs under the next tile.
 //   kHidden  dh of 256 neurons.  Its dz is summed over the tokens in fp32 (db_g), and the tensor cores truncate when they add onto an
-//            accumulator: the sum comes out low by 5e-8 of its typical size for every 64 of K (3e-6 at K = 4096).  So runs of 512 k
-//            get an accumulator of their own, eight warps add the runs up in registers, rounding to nearest (4e-7), and
+//            accumulator: the sum comes out low by 5e-8 of its typical size for every 64 of K (3e-6 at K = 4096).  So runs of 768 k
+//            get an accumulator of their own, eight warps add the runs up in registers, rounding to nearest (7e-7), and
 //            put them into the other half of tensor memory, where four more warps make dz, du and h of them under the next tile.
 //
 // Epilogues leave through shared memory: boxes of 32 rows x 64 columns, 128-byte swizzle, which tensor-map stores take to the
 // caller's rows, whatever their stride and alignment, cut off at the matrix's edges.
 //
 // Tiles are dealt to the pairs round robin.  What is left for a last, partly idle round is cut along K instead so that all pairs get
-// the same share of it: each leaves its piece of a tile as fp32 in a workspace, and whoever finishes last, warp by warp, adds up
-// the pieces in their order in K.  Nobody waits for anybody, and which warp adds does not change what it adds.
+// the same share of it: each leaves its piece of a tile as fp32 in a workspace, and train_join_kernel adds up the pieces in their
+// order in K and does the epilogue.
 // Every wait is bounded by a cycle budget; on expiry the status word is set, all roles wind down and tensor memory is given back.
 #include "fused_kernel.cuh"
 #include "train_umma.cuh"
@@ -102,7 +102,6 @@ __global__ void __launch_bounds__(Form<EPI>::kThreads, 1) train_umma_kernel(cons
   extern __shared__ uint8_t smem_raw[];
   __shared__ int abort_word;
   __shared__ uint32_t tmem_slot;
-  __shared__ int finished[kAdders];  // kHidden: whether a warp's part of the tile is complete
   __shared__ __align__(8) uint64_t bars[2 * kStages + 4 + 2 + 4];
   volatile int* const abort_flag = &abort_word;
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
@@ -249,8 +248,7 @@ __global__ void __launch_bounds__(Form<EPI>::kThreads, 1) train_umma_kernel(cons
       const int row0 = at.m * kPairRows + rank * 128 + 32 * quad;  // this warp's first row
       const bool rows = row0 < e.M;                                // has any: the others only keep step
       const bool cut = is_cut(p, it);
-      uint32_t* counter = p.counters + (size_t)(it.tile - p.whole) * 32 + rank * 2 * kAdders + (warp - 4);
-      const size_t part = ((size_t)rank * kAdders + (warp - 4)) * (F::kWide * kChunks * 512);  // of a piece, in floats
+      float* const piece = cut ? piece_of(p, walk, pair, it.tile) + (size_t)(rank * 128 + 32 * quad + lane) * (256 * F::kWide) : nullptr;  // this lane's row
       if constexpr (EPI == kEpiHidden) {
         float acc[16 * kChunks];
 #pragma unroll
@@ -272,31 +270,16 @@ __global__ void __launch_bounds__(Form<EPI>::kThreads, 1) train_umma_kernel(cons
           give_back(0);
         }
         if (!ok) break;
-        bool finish = rows;
-        if (cut && rows) {
-          const Cut of(p, walk, it);
-          float* out = of.place(p, walk, pair) + part;
+        if (cut) {
 #pragma unroll
-          for (int c = 0; c < kChunks; ++c) put_piece(out, c, lane, acc + 16 * c);
-          finish = last_piece(counter, of.pieces, lane);
-          if (finish) {
-#pragma unroll
-            for (int i = 0; i < 16 * kChunks; ++i) acc[i] = 0.f;
-#pragma unroll 1
-            for (int q = of.first; q < of.first + of.pieces; ++q) {
-              const float* in = of.place(p, walk, q) + part;
-#pragma unroll
-              for (int c = 0; c < kChunks; ++c) {
-                add_piece(in, c, lane, acc + 16 * c);
-                asm volatile("" ::: "memory");  // sixteen values under way at a time: the registers are full
-              }
-            }
-          }
+          for (int c = 0; c < kChunks; ++c)
+            if (rows) put_piece(piece + column(c), acc + 16 * c);
+          continue;
         }
         ok = __all_sync(0xffffffffu, mbar_wait(sums_empty, sums_phase, abort_flag, p.status, p.budget));
         if (!ok) break;
         sums_phase ^= 1;
-        if (finish) {
+        if (rows) {
           fence_after();
 #pragma unroll
           for (int c = 0; c < kChunks; ++c) tmem_st16(tmem + 256 + lanes + column(c), acc + 16 * c);
@@ -304,10 +287,7 @@ __global__ void __launch_bounds__(Form<EPI>::kThreads, 1) train_umma_kernel(cons
           fence_before();
         }
         __syncwarp();
-        if (lane == 0) {
-          reinterpret_cast<volatile int*>(finished)[warp - 4] = finish;
-          arrive(sums_full);
-        }
+        if (lane == 0) arrive(sums_full);
       } else {
         const int halves = halves_of(at);
         for (int h = 0; h < halves; ++h) {
@@ -315,33 +295,19 @@ __global__ void __launch_bounds__(Form<EPI>::kThreads, 1) train_umma_kernel(cons
           ok = wait_full(buffer);
           if (!ok) break;
           const uint32_t acc = tmem + lanes + buffer * 256;
-          bool finish = rows;
-          const size_t part_h = part + (size_t)h * (kChunks * 512);
+          auto sums = [&](int c, float* v) {
+            tmem_ld16(acc + column(c), v);
+            tmem_arrived(v);
+          };
           if (cut && rows) {
-            const Cut of(p, walk, it);
-            float* out = of.place(p, walk, pair) + part_h;
 #pragma unroll 2
             for (int c = 0; c < kChunks; ++c) {
               float v[16];
-              tmem_ld16(acc + column(c), v);
-              tmem_arrived(v);
-              put_piece(out, c, lane, v);
+              sums(c, v);
+              put_piece(piece + 256 * h + column(c), v);
             }
-            finish = last_piece(counter + h * kAdders, of.pieces, lane);
           }
-          auto sums = [&](int c, float* v) {
-            if (!cut) {
-              tmem_ld16(acc + column(c), v);
-              tmem_arrived(v);
-              return;
-            }
-#pragma unroll
-            for (int i = 0; i < 16; ++i) v[i] = 0.f;
-            const Cut of(p, walk, it);
-#pragma unroll 1
-            for (int q = of.first; q < of.first + of.pieces; ++q) add_piece(of.place(p, walk, q) + part_h, c, lane, v);
-          };
-          if (finish) {
+          if (rows && !cut) {
             if constexpr (EPI == kEpiStore) {
               const int n0 = at.n * F::kTileCols + 256 * h + 128 * half;
 #pragma unroll 1
@@ -421,6 +387,7 @@ __global__ void __launch_bounds__(Form<EPI>::kThreads, 1) train_umma_kernel(cons
     int sums_phase = 0, in_phase = 0;
     bool ok = true;
     while (ok && walk.step(p, it)) {
+      if (is_cut(p, it)) continue;
       const Place at = place_of(p, it.tile);
       const int row0 = at.m * kPairRows + rank * 128 + 32 * quad;
       const bool rows = row0 < e.M;
@@ -441,12 +408,10 @@ __global__ void __launch_bounds__(Form<EPI>::kThreads, 1) train_umma_kernel(cons
         ok = __all_sync(0xffffffffu, mbar_wait(bar, in_phase, abort_flag, p.status, p.budget));
         if (!ok) break;
         in_phase ^= 1;
-        const bool mine = reinterpret_cast<volatile int*>(finished)[quad + 4 * (x >> 1)];
         const int n0 = at.n * 256 + 64 * x;
-        if (mine) boxes_free(lane);
+        boxes_free(lane);
 #pragma unroll 1
         for (int q = 0; q < 4; ++q) {
-          if (!mine) break;
           float dh[16], a[16], da[16], bv[16], db[16];
           tmem_ld16(tmem + 256 + lanes + 64 * x + 16 * q, dh);
           Sixteen t;
@@ -470,10 +435,9 @@ __global__ void __launch_bounds__(Form<EPI>::kThreads, 1) train_umma_kernel(cons
             if (!(lane & 1) && n < e.N) e.db[(int64_t)(row0 >> 5) * e.ld_h + n] = sum;
           }
         }
-        if (mine) boxes_written();
-        else __syncwarp();
+        boxes_written();
         if (x + 1 < n_boxes) fetch(x + 1);
-        if (mine && lane == 0) {
+        if (lane == 0) {
           if (e.dz) box_store(&maps.out[0], box, n0, row0);
           if (e.du) box_store(&maps.out[1], box + kBoxBytes, n0, row0);
           if (e.h) box_store(&maps.out[2], box + 2 * kBoxBytes, n0, row0);
@@ -544,7 +508,9 @@ cudaError_t launch_one(const TrainUmma& t, int pairs, cudaStream_t s) {
   static unsigned long long configured = 0;
   const cudaError_t err = allow_dynamic_smem(train_umma_kernel<EPI>, F::kSmemBytes, configured);
   if (err != cudaSuccess) return err;
-  return launch_clusters(2, train_umma_kernel<EPI>, dim3(2 * pairs), dim3(F::kThreads), F::kSmemBytes, s, p, maps);
+  const cudaError_t launched = launch_clusters(2, train_umma_kernel<EPI>, dim3(2 * pairs), dim3(F::kThreads), F::kSmemBytes, s, p, maps);
+  if (launched != cudaSuccess || p.whole == p.tiles) return launched;
+  return launch_train_join(p, EPI, false, pairs, s);
 }
 
 }  // namespace
@@ -593,13 +559,13 @@ int plan_umma(const TrainUmma& t, int cols, UmmaParams& p, int pairs) {
   p.a_mn = !g.a_major_k;
   p.b_mn = !g.b_major_k;
   p.partial = t.partial;
-  p.counters = t.counters;
   p.status = t.status;
   p.budget = fused_test_knobs().wait_cycles;
-  // Whole rounds of tiles, then the rest cut along K, unless a pair's share of it is so small that pieces cost more than they save.
+  // Whole rounds of tiles, then the rest cut along K where that saves the time of a dozen K blocks or more (6 us; the pieces and the
+  // kernel that joins them cost about that: 1000 tokens, 4096 x 14336, JOINSTORY).
   p.whole = p.tiles / pairs * pairs;
   const long long rest = p.tiles - p.whole;
-  if (!t.partial || rest == 0 || rest * p.units < pairs || rest * p.units * p.unit_blocks < kCutBlocks * pairs) {
+  if (!t.partial || rest == 0 || rest * p.units < pairs || (pairs - rest) * p.units * p.unit_blocks < 12ll * pairs) {
     p.whole = p.tiles;
     if (p.tiles < pairs) pairs = p.tiles;
   }

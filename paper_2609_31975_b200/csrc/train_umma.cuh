@@ -12,9 +12,8 @@ constexpr int kDeep = 64;                    // bf16 elements of one 128-byte sw
 constexpr int kHalfBytes = 128 * kDeep * 2;  // 128 rows of a K block
 constexpr int kLimbBlocks = 4;               // fp32: K blocks of a run, which is six times as long
 constexpr int kLimbUnit = 6 * kLimbBlocks;
-constexpr int kRunBlocks = 8;                // dh: K blocks of a run
+constexpr int kRunBlocks = 12;               // dh: K blocks of a run
 
-constexpr int kCutBlocks = 16;               // K blocks that a pair's share of the cut tiles has at least
 
 struct UmmaParams {
   TrainEpilogue epi;
@@ -26,7 +25,6 @@ struct UmmaParams {
   int a_mn, b_mn;
   float* partial;
   size_t piece;                       // floats of a pair's piece of a tile
-  uint32_t* counters;
   int32_t* status;
   long long budget;
 };
@@ -97,52 +95,19 @@ __device__ __forceinline__ void block_of(const UmmaParams& p, int u, int j, int&
   }
 }
 
-// The pieces of a cut tile, in the order of K: consecutive pairs have one each, the first of them perhaps as its second piece.
-struct Cut {
-  int first, pieces;
-  long long lo;  // the tile's first unit among those of all cut tiles
-  __device__ __forceinline__ Cut(const UmmaParams& p, const Walk& w, const Item& it) {
-    lo = (long long)(it.tile - p.whole) * p.units;
-    const long long all = (long long)(p.tiles - p.whole) * p.units, hi = lo + p.units;
-    first = (int)(lo * w.pairs / all);
-    while (w.share(first + 1) <= lo) ++first;
-    while (first > 0 && w.share(first) > lo) --first;
-    int last = first;
-    while (w.share(last + 1) < hi) ++last;
-    pieces = last - first + 1;
-  }
-  // Where pair `q` keeps its piece of this tile.
-  __device__ __forceinline__ float* place(const UmmaParams& p, const Walk& w, int q) const {
-    return p.partial + (size_t)(2 * q + (w.share(q) < lo ? 1 : 0)) * p.piece;
-  }
-};
 __device__ __forceinline__ bool is_cut(const UmmaParams& p, const Item& it) { return it.u0 > 0 || it.u1 < p.units; }
-
-// One warp has stored its part of a piece; true for the warp that finds all the others there.  The counter is left at zero.
-__device__ __forceinline__ bool last_piece(uint32_t* counter, int pieces, int lane) {
-  __threadfence();
-  __syncwarp();
-  uint32_t before = 0;
-  if (lane == 0) before = atomicAdd(counter, 1u);
-  before = __shfl_sync(0xffffffffu, before, 0);
-  if (before != (uint32_t)(pieces - 1)) return false;
-  __threadfence();
-  if (lane == 0) *counter = 0;
-  return true;
+// Where a pair leaves its piece of a cut tile, [256][columns of the accumulators] fp32: a pair has at most two, of the tile that its
+// share begins in and of the one after.
+__device__ __forceinline__ float* piece_of(const UmmaParams& p, const Walk& w, int pair, int tile) {
+  return p.partial + (size_t)(2 * pair + (w.share(pair) < (tile - p.whole) * p.units ? 1 : 0)) * p.piece;
 }
-// Sixteen columns of a warp's 32 rows in a piece: four rows of 512 bytes.
-__device__ __forceinline__ void put_piece(float* part, int chunk, int lane, const float* v) {
-  float4* out = reinterpret_cast<float4*>(part) + (size_t)chunk * 128 + lane;
+// Sixteen columns of a row of a piece.
+__device__ __forceinline__ void put_piece(float* at, const float* v) {
 #pragma unroll
-  for (int q = 0; q < 4; ++q) __stcg(out + 32 * q, make_float4(v[4 * q], v[4 * q + 1], v[4 * q + 2], v[4 * q + 3]));
-}
-__device__ __forceinline__ void add_piece(const float* part, int chunk, int lane, float* v) {
-  const float4* in = reinterpret_cast<const float4*>(part) + (size_t)chunk * 128 + lane;
-#pragma unroll
-  for (int q = 0; q < 4; ++q) {
-    const float4 f = __ldcg(in + 32 * q);
-    v[4 * q] += f.x; v[4 * q + 1] += f.y; v[4 * q + 2] += f.z; v[4 * q + 3] += f.w;
-  }
+  for (int h = 0; h < 2; ++h)
+    asm volatile("st.global.v8.f32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};" ::"l"(at + 8 * h), "f"(v[8 * h]), "f"(v[8 * h + 1]), "f"(v[8 * h + 2]), "f"(v[8 * h + 3]),
+                 "f"(v[8 * h + 4]), "f"(v[8 * h + 5]), "f"(v[8 * h + 6]), "f"(v[8 * h + 7])
+                 : "memory");
 }
 
 __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
@@ -209,5 +174,7 @@ bool make_operand_maps(const TrainUmma& t, CUtensorMap* a, CUtensorMap* b);
 int plan_umma(const TrainUmma& t, int cols, UmmaParams& p, int pairs);
 
 cudaError_t launch_train_umma_f32(const TrainUmma& t, int pairs, cudaStream_t s);
+// The epilogue of the tiles that were cut along K, after the launch that left their pieces.
+cudaError_t launch_train_join(const UmmaParams& p, int epilogue, bool f32, int pairs, cudaStream_t s);
 
 }  // namespace sffn

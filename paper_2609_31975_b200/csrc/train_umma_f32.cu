@@ -258,32 +258,15 @@ __global__ void __launch_bounds__(kThreads, 1) train_umma_f32_kernel(const __gri
         tmem_arrived(v);
       };
       // A tile that several pairs share: this warp's part of it is 16 KB of every piece.
-      bool finish = true;
-      const bool cut = is_cut(p, it);
-      const size_t region = ((size_t)rank * kEpilogueWarps + (warp - 4)) * (16 * kChunks * 32);  // floats
-      if (cut) {
-        const Cut of(p, walk, it);
-        float* out = of.place(p, walk, pair) + region;
+      if (is_cut(p, it)) {
+        float* piece = piece_of(p, walk, pair, it.tile) + (size_t)(rank * 128 + 32 * quad + lane) * kCols;
 #pragma unroll 2
         for (int c = 0; c < kChunks; ++c) {
           float v[16];
           own(c, v);
-          put_piece(out, c, lane, v);
+          if (row) put_piece(piece + column(c), v);
         }
-        finish = last_piece(p.counters + (it.tile - p.whole) * 16 + rank * kEpilogueWarps + (warp - 4), of.pieces, lane);
-      }
-      auto sums = [&](int c, float* v) {
-        if (!cut) {
-          own(c, v);
-          return;
-        }
-#pragma unroll
-        for (int i = 0; i < 16; ++i) v[i] = 0.f;
-        const Cut of(p, walk, it);
-#pragma unroll 1
-        for (int q = of.first; q < of.first + of.pieces; ++q) add_piece(of.place(p, walk, q) + region, c, lane, v);
-      };
-      if (finish) {
+      } else {
         if constexpr (EPI == kEpiStore) {
           void* out = e.out[at.batch];
           const bool wide = wide_user && (reinterpret_cast<uintptr_t>(out) & 31) == 0;
@@ -291,7 +274,7 @@ __global__ void __launch_bounds__(kThreads, 1) train_umma_f32_kernel(const __gri
           for (int c = 0; c < kOut; ++c) {
             const int n = n0 + 16 * c;
             float v[16];
-            sums(c, v);
+            own(c, v);
             if (row && n < e.N) store16(out, m * e.ld_out + n, v, min(16, e.N - n), wide);
           }
         } else if constexpr (EPI == kEpiGateUp) {
@@ -299,8 +282,8 @@ __global__ void __launch_bounds__(kThreads, 1) train_umma_f32_kernel(const __gri
           for (int c = 0; c < kOut; ++c) {
             const int n = n0 + 16 * c;
             float z[16], u[16];
-            sums(c, z);
-            sums(c + 4, u);
+            own(c, z);
+            own(c + 4, u);
             const int left = min(16, e.N - n);
             if (e.bias) {
               const float bias = lane < left ? e.bias[n + lane] : 0.f;
@@ -340,7 +323,7 @@ __global__ void __launch_bounds__(kThreads, 1) train_umma_f32_kernel(const __gri
             slope16<false>(e.act, rz, a, da);
             slope16<false>(e.act_up, ru, bv, db);
             if (c + 1 < kOut) fetch(c + 1);
-            sums(c, dh);
+            own(c, dh);
 #pragma unroll
             for (int i = 0; i < 16; ++i) {
               db[i] *= dh[i] * a[i];   // du
@@ -417,7 +400,9 @@ cudaError_t launch_one(const UmmaParams& p, const Maps& maps, int pairs, cudaStr
   static unsigned long long configured = 0;
   const cudaError_t e = allow_dynamic_smem(train_umma_f32_kernel<EPI>, kSmemBytes, configured);
   if (e != cudaSuccess) return e;
-  return launch_clusters(2, train_umma_f32_kernel<EPI>, dim3(2 * pairs), dim3(kThreads), kSmemBytes, s, p, maps);
+  const cudaError_t launched = launch_clusters(2, train_umma_f32_kernel<EPI>, dim3(2 * pairs), dim3(kThreads), kSmemBytes, s, p, maps);
+  if (launched != cudaSuccess || p.whole == p.tiles) return launched;
+  return launch_train_join(p, EPI, true, pairs, s);
 }
 
 }  // namespace
