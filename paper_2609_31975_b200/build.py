@@ -11,6 +11,7 @@ from __future__ import annotations
 import os
 import subprocess
 import sys
+import sysconfig
 from concurrent.futures import ThreadPoolExecutor
 from pathlib import Path
 
@@ -18,6 +19,7 @@ PKG = Path(__file__).resolve().parent
 ROOT = PKG.parent
 CSRC = PKG / "csrc"
 LIB = PKG / "libsparse_ffn.so"
+CALLS = PKG / "_training.so"  # the training calls' Python side (csrc/torch_calls.cpp)
 OBJ = PKG / "build"
 SOURCES = ["api.cu", "general_kernels.cu", "fused_kernel.cu", "fused_tc_kernel.cu", "static_entry.cu",
            "batched_kernels.cu", "umma_kernels.cu", "cast_kernels.cu", "optim_kernels.cu", "train_simt.cu", "train_umma.cu", "train_umma_f32.cu", "train_join.cu", "train_api.cu"]
@@ -28,7 +30,32 @@ def _headers_mtime() -> float:
     return max(d.stat().st_mtime for d in deps)
 
 
+def build_calls(force: bool = False) -> Path:
+    """Compiles the module that checks and marshals the training calls' tensors, against the torch that is installed."""
+    src = CSRC / "torch_calls.cpp"
+    newest = max(src.stat().st_mtime, (ROOT / "include" / "sparse_ffn.h").stat().st_mtime)
+    if not force and CALLS.exists() and CALLS.stat().st_mtime >= newest:
+        return CALLS
+    import torch
+
+    at = Path(torch.__file__).resolve().parent
+    includes = [at / "include", at / "include" / "torch" / "csrc" / "api" / "include", Path(sysconfig.get_paths()["include"]),
+                Path(os.environ.get("CUDA_HOME", "/usr/local/cuda")) / "include"]
+    tmp = CALLS.with_suffix(f".{os.getpid()}.tmp")
+    cmd = [os.environ.get("CXX", "g++"), "-O2", "-std=c++17", "-fPIC", "-shared", "-fvisibility=hidden",
+           f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}", "-I", str(ROOT / "include")]
+    for p in includes:
+        cmd += ["-isystem", str(p)]
+    cmd += [str(src), "-o", str(tmp), "-L", str(at / "lib"), "-lc10", "-lc10_cuda", "-ltorch_cpu", "-ltorch_python"]
+    r = subprocess.run(cmd, capture_output=True, text=True)
+    if r.returncode != 0:
+        raise RuntimeError(f"{src.name}:\n{r.stdout}\n{r.stderr}")
+    os.replace(tmp, CALLS)
+    return CALLS
+
+
 def build(force: bool = False, verbose: bool = False, trace: bool = False, debug: bool = False) -> Path:
+    build_calls(force)
     lib = PKG / "libsparse_ffn_trace.so" if trace else PKG / "libsparse_ffn_debug.so" if debug else LIB
     newest = max(_headers_mtime(), max((CSRC / s).stat().st_mtime for s in SOURCES))
     if not force and lib.exists() and lib.stat().st_mtime >= newest:
