@@ -1,6 +1,6 @@
 // Products of small training calls in fp32 FMAs (fp32 storage; larger calls split their operands for the tensor cores).
 //
-// A CTA owns a 32 x 64 tile of C, or z and u of 32 tokens x 32 neurons; a thread 2 x 4 of it.  Pieces of 32 k go through
+// A CTA owns a 32 x 64 tile of C, or z and u of 32 tokens x 32 neurons; a thread 4 x 4 of it.  Pieces of 64 k go through
 // registers into [k][m] and [k][n] arrays, whichever way an operand lies in memory, the next piece under way while one is
 // multiplied.  Such a call has few tiles and is bound by latency, so K is cut among up to eight CTAs of a cluster: each
 // leaves its sums in shared memory and takes a share of the tile's rows, which it adds up over all of them, in order.
@@ -9,7 +9,7 @@
 namespace sffn {
 namespace {
 
-constexpr int kRows = 32, kCols = 64, kDepth = 32, kThreads = 256;
+constexpr int kRows = 32, kCols = 64, kDepth = 64, kThreads = 128;
 constexpr int kMaxSplit = 8;
 
 // A thread's share of a [kDepth][N] piece: N / 32 times four values, consecutive in memory.
@@ -18,13 +18,18 @@ struct Piece {
   static constexpr int kQuads = N * kDepth / 4 / kThreads;
   float4 v[kQuads];
 
+  // Quad i of a K-major piece: two lanes take 32 bytes of a row, a warp sixteen rows, so that its four stores (one a k) meet no bank
+  // twice.
+  __device__ __forceinline__ static int row_of(int i) { return (i >> 5) % (N / 16) * 16 + ((i & 31) >> 1); }
+  __device__ __forceinline__ static int k_of(int i) { return ((i >> 5) / (N / 16) * 2 + (i & 1)) * 4; }
+
   // rows are a multiple of 16 bytes apart; along an axis that ends inside a quad what lies beyond is not looked at
   __device__ __forceinline__ void fetch(const TrainOperand& o, bool major_k, int row0, int rows, int k0, int k1) {
     const float* p = static_cast<const float*>(o.data);
 #pragma unroll
     for (int q = 0; q < kQuads; ++q) {
       const int i = threadIdx.x + q * kThreads;
-      const int r = major_k ? i / (kDepth / 4) : i % (N / 4) * 4, k = major_k ? i % (kDepth / 4) * 4 : i / (N / 4);
+      const int r = major_k ? row_of(i) : i % (N / 4) * 4, k = major_k ? k_of(i) : i / (N / 4);
       const int line = major_k ? row0 + r : k0 + k, at = major_k ? k0 + k : row0 + r, lines = major_k ? rows : k1, end = major_k ? k1 : rows;
       float4 f = make_float4(0.f, 0.f, 0.f, 0.f);
       if (line < lines && at < end) {
@@ -45,7 +50,7 @@ struct Piece {
     for (int q = 0; q < kQuads; ++q) {
       const int i = threadIdx.x + q * kThreads;
       if (major_k) {
-        const int r = i / (kDepth / 4), k = i % (kDepth / 4) * 4;
+        const int r = row_of(i), k = k_of(i);
         s[k][r] = v[q].x; s[k + 1][r] = v[q].y; s[k + 2][r] = v[q].z; s[k + 3][r] = v[q].w;
       } else {
         *reinterpret_cast<float4*>(&s[i / (N / 4)][i % (N / 4) * 4]) = v[q];
@@ -102,7 +107,7 @@ __global__ void __launch_bounds__(kThreads) train_simt_kernel(const __grid_const
   // K of all parts in a row, in pieces
   const int parts = kDual ? 1 : g.parts, per = (g.K + kDepth - 1) / kDepth, pieces = parts * per;
   const int first = (int)((long long)pieces * split / splits), last = (int)((long long)pieces * (split + 1) / splits);
-  float acc[2][4] = {};
+  float acc[4][4] = {};
   Piece<kRows> pa;
   Piece<kDual ? kNeurons : kCols> pb;
   Piece<kDual ? kNeurons : kRows> pu;  // kDual: of W_up
@@ -117,7 +122,7 @@ __global__ void __launch_bounds__(kThreads) train_simt_kernel(const __grid_const
     if constexpr (kDual) {  // always K-major
 #pragma unroll
       for (int q = 0; q < Piece<kNeurons>::kQuads; ++q) {
-        const int i = threadIdx.x + q * kThreads, r = i / (kDepth / 4), k = i % (kDepth / 4) * 4;
+        const int i = threadIdx.x + q * kThreads, r = pb.row_of(i), k = pb.k_of(i);
         sb[k][r] = pb.v[q].x; sb[k + 1][r] = pb.v[q].y; sb[k + 2][r] = pb.v[q].z; sb[k + 3][r] = pb.v[q].w;
         sb[k][kNeurons + r] = pu.v[q].x; sb[k + 1][kNeurons + r] = pu.v[q].y; sb[k + 2][kNeurons + r] = pu.v[q].z; sb[k + 3][kNeurons + r] = pu.v[q].w;
       }
@@ -132,15 +137,17 @@ __global__ void __launch_bounds__(kThreads) train_simt_kernel(const __grid_const
     if (i + 1 < last) fetch(i + 1);
 #pragma unroll 8
     for (int k = 0; k < kDepth; ++k) {
-      const float2 a = *reinterpret_cast<const float2*>(&sa[k][2 * ty]);
-      const float4 b = *reinterpret_cast<const float4*>(&sb[k][4 * tx]);
-      acc[0][0] = fmaf(a.x, b.x, acc[0][0]); acc[0][1] = fmaf(a.x, b.y, acc[0][1]); acc[0][2] = fmaf(a.x, b.z, acc[0][2]); acc[0][3] = fmaf(a.x, b.w, acc[0][3]);
-      acc[1][0] = fmaf(a.y, b.x, acc[1][0]); acc[1][1] = fmaf(a.y, b.y, acc[1][1]); acc[1][2] = fmaf(a.y, b.z, acc[1][2]); acc[1][3] = fmaf(a.y, b.w, acc[1][3]);
+      const float4 a = *reinterpret_cast<const float4*>(&sa[k][4 * ty]), b = *reinterpret_cast<const float4*>(&sb[k][4 * tx]);
+      const float av[4] = {a.x, a.y, a.z, a.w}, bv[4] = {b.x, b.y, b.z, b.w};
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) acc[i][j] = fmaf(av[i], bv[j], acc[i][j]);
     }
     __syncthreads();
   }
 #pragma unroll
-  for (int i = 0; i < 2; ++i) *reinterpret_cast<float4*>(&tile[2 * ty + i][4 * tx]) = make_float4(acc[i][0], acc[i][1], acc[i][2], acc[i][3]);
+  for (int i = 0; i < 4; ++i) *reinterpret_cast<float4*>(&tile[4 * ty + i][4 * tx]) = make_float4(acc[i][0], acc[i][1], acc[i][2], acc[i][3]);
   if (splits > 1) cluster_meet();
   else __syncthreads();
 
@@ -153,11 +160,12 @@ __global__ void __launch_bounds__(kThreads) train_simt_kernel(const __grid_const
       v[0] = f.x; v[1] = f.y; v[2] = f.z; v[3] = f.w;
       return;
     }
+    float4 f[kMaxSplit];  // every load is under way before the first is added
+#pragma unroll
+    for (int s = 0; s < kMaxSplit; ++s) f[s] = s < splits ? remote_quad(&tile[r][c], s) : make_float4(0.f, 0.f, 0.f, 0.f);
     v[0] = v[1] = v[2] = v[3] = 0.f;
-    for (int s = 0; s < splits; ++s) {
-      const float4 f = remote_quad(&tile[r][c], s);
-      v[0] += f.x; v[1] += f.y; v[2] += f.z; v[3] += f.w;
-    }
+#pragma unroll
+    for (int s = 0; s < kMaxSplit; ++s) { v[0] += f[s].x; v[1] += f[s].y; v[2] += f[s].z; v[3] += f[s].w; }
   };
   float* const down = pool;  // kHidden: [rows][kCols] of dz
   static_assert(kRows * kCols <= kDepth * (kRows + 4 + kCols + 4), "dz of a tile fits the operands' arrays");
@@ -236,13 +244,13 @@ __global__ void __launch_bounds__(256) train_column_sums_kernel(const float* par
   }
 }
 
-// CTAs that share a tile's K: as long as all run at once, and each has two pieces.
+// CTAs that share a tile's K: as long as all run at once, and each has a piece.
 int splits_for(const TrainGemm& g) {
   const int neurons = g.epilogue == kEpiGateUp ? kCols / 2 : kCols;
   const long long tiles = (long long)((g.M + kRows - 1) / kRows) * ((g.N + neurons - 1) / neurons) * g.batch;
   const int pieces = (g.epilogue == kEpiGateUp ? 1 : g.parts) * ((g.K + kDepth - 1) / kDepth);
   int s = 1;
-  while (s < kMaxSplit && tiles * s * 2 <= 2 * 148 && pieces >= 4 * s) s *= 2;
+  while (s < kMaxSplit && tiles * s * 2 <= 2 * 148 && pieces >= 2 * s) s *= 2;
   return s;
 }
 
