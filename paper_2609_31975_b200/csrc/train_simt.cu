@@ -1,6 +1,6 @@
 // Products of small training calls in fp32 FMAs (fp32 storage; larger calls split their operands for the tensor cores).
 //
-// A CTA owns a 32 x 64 tile of C, or z and u of 32 tokens x 32 neurons; a thread 4 x 4 of it.  Pieces of 64 k go through
+// A CTA owns a 32 x 64 tile of C, or z and u of 32 tokens x 32 neurons; two threads (of half of its k each) 4 x 4 of it.  Pieces of 64 k go through
 // registers into [k][m] and [k][n] arrays, whichever way an operand lies in memory, the next piece under way while one is
 // multiplied.  Such a call has few tiles and is bound by latency, so K is cut among up to eight CTAs of a cluster: each
 // leaves its sums in shared memory and takes a share of the tile's rows, which it adds up over all of them, in order.
@@ -9,7 +9,7 @@
 namespace sffn {
 namespace {
 
-constexpr int kRows = 32, kCols = 64, kDepth = 64, kThreads = 128;
+constexpr int kRows = 32, kCols = 64, kDepth = 64, kThreads = 256;
 constexpr int kMaxSplit = 8;
 
 // A thread's share of a [kDepth][N] piece: N / 32 times four values, consecutive in memory.
@@ -100,7 +100,7 @@ __global__ void __launch_bounds__(kThreads) train_simt_kernel(const __grid_const
   __shared__ __align__(16) float tile[kRows][kCols + 4];
   pdl_launch_dependents();
   pdl_wait();
-  const int tx = threadIdx.x & 15, ty = threadIdx.x >> 4;
+  const int tx = threadIdx.x & 15, ty = (threadIdx.x >> 4) & 7, half = threadIdx.x >> 7;  // half: of a piece's k
   const int m_tiles = (g.M + kRows - 1) / kRows, n_tiles = (g.N + kNeurons - 1) / kNeurons;
   const int at_tile = blockIdx.x / splits, split = blockIdx.x - at_tile * splits, at_row = at_tile / n_tiles, z = at_row / m_tiles;
   const int m0 = (at_row - z * m_tiles) * kRows, n0 = (at_tile - at_row * n_tiles) * kNeurons;
@@ -136,7 +136,8 @@ __global__ void __launch_bounds__(kThreads) train_simt_kernel(const __grid_const
     __syncthreads();
     if (i + 1 < last) fetch(i + 1);
 #pragma unroll 8
-    for (int k = 0; k < kDepth; ++k) {
+    for (int q = 0; q < kDepth / 2; ++q) {
+      const int k = half * (kDepth / 2) + q;
       const float4 a = *reinterpret_cast<const float4*>(&sa[k][4 * ty]), b = *reinterpret_cast<const float4*>(&sb[k][4 * tx]);
       const float av[4] = {a.x, a.y, a.z, a.w}, bv[4] = {b.x, b.y, b.z, b.w};
 #pragma unroll
@@ -146,8 +147,19 @@ __global__ void __launch_bounds__(kThreads) train_simt_kernel(const __grid_const
     }
     __syncthreads();
   }
+  float(*const other)[kCols + 4] = reinterpret_cast<float(*)[kCols + 4]>(pool);  // the operands' arrays are free
+  if (half) {
 #pragma unroll
-  for (int i = 0; i < 4; ++i) *reinterpret_cast<float4*>(&tile[4 * ty + i][4 * tx]) = make_float4(acc[i][0], acc[i][1], acc[i][2], acc[i][3]);
+    for (int i = 0; i < 4; ++i) *reinterpret_cast<float4*>(&other[4 * ty + i][4 * tx]) = make_float4(acc[i][0], acc[i][1], acc[i][2], acc[i][3]);
+  }
+  __syncthreads();
+  if (!half) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const float4 o = *reinterpret_cast<const float4*>(&other[4 * ty + i][4 * tx]);
+      *reinterpret_cast<float4*>(&tile[4 * ty + i][4 * tx]) = make_float4(acc[i][0] + o.x, acc[i][1] + o.y, acc[i][2] + o.z, acc[i][3] + o.w);
+    }
+  }
   if (splits > 1) cluster_meet();
   else __syncthreads();
 
@@ -168,7 +180,7 @@ __global__ void __launch_bounds__(kThreads) train_simt_kernel(const __grid_const
     for (int s = 0; s < kMaxSplit; ++s) { v[0] += f[s].x; v[1] += f[s].y; v[2] += f[s].z; v[3] += f[s].w; }
   };
   float* const down = pool;  // kHidden: [rows][kCols] of dz
-  static_assert(kRows * kCols <= kDepth * (kRows + 4 + kCols + 4), "dz of a tile fits the operands' arrays");
+  static_assert(kRows * (kCols + 4) <= kDepth * (kRows + 4 + kCols + 4), "a tile fits the operands' arrays");
   for (int i = threadIdx.x; i < rows * (kNeurons / 4); i += kThreads) {
     const int r = i / (kNeurons / 4), c = i % (kNeurons / 4) * 4, m = m0 + r0 + r, n = n0 + c;
     const int left = m < g.M ? min(4, g.N - n) : 0;
