@@ -82,6 +82,21 @@ __device__ __forceinline__ void boxes_written() {
   asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
   __syncwarp();
 }
+// kStore: half boxes of 32 columns, 64-byte swizzle, two a warp: one is filled while the other's store reads it.  (With one box
+// of 64 columns a warp a tile of one K block took 7 us, all of it waits for stores: 5 tokens, 4096 x 14336, gradients of the weights
+// 102 us, FEWDW now.)
+__device__ __forceinline__ void half_box_put(uint32_t box, int lane, int q, const float* v) {
+  const uint32_t row = box + lane * 64;
+#pragma unroll
+  for (int i = 0; i < 2; ++i)
+    asm volatile("st.shared.v4.b32 [%0], {%1,%2,%3,%4};" ::"r"(row + (((2 * q + i) ^ ((lane >> 1) & 3)) << 4)), "r"(pack_bf16(v[8 * i], v[8 * i + 1])),
+                 "r"(pack_bf16(v[8 * i + 2], v[8 * i + 3])), "r"(pack_bf16(v[8 * i + 4], v[8 * i + 5])), "r"(pack_bf16(v[8 * i + 6], v[8 * i + 7]))
+                 : "memory");
+}
+__device__ __forceinline__ void other_box_free(int lane) {
+  if (lane == 0) asm volatile("cp.async.bulk.wait_group.read 1;" ::: "memory");
+  __syncwarp();
+}
 __device__ __forceinline__ void box_store(const CUtensorMap* map, uint32_t box, int c0, int c1) {
   asm volatile("cp.async.bulk.tensor.2d.global.shared::cta.bulk_group [%0, {%1, %2}], [%3];" ::"l"(map), "r"(c0), "r"(c1), "r"(box) : "memory");
 }
@@ -311,18 +326,19 @@ __global__ void __launch_bounds__(Form<EPI>::kThreads, 1) train_umma_kernel(cons
             if constexpr (EPI == kEpiStore) {
               const int n0 = at.n * F::kTileCols + 256 * h + 128 * half;
 #pragma unroll 1
-              for (int x = 0; x < 2; ++x) {
-                boxes_free(lane);
+              for (int x = 0; x < 4; ++x) {
+                const uint32_t to = box + (x & 1) * (kBoxBytes / 2);
+                other_box_free(lane);
 #pragma unroll
-                for (int q = 0; q < 4; ++q) {
+                for (int q = 0; q < 2; ++q) {
                   float v[16];
-                  sums(4 * x + q, v);
-                  box_put(box, lane, q, v);
+                  sums(2 * x + q, v);
+                  half_box_put(to, lane, q, v);
                 }
                 boxes_written();
-                if (lane == 0 && n0 + 64 * x < e.N) {
-                  box_store(&maps.out[at.batch], box, n0 + 64 * x, row0);
-                  boxes_leave();
+                if (lane == 0) {
+                  if (n0 + 32 * x < e.N) box_store(&maps.out[at.batch], to, n0 + 32 * x, row0);
+                  boxes_leave();  // a group for each half box, so that all but the last one means the other one
                 }
               }
             } else {
@@ -477,16 +493,16 @@ EncodeTiledFn encode_fn() {
   return fn;
 }
 
-// A bf16 matrix [rows, width] in boxes of 64 columns x 32 rows, 128-byte swizzle.
-bool make_box_map(CUtensorMap* m, const void* base, int64_t width, int64_t rows, int64_t ld) {
+// A bf16 matrix [rows, width] in boxes of 64 (32) columns x 32 rows, 128- (64-) byte swizzle.
+bool make_box_map(CUtensorMap* m, const void* base, int64_t width, int64_t rows, int64_t ld, bool half = false) {
   EncodeTiledFn fn = encode_fn();
   if (!fn) return false;
   const cuuint64_t dims[2] = {(cuuint64_t)width, (cuuint64_t)rows};
   const cuuint64_t strides[1] = {(cuuint64_t)ld * 2};
-  const cuuint32_t box[2] = {64, 32};
+  const cuuint32_t box[2] = {half ? 32u : 64u, 32};
   const cuuint32_t steps[2] = {1, 1};
   return fn(m, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, const_cast<void*>(base), dims, strides, box, steps, CU_TENSOR_MAP_INTERLEAVE_NONE,
-            CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+            half ? CU_TENSOR_MAP_SWIZZLE_64B : CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
 template <int EPI>
@@ -502,7 +518,7 @@ cudaError_t launch_one(const TrainUmma& t, int pairs, cudaStream_t s) {
   void* const out[3] = {EPI == kEpiStore ? e.out[0] : EPI == kEpiGateUp ? e.z : e.dz, EPI == kEpiStore ? e.out[1] : EPI == kEpiGateUp ? e.u : e.du,
                         EPI == kEpiStore ? e.out[2] : e.h};
   for (int i = 0; i < 3; ++i)
-    if (out[i]) fine = fine && make_box_map(&maps.out[i], out[i], EPI == kEpiGateUp && i < 2 ? g.N < 8 ? 8 : g.N & ~7 : g.N, g.M, EPI == kEpiStore ? e.ld_out : EPI == kEpiGateUp && i < 2 ? e.ld_zu : e.ld_h);
+    if (out[i]) fine = fine && make_box_map(&maps.out[i], out[i], EPI == kEpiGateUp && i < 2 ? g.N < 8 ? 8 : g.N & ~7 : g.N, g.M, EPI == kEpiStore ? e.ld_out : EPI == kEpiGateUp && i < 2 ? e.ld_zu : e.ld_h, EPI == kEpiStore);
   if (EPI == kEpiHidden) fine = fine && make_box_map(&maps.in[0], e.z, g.N, g.M, e.ld_zu) && make_box_map(&maps.in[1], e.u, g.N, g.M, e.ld_zu);
   if (!fine) return cudaErrorInvalidValue;
   static unsigned long long configured = 0;
