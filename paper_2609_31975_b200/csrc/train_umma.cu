@@ -82,9 +82,7 @@ __device__ __forceinline__ void boxes_written() {
   asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
   __syncwarp();
 }
-// kStore: half boxes of 32 columns, 64-byte swizzle, two a warp: one is filled while the other's store reads it.  (With one box
-// of 64 columns a warp a tile of one K block took 7 us, all of it waits for stores: 5 tokens, 4096 x 14336, gradients of the weights
-// 102 us, FEWDW now.)
+// kStore: half boxes of 32 columns, 64-byte swizzle, two a warp: one is filled while the other's store reads it.
 __device__ __forceinline__ void half_box_put(uint32_t box, int lane, int q, const float* v) {
   const uint32_t row = box + lane * 64;
 #pragma unroll
@@ -159,7 +157,8 @@ __global__ void __launch_bounds__(Form<EPI>::kThreads, 1) train_umma_kernel(cons
 
   if (warp < 4) {
     if constexpr (EPI == kEpiHidden) asm volatile("setmaxnreg.dec.sync.aligned.u32 56;");
-    if (warp == 0 && lane == 0) {
+    auto wait_all = [&](uint32_t bar, uint32_t parity) { return __all_sync(0xffffffffu, mbar_wait(bar, parity, abort_flag, p.status, p.budget)) != 0; };
+    if (warp == 0) {
       int s = 0, phase = 0;
       bool ok = true;
       while (ok && walk.step(p, it)) {
@@ -167,70 +166,89 @@ __global__ void __launch_bounds__(Form<EPI>::kThreads, 1) train_umma_kernel(cons
         const int m0 = at.m * kPairRows + rank * 128, halves = halves_of(at);
         const int n0 = at.n * F::kTileCols + (EPI == kEpiGateUp ? 0 : rank * 128);
         for (int u = it.u0; u < it.u1; ++u) {
-          ok = mbar_wait(empty + 8 * s, phase ^ 1, abort_flag, p.status, p.budget);
+          ok = wait_all(empty + 8 * s, phase ^ 1);
           if (!ok) break;
-          const int part = u >= p.blocks ? 1 : 0, k0 = (u - part * p.blocks) * kDeep, which = p.batch > 1 ? at.batch : part;
-          const CUtensorMap* ma = &maps.a[EPI == kEpiGateUp ? 0 : which];
-          const CUtensorMap* mb = &maps.b[EPI == kEpiGateUp ? rank : which];
-          const uint32_t bar = map_rank(full + 8 * s, 0), da = ring + s * F::kStageBytes;
-          if (rank == 0) mbar_expect_tx(full + 8 * s, 2 * (1 + halves) * kHalfBytes);
-          if (p.a_mn) {
-            tma_tile_3d(da, ma, m0, k0, 0, bar);
-            tma_tile_3d(da + kHalfBytes / 2, ma, m0 + 64, k0, 0, bar);
-          } else {
-            tma_tile_3d(da, ma, k0, m0, 0, bar);
-          }
-          for (int h = 0; h < halves; ++h) {
-            const uint32_t db = da + (1 + h) * kHalfBytes;
-            const int n = n0 + 256 * h;
-            if (p.b_mn) {
-              tma_tile_3d(db, mb, n, k0, 0, bar);
-              tma_tile_3d(db + kHalfBytes / 2, mb, n + 64, k0, 0, bar);
+          if (elect_one()) {
+            const int part = u >= p.blocks ? 1 : 0, k0 = (u - part * p.blocks) * kDeep, which = p.batch > 1 ? at.batch : part;
+            const CUtensorMap* ma = &maps.a[EPI == kEpiGateUp ? 0 : which];
+            const CUtensorMap* mb = &maps.b[EPI == kEpiGateUp ? rank : which];
+            const uint32_t bar = map_rank(full + 8 * s, 0), da = ring + s * F::kStageBytes;
+            if (rank == 0) mbar_expect_tx(full + 8 * s, 2 * (1 + halves) * kHalfBytes);
+            if (p.a_mn) {
+              tma_tile_3d(da, ma, m0, k0, 0, bar);
+              tma_tile_3d(da + kHalfBytes / 2, ma, m0 + 64, k0, 0, bar);
             } else {
-              tma_tile_3d(db, mb, k0, n, 0, bar);
+              tma_tile_3d(da, ma, k0, m0, 0, bar);
+            }
+            for (int h = 0; h < halves; ++h) {
+              const uint32_t db = da + (1 + h) * kHalfBytes;
+              const int n = n0 + 256 * h;
+              if (p.b_mn) {
+                tma_tile_3d(db, mb, n, k0, 0, bar);
+                tma_tile_3d(db + kHalfBytes / 2, mb, n + 64, k0, 0, bar);
+              } else {
+                tma_tile_3d(db, mb, k0, n, 0, bar);
+              }
             }
           }
+          __syncwarp();
           if (++s == kStages) { s = 0; phase ^= 1; }
         }
       }
-    } else if (warp == 1 && lane == 0 && rank == 0) {
+    } else if (warp == 1 && rank == 0) {
       const uint32_t idesc = idesc_bf16(kPairRows, 256, p.a_mn, p.b_mn);
       const uint64_t a0 = p.a_mn ? desc_mn_major(ring, kHalfBytes / 2) : desc_k_major(ring);
       const uint64_t b0 = p.b_mn ? desc_mn_major(ring + kHalfBytes, kHalfBytes / 2) : desc_k_major(ring + kHalfBytes);
       const uint32_t a_step = p.a_mn ? 2048 >> 4 : 32 >> 4, b_step = p.b_mn ? 2048 >> 4 : 32 >> 4;  // sixteen k
       int s = 0, phase = 0, b = 0, acc_phase[2] = {1, 1};
+      // the MMAs of a K block into one accumulator
+      auto multiply = [&](int buffer, int h, uint32_t more) {
+        const uint32_t off = (uint32_t)(s * F::kStageBytes) >> 4;
+#pragma unroll
+        for (int k = 0; k < kDeep / 16; ++k)
+          umma_pair(tmem + buffer * 256, a0 + off + k * a_step, b0 + off + h * (kHalfBytes >> 4) + k * b_step, idesc, k > 0 ? 1u : more);
+      };
       bool ok = true;
       while (ok && walk.step(p, it)) {
         const int halves = halves_of(place_of(p, it.tile));
         for (int u = it.u0; ok && u < it.u1;) {
           const int end = EPI == kEpiHidden ? min(it.u1, u + p.run_units) : it.u1;
-          for (int n = u; n < end; ++n) {
-            ok = mbar_wait(full + 8 * s, phase, abort_flag, p.status, p.budget);
-            if (!ok) break;
-            fence_after();
-            const uint32_t off = (uint32_t)(s * F::kStageBytes) >> 4;
-            for (int h = 0; h < halves; ++h) {
-              const int buffer = F::kWide == 2 ? h : b;
-              if (n == u) {
-                ok = mbar_wait(acc_empty + 8 * buffer, buffer ? acc_phase[1] : acc_phase[0], abort_flag, p.status, p.budget);
-                if (!ok) break;
-                fence_after();
-              }
-#pragma unroll
-              for (int k = 0; k < kDeep / 16; ++k)
-                umma_pair(tmem + buffer * 256, a0 + off + k * a_step, b0 + off + h * (kHalfBytes >> 4) + k * b_step, idesc, n > u || k > 0);
-            }
-            if (!ok) break;
-            commit_pair(empty + 8 * s);
-            if (++s == kStages) { s = 0; phase ^= 1; }
-          }
+          // the first block waits for the accumulators, half by half; where it is the only one, a half is handed over at once
+          ok = wait_all(full + 8 * s, phase);
           if (!ok) break;
           for (int h = 0; h < halves; ++h) {
             const int buffer = F::kWide == 2 ? h : b;
-            commit_pair(acc_full + 8 * buffer);
+            ok = wait_all(acc_empty + 8 * buffer, buffer ? acc_phase[1] : acc_phase[0]);
+            if (!ok) break;
             if (buffer) acc_phase[1] ^= 1;
             else acc_phase[0] ^= 1;
+            fence_after();
+            if (elect_one()) {
+              multiply(buffer, h, 0);
+              if (end - u == 1) commit_pair(acc_full + 8 * buffer);
+              if (h == halves - 1) commit_pair(empty + 8 * s);
+            }
+            __syncwarp();
           }
+          if (!ok) break;
+          if (++s == kStages) { s = 0; phase ^= 1; }
+          for (int n = u + 1; n < end; ++n) {
+            ok = wait_all(full + 8 * s, phase);
+            if (!ok) break;
+            fence_after();
+            if (elect_one()) {
+              multiply(F::kWide == 2 ? 0 : b, 0, 1);
+              if (F::kWide == 2 && halves == 2) multiply(1, 1, 1);
+              commit_pair(empty + 8 * s);
+              if (n == end - 1) {
+                commit_pair(acc_full + 8 * (F::kWide == 2 ? 0 : b));
+                if (F::kWide == 2 && halves == 2) commit_pair(acc_full + 8);
+              }
+            }
+            __syncwarp();
+            if (++s == kStages) { s = 0; phase ^= 1; }
+          }
+          if (!ok) break;
           if (EPI == kEpiGateUp) b ^= 1;
           u = end;
         }
