@@ -586,10 +586,8 @@ int plan_umma(const TrainUmma& t, int cols, UmmaParams& p, int pairs) {
   if (tiles > (1 << 30)) return 0;
   p.tiles = (int)tiles;
   p.blocks = (g.K + kDeep - 1) / kDeep;
-  if (t.f32) p.blocks = (p.blocks + kLimbBlocks - 1) / kLimbBlocks * kLimbBlocks;
-  p.unit_blocks = t.f32 ? kLimbUnit : 1;
-  p.units = (g.epilogue == kEpiGateUp ? 1 : g.parts) * p.blocks / (t.f32 ? kLimbBlocks : 1);
-  p.run_units = t.f32 ? 1 : kRunBlocks;
+  p.units = (g.epilogue == kEpiGateUp ? 1 : g.parts) * p.blocks;
+  p.run_units = t.f32 ? kLimbRun : kRunBlocks;
   p.a_mn = !g.a_major_k;
   p.b_mn = !g.b_major_k;
   p.partial = t.partial;
@@ -599,7 +597,7 @@ int plan_umma(const TrainUmma& t, int cols, UmmaParams& p, int pairs) {
   // kernel that joins them cost about that: 1000 tokens, 4096 x 14336, JOINSTORY).
   p.whole = p.tiles / pairs * pairs;
   const long long rest = p.tiles - p.whole;
-  if (!t.partial || rest == 0 || rest * p.units < pairs || (pairs - rest) * p.units * p.unit_blocks < 12ll * pairs) {
+  if (!t.partial || rest == 0 || rest * p.units < pairs || (pairs - rest) * p.units * (t.f32 ? kLimbProducts : 1) < 12ll * pairs) {
     p.whole = p.tiles;
     if (p.tiles < pairs) pairs = p.tiles;
   }

@@ -10,16 +10,16 @@ namespace sffn {
 constexpr int kPairRows = 256;               // rows of a pair's tile
 constexpr int kDeep = 64;                    // bf16 elements of one 128-byte swizzle row: a K block
 constexpr int kHalfBytes = 128 * kDeep * 2;  // 128 rows of a K block
-constexpr int kLimbBlocks = 4;               // fp32: K blocks of a run, which is six times as long
-constexpr int kLimbUnit = 6 * kLimbBlocks;
+constexpr int kLimbProducts = 6;             // fp32: products of a K block
+constexpr int kLimbRun = 2;                  // K blocks of a run
 constexpr int kRunBlocks = 12;               // dh: K blocks of a run
 
 
 struct UmmaParams {
   TrainEpilogue epi;
   int m_tiles, n_tiles, tiles;        // tiles = m_tiles * n_tiles * batch
-  int blocks;                         // K blocks of a part (fp32: rounded up to runs)
-  int units, unit_blocks, run_units;  // a tile's K in units (what is not cut), K blocks of a unit, units of a run
+  int blocks;                         // K blocks of a part
+  int units, run_units;               // a tile's K blocks, those of a run
   int whole;                          // tiles dealt whole; the others are cut along K
   int batch, tile_cols;
   int a_mn, b_mn;
@@ -77,22 +77,6 @@ __device__ __forceinline__ Place place_of(const UmmaParams& p, int tile) {
   at.m = first + tile % rows;
   at.n = tile / rows;
   return at;
-}
-
-// K block j of unit u: which part, which block of it, which terms.
-__device__ __forceinline__ void block_of(const UmmaParams& p, int u, int j, int& part, int& kb, int& la, int& lb) {
-  if (p.unit_blocks == 1) {
-    part = u >= p.blocks ? 1 : 0;
-    kb = u - part * p.blocks;
-    la = lb = 0;
-  } else {
-    const int first = u * kLimbBlocks;
-    part = first >= p.blocks ? 1 : 0;
-    kb = first - part * p.blocks + j % kLimbBlocks;
-    const int product = j / kLimbBlocks;  // (0,2) (2,0) (1,1) (0,1) (1,0) (0,0)
-    la = product == 1 ? 2 : product == 2 || product == 4 ? 1 : 0;
-    lb = product == 0 ? 2 : product == 2 || product == 3 ? 1 : 0;
-  }
 }
 
 __device__ __forceinline__ bool is_cut(const UmmaParams& p, const Item& it) { return it.u0 > 0 || it.u1 < p.units; }

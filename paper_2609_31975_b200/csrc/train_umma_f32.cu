@@ -1,9 +1,12 @@
 // Products of the training calls in fp32 on the tensor cores: every operand is three bf16 terms (24 bits), a product the six of
 // the terms' products above 2^-27.
 //
-// Tiles, roles and cut tiles as in train_umma.cu.  The tensor cores truncate when they add onto an accumulator (a sum over K = 2688
-// comes out low by 1e-6 of its typical size): runs of 256 k get an accumulator of their own, products of the smallest terms
-// first, and the epilogue warps add the runs up in registers, rounding to nearest.
+// Tiles (256 columns), roles and cut tiles as in train_umma.cu.  A K block's six operands, three terms of each, are in shared memory
+// at once, 16 KB a CTA each, and all six products are taken from there: half the bytes of copying two operands for every product,
+// which the copies (10 TB/s from L2 at most) would bound.  Two blocks fit; each operand's place is given back, and filled for
+// the block after next, as soon as its last product is through, so the copies have at least half a block's time more.
+// The tensor cores truncate when they add onto an accumulator (5e-8 of a sum's typical size for every 16 MMAs): runs of two K
+// blocks get an accumulator of their own, and the epilogue warps add the runs up in registers, rounding to nearest.
 #include "fused_kernel.cuh"
 #include "train_umma.cuh"
 
@@ -13,11 +16,10 @@ namespace {
 using namespace tc;
 
 constexpr int kCols = 256;
-constexpr int kStageBytes = 2 * kHalfBytes;
-constexpr int kStages = 6;
+constexpr int kPlaces = 12;  // of operands: a_0 a_1 a_2 b_0 b_1 b_2, of two K blocks
 constexpr int kThreads = 384;
 constexpr int kEpilogueWarps = 8;
-constexpr int kSmemBytes = kStages * kStageBytes + 1024 + 256;
+constexpr int kSmemBytes = kPlaces * kHalfBytes + 1024 + 256;
 
 struct Maps {
   CUtensorMap a[3], b[3];
@@ -94,15 +96,15 @@ __global__ void __launch_bounds__(kThreads, 1) train_umma_f32_kernel(const __gri
   extern __shared__ uint8_t smem_raw[];
   __shared__ int abort_word;
   __shared__ uint32_t tmem_slot;
-  __shared__ __align__(8) uint64_t bars[2 * kStages + 4];
+  __shared__ __align__(8) uint64_t bars[2 * kPlaces + 4];
   volatile int* const abort_flag = &abort_word;
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const uint32_t ring = (smem_u32(smem_raw) + 1023u) & ~1023u;
-  const uint32_t full = smem_u32(bars), empty = full + 8 * kStages, acc_full = empty + 8 * kStages, acc_empty = acc_full + 16;
+  const uint32_t full = smem_u32(bars), empty = full + 8 * kPlaces, acc_full = empty + 8 * kPlaces, acc_empty = acc_full + 16;
   const int rank = (int)cluster_rank(), pair = (int)blockIdx.x >> 1, pairs = (int)gridDim.x >> 1;
 
   if (tid == 0) {
-    for (int s = 0; s < kStages; ++s) {
+    for (int s = 0; s < kPlaces; ++s) {
       mbar_init(full + 8 * s, 1);
       mbar_init(empty + 8 * s, 1);
     }
@@ -128,70 +130,78 @@ __global__ void __launch_bounds__(kThreads, 1) train_umma_f32_kernel(const __gri
     asm volatile("setmaxnreg.dec.sync.aligned.u32 64;");
     Walk walk(p, pairs, pair);
     Item it;
-    if (warp == 0 && lane == 0) {
-      int s = 0, phase = 0;
-      bool ok = true;
+    auto wait_all = [&](uint32_t bar, uint32_t parity) { return __all_sync(0xffffffffu, mbar_wait(bar, parity, abort_flag, p.status, p.budget)) != 0; };
+    uint32_t block = 0;  // K blocks so far: the places 6 (block mod 2) .., every other phase
+    bool ok = true;
+    if (warp == 0) {
       while (ok && walk.step(p, it)) {
         const Place at = place_of(p, it.tile);
         const int m0 = at.m * kPairRows + rank * 128;
         const int n0 = at.n * p.tile_cols + (EPI == kEpiGateUp ? 0 : rank * 128);
-        for (int u = it.u0; ok && u < it.u1; ++u)
-          for (int j = 0; j < p.unit_blocks; ++j) {
-            ok = mbar_wait(empty + 8 * s, phase ^ 1, abort_flag, p.status, p.budget);
+        for (int u = it.u0; ok && u < it.u1; ++u, ++block) {
+          const int part = u >= p.blocks ? 1 : 0, k0 = (u - part * p.blocks) * kDeep, which = p.batch > 1 ? at.batch : part;
+          const uint32_t first = 6 * (block & 1), phase = (block >> 1) & 1;
+          // in the order of their first products
+#pragma unroll
+          for (int i = 0; i < 6; ++i) {
+            constexpr int kOrder[6] = {1, 4, 0, 5, 3, 2};
+            const int o = kOrder[i], term = o % 3;
+            const uint32_t place = first + o;
+            ok = wait_all(empty + 8 * place, phase ^ 1);
             if (!ok) break;
-            int part, kb, la, lb;
-            block_of(p, u, j, part, kb, la, lb);
-            const int which = p.batch > 1 ? at.batch : part;
-            const CUtensorMap* ma = &maps.a[EPI == kEpiGateUp ? 0 : which];
-            const CUtensorMap* mb = &maps.b[EPI == kEpiGateUp ? rank : which];
-            const uint32_t bar = map_rank(full + 8 * s, 0), da = ring + s * kStageBytes, db = da + kHalfBytes;
-            if (rank == 0) mbar_expect_tx(full + 8 * s, 2 * kStageBytes);
-            const int k0 = kb * kDeep;
-            if (p.a_mn) {
-              tma_tile_3d(da, ma, m0, k0, la, bar);
-              tma_tile_3d(da + kHalfBytes / 2, ma, m0 + 64, k0, la, bar);
-            } else {
-              tma_tile_3d(da, ma, k0, m0, la, bar);
+            if (elect_one()) {
+              const bool of_a = o < 3, mn = of_a ? p.a_mn : p.b_mn;
+              const CUtensorMap* map = of_a ? &maps.a[EPI == kEpiGateUp ? 0 : which] : &maps.b[EPI == kEpiGateUp ? rank : which];
+              const uint32_t bar = map_rank(full + 8 * place, 0), to = ring + place * kHalfBytes;
+              const int r0 = of_a ? m0 : n0;
+              if (rank == 0) mbar_expect_tx(full + 8 * place, 2 * kHalfBytes);
+              if (mn) {
+                tma_tile_3d(to, map, r0, k0, term, bar);
+                tma_tile_3d(to + kHalfBytes / 2, map, r0 + 64, k0, term, bar);
+              } else {
+                tma_tile_3d(to, map, k0, r0, term, bar);
+              }
             }
-            if (p.b_mn) {
-              tma_tile_3d(db, mb, n0, k0, lb, bar);
-              tma_tile_3d(db + kHalfBytes / 2, mb, n0 + 64, k0, lb, bar);
-            } else {
-              tma_tile_3d(db, mb, k0, n0, lb, bar);
-            }
-            if (++s == kStages) { s = 0; phase ^= 1; }
+            __syncwarp();
           }
+        }
       }
-    } else if (warp == 1 && lane == 0 && rank == 0) {
+    } else if (warp == 1 && rank == 0) {
       const uint32_t idesc = idesc_bf16(kPairRows, kCols, p.a_mn, p.b_mn);
       const uint64_t a0 = p.a_mn ? desc_mn_major(ring, kHalfBytes / 2) : desc_k_major(ring);
-      const uint64_t b0 = p.b_mn ? desc_mn_major(ring + kHalfBytes, kHalfBytes / 2) : desc_k_major(ring + kHalfBytes);
+      const uint64_t b0 = (p.b_mn ? desc_mn_major(ring, kHalfBytes / 2) : desc_k_major(ring)) + 3 * (kHalfBytes >> 4);
       const uint32_t a_step = p.a_mn ? 2048 >> 4 : 32 >> 4, b_step = p.b_mn ? 2048 >> 4 : 32 >> 4;  // sixteen k
-      int s = 0, phase = 0, b = 0, b_phase = 0;
-      bool ok = true;
+      int b = 0, b_phase = 0;
       while (ok && walk.step(p, it)) {
         for (int u = it.u0; ok && u < it.u1;) {
           const int end = min(it.u1, u + p.run_units);
-          ok = mbar_wait(acc_empty + 8 * b, b_phase ^ 1, abort_flag, p.status, p.budget);
+          ok = wait_all(acc_empty + 8 * b, b_phase ^ 1);
           if (!ok) break;
           fence_after();
           const uint32_t acc = tmem + b * kCols;
-          uint32_t more = 0;
-          for (int n = (end - u) * p.unit_blocks; n > 0; --n) {
-            ok = mbar_wait(full + 8 * s, phase, abort_flag, p.status, p.budget);
-            if (!ok) break;
-            fence_after();
-            const uint32_t off = (uint32_t)(s * kStageBytes) >> 4;
+          for (int n = u; ok && n < end; ++n, ++block) {
+            const uint32_t first = 6 * (block & 1), phase = (block >> 1) & 1, off = first * (kHalfBytes >> 4);
+            // a1 b1, a0 b1, a0 b2, a0 b0, a1 b0, a2 b0: operands come in, and go, one or two at a time
 #pragma unroll
-            for (int k = 0; k < kDeep / 16; ++k) {
-              umma_pair(acc, a0 + off + k * a_step, b0 + off + k * b_step, idesc, more);
-              more = 1;
+            for (int i = 0; i < 6; ++i) {
+              constexpr int kA[6] = {1, 0, 0, 0, 1, 2}, kB[6] = {1, 1, 2, 0, 0, 0};
+              constexpr int kWait[6] = {1, 0, 5, 3, -1, 2}, kGive[6] = {-1, 4, 5, 0, 1, 2};
+              if (i == 0) ok = wait_all(full + 8 * (first + 4), phase);
+              if (ok && kWait[i] >= 0) ok = wait_all(full + 8 * (first + kWait[i]), phase);
+              if (!ok) break;
+              fence_after();
+              if (elect_one()) {
+#pragma unroll
+                for (int k = 0; k < kDeep / 16; ++k)
+                  umma_pair(acc, a0 + off + kA[i] * (kHalfBytes >> 4) + k * a_step, b0 + off + kB[i] * (kHalfBytes >> 4) + k * b_step, idesc, n > u || i > 0 || k > 0);
+                if (kGive[i] >= 0) commit_pair(empty + 8 * (first + kGive[i]));
+                if (i == 5) commit_pair(empty + 8 * (first + 3));
+                if (i == 5 && n == end - 1) commit_pair(acc_full + 8 * b);
+              }
+              __syncwarp();
             }
-            commit_pair(empty + 8 * s);
-            if (++s == kStages) { s = 0; phase ^= 1; }
           }
           if (!ok) break;
-          commit_pair(acc_full + 8 * b);
           b ^= 1;
           if (b == 0) b_phase ^= 1;
           u = end;
