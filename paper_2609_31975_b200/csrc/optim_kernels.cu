@@ -316,12 +316,12 @@ __device__ __forceinline__ uint32_t two_bf16(f2 v) {
 }
 
 // Eight entries of a lane as four pairs.  Entry j of a lane: 8 lane + j where vectors are used (WIDE), 32 j + lane otherwise.
-// CODES: the moments are held in codes.
-template <bool CODES, bool WIDE, typename List>
+// CODES: the moments are held in codes.  HALF: bf16 parameters without copies, which the kernel then need not look up.
+template <bool CODES, bool WIDE, bool HALF, typename List>
 __device__ __forceinline__ void finish_group(const List& c, const StepEntry& t, uint32_t group, float coef, int lane, f2* w, f2* g, f2* m, f2* v) {
   const uint32_t kind = t.kind;
   const long long first = (long long)group * kGroup;
-  const bool p_bf16 = kind & kPBf16, master = kind & kMaster;
+  const bool p_bf16 = HALF || (kind & kPBf16), master = !HALF && (kind & kMaster);
   const int left = WIDE ? kGroup : (int)min((long long)kGroup, t.n - first);
   float sm, sv;
   float most_m = 0.f, most_v = 0.f;
@@ -347,27 +347,26 @@ __device__ __forceinline__ void finish_group(const List& c, const StepEntry& t, 
     sm = group_scale(warp_most(most_m), im);
     sv = group_scale(warp_most(most_v), iv);
     const float half = 65025.f * sqrt_approx(iv);  // sqrt(255^4 / scale)
-    float near = 0.f;
+    float near = 0.f, least = 1.f;
 #pragma unroll
     for (int q = 0; q < 4; ++q) {
       float m0, m1;
       halves(m[q], m0, m1);
       const f2 a = mul2(pack2(__fmul_rn(fabsf(m0), im), __fmul_rn(fabsf(m1), im)), both(16129.f));
-      const f2 b = mul2(mul2(v[q], both(iv)), both(4228250624.f));
       const f2 hr = mul2(root[q], both(half));
       const f2 sa = pack2(copysignf(sqrt_approx(low(a)), m0), copysignf(sqrt_approx(high(a)), m1));
-      const f2 big = mul2(b, both(8.507059e37f));  // 2^126: beyond one for every b that counts
-      const f2 sb = pack2(fmaxf(sqrt_approx(low(hr)), fminf(low(big), 0.6f)), fmaxf(sqrt_approx(high(hr)), fminf(high(big), 0.6f)));
+      const f2 sb = pack2(sqrt_approx(low(hr)), sqrt_approx(high(hr)));
       const f2 na = add2_b64(sa, both(kMagic)), nb = add2_b64(sb, both(kMagic));
       const f2 da = fma2_b64(add2_b64(na, both(-kMagic)), both(-1.f), sa), db = fma2_b64(add2_b64(nb, both(-kMagic)), both(-1.f), sb);
       near = fmaxf(near, fmaxf(fabsf(low(da)), fabsf(high(da))));
       near = fmaxf(near, fmaxf(fabsf(low(db)), fabsf(high(db))));
+      least = fminf(least, fminf(low(sb), high(sb)));
       cm[2 * q] = __float_as_uint(low(na)); cm[2 * q + 1] = __float_as_uint(high(na));
       cv[2 * q] = __float_as_uint(low(nb)); cv[2 * q + 1] = __float_as_uint(high(nb));
     }
-    // The edges decide: a root near one, a scale below 2^-90 (single values may have counted as zeros when their roots were
-    // taken) or above one (quotients may have).
-    if (__any_sync(0xffffffffu, near > 0.5f - kNear) || iv > 1.2379400392853803e27f || sv > 1.f) {
+    // The edges decide: a root near one; a v whose code would be 0, as 0 is for zeros only (a group of nothing else aside); a scale
+    // below 2^-90, as single values may have counted as zeros when their roots were taken.
+    if (__any_sync(0xffffffffu, near > 0.5f - kNear || (least < 0.6f && iv != 0.f)) || iv > 1.2379400392853803e27f) {
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
         const float mj = j & 1 ? high(m[j / 2]) : low(m[j / 2]), vj = j & 1 ? high(v[j / 2]) : low(v[j / 2]);
@@ -492,7 +491,7 @@ __device__ __forceinline__ void step_group(const List& c, const StepEntry& t, ui
       w[q] = pack2(e[0][0], e[0][1]); g[q] = pack2(e[1][0], e[1][1]); m[q] = pack2(e[2][0], e[2][1]); v[q] = pack2(e[3][0], e[3][1]);
     }
   }
-  finish_group<CODES, WIDE>(c, t, group, coef, lane, w, g, m, v);
+  finish_group<CODES, WIDE, false>(c, t, group, coef, lane, w, g, m, v);
 }
 
 // bf16 parameters and gradients, moments in codes: a group's 24 bytes a lane.
@@ -517,7 +516,7 @@ struct HalfGroup {
     const f2 um = both(unit_m(sm)), uv = both(unit_v(sv));
     codes_m(m.x, um, pm); codes_m(m.y, um, pm + 2);
     codes_v(v.x, uv, pv); codes_v(v.y, uv, pv + 2);
-    finish_group<true, true>(c, t, group, coef, lane, pw, pg, pm, pv);
+    finish_group<true, true, true>(c, t, group, coef, lane, pw, pg, pm, pv);
   }
 };
 
