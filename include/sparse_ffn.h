@@ -436,7 +436,8 @@ const char* sffn_status_string(int status);
  *                       its partial result, so that the CTAs which sum the partials see their (bounded) wait run out
  *                       and record SFFN_ERR_TIMEOUT (-1 = none, the default; use it with a small WAIT_CYCLES)
  *   DROP_STAGE          index of a stage of the batched gate kernel whose weight copy CTA 0 leaves out, so that the wait
- *                       for it runs out and the kernel winds down and releases its TMEM columns (-1 = none, the default)
+ *                       for it runs out and the kernel winds down and releases its TMEM columns (-1 = none, the default);
+ *                       the same of a training call on the tensor cores, in each of its products (K blocks of CTA 0)
  *   RING_GATE_SLOTS, RING_ACT_SLOTS, RING_PARKED_STAGES
  *                       tensor-core gate kernel: split of its shared-memory rings and the number of gate stages it
  *                       prefetches into idle act slots at the start of a call (0, 0, -1 = planned)

@@ -60,13 +60,13 @@ __device__ __forceinline__ void store_hidden(void* base, int64_t at, int64_t lim
 }
 
 template <int EPI, typename T>
-__global__ void __launch_bounds__(join_threads(EPI)) train_join_kernel(const __grid_constant__ UmmaParams p, int pairs, int acc_cols, int rows) {
+__global__ void __launch_bounds__(join_threads(EPI)) train_join_kernel(const __grid_constant__ UmmaParams p, int pairs, int acc_cols, int rows, int groups) {
   __shared__ float down[EPI == kEpiHidden ? 32 : 1][kJoinCols];
   __shared__ const float* place[kTrainUmmaPairs];
   constexpr bool kFast = sizeof(T) == 2;
   pdl_launch_dependents();
   const TrainEpilogue& e = p.epi;
-  const int across = (p.tile_cols + kJoinCols - 1) / kJoinCols, per = across * (kPairRows / rows);
+  const int across = (p.tile_cols + kJoinCols - 1) / kJoinCols, per = across * groups;  // groups of rows of a tile
   const int t = blockIdx.x / per, in = blockIdx.x - t * per, r0 = in / across * rows, c0 = in % across * kJoinCols;
   const Place at = place_of(p, p.whole + t);
   const int m0 = at.m * kPairRows + r0, n0 = at.n * p.tile_cols + c0;
@@ -155,13 +155,14 @@ __global__ void __launch_bounds__(join_threads(EPI)) train_join_kernel(const __g
 cudaError_t launch_train_join(const UmmaParams& p, int epilogue, bool f32, int pairs, cudaStream_t s) {
   const int across = (p.tile_cols + kJoinCols - 1) / kJoinCols, cols = (int)(p.piece / kPairRows);
   const int tiles = (p.tiles - p.whole) * across, rows = epilogue == kEpiHidden || tiles >= 148 ? 32 : 8;
-  const dim3 grid((unsigned)(tiles * (kPairRows / rows))), block(join_threads(epilogue));
-  if (epilogue == kEpiStore) return f32 ? launch_pdl(train_join_kernel<kEpiStore, float>, grid, block, 0, s, p, pairs, cols, rows)
-                                        : launch_pdl(train_join_kernel<kEpiStore, __nv_bfloat16>, grid, block, 0, s, p, pairs, cols, rows);
-  if (epilogue == kEpiGateUp) return f32 ? launch_pdl(train_join_kernel<kEpiGateUp, float>, grid, block, 0, s, p, pairs, cols, rows)
-                                         : launch_pdl(train_join_kernel<kEpiGateUp, __nv_bfloat16>, grid, block, 0, s, p, pairs, cols, rows);
-  return f32 ? launch_pdl(train_join_kernel<kEpiHidden, float>, grid, block, 0, s, p, pairs, cols, rows)
-             : launch_pdl(train_join_kernel<kEpiHidden, __nv_bfloat16>, grid, block, 0, s, p, pairs, cols, rows);
+  const int tall = p.m_tiles > 1 || p.epi.M > kPairRows ? kPairRows : p.epi.M, groups = (tall + rows - 1) / rows;
+  const dim3 grid((unsigned)(tiles * groups)), block(join_threads(epilogue));
+  if (epilogue == kEpiStore) return f32 ? launch_pdl(train_join_kernel<kEpiStore, float>, grid, block, 0, s, p, pairs, cols, rows, groups)
+                                        : launch_pdl(train_join_kernel<kEpiStore, __nv_bfloat16>, grid, block, 0, s, p, pairs, cols, rows, groups);
+  if (epilogue == kEpiGateUp) return f32 ? launch_pdl(train_join_kernel<kEpiGateUp, float>, grid, block, 0, s, p, pairs, cols, rows, groups)
+                                         : launch_pdl(train_join_kernel<kEpiGateUp, __nv_bfloat16>, grid, block, 0, s, p, pairs, cols, rows, groups);
+  return f32 ? launch_pdl(train_join_kernel<kEpiHidden, float>, grid, block, 0, s, p, pairs, cols, rows, groups)
+             : launch_pdl(train_join_kernel<kEpiHidden, __nv_bfloat16>, grid, block, 0, s, p, pairs, cols, rows, groups);
 }
 
 }  // namespace sffn

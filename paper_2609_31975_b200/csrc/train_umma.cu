@@ -159,7 +159,7 @@ __global__ void __launch_bounds__(Form<EPI>::kThreads, 1) train_umma_kernel(cons
     if constexpr (EPI == kEpiHidden) asm volatile("setmaxnreg.dec.sync.aligned.u32 56;");
     auto wait_all = [&](uint32_t bar, uint32_t parity) { return __all_sync(0xffffffffu, mbar_wait(bar, parity, abort_flag, p.status, p.budget)) != 0; };
     if (warp == 0) {
-      int s = 0, phase = 0;
+      int s = 0, phase = 0, left_out = blockIdx.x == 0 ? p.drop : -1;
       bool ok = true;
       while (ok && walk.step(p, it)) {
         const Place at = place_of(p, it.tile);
@@ -174,7 +174,8 @@ __global__ void __launch_bounds__(Form<EPI>::kThreads, 1) train_umma_kernel(cons
             const CUtensorMap* mb = &maps.b[EPI == kEpiGateUp ? rank : which];
             const uint32_t bar = map_rank(full + 8 * s, 0), da = ring + s * F::kStageBytes;
             if (rank == 0) mbar_expect_tx(full + 8 * s, 2 * (1 + halves) * kHalfBytes);
-            if (p.a_mn) {
+            if (left_out-- == 0) {
+            } else if (p.a_mn) {
               tma_tile_3d(da, ma, m0, k0, 0, bar);
               tma_tile_3d(da + kHalfBytes / 2, ma, m0 + 64, k0, 0, bar);
             } else {
@@ -593,6 +594,7 @@ int plan_umma(const TrainUmma& t, int cols, UmmaParams& p, int pairs) {
   p.partial = t.partial;
   p.status = t.status;
   p.budget = fused_test_knobs().wait_cycles;
+  p.drop = fused_test_knobs().drop_stage;
   // Whole rounds of tiles, then the rest cut along K where that saves the time of a dozen K blocks or more (6 us; the pieces and the
   // kernel that joins them cost about that: 1000 tokens, 4096 x 14336, JOINSTORY).
   p.whole = p.tiles / pairs * pairs;

@@ -27,6 +27,7 @@ struct UmmaParams {
   size_t piece;                       // floats of a pair's piece of a tile
   int32_t* status;
   long long budget;
+  int drop;                           // test hook: a K block whose rows of A CTA 0 leaves out, so that the wait for them runs out (-1: none)
 };
 
 // One piece of work of a pair of CTAs: units [u0, u1) of a tile.

@@ -134,6 +134,7 @@ __global__ void __launch_bounds__(kThreads, 1) train_umma_f32_kernel(const __gri
     uint32_t block = 0;  // K blocks so far: the places 6 (block mod 2) .., every other phase
     bool ok = true;
     if (warp == 0) {
+      int left_out = blockIdx.x == 0 ? p.drop : -1;
       while (ok && walk.step(p, it)) {
         const Place at = place_of(p, it.tile);
         const int m0 = at.m * kPairRows + rank * 128;
@@ -155,7 +156,8 @@ __global__ void __launch_bounds__(kThreads, 1) train_umma_f32_kernel(const __gri
               const uint32_t bar = map_rank(full + 8 * place, 0), to = ring + place * kHalfBytes;
               const int r0 = of_a ? m0 : n0;
               if (rank == 0) mbar_expect_tx(full + 8 * place, 2 * kHalfBytes);
-              if (mn) {
+              if (o == 0 && left_out-- == 0) {
+              } else if (mn) {
                 tma_tile_3d(to, map, r0, k0, term, bar);
                 tma_tile_3d(to + kHalfBytes / 2, map, r0 + 64, k0, term, bar);
               } else {

@@ -50,12 +50,18 @@ def _keep(index, stream, what, nbytes):
     return t
 
 
-def training_status(device="cuda:0") -> int:
-    """0, or the status that a training call on the device left because a bounded wait inside a kernel ran out (synchronises)."""
+def training_status(device="cuda:0", reset=False) -> int:
+    """0, or the status that a training call on the device left because a bounded wait inside a kernel ran out (synchronises).  It
+    stays until ``reset``; what such a call was to write is not to be used."""
     device = torch.device(device)
     index = torch.cuda.current_device() if device.index is None else device.index
     torch.cuda.synchronize(index)
-    return max([int(t[:4].view(torch.int32).item()) for (d, _, what), t in _kept.items() if d == index and what == "status"], default=0)
+    word = _kept.get((index, None, "status"))
+    status = 0 if word is None else int(word[:4].view(torch.int32).item())
+    if reset and word is not None:
+        word.zero_()
+        torch.cuda.synchronize(index)
+    return status
 
 
 def _looked_at():
