@@ -22,7 +22,7 @@ LIB = PKG / "libsparse_ffn.so"
 CALLS = PKG / "_training.so"  # the training calls' Python side (csrc/torch_calls.cpp)
 OBJ = PKG / "build"
 SOURCES = ["api.cu", "general_kernels.cu", "fused_kernel.cu", "fused_tc_kernel.cu", "static_entry.cu",
-           "batched_kernels.cu", "umma_kernels.cu", "cast_kernels.cu", "optim_kernels.cu", "train_simt.cu", "train_umma.cu", "train_umma_f32.cu", "train_join.cu", "train_api.cu"]
+           "batched_kernels.cu", "umma_kernels.cu", "cast_kernels.cu", "optim_kernels.cu", "train_simt.cu", "train_umma.cu", "train_umma_f32.cu", "train_join.cu", "train_outer.cu", "train_api.cu"]
 
 
 def _headers_mtime() -> float:

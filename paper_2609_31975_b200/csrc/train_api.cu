@@ -20,7 +20,8 @@ namespace {
     }                                                     \
   } while (0)
 
-constexpr double kSplitProducts = 1e8;  // T D H
+constexpr double kSplitProducts = 1.5e8;  // T D H
+constexpr int kFewTokens = 16;
 constexpr int kMaxRows = 1 << 22;  // tokens, and neurons: the kernels' grids and tensor maps have room for so many
 
 inline bool aligned(const void* p, uintptr_t a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) == 0; }
@@ -39,7 +40,7 @@ int sm_count(int* n) {
 
 // Which kernels serve a call: tensor cores for bf16, and for fp32 from the size on at which splitting every operand into three
 // terms and multiplying them six times is faster than fp32 FMAs.
-bool on_tensor_cores(int T, int D, int H, int dtype) { return dtype == SFFN_BF16 || (double)T * D * H >= kSplitProducts; }
+bool on_tensor_cores(int T, int D, int H, int dtype) { return dtype == SFFN_BF16 || (T > kFewTokens && (double)T * D * H >= kSplitProducts); }
 
 struct TrainLayout {
   bool umma, split;         // split: operands in three bf16 terms
@@ -106,6 +107,7 @@ struct Products {
   cudaError_t run(sffn::TrainGemm& g, const int64_t* limb_a, const int64_t* limb_b, int* lines = nullptr) const {
     int unused = 0;
     g.epi.limb = L.limb_h;
+    if (!g.a_major_k && !L.split && g.K <= (c->dtype == SFFN_BF16 ? sffn::kOuterBf16 : sffn::kOuterF32)) return sffn::launch_train_outer(g, c->dtype, s);
     if (!L.umma) return sffn::launch_train_simt(g, lines ? lines : &unused, s);
     if (lines) *lines = L.lines;
     sffn::TrainUmma t{};

@@ -9,19 +9,21 @@
 namespace sffn {
 namespace {
 
-constexpr int kRows = 32, kCols = 64, kDepth = 64, kThreads = 256;
+constexpr int kCols = 64, kDepth = 64, kThreads = 256;
 constexpr int kMaxSplit = 8;
+constexpr int kFewRows = 16;  // up to so many, tiles of 8 rows
 
-// A thread's share of a [kDepth][N] piece: N / 32 times four values, consecutive in memory.
+// A thread's share of a [kDepth][N] piece: quads of four values, consecutive in memory.
 template <int N>
 struct Piece {
-  static constexpr int kQuads = N * kDepth / 4 / kThreads;
+  static constexpr int kAll = N * kDepth / 4, kQuads = (kAll + kThreads - 1) / kThreads;
   float4 v[kQuads];
 
-  // Quad i of a K-major piece: two lanes take 32 bytes of a row, a warp sixteen rows, so that its four stores (one a k) meet no bank
-  // twice.
-  __device__ __forceinline__ static int row_of(int i) { return (i >> 5) % (N / 16) * 16 + ((i & 31) >> 1); }
-  __device__ __forceinline__ static int k_of(int i) { return ((i >> 5) / (N / 16) * 2 + (i & 1)) * 4; }
+  // Quad i of a K-major piece: two lanes take 32 bytes of a row (four 64, of eight rows), a warp sixteen rows, so that its four stores
+  // (one a k) meet no bank twice.
+  static constexpr int kShare = N < 16 ? 4 : 2, kTall = 32 / kShare;
+  __device__ __forceinline__ static int row_of(int i) { return (i >> 5) % (N / kTall) * kTall + (i & 31) / kShare; }
+  __device__ __forceinline__ static int k_of(int i) { return ((i >> 5) / (N / kTall) * kShare + i % kShare) * 4; }
 
   // rows are a multiple of 16 bytes apart; along an axis that ends inside a quad what lies beyond is not looked at
   __device__ __forceinline__ void fetch(const TrainOperand& o, bool major_k, int row0, int rows, int k0, int k1) {
@@ -32,7 +34,7 @@ struct Piece {
       const int r = major_k ? row_of(i) : i % (N / 4) * 4, k = major_k ? k_of(i) : i / (N / 4);
       const int line = major_k ? row0 + r : k0 + k, at = major_k ? k0 + k : row0 + r, lines = major_k ? rows : k1, end = major_k ? k1 : rows;
       float4 f = make_float4(0.f, 0.f, 0.f, 0.f);
-      if (line < lines && at < end) {
+      if (i < kAll && line < lines && at < end) {
         const float* s = p + line * o.ld + at;
         if (at + 4 <= end) {
           f = *reinterpret_cast<const float4*>(s);
@@ -49,6 +51,7 @@ struct Piece {
 #pragma unroll
     for (int q = 0; q < kQuads; ++q) {
       const int i = threadIdx.x + q * kThreads;
+      if (i >= kAll) continue;
       if (major_k) {
         const int r = row_of(i), k = k_of(i);
         s[k][r] = v[q].x; s[k + 1][r] = v[q].y; s[k + 2][r] = v[q].z; s[k + 3][r] = v[q].w;
@@ -89,8 +92,9 @@ __device__ __forceinline__ void get4(const void* base, int64_t at, float* v, int
   }
 }
 
-// A cluster of `splits` CTAs for each tile, tiles along N first, then along M, then of the batch.
-template <int EPI>
+// A cluster of `splits` CTAs for each tile, tiles along M first (what a short batch has few of: they share the weights' rows in L2),
+// then along N, then of the batch.  kRows: 32, or 8 for a handful of tokens, where 32 rows of products would be mostly of zeros.
+template <int EPI, int kRows>
 __global__ void __launch_bounds__(kThreads) train_simt_kernel(const __grid_constant__ TrainGemm g, int splits) {
   constexpr bool kDual = EPI == kEpiGateUp;
   constexpr int kNeurons = kDual ? kCols / 2 : kCols;  // output columns of a tile
@@ -98,12 +102,13 @@ __global__ void __launch_bounds__(kThreads) train_simt_kernel(const __grid_const
   float(*const sa)[kRows + 4] = reinterpret_cast<float(*)[kRows + 4]>(pool);
   float(*const sb)[kCols + 4] = reinterpret_cast<float(*)[kCols + 4]>(pool + kDepth * (kRows + 4));  // kDual: columns of W_g, then of W_up
   __shared__ __align__(16) float tile[kRows][kCols + 4];
+  constexpr int kSide = 16 * (kRows / 4), kParts = kThreads / kSide, kShare = kDepth / kParts;  // threads of a tile; parts of a piece's k
   pdl_launch_dependents();
   pdl_wait();
-  const int tx = threadIdx.x & 15, ty = (threadIdx.x >> 4) & 7, half = threadIdx.x >> 7;  // half: of a piece's k
+  const int tx = threadIdx.x & 15, ty = threadIdx.x / 16 % (kRows / 4), part_k = threadIdx.x / kSide;
   const int m_tiles = (g.M + kRows - 1) / kRows, n_tiles = (g.N + kNeurons - 1) / kNeurons;
-  const int at_tile = blockIdx.x / splits, split = blockIdx.x - at_tile * splits, at_row = at_tile / n_tiles, z = at_row / m_tiles;
-  const int m0 = (at_row - z * m_tiles) * kRows, n0 = (at_tile - at_row * n_tiles) * kNeurons;
+  const int at_tile = blockIdx.x / splits, split = blockIdx.x - at_tile * splits, at_col = at_tile / m_tiles, z = at_col / n_tiles;
+  const int m0 = (at_tile - at_col * m_tiles) * kRows, n0 = (at_col - z * n_tiles) * kNeurons;
   // K of all parts in a row, in pieces
   const int parts = kDual ? 1 : g.parts, per = (g.K + kDepth - 1) / kDepth, pieces = parts * per;
   const int first = (int)((long long)pieces * split / splits), last = (int)((long long)pieces * (split + 1) / splits);
@@ -135,9 +140,10 @@ __global__ void __launch_bounds__(kThreads) train_simt_kernel(const __grid_const
     store();
     __syncthreads();
     if (i + 1 < last) fetch(i + 1);
+    const int left_k = g.K - i % per * kDepth, k_end = min(kShare, left_k - part_k * kShare);  // the last piece of K may be short
 #pragma unroll 8
-    for (int q = 0; q < kDepth / 2; ++q) {
-      const int k = half * (kDepth / 2) + q;
+    for (int q = 0; q < k_end; ++q) {
+      const int k = part_k * kShare + q;
       const float4 a = *reinterpret_cast<const float4*>(&sa[k][4 * ty]), b = *reinterpret_cast<const float4*>(&sb[k][4 * tx]);
       const float av[4] = {a.x, a.y, a.z, a.w}, bv[4] = {b.x, b.y, b.z, b.w};
 #pragma unroll
@@ -147,17 +153,22 @@ __global__ void __launch_bounds__(kThreads) train_simt_kernel(const __grid_const
     }
     __syncthreads();
   }
-  float(*const other)[kCols + 4] = reinterpret_cast<float(*)[kCols + 4]>(pool);  // the operands' arrays are free
-  if (half) {
+  float(*const other)[kRows][kCols + 4] = reinterpret_cast<float(*)[kRows][kCols + 4]>(pool);  // the operands' arrays are free
+  static_assert((kParts - 1) * kRows * (kCols + 4) <= kDepth * (kRows + 4 + kCols + 4), "the parts' sums fit the operands' arrays");
+  if (part_k > 0) {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) *reinterpret_cast<float4*>(&other[4 * ty + i][4 * tx]) = make_float4(acc[i][0], acc[i][1], acc[i][2], acc[i][3]);
+    for (int i = 0; i < 4; ++i) *reinterpret_cast<float4*>(&other[part_k - 1][4 * ty + i][4 * tx]) = make_float4(acc[i][0], acc[i][1], acc[i][2], acc[i][3]);
   }
   __syncthreads();
-  if (!half) {
+  if (part_k == 0) {
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      const float4 o = *reinterpret_cast<const float4*>(&other[4 * ty + i][4 * tx]);
-      *reinterpret_cast<float4*>(&tile[4 * ty + i][4 * tx]) = make_float4(acc[i][0] + o.x, acc[i][1] + o.y, acc[i][2] + o.z, acc[i][3] + o.w);
+#pragma unroll
+      for (int q = 0; q < kParts - 1; ++q) {
+        const float4 o = *reinterpret_cast<const float4*>(&other[q][4 * ty + i][4 * tx]);
+        acc[i][0] += o.x; acc[i][1] += o.y; acc[i][2] += o.z; acc[i][3] += o.w;
+      }
+      *reinterpret_cast<float4*>(&tile[4 * ty + i][4 * tx]) = make_float4(acc[i][0], acc[i][1], acc[i][2], acc[i][3]);
     }
   }
   if (splits > 1) cluster_meet();
@@ -256,30 +267,33 @@ __global__ void __launch_bounds__(256) train_column_sums_kernel(const float* par
   }
 }
 
-// CTAs that share a tile's K: as long as all run at once, and each has a piece.
-int splits_for(const TrainGemm& g) {
+// CTAs that share a tile's K: until there are a few for every SM, while each keeps two pieces.
+int splits_for(const TrainGemm& g, int rows) {
   const int neurons = g.epilogue == kEpiGateUp ? kCols / 2 : kCols;
-  const long long tiles = (long long)((g.M + kRows - 1) / kRows) * ((g.N + neurons - 1) / neurons) * g.batch;
+  const long long tiles = (long long)((g.M + rows - 1) / rows) * ((g.N + neurons - 1) / neurons) * g.batch;
   const int pieces = (g.epilogue == kEpiGateUp ? 1 : g.parts) * ((g.K + kDepth - 1) / kDepth);
   int s = 1;
-  while (s < kMaxSplit && tiles * s * 2 <= 2 * 148 && pieces >= 2 * s) s *= 2;
+  while (s < kMaxSplit && tiles * s < 6 * 148 && pieces >= 2 * s) s *= 2;
   return s;
 }
 
 }  // namespace
 
-int train_simt_lines(int M) { return (M + kRows - 1) / kRows * kMaxSplit; }
+int train_simt_lines(int M) { return (M + 31) / 32 * kMaxSplit * (M <= kFewRows ? kFewRows / 8 : 1); }
 
-cudaError_t launch_train_simt(const TrainGemm& g, int* lines, cudaStream_t s) {
-  const int neurons = g.epilogue == kEpiGateUp ? kCols / 2 : kCols, splits = splits_for(g);
-  const int m_tiles = (g.M + kRows - 1) / kRows;
+template <int EPI>
+static cudaError_t launch_epilogue(const TrainGemm& g, int* lines, cudaStream_t s) {
+  const int rows = g.M <= kFewRows ? 8 : 32;
+  const int neurons = EPI == kEpiGateUp ? kCols / 2 : kCols, splits = splits_for(g, rows), m_tiles = (g.M + rows - 1) / rows;
   const long long ctas = (long long)splits * ((g.N + neurons - 1) / neurons) * m_tiles * g.batch;
   if (ctas > 0x7fffffff) return cudaErrorInvalidValue;
-  const dim3 grid((unsigned)ctas);
   *lines = m_tiles * splits;
-  if (g.epilogue == kEpiStore) return launch_clusters(splits, train_simt_kernel<kEpiStore>, grid, dim3(kThreads), 0, s, g, splits);
-  if (g.epilogue == kEpiGateUp) return launch_clusters(splits, train_simt_kernel<kEpiGateUp>, grid, dim3(kThreads), 0, s, g, splits);
-  return launch_clusters(splits, train_simt_kernel<kEpiHidden>, grid, dim3(kThreads), 0, s, g, splits);
+  return launch_clusters(splits, rows == 8 ? train_simt_kernel<EPI, 8> : train_simt_kernel<EPI, 32>, dim3((unsigned)ctas), dim3(kThreads), 0, s, g, splits);
+}
+
+cudaError_t launch_train_simt(const TrainGemm& g, int* lines, cudaStream_t s) {
+  return g.epilogue == kEpiStore ? launch_epilogue<kEpiStore>(g, lines, s)
+         : g.epilogue == kEpiGateUp ? launch_epilogue<kEpiGateUp>(g, lines, s) : launch_epilogue<kEpiHidden>(g, lines, s);
 }
 
 cudaError_t launch_train_column_sums(const float* partial, int lines, int64_t ld, int N, float* out, cudaStream_t s) {
