@@ -80,7 +80,7 @@ int train_simt_lines(int M);
 cudaError_t launch_train_simt(const TrainGemm& g, int* lines, cudaStream_t s);
 // Plain products of small K whose operands both lie with K as rows (train_outer.cu), rows of A padded to a multiple of eight
 // values, operands as they are stored (no terms), K at most kOuterF32 / kOuterBf16.
-constexpr int kOuterF32 = 16, kOuterBf16 = 8;
+constexpr int kOuterF32 = 16, kOuterBf16 = 4;
 cudaError_t launch_train_outer(const TrainGemm& g, int dtype, cudaStream_t s);
 // db_g[j] = sum over `lines` lines of partial sums, in order; 0 for no line.
 cudaError_t launch_train_column_sums(const float* partial, int lines, int64_t ld, int N, float* out, cudaStream_t s);
