@@ -292,3 +292,27 @@ def test_refusals(lib):
         lib.adamw_state(p, 16)
     lib.adamw_step([], [], [], 1, lr=1e-3)
     assert lib.adamw_state_values([]) == []
+
+
+def test_offsets_beyond_32_bits(lib):
+    """A tensor of more than 2^32 bytes and 2^31 entries: its last groups as the same entries by themselves."""
+    n, m = 2 ** 31 + 700, 256 * 40 + 700 % 256
+    g = gen(5)
+    p, grad = (torch.zeros(n, dtype=BF16, device=DEV) for _ in range(2))
+    p[-m:] = torch.randn(m, generator=g, device=DEV).bfloat16()
+    grad[-m:] = torch.randn(m, generator=g, device=DEV).bfloat16()
+    q, h = p[-m:].clone(), grad[-m:].clone()
+    s, r = lib.adamw_state(p, 8), lib.adamw_state(q, 8)
+    assert (n - m) % 256 == 0
+    norm = lib.grad_norm([grad])
+    assert abs(norm.item() - h.double().norm().item()) <= 1e-6 * norm.item()
+    for k in (1, 2):
+        lib.adamw_step([p], [grad], [s], k, grad_norm=norm, max_norm=1.0, **HYPER)
+        lib.adamw_step([q], [h], [r], k, grad_norm=norm, max_norm=1.0, **HYPER)
+    torch.cuda.synchronize()
+    assert torch.equal(p[-m:], q) and not p[:-m].any()
+    assert torch.equal(s["m"][-m:], r["m"]) and torch.equal(s["v"][-m:], r["v"]) and not s["v"][:-m].any()
+    groups = r["m_scale"].numel()
+    assert torch.equal(s["m_scale"][-groups:], r["m_scale"]) and torch.equal(s["v_scale"][-groups:], r["v_scale"])
+    values = lib.adamw_state_values([s])[0]
+    assert torch.equal(values["m"][-m:], lib.adamw_state_values([r])[0]["m"])

@@ -245,3 +245,28 @@ def test_refusals(lib):
         lib.gated_ffn_backward(*b, out=dict(dW_g=torch.zeros(40, 64, device=DEV)))
     with pytest.raises(TypeError):
         lib.gated_ffn_backward(b[0], b[1], t["z"], torch.zeros(16, 48, dtype=torch.bfloat16, device=DEV)[:, :40], *b[4:])
+
+def test_offsets_beyond_32_bits(lib):
+    """z and u of more than 2^31 entries: the last rows against the same rows by themselves."""
+    T, D, H = 150_001, 64, 14336
+    g = torch.Generator(device=DEV)
+    g.manual_seed(71)
+    x = torch.randn(T, D, generator=g, device=DEV).bfloat16()
+    W = [(torch.randn(H, D, generator=g, device=DEV) * D ** -0.5).bfloat16() for _ in range(3)]
+    b_g = torch.randn(H, generator=g, device=DEV)
+    y, z, u = lib.gated_ffn_forward(x, W[0], b_g, W[1], W[2])
+    n = 300
+    y1, z1, u1 = lib.gated_ffn_forward(x[-n:], W[0], b_g, W[1], W[2])
+    torch.cuda.synchronize()
+    assert z.numel() > 2 ** 31
+    # tiles lie differently over the rows, and a tile may be cut along K (64 here: it is not): the same sums
+    assert torch.equal(z[-n:], z1) and torch.equal(u[-n:], u1)
+    assert (y[-n:].double() - y1.double()).abs().max() <= 2 ** -7 * y1.double().abs().max()
+    dy = torch.zeros(T, D, device=DEV, dtype=torch.bfloat16)
+    dy[-n:] = torch.randn(n, D, generator=g, device=DEV)
+    got = lib.gated_ffn_backward(dy, x, z, u, *W)                      # rows without a gradient add nothing
+    want = lib.gated_ffn_backward(dy[-n:], x[-n:], z1, u1, *W)
+    assert (got["dx"][:-n] == 0).all()
+    for k in ("dx", "dW_g", "dW_up", "dW_down", "db_g"):
+        a, b = got[k][-n:] if k == "dx" else got[k], want[k]
+        assert (a.double() - b.double()).norm() <= 2 ** -8 * b.double().norm(), k
