@@ -59,11 +59,13 @@ __device__ __forceinline__ void store_hidden(void* base, int64_t at, int64_t lim
   }
 }
 
-template <int EPI, typename T>
-__global__ void __launch_bounds__(join_threads(EPI)) train_join_kernel(const __grid_constant__ UmmaParams p, int pairs, int acc_cols, int rows, int groups) {
+// kEach: rows of a thread.
+template <int EPI, typename T, int kEach>
+__global__ void __launch_bounds__(join_threads(EPI)) train_join_kernel(const __grid_constant__ UmmaParams p, int pairs, int acc_cols, int groups) {
+  constexpr bool kFast = sizeof(T) == 2;
+  constexpr int kHigh = join_threads(EPI) / (kJoinCols / 4), rows = kHigh * kEach;
   __shared__ float down[EPI == kEpiHidden ? 32 : 1][kJoinCols];
   __shared__ const float* place[kTrainUmmaPairs];
-  constexpr bool kFast = sizeof(T) == 2;
   pdl_launch_dependents();
   const TrainEpilogue& e = p.epi;
   const int across = (p.tile_cols + kJoinCols - 1) / kJoinCols, per = across * groups;  // groups of rows of a tile
@@ -71,35 +73,43 @@ __global__ void __launch_bounds__(join_threads(EPI)) train_join_kernel(const __g
   const Place at = place_of(p, p.whole + t);
   const int m0 = at.m * kPairRows + r0, n0 = at.n * p.tile_cols + c0;
   if (m0 >= e.M || n0 >= e.N) return;
-  // the pairs whose shares of the cut tiles overlap this one, and where their pieces are
+  // The pairs whose shares of the cut tiles overlap this one, and where their pieces are: a thread looks at one pair.
   const Walk walk(p, pairs, 0);
-  const long long lo = (long long)t * p.units, hi = lo + p.units, all = (long long)(p.tiles - p.whole) * p.units;
-  int first = (int)(lo * pairs / all);
-  while (walk.share(first + 1) <= lo) ++first;
-  while (first > 0 && walk.share(first) > lo) --first;
-  int pieces = 1;
-  while (walk.share(first + pieces) < hi) ++pieces;
-  if (threadIdx.x < pieces) place[threadIdx.x] = piece_of(p, walk, first + threadIdx.x, p.whole + t);
+  const int lo = t * p.units, hi = lo + p.units;
+  int mine = 0, before = 0;
+  if (threadIdx.x < pairs) {
+    const int from = walk.share(threadIdx.x), to = walk.share(threadIdx.x + 1);
+    mine = from < hi && to > lo;
+    before = to <= lo;
+  }
+  const int first = __syncthreads_count(before), pieces = __syncthreads_count(mine);
+  if (mine) place[threadIdx.x - first] = piece_of(p, walk, threadIdx.x, p.whole + t);
   __syncthreads();
   pdl_wait();
 
-  for (int r = threadIdx.x / (kJoinCols / 4); r < rows; r += join_threads(EPI) / (kJoinCols / 4)) {
-    const int c = threadIdx.x % (kJoinCols / 4) * 4, m = m0 + r, n = n0 + c;
-    const int left = m < e.M ? min(4, e.N - n) : 0;
-    float v[4] = {}, u[4] = {};
-    if (left > 0) {
-      const size_t off = (size_t)(r0 + r) * acc_cols + c0 + c;
-#pragma unroll 8
-      for (int q = 0; q < pieces; ++q) {
-        const float* piece = place[q] + off;
-        const float4 f = __ldcg(reinterpret_cast<const float4*>(piece));
-        v[0] += f.x; v[1] += f.y; v[2] += f.z; v[3] += f.w;
-        if constexpr (EPI == kEpiGateUp) {
-          const float4 g = __ldcg(reinterpret_cast<const float4*>(piece + 128));
-          u[0] += g.x; u[1] += g.y; u[2] += g.z; u[3] += g.w;
-        }
+  const int c = threadIdx.x % (kJoinCols / 4) * 4, r1 = threadIdx.x / (kJoinCols / 4), n = n0 + c;
+  float sum_v[kEach][4] = {}, sum_u[EPI == kEpiGateUp ? kEach : 1][4] = {};
+  const size_t off = (size_t)(r0 + r1) * acc_cols + c0 + c;
+#pragma unroll (EPI == kEpiGateUp ? 8 / kEach : 16 / kEach)
+  for (int q = 0; q < pieces; ++q) {
+    const float* piece = place[q] + off;
+#pragma unroll
+    for (int x = 0; x < kEach; ++x) {
+      if (m0 + r1 + x * kHigh >= e.M) continue;  // rows that no pair has written
+      const float4 f = __ldcg(reinterpret_cast<const float4*>(piece + (size_t)x * kHigh * acc_cols));
+      sum_v[x][0] += f.x; sum_v[x][1] += f.y; sum_v[x][2] += f.z; sum_v[x][3] += f.w;
+      if constexpr (EPI == kEpiGateUp) {
+        const float4 g = __ldcg(reinterpret_cast<const float4*>(piece + (size_t)x * kHigh * acc_cols + 128));
+        sum_u[x][0] += g.x; sum_u[x][1] += g.y; sum_u[x][2] += g.z; sum_u[x][3] += g.w;
       }
     }
+  }
+#pragma unroll
+  for (int x = 0; x < kEach; ++x) {
+    const int r = r1 + x * kHigh, m = m0 + r;
+    const int left = m < e.M ? min(4, e.N - n) : 0;
+    float (&v)[4] = sum_v[x];
+    float (&u)[4] = sum_u[EPI == kEpiGateUp ? x : 0];
     if constexpr (EPI == kEpiStore) {
       if (left > 0) store4(static_cast<T*>(e.out[at.batch]) + m * e.ld_out + n, v, left);
     } else if constexpr (EPI == kEpiGateUp) {
@@ -150,19 +160,24 @@ __global__ void __launch_bounds__(join_threads(EPI)) train_join_kernel(const __g
   }
 }
 
+template <int EPI, typename T, int kEach>
+cudaError_t launch(const UmmaParams& p, int pairs, cudaStream_t s) {
+  const int across = (p.tile_cols + kJoinCols - 1) / kJoinCols, cols = (int)(p.piece / kPairRows), rows = join_threads(EPI) / (kJoinCols / 4) * kEach;
+  const int tall = p.m_tiles > 1 || p.epi.M > kPairRows ? kPairRows : p.epi.M, groups = (tall + rows - 1) / rows;
+  return launch_pdl(train_join_kernel<EPI, T, kEach>, dim3((unsigned)((p.tiles - p.whole) * across * groups)), dim3(join_threads(EPI)), 0, s, p, pairs, cols, groups);
+}
+template <typename T>
+cudaError_t launch(const UmmaParams& p, int epilogue, int pairs, cudaStream_t s) {
+  const bool many = (long long)(p.tiles - p.whole) * p.tile_cols / kJoinCols >= 148;
+  if (epilogue == kEpiStore) return many ? launch<kEpiStore, T, 4>(p, pairs, s) : launch<kEpiStore, T, 1>(p, pairs, s);
+  if (epilogue == kEpiGateUp) return many ? launch<kEpiGateUp, T, 4>(p, pairs, s) : launch<kEpiGateUp, T, 1>(p, pairs, s);
+  return launch<kEpiHidden, T, 1>(p, pairs, s);
+}
+
 }  // namespace
 
 cudaError_t launch_train_join(const UmmaParams& p, int epilogue, bool f32, int pairs, cudaStream_t s) {
-  const int across = (p.tile_cols + kJoinCols - 1) / kJoinCols, cols = (int)(p.piece / kPairRows);
-  const int tiles = (p.tiles - p.whole) * across, rows = epilogue == kEpiHidden || tiles >= 148 ? 32 : 8;
-  const int tall = p.m_tiles > 1 || p.epi.M > kPairRows ? kPairRows : p.epi.M, groups = (tall + rows - 1) / rows;
-  const dim3 grid((unsigned)(tiles * groups)), block(join_threads(epilogue));
-  if (epilogue == kEpiStore) return f32 ? launch_pdl(train_join_kernel<kEpiStore, float>, grid, block, 0, s, p, pairs, cols, rows, groups)
-                                        : launch_pdl(train_join_kernel<kEpiStore, __nv_bfloat16>, grid, block, 0, s, p, pairs, cols, rows, groups);
-  if (epilogue == kEpiGateUp) return f32 ? launch_pdl(train_join_kernel<kEpiGateUp, float>, grid, block, 0, s, p, pairs, cols, rows, groups)
-                                         : launch_pdl(train_join_kernel<kEpiGateUp, __nv_bfloat16>, grid, block, 0, s, p, pairs, cols, rows, groups);
-  return f32 ? launch_pdl(train_join_kernel<kEpiHidden, float>, grid, block, 0, s, p, pairs, cols, rows, groups)
-             : launch_pdl(train_join_kernel<kEpiHidden, __nv_bfloat16>, grid, block, 0, s, p, pairs, cols, rows, groups);
+  return f32 ? launch<float>(p, epilogue, pairs, s) : launch<__nv_bfloat16>(p, epilogue, pairs, s);
 }
 
 }  // namespace sffn

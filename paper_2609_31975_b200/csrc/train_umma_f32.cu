@@ -5,7 +5,7 @@
 // at once, 16 KB a CTA each, and all six products are taken from there: half the bytes of copying two operands for every product,
 // which the copies (10 TB/s from L2 at most) would bound.  Two blocks fit; each operand's place is given back, and filled for
 // the block after next, as soon as its last product is through, so the copies have at least half a block's time more.
-// The tensor cores truncate when they add onto an accumulator (5e-8 of a sum's typical size for every 16 MMAs): runs of two K
+// The tensor cores truncate when they add onto an accumulator (5e-8 of a sum's typical size for every four MMAs): runs of two K
 // blocks get an accumulator of their own, and the epilogue warps add the runs up in registers, rounding to nearest.
 #include "fused_kernel.cuh"
 #include "train_umma.cuh"
