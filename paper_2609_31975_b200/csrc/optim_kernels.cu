@@ -261,6 +261,24 @@ __device__ __forceinline__ uint32_t code_of_fourth(float v, float q) {
   return max(code, v > 0.f ? 1 : 0);      // what is not zero stays so: it divides
 }
 
+// Low bytes of four words.
+__device__ __forceinline__ uint32_t low_bytes(uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
+  return __byte_perm(__byte_perm(a, b, 0x0040), __byte_perm(c, d, 0x0040), 0x5410);
+}
+// The codes of eight entries by the edges: m's in x, y, v's in z, w.  Out of line: few groups come here, and its registers would be
+// the others'.
+__device__ __noinline__ uint4 exact_codes(f2 m0, f2 m1, f2 m2, f2 m3, f2 v0, f2 v1, f2 v2, f2 v3, float im, float iv) {
+  const f2 m[4] = {m0, m1, m2, m3}, v[4] = {v0, v1, v2, v3};
+  uint32_t a[8], b[8];
+#pragma unroll
+  for (int j = 0; j < 8; ++j) {
+    const float mj = j & 1 ? high(m[j / 2]) : low(m[j / 2]), vj = j & 1 ? high(v[j / 2]) : low(v[j / 2]);
+    a[j] = code_of_square(mj, __fmul_rn(__fmul_rn(fabsf(mj), im), 16129.f));
+    b[j] = code_of_fourth(vj, __fmul_rn(__fmul_rn(vj, iv), 4228250624.f));
+  }
+  return make_uint4(low_bytes(a[0], a[1], a[2], a[3]), low_bytes(a[4], a[5], a[6], a[7]), low_bytes(b[0], b[1], b[2], b[3]), low_bytes(b[4], b[5], b[6], b[7]));
+}
+
 __device__ __forceinline__ float code_m(int c, float unit) { return __fmul_rn((float)(c * abs(c)), unit); }
 __device__ __forceinline__ float code_v(int c, float unit) {
   const float t = (float)(c * c);
@@ -341,47 +359,37 @@ __device__ __forceinline__ void finish_group(const List& c, const StepEntry& t, 
       most_v = max_nan(most_v, max_nan(low(v[q]), high(v[q])));
     }
   }
-  uint32_t cm[8], cv[8];
+  uint4 codes = make_uint4(0, 0, 0, 0);  // m's in x, y, v's in z, w
   if constexpr (CODES) {
     float im, iv;
     sm = group_scale(warp_most(most_m), im);
     sv = group_scale(warp_most(most_v), iv);
     const float half = 65025.f * sqrt_approx(iv);  // sqrt(255^4 / scale)
     float near = 0.f, least = 1.f;
+    uint32_t a[8], b[8];
 #pragma unroll
     for (int q = 0; q < 4; ++q) {
       float m0, m1;
       halves(m[q], m0, m1);
-      const f2 a = mul2(pack2(__fmul_rn(fabsf(m0), im), __fmul_rn(fabsf(m1), im)), both(16129.f));
+      const f2 square = mul2(pack2(__fmul_rn(fabsf(m0), im), __fmul_rn(fabsf(m1), im)), both(16129.f));
       const f2 hr = mul2(root[q], both(half));
-      const f2 sa = pack2(copysignf(sqrt_approx(low(a)), m0), copysignf(sqrt_approx(high(a)), m1));
+      const f2 sa = pack2(copysignf(sqrt_approx(low(square)), m0), copysignf(sqrt_approx(high(square)), m1));
       const f2 sb = pack2(sqrt_approx(low(hr)), sqrt_approx(high(hr)));
       const f2 na = add2_b64(sa, both(kMagic)), nb = add2_b64(sb, both(kMagic));
       const f2 da = fma2_b64(add2_b64(na, both(-kMagic)), both(-1.f), sa), db = fma2_b64(add2_b64(nb, both(-kMagic)), both(-1.f), sb);
       near = fmaxf(near, fmaxf(fabsf(low(da)), fabsf(high(da))));
       near = fmaxf(near, fmaxf(fabsf(low(db)), fabsf(high(db))));
       least = fminf(least, fminf(low(sb), high(sb)));
-      cm[2 * q] = __float_as_uint(low(na)); cm[2 * q + 1] = __float_as_uint(high(na));
-      cv[2 * q] = __float_as_uint(low(nb)); cv[2 * q + 1] = __float_as_uint(high(nb));
+      a[2 * q] = __float_as_uint(low(na)); a[2 * q + 1] = __float_as_uint(high(na));
+      b[2 * q] = __float_as_uint(low(nb)); b[2 * q + 1] = __float_as_uint(high(nb));
     }
+    codes = make_uint4(low_bytes(a[0], a[1], a[2], a[3]), low_bytes(a[4], a[5], a[6], a[7]), low_bytes(b[0], b[1], b[2], b[3]), low_bytes(b[4], b[5], b[6], b[7]));
     // The edges decide: a root near one; a v whose code would be 0, as 0 is for zeros only (a group of nothing else aside); a scale
     // below 2^-90, as single values may have counted as zeros when their roots were taken.
-    if (__any_sync(0xffffffffu, near > 0.5f - kNear || (least < 0.6f && iv != 0.f)) || iv > 1.2379400392853803e27f) {
-#pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        const float mj = j & 1 ? high(m[j / 2]) : low(m[j / 2]), vj = j & 1 ? high(v[j / 2]) : low(v[j / 2]);
-        cm[j] = code_of_square(mj, __fmul_rn(__fmul_rn(fabsf(mj), im), 16129.f));
-        cv[j] = code_of_fourth(vj, __fmul_rn(__fmul_rn(vj, iv), 4228250624.f));
-      }
-    }
-    if (im == 0.f) {
-#pragma unroll
-      for (int j = 0; j < 8; ++j) cm[j] = 0;
-    }
-    if (iv == 0.f) {
-#pragma unroll
-      for (int j = 0; j < 8; ++j) cv[j] = 0;
-    }
+    if (__any_sync(0xffffffffu, near > 0.5f - kNear || (least < 0.6f && iv != 0.f)) || iv > 1.2379400392853803e27f)
+      codes = exact_codes(m[0], m[1], m[2], m[3], v[0], v[1], v[2], v[3], im, iv);
+    if (im == 0.f) codes.x = codes.y = 0;
+    if (iv == 0.f) codes.z = codes.w = 0;
     if (lane == 0) {
       t.m_scale[group] = sm;
       t.v_scale[group] = sv;
@@ -396,14 +404,8 @@ __device__ __forceinline__ void finish_group(const List& c, const StepEntry& t, 
       st32(static_cast<float*>(t.p) + at, w);
     }
     if constexpr (CODES) {
-      uint32_t a[2], b[2];
-#pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        a[h] = __byte_perm(__byte_perm(cm[4 * h], cm[4 * h + 1], 0x0040), __byte_perm(cm[4 * h + 2], cm[4 * h + 3], 0x0040), 0x5410);
-        b[h] = __byte_perm(__byte_perm(cv[4 * h], cv[4 * h + 1], 0x0040), __byte_perm(cv[4 * h + 2], cv[4 * h + 3], 0x0040), 0x5410);
-      }
-      *reinterpret_cast<uint2*>(static_cast<int8_t*>(t.m) + at) = make_uint2(a[0], a[1]);
-      *reinterpret_cast<uint2*>(static_cast<uint8_t*>(t.v) + at) = make_uint2(b[0], b[1]);
+      *reinterpret_cast<uint2*>(static_cast<int8_t*>(t.m) + at) = make_uint2(codes.x, codes.y);
+      *reinterpret_cast<uint2*>(static_cast<uint8_t*>(t.v) + at) = make_uint2(codes.z, codes.w);
     } else {
       st32(static_cast<float*>(t.m) + at, m);
       st32(static_cast<float*>(t.v) + at, v);
@@ -422,8 +424,8 @@ __device__ __forceinline__ void finish_group(const List& c, const StepEntry& t, 
         static_cast<float*>(t.p)[at] = wj;
       }
       if (CODES) {
-        static_cast<int8_t*>(t.m)[at] = (int8_t)cm[j];
-        static_cast<uint8_t*>(t.v)[at] = (uint8_t)cv[j];
+        static_cast<int8_t*>(t.m)[at] = (int8_t)((j < 4 ? codes.x : codes.y) >> (8 * (j & 3)));
+        static_cast<uint8_t*>(t.v)[at] = (uint8_t)((j < 4 ? codes.z : codes.w) >> (8 * (j & 3)));
       } else {
         static_cast<float*>(t.m)[at] = j & 1 ? high(m[j / 2]) : low(m[j / 2]);
         static_cast<float*>(t.v)[at] = j & 1 ? high(v[j / 2]) : low(v[j / 2]);
