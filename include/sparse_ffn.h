@@ -314,7 +314,8 @@ int sffn_lopa_residual(const float* W, const int32_t* g_idx, const int8_t* g_sig
  * follow the step that wrote them) -- but the inference calls above may start reading weights early, so put a stream
  * or event synchronisation between sffn_adamw_step and the next sparse_ffn_forward on the same weights.
  * `status` (device int32, zeroed by the caller once) receives SFFN_ERR_TIMEOUT if a bounded wait inside a kernel runs
- * out; it is never cleared by the library.  Results are bitwise the same on every call with the same inputs.
+ * out; it is never cleared by the library.  Results are bitwise the same on every call with the same inputs
+ * and the same outputs asked for.
  *
  * T tokens, x [T, D], weights as above (W_down transposed, [H, D]):
  *     z = x W_g^T + b_g,   u = x W_up^T,   h = A(z) . A_3(u),   y = h W_down.

@@ -2,7 +2,8 @@
 //
 // A CTA owns a 32 x 64 tile of C, or z and u of 32 tokens x 32 neurons; two threads 4 x 4 of it, a half of a piece's k each.  For up
 // to 16 rows: 8 x 64 tiles, eight threads an eighth of the k each.  Pieces of 64 k go through registers into [k][m] and [k][n]
-// arrays, whichever way an operand lies in memory, the next piece under way while one is multiplied.  Such a call has few tiles and is bound by latency, so K is cut among up to eight CTAs of a cluster: each
+// arrays, whichever way an operand lies in memory, the next piece under way while one is multiplied.  Such a call has few tiles and
+// is bound by latency, so K is cut among up to eight CTAs of a cluster: each
 // leaves its sums in shared memory and takes a share of the tile's rows, which it adds up over all of them, in order.
 // 64 tokens, 256 x 1024: forward 16 us, backward 29 us as a graph, of which launches 4 and 6, FMAs 4 and 10, the clusters' exchange 4 and
 // 2 (59 and 114 us without clusters); with few tokens bound by the weights' bytes: 1 token, 4096 x 14336, forward 264 us for 705 MB.

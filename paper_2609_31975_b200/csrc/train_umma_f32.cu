@@ -7,6 +7,8 @@
 // the block after next, as soon as its last product is through, so the copies have at least half a block's time more.
 // The tensor cores truncate when they add onto an accumulator (5e-8 of a sum's typical size for every four MMAs): runs of two K
 // blocks get an accumulator of their own, and the epilogue warps add the runs up in registers, rounding to nearest.
+// Error from 64 bits 3.7e-7 where fp32 FMAs leave 1.1e-6.  500 tokens, 3840 x 14230, backward 1.9 ms (2.3 with two operands copied for
+// every product): three products of 278, 433 and 659 us, 1.2 to 1.5 PFLOP/s of bf16, and 305 us for the terms of the weights.
 #include "fused_kernel.cuh"
 #include "train_umma.cuh"
 
