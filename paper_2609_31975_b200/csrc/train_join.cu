@@ -62,7 +62,7 @@ __device__ __forceinline__ void store_hidden(void* base, int64_t at, int64_t lim
 
 // kEach: rows of a thread.
 template <int EPI, typename T, int kEach>
-__global__ void __launch_bounds__(join_threads(EPI)) train_join_kernel(const __grid_constant__ UmmaParams p, int pairs, int acc_cols, int groups) {
+__global__ void __launch_bounds__(join_threads(EPI)) train_join_kernel(const __grid_constant__ UmmaParams p, int acc_cols, int groups) {
   constexpr bool kFast = sizeof(T) == 2;
   constexpr int kHigh = join_threads(EPI) / (kJoinCols / 4), rows = kHigh * kEach;
   __shared__ float down[EPI == kEpiHidden ? 32 : 1][kJoinCols];
@@ -75,10 +75,10 @@ __global__ void __launch_bounds__(join_threads(EPI)) train_join_kernel(const __g
   const int m0 = at.m * kPairRows + r0, n0 = at.n * p.tile_cols + c0;
   if (m0 >= e.M || n0 >= e.N) return;
   // The pairs whose shares of the cut tiles overlap this one, and where their pieces are: a thread looks at one pair.
-  const Walk walk(p, pairs, 0);
+  const Walk walk(p, p.cut_pairs, 0);
   const int lo = t * p.units, hi = lo + p.units;
   int mine = 0, before = 0;
-  if (threadIdx.x < pairs) {
+  if (threadIdx.x < p.cut_pairs) {
     const int from = walk.share(threadIdx.x), to = walk.share(threadIdx.x + 1);
     mine = from < hi && to > lo;
     before = to <= lo;
@@ -162,23 +162,23 @@ __global__ void __launch_bounds__(join_threads(EPI)) train_join_kernel(const __g
 }
 
 template <int EPI, typename T, int kEach>
-cudaError_t launch(const UmmaParams& p, int pairs, cudaStream_t s) {
+cudaError_t launch(const UmmaParams& p, cudaStream_t s) {
   const int across = (p.tile_cols + kJoinCols - 1) / kJoinCols, cols = (int)(p.piece / kPairRows), rows = join_threads(EPI) / (kJoinCols / 4) * kEach;
   const int tall = p.m_tiles > 1 || p.epi.M > kPairRows ? kPairRows : p.epi.M, groups = (tall + rows - 1) / rows;
-  return launch_pdl(train_join_kernel<EPI, T, kEach>, dim3((unsigned)((p.tiles - p.whole) * across * groups)), dim3(join_threads(EPI)), 0, s, p, pairs, cols, groups);
+  return launch_pdl(train_join_kernel<EPI, T, kEach>, dim3((unsigned)((p.tiles - p.whole) * across * groups)), dim3(join_threads(EPI)), 0, s, p, cols, groups);
 }
 template <typename T>
-cudaError_t launch(const UmmaParams& p, int epilogue, int pairs, cudaStream_t s) {
+cudaError_t launch(const UmmaParams& p, int epilogue, cudaStream_t s) {
   const bool many = (long long)(p.tiles - p.whole) * p.tile_cols / kJoinCols >= 148;
-  if (epilogue == kEpiStore) return many ? launch<kEpiStore, T, 4>(p, pairs, s) : launch<kEpiStore, T, 1>(p, pairs, s);
-  if (epilogue == kEpiGateUp) return many ? launch<kEpiGateUp, T, 4>(p, pairs, s) : launch<kEpiGateUp, T, 1>(p, pairs, s);
-  return launch<kEpiHidden, T, 1>(p, pairs, s);
+  if (epilogue == kEpiStore) return many ? launch<kEpiStore, T, 4>(p, s) : launch<kEpiStore, T, 1>(p, s);
+  if (epilogue == kEpiGateUp) return many ? launch<kEpiGateUp, T, 4>(p, s) : launch<kEpiGateUp, T, 1>(p, s);
+  return launch<kEpiHidden, T, 1>(p, s);
 }
 
 }  // namespace
 
-cudaError_t launch_train_join(const UmmaParams& p, int epilogue, bool f32, int pairs, cudaStream_t s) {
-  return f32 ? launch<float>(p, epilogue, pairs, s) : launch<__nv_bfloat16>(p, epilogue, pairs, s);
+cudaError_t launch_train_join(const UmmaParams& p, int epilogue, bool f32, cudaStream_t s) {
+  return f32 ? launch<float>(p, epilogue, s) : launch<__nv_bfloat16>(p, epilogue, s);
 }
 
 }  // namespace sffn

@@ -21,6 +21,8 @@
 // the same share of it: each leaves its piece of a tile as fp32 in a workspace, and train_join_kernel adds up the pieces in their
 // order in K and does the epilogue.
 // Every wait is bounded by a cycle budget; on expiry the status word is set, all roles wind down and tensor memory is given back.
+#include <cmath>
+
 #include "fused_kernel.cuh"
 #include "train_umma.cuh"
 
@@ -545,7 +547,7 @@ cudaError_t launch_one(const TrainUmma& t, int pairs, cudaStream_t s) {
   if (err != cudaSuccess) return err;
   const cudaError_t launched = launch_clusters(2, train_umma_kernel<EPI>, dim3(2 * pairs), dim3(F::kThreads), F::kSmemBytes, s, p, maps);
   if (launched != cudaSuccess || p.whole == p.tiles) return launched;
-  return launch_train_join(p, EPI, false, pairs, s);
+  return launch_train_join(p, EPI, false, s);
 }
 
 }  // namespace
@@ -565,13 +567,13 @@ bool make_operand_maps(const TrainUmma& t, CUtensorMap* a, CUtensorMap* b) {
   const TrainGemm& g = t.g;
   const int na = g.epilogue == kEpiGateUp ? 1 : g.batch > 1 ? g.batch : g.parts, nb = g.batch > 1 ? g.batch : g.parts;
   const int terms = t.f32 ? 3 : 1;
-  for (int i = 0; i < 3; ++i) {
-    const int ia = i < na ? i : 0, ib = i < nb ? i : 0;
-    const bool fine = (g.a_major_k ? make_train_map(&a[i], g.a[ia].data, g.K, g.M, g.a[ia].ld, terms, t.limb_a[ia], 128)
-                                   : make_train_map(&a[i], g.a[ia].data, g.M, g.K, g.a[ia].ld, terms, t.limb_a[ia], 64)) &&
-                      (g.b_major_k ? make_train_map(&b[i], g.b[ib].data, g.K, g.N, g.b[ib].ld, terms, t.limb_b[ib], 128)
-                                   : make_train_map(&b[i], g.b[ib].data, g.N, g.K, g.b[ib].ld, terms, t.limb_b[ib], 64));
-    if (!fine) return false;
+  for (int i = 0; i < 3; ++i) {  // the first one again where there are fewer
+    if (i >= na) a[i] = a[0];
+    else if (!(g.a_major_k ? make_train_map(&a[i], g.a[i].data, g.K, g.M, g.a[i].ld, terms, t.limb_a[i], 128)
+                           : make_train_map(&a[i], g.a[i].data, g.M, g.K, g.a[i].ld, terms, t.limb_a[i], 64))) return false;
+    if (i >= nb) b[i] = b[0];
+    else if (!(g.b_major_k ? make_train_map(&b[i], g.b[i].data, g.K, g.N, g.b[i].ld, terms, t.limb_b[i], 128)
+                           : make_train_map(&b[i], g.b[i].data, g.N, g.K, g.b[i].ld, terms, t.limb_b[i], 64))) return false;
   }
   return true;
 }
@@ -595,15 +597,27 @@ int plan_umma(const TrainUmma& t, int cols, UmmaParams& p, int pairs) {
   p.status = t.status;
   p.budget = fused_test_knobs().wait_cycles;
   p.drop = fused_test_knobs().drop_stage;
-  // Whole rounds of tiles, then the rest cut along K where that saves the time of a dozen K blocks or more (6 us; the pieces and the
-  // kernel that joins them cost about that).  1000 tokens, 4096 x 14336: 448 tiles of z and u in 6.05 rounds of 74 instead of 7, 181
-  // and 13 us for the join instead of 213; 5 tokens, dx: 8 tiles on all pairs, 53 and 6 us.
-  p.whole = p.tiles / pairs * pairs;
-  const long long rest = p.tiles - p.whole;
-  if (!t.partial || rest == 0 || rest * p.units < pairs || (pairs - rest) * p.units * (t.f32 ? kLimbProducts : 1) < 12ll * pairs) {
-    p.whole = p.tiles;
-    if (p.tiles < pairs) pairs = p.tiles;
+  // Whole rounds of tiles, then the rest: whole too, or cut along K, into `split` equal pieces a tile, one a pair, or so that all pairs
+  // get the same share, of one tile or of two.  What is shortest, counted in K blocks of a product (half a microsecond): a piece's
+  // rows are written to the workspace (8 for 256 rows of 256 columns), and a kernel of its own joins the pieces (5, and a half for each of a tile's).
+  // 4096 x 14336, bf16, shares for all / with equal pieces: 200, 500, 1000 tokens forward 122 / 114, 193 / 167, 314 / 289 us, 1000
+  // tokens backward 709 / 625; 1121 x 496 x 1728 backward 94 / 72; 6863 x 528 x 1984 backward 204 / 182.
+  const int rest = p.tiles % pairs;
+  p.whole = p.tiles;
+  if (t.partial && rest > 0) {
+    const double units = p.units, products = t.f32 ? kLimbProducts : 1, piece = 1.0 + (cols > 256 ? 16.0 : 8.0) * (g.M < kPairRows ? g.M : kPairRows) / kPairRows;
+    double best = units * products;
+    for (int split = 2; split <= pairs / rest && split <= p.units; ++split) {
+      const double time = std::ceil(units / split) * products + piece + 5.0 + 0.5 * split;
+      if (time < best) {
+        best = time;
+        p.cut_pairs = rest * split;
+      }
+    }
+    if ((long long)rest * p.units >= pairs && std::ceil(units * rest / pairs) * products + 2.0 * piece + 5.5 + 0.5 * pairs / rest < best) p.cut_pairs = pairs;
+    if (p.cut_pairs > 0) p.whole = p.tiles - rest;
   }
+  if (p.whole < pairs) pairs = p.whole > p.cut_pairs ? p.whole : p.cut_pairs;
   return pairs;
 }
 

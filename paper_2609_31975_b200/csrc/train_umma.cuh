@@ -20,7 +20,8 @@ struct UmmaParams {
   int m_tiles, n_tiles, tiles;        // tiles = m_tiles * n_tiles * batch
   int blocks;                         // K blocks of a part
   int units, run_units;               // a tile's K blocks, those of a run
-  int whole;                          // tiles dealt whole; the others are cut along K
+  int whole;                          // tiles dealt whole; the others are cut along K,
+  int cut_pairs;                      // among so many pairs
   int batch, tile_cols;
   int a_mn, b_mn;
   float* partial;
@@ -36,15 +37,18 @@ struct Item {
 };
 // A pair's items in order: its share of the tiles that are cut, then whole tiles.
 struct Walk {
-  int pairs, pair, cut, units, lo, hi, next;  // lo, hi: its units of all cut tiles in a row
-  __device__ __forceinline__ Walk(const UmmaParams& p, int pairs_, int pair_) {
-    pairs = pairs_; pair = pair_; units = p.units;
+  int pairs, cut_pairs, cut, units, lo, hi, next;  // lo, hi: its units of all cut tiles in a row
+  __device__ __forceinline__ Walk(const UmmaParams& p, int pairs_, int pair) {
+    pairs = pairs_; cut_pairs = p.cut_pairs; units = p.units;
     cut = p.tiles - p.whole;
-    lo = share(pair);
-    hi = share(pair + 1);
+    lo = hi = 0;
+    if (pair < cut_pairs) {
+      lo = share(pair);
+      hi = share(pair + 1);
+    }
     next = pair;
   }
-  __device__ __forceinline__ int share(int q) const { return (int)((long long)cut * units * q / pairs); }
+  __device__ __forceinline__ int share(int q) const { return (int)((long long)cut * units * q / cut_pairs); }
   __device__ __forceinline__ bool step(const UmmaParams& p, Item& it) {
     if (lo < hi) {
       const int t = lo / units;
@@ -160,6 +164,6 @@ int plan_umma(const TrainUmma& t, int cols, UmmaParams& p, int pairs);
 
 cudaError_t launch_train_umma_f32(const TrainUmma& t, int pairs, cudaStream_t s);
 // The epilogue of the tiles that were cut along K, after the launch that left their pieces.
-cudaError_t launch_train_join(const UmmaParams& p, int epilogue, bool f32, int pairs, cudaStream_t s);
+cudaError_t launch_train_join(const UmmaParams& p, int epilogue, bool f32, cudaStream_t s);
 
 }  // namespace sffn

@@ -416,7 +416,7 @@ cudaError_t launch_one(const UmmaParams& p, const Maps& maps, int pairs, cudaStr
   if (e != cudaSuccess) return e;
   const cudaError_t launched = launch_clusters(2, train_umma_f32_kernel<EPI>, dim3(2 * pairs), dim3(kThreads), kSmemBytes, s, p, maps);
   if (launched != cudaSuccess || p.whole == p.tiles) return launched;
-  return launch_train_join(p, EPI, true, pairs, s);
+  return launch_train_join(p, EPI, true, s);
 }
 
 }  // namespace
