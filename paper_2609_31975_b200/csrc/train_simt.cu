@@ -82,7 +82,9 @@ __device__ __forceinline__ void put4(void* base, int64_t at, const float* v, int
   if (n == 4) {
     *reinterpret_cast<float4*>(p) = make_float4(v[0], v[1], v[2], v[3]);
   } else {
-    for (int i = 0; i < n; ++i) p[i] = v[i];
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      if (i < n) p[i] = v[i];
   }
 }
 __device__ __forceinline__ void get4(const void* base, int64_t at, float* v, int n) {

@@ -76,6 +76,14 @@ def test_a_wide_ffn_with_many_tokens(lib, dtype):
     check_backward(lib, t, "relu", None, "wide")
 
 
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16], ids=["f32", "bf16"])
+@pytest.mark.parametrize("T,D,H", [(300, 2048, 2045), (300, 2048, 2046), (300, 2048, 2047), (40, 2048, 4097), (520, 1032, 4099)])
+def test_tiles_cut_along_k_with_hidden_widths_that_four_does_not_divide(lib, T, D, H, dtype):
+    t = make(T, D, H, dtype, T + H)
+    check_forward(lib, t, "sqrelu", "silu", f"forward {T}x{D}x{H}")
+    check_backward(lib, t, "sqrelu", "silu", f"backward {T}x{D}x{H}")
+
+
 def strided(t, extra, before):
     """The same values as rows of a wider matrix whose other columns hold a marker."""
     T, N = t.shape
