@@ -5,10 +5,12 @@
 // at once, 16 KB a CTA each, and all six products are taken from there: half the bytes of copying two operands for every product,
 // which the copies (10 TB/s from L2 at most) would bound.  Two blocks fit; each operand's place is given back, and filled for
 // the block after next, as soon as its last product is through, so the copies have at least half a block's time more.
-// The tensor cores truncate when they add onto an accumulator (5e-8 of a sum's typical size for every four MMAs): runs of two K
-// blocks get an accumulator of their own, and the epilogue warps add the runs up in registers, rounding to nearest.
-// Error from 64 bits 3.7e-7 where fp32 FMAs leave 1.1e-6.  500 tokens, 3840 x 14230, backward 1.9 ms (2.3 with two operands copied for
-// every product): three products of 278, 433 and 659 us, 1.2 to 1.5 PFLOP/s of bf16, and 305 us for the terms of the weights.
+// The tensor cores truncate when they add onto an accumulator (5e-8 of its size for every four MMAs): runs of two K blocks get an
+// accumulator of their own, its small products first while it is small, and the epilogue warps add the runs up in registers, rounding
+// to nearest.  Relative error of y (800 tokens, 512 x 1536, squared RELU) / time of a backward pass (500 tokens, 3840 x 14230): 6.2e-7
+// / 1.84 ms, fp32 FMAs 8.0e-7; each block's six products in turn 1.6e-6 / 1.83, runs of one block 2.8e-7 / 1.96, both blocks'
+// a0 b0 at the end 4.0e-7 / 1.87 (their places come back too late for the next run).
+// Three products of 278, 433 and 659 us there, 1.2 to 1.5 PFLOP/s of bf16, and 305 us for the terms of the weights.
 #include "fused_kernel.cuh"
 #include "train_umma.cuh"
 
@@ -147,7 +149,7 @@ __global__ void __launch_bounds__(kThreads, 1) train_umma_f32_kernel(const __gri
           // in the order of their first products
 #pragma unroll
           for (int i = 0; i < 6; ++i) {
-            constexpr int kOrder[6] = {1, 4, 0, 5, 3, 2};
+            constexpr int kOrder[6] = {1, 4, 2, 5, 3, 0};
             const int o = kOrder[i], term = o % 3;
             const uint32_t place = first + o;
             ok = wait_all(empty + 8 * place, phase ^ 1);
@@ -178,33 +180,36 @@ __global__ void __launch_bounds__(kThreads, 1) train_umma_f32_kernel(const __gri
       int b = 0, b_phase = 0;
       while (ok && walk.step(p, it)) {
         for (int u = it.u0; ok && u < it.u1;) {
+          static_assert(kLimbRun == 2);
           const int end = min(it.u1, u + p.run_units);
           ok = wait_all(acc_empty + 8 * b, b_phase ^ 1);
           if (!ok) break;
           fence_after();
           const uint32_t acc = tmem + b * kCols;
-          for (int n = u; ok && n < end; ++n, ++block) {
-            const uint32_t first = 6 * (block & 1), phase = (block >> 1) & 1, off = first * (kHalfBytes >> 4);
-            // a1 b1, a0 b1, a0 b2, a0 b0, a1 b0, a2 b0: operands come in, and go, one or two at a time
+          const bool two = end - u == 2;
+          // a1 b1, a1 b0, a2 b0, a0 b1, a0 b2 of both blocks, then a0 b0 of both; the first block's one product early, for its places
 #pragma unroll
-            for (int i = 0; i < 6; ++i) {
-              constexpr int kA[6] = {1, 0, 0, 0, 1, 2}, kB[6] = {1, 1, 2, 0, 0, 0};
-              constexpr int kWait[6] = {1, 0, 5, 3, -1, 2}, kGive[6] = {-1, 4, 5, 0, 1, 2};
-              if (i == 0) ok = wait_all(full + 8 * (first + 4), phase);
-              if (ok && kWait[i] >= 0) ok = wait_all(full + 8 * (first + kWait[i]), phase);
-              if (!ok) break;
-              fence_after();
-              if (elect_one()) {
+          for (int i = 0; i < 12; ++i) {
+            constexpr int kBlock[12] = {0, 0, 0, 0, 0, 1, 1, 1, 1, 0, 1, 1};
+            constexpr int kA[12] = {1, 1, 2, 0, 0, 1, 1, 2, 0, 0, 0, 0}, kB[12] = {1, 0, 0, 1, 2, 1, 0, 0, 1, 0, 2, 0};
+            constexpr int kWait[12] = {1, 3, 2, 0, 5, 1, 3, 2, 0, -1, 5, -1}, kGive[12] = {-1, 1, 2, 4, 5, -1, 1, 2, 4, 0, 5, 0};
+            if (kBlock[i] && !two) continue;
+            const uint32_t at = block + kBlock[i], first = 6 * (at & 1), phase = (at >> 1) & 1, off = first * (kHalfBytes >> 4);
+            if (kWait[i] == 1) ok = wait_all(full + 8 * (first + 4), phase);
+            if (ok && kWait[i] >= 0) ok = wait_all(full + 8 * (first + kWait[i]), phase);
+            if (!ok) break;
+            fence_after();
+            if (elect_one()) {
 #pragma unroll
-                for (int k = 0; k < kDeep / 16; ++k)
-                  umma_pair(acc, a0 + off + kA[i] * (kHalfBytes >> 4) + k * a_step, b0 + off + kB[i] * (kHalfBytes >> 4) + k * b_step, idesc, n > u || i > 0 || k > 0);
-                if (kGive[i] >= 0) commit_pair(empty + 8 * (first + kGive[i]));
-                if (i == 5) commit_pair(empty + 8 * (first + 3));
-                if (i == 5 && n == end - 1) commit_pair(acc_full + 8 * b);
-              }
-              __syncwarp();
+              for (int k = 0; k < kDeep / 16; ++k)
+                umma_pair(acc, a0 + off + kA[i] * (kHalfBytes >> 4) + k * a_step, b0 + off + kB[i] * (kHalfBytes >> 4) + k * b_step, idesc, i > 0 || k > 0);
+              if (kGive[i] >= 0) commit_pair(empty + 8 * (first + kGive[i]));
+              if (kGive[i] == 0) commit_pair(empty + 8 * (first + 3));
+              if (i == (two ? 11 : 9)) commit_pair(acc_full + 8 * b);
             }
+            __syncwarp();
           }
+          block += end - u;
           if (!ok) break;
           b ^= 1;
           if (b == 0) b_phase ^= 1;
