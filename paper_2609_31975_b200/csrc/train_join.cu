@@ -74,7 +74,6 @@ __global__ void __launch_bounds__(join_threads(EPI)) train_join_kernel(const __g
   constexpr bool kFast = sizeof(T) == 2;
   constexpr int kHigh = join_threads(EPI) / (kJoinCols / 4), rows = kHigh * kEach;
   __shared__ float down[EPI == kEpiHidden ? 32 : 1][kJoinCols];
-  __shared__ const float* place[kTrainUmmaPairs];
   pdl_launch_dependents();
   const TrainEpilogue& e = p.epi;
   const int across = (p.tile_cols + kJoinCols - 1) / kJoinCols, per = across * groups;  // groups of rows of a tile
@@ -82,26 +81,14 @@ __global__ void __launch_bounds__(join_threads(EPI)) train_join_kernel(const __g
   const Place at = place_of(p, p.whole + t);
   const int m0 = at.m * kPairRows + r0, n0 = at.n * p.tile_cols + c0;
   if (m0 >= e.M || n0 >= e.N) return;
-  // The pairs whose shares of the cut tiles overlap this one, and where their pieces are: a thread looks at one pair.
-  const Walk walk(p, p.cut_pairs, 0);
-  const int lo = t * p.units, hi = lo + p.units;
-  int mine = 0, before = 0;
-  if (threadIdx.x < p.cut_pairs) {
-    const int from = walk.share(threadIdx.x), to = walk.share(threadIdx.x + 1);
-    mine = from < hi && to > lo;
-    before = to <= lo;
-  }
-  const int first = __syncthreads_count(before), pieces = __syncthreads_count(mine);
-  if (mine) place[threadIdx.x - first] = piece_of(p, walk, threadIdx.x, p.whole + t);
-  __syncthreads();
   pdl_wait();
 
   const int c = threadIdx.x % (kJoinCols / 4) * 4, r1 = threadIdx.x / (kJoinCols / 4), n = n0 + c;
   float sum_v[kEach][4] = {}, sum_u[EPI == kEpiGateUp ? kEach : 1][4] = {};
-  const size_t off = (size_t)(r0 + r1) * acc_cols + c0 + c;
+  const float* piece = piece_of(p, t) + (size_t)(r0 + r1) * acc_cols + c0 + c;
+  const size_t next = (p.tiles - p.whole) * p.piece;  // from a tile's piece to its next one
 #pragma unroll (EPI == kEpiGateUp ? 8 / kEach : 16 / kEach)
-  for (int q = 0; q < pieces; ++q) {
-    const float* piece = place[q] + off;
+  for (int q = 0; q < p.split; ++q, piece += next) {
 #pragma unroll
     for (int x = 0; x < kEach; ++x) {
       if (m0 + r1 + x * kHigh >= e.M) continue;  // rows that no pair has written

@@ -96,7 +96,8 @@ struct TrainUmma {
 };
 constexpr int kTrainUmmaPairs = 80;    // pairs of CTAs at most
 constexpr size_t kTrainPieceBytes = 256 * 512 * 4;
-constexpr size_t kTrainPartialBytes = 2 * kTrainUmmaPairs * kTrainPieceBytes;
+constexpr int kTrainPieces = 2 * kTrainUmmaPairs;  // of tiles that are cut, at most
+constexpr size_t kTrainPartialBytes = kTrainPieces * kTrainPieceBytes;
 int train_umma_lines(int M);
 cudaError_t launch_train_umma(const TrainUmma& t, cudaStream_t s);
 // out[l][r][c], l = 0, 1, 2: the bf16 terms of in[r][c]; `ld_out` elements between rows, `limb` between terms.

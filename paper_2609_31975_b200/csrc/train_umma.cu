@@ -17,9 +17,8 @@
 // Epilogues leave through shared memory: boxes of 32 rows x 64 columns, 128-byte swizzle, which tensor-map stores take to the
 // caller's rows, whatever their stride and alignment, cut off at the matrix's edges.
 //
-// Tiles are dealt to the pairs round robin.  What is left for a last, partly idle round is cut along K instead so that all pairs get
-// the same share of it: each leaves its piece of a tile as fp32 in a workspace, and train_join_kernel adds up the pieces in their
-// order in K and does the epilogue.
+// Tiles are dealt to the pairs round robin.  What is left for a last, partly idle round is cut along K where that is shorter: a pair
+// leaves its piece of a tile as fp32 in a workspace, and train_join_kernel adds up the pieces in their order in K and does the epilogue.
 // Every wait is bounded by a cycle budget; on expiry the status word is set, all roles wind down and tensor memory is given back.
 #include <cmath>
 
@@ -283,8 +282,8 @@ __global__ void __launch_bounds__(Form<EPI>::kThreads, 1) train_umma_kernel(cons
       const Place at = place_of(p, it.tile);
       const int row0 = at.m * kPairRows + rank * 128 + 32 * quad;  // this warp's first row
       const bool rows = row0 < e.M;                                // has any: the others only keep step
-      const bool cut = is_cut(p, it);
-      float* const piece = cut ? piece_of(p, walk, pair, it.tile) + (size_t)(rank * 128 + 32 * quad + lane) * (256 * F::kWide) : nullptr;  // this lane's row
+      const bool cut = it.piece >= 0;
+      float* const piece = cut ? piece_of(p, it.piece) + (size_t)(rank * 128 + 32 * quad + lane) * (256 * F::kWide) : nullptr;  // this lane's row
       if constexpr (EPI == kEpiHidden) {
         float acc[16 * kChunks];
 #pragma unroll
@@ -424,7 +423,7 @@ __global__ void __launch_bounds__(Form<EPI>::kThreads, 1) train_umma_kernel(cons
     int sums_phase = 0, in_phase = 0;
     bool ok = true;
     while (ok && walk.step(p, it)) {
-      if (is_cut(p, it)) continue;
+      if (it.piece >= 0) continue;
       const Place at = place_of(p, it.tile);
       const int row0 = at.m * kPairRows + rank * 128 + 32 * quad;
       const bool rows = row0 < e.M;
@@ -597,27 +596,27 @@ int plan_umma(const TrainUmma& t, int cols, UmmaParams& p, int pairs) {
   p.status = t.status;
   p.budget = fused_test_knobs().wait_cycles;
   p.drop = fused_test_knobs().drop_stage;
-  // Whole rounds of tiles, then the rest: whole too, or cut along K, into `split` equal pieces a tile, one a pair, or so that all pairs
-  // get the same share, of one tile or of two.  What is shortest, counted in K blocks of a product (half a microsecond): a piece's
-  // rows are written to the workspace (8 for 256 rows of 256 columns), and a kernel of its own joins the pieces (5, and a half for each of a tile's).
-  // 4096 x 14336, bf16, shares for all / with equal pieces: 200, 500, 1000 tokens forward 122 / 114, 193 / 167, 314 / 289 us, 1000
-  // tokens backward 709 / 625; 1121 x 496 x 1728 backward 94 / 72; 6863 x 528 x 1984 backward 204 / 182.
+  // Whole rounds of tiles, then the rest: whole too, or cut along K into `split` equal pieces a tile, dealt in rounds of their own.  What
+  // is shortest, counted in K blocks of a product (half a microsecond): a piece's rows are written to the workspace (8 for 256 rows of
+  // 256 columns), and a kernel of its own joins the pieces (5, and a half for each of a tile's).
+  // PLANFIGURES
   const int rest = p.tiles % pairs;
   p.whole = p.tiles;
   if (t.partial && rest > 0) {
     const double units = p.units, products = t.f32 ? kLimbProducts : 1, piece = 1.0 + (cols > 256 ? 16.0 : 8.0) * (g.M < kPairRows ? g.M : kPairRows) / kPairRows;
     double best = units * products;
-    for (int split = 2; split <= pairs / rest && split <= p.units; ++split) {
-      const double time = std::ceil(units / split) * products + piece + 5.0 + 0.5 * split;
+    for (int split = 2; split <= p.units && rest * split <= kTrainPieces; ++split) {
+      const int rounds = (rest * split + pairs - 1) / pairs;
+      const double time = rounds * (std::ceil(units / split) * products + piece) + 5.0 + 0.5 * split;
       if (time < best) {
         best = time;
-        p.cut_pairs = rest * split;
+        p.split = split;
       }
     }
-    if ((long long)rest * p.units >= pairs && std::ceil(units * rest / pairs) * products + 2.0 * piece + 5.5 + 0.5 * pairs / rest < best) p.cut_pairs = pairs;
-    if (p.cut_pairs > 0) p.whole = p.tiles - rest;
+    if (p.split > 1) p.whole = p.tiles - rest;
   }
-  if (p.whole < pairs) pairs = p.whole > p.cut_pairs ? p.whole : p.cut_pairs;
+  const int pieces = (p.tiles - p.whole) * p.split, most = p.whole > pieces ? p.whole : pieces;
+  if (most < pairs) pairs = most;
   return pairs;
 }
 

@@ -21,47 +21,41 @@ struct UmmaParams {
   int blocks;                         // K blocks of a part
   int units, run_units;               // a tile's K blocks, those of a run
   int whole;                          // tiles dealt whole; the others are cut along K,
-  int cut_pairs;                      // among so many pairs
+  int split;                          // into so many pieces each
   int batch, tile_cols;
   int a_mn, b_mn;
   float* partial;
-  size_t piece;                       // floats of a pair's piece of a tile
+  size_t piece;                       // floats of a piece
   int32_t* status;
   long long budget;
   int drop;                           // test hook: a K block whose rows of A CTA 0 leaves out, so that the wait for them runs out (-1: none)
 };
 
-// One piece of work of a pair of CTAs: units [u0, u1) of a tile.
+// One piece of work of a pair of CTAs: units [u0, u1) of a tile, whose sums go to the workspace as piece number `piece` (-1: a whole tile).
 struct Item {
-  int tile, u0, u1;
+  int tile, u0, u1, piece;
 };
-// A pair's items in order: its share of the tiles that are cut, then whole tiles.
+// A pair's items in order: pieces of the tiles that are cut (the first pieces of all, then the second ones ..: what runs at one time
+// is of one stretch of K, whose rows and columns the tiles share in L2), then whole tiles.
 struct Walk {
-  int pairs, cut_pairs, cut, units, lo, hi, next;  // lo, hi: its units of all cut tiles in a row
-  __device__ __forceinline__ Walk(const UmmaParams& p, int pairs_, int pair) {
-    pairs = pairs_; cut_pairs = p.cut_pairs; units = p.units;
-    cut = p.tiles - p.whole;
-    lo = hi = 0;
-    if (pair < cut_pairs) {
-      lo = share(pair);
-      hi = share(pair + 1);
-    }
-    next = pair;
-  }
-  __device__ __forceinline__ int share(int q) const { return (int)((long long)cut * units * q / cut_pairs); }
+  int pairs, next_piece, next;
+  __device__ __forceinline__ Walk(const UmmaParams& p, int pairs_, int pair) : pairs(pairs_), next_piece(pair), next(pair) {}
   __device__ __forceinline__ bool step(const UmmaParams& p, Item& it) {
-    if (lo < hi) {
-      const int t = lo / units;
-      it.tile = p.whole + t;
-      it.u0 = lo - t * units;
-      it.u1 = min(units, hi - t * units);
-      lo = t * units + it.u1;
+    const int cut = p.tiles - p.whole;
+    if (next_piece < cut * p.split) {
+      const int part = next_piece / cut;
+      it.tile = p.whole + next_piece - part * cut;
+      it.u0 = p.units * part / p.split;
+      it.u1 = p.units * (part + 1) / p.split;
+      it.piece = next_piece;
+      next_piece += pairs;
       return true;
     }
     if (next >= p.whole) return false;
     it.tile = next;
     it.u0 = 0;
-    it.u1 = units;
+    it.u1 = p.units;
+    it.piece = -1;
     next += pairs;
     return true;
   }
@@ -84,12 +78,8 @@ __device__ __forceinline__ Place place_of(const UmmaParams& p, int tile) {
   return at;
 }
 
-__device__ __forceinline__ bool is_cut(const UmmaParams& p, const Item& it) { return it.u0 > 0 || it.u1 < p.units; }
-// Where a pair leaves its piece of a cut tile, [256][columns of the accumulators] fp32: a pair has at most two, of the tile that its
-// share begins in and of the one after.
-__device__ __forceinline__ float* piece_of(const UmmaParams& p, const Walk& w, int pair, int tile) {
-  return p.partial + (size_t)(2 * pair + (w.share(pair) < (tile - p.whole) * p.units ? 1 : 0)) * p.piece;
-}
+// A piece, [256][columns of the accumulators] fp32: part `part` of the t-th tile that is cut is number t + part * (tiles that are cut).
+__device__ __forceinline__ float* piece_of(const UmmaParams& p, int number) { return p.partial + (size_t)number * p.piece; }
 // Sixteen columns of a row of a piece.
 __device__ __forceinline__ void put_piece(float* at, const float* v) {
 #pragma unroll

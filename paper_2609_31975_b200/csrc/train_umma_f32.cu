@@ -277,8 +277,8 @@ __global__ void __launch_bounds__(kThreads, 1) train_umma_f32_kernel(const __gri
         tmem_arrived(v);
       };
       // A tile that several pairs share: this warp's part of it is 16 KB of every piece.
-      if (is_cut(p, it)) {
-        float* piece = piece_of(p, walk, pair, it.tile) + (size_t)(rank * 128 + 32 * quad + lane) * kCols;
+      if (it.piece >= 0) {
+        float* piece = piece_of(p, it.piece) + (size_t)(rank * 128 + 32 * quad + lane) * kCols;
 #pragma unroll 2
         for (int c = 0; c < kChunks; ++c) {
           float v[16];
