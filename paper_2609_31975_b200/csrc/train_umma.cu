@@ -30,7 +30,8 @@ namespace {
 
 using namespace tc;
 
-constexpr int kStages = 4;
+constexpr int kStages = 4;           // of whole K blocks; the ring holds up to kMostStages of fewer rows of A
+constexpr int kMostStages = 6, kFewRows = 64;
 constexpr int kBoxBytes = 32 * 128;  // 32 rows x 64 bf16 columns
 constexpr int kAdders = 8;           // warps 4-11
 
@@ -116,16 +117,16 @@ __global__ void __launch_bounds__(Form<EPI>::kThreads, 1) train_umma_kernel(cons
   extern __shared__ uint8_t smem_raw[];
   __shared__ int abort_word;
   __shared__ uint32_t tmem_slot;
-  __shared__ __align__(8) uint64_t bars[2 * kStages + 4 + 2 + 4];
+  __shared__ __align__(8) uint64_t bars[2 * kMostStages + 4 + 2 + 4];
   volatile int* const abort_flag = &abort_word;
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const uint32_t ring = (smem_u32(smem_raw) + 1023u) & ~1023u, boxes = ring + kStages * F::kStageBytes;
-  const uint32_t full = smem_u32(bars), empty = full + 8 * kStages, acc_full = empty + 8 * kStages, acc_empty = acc_full + 16;
+  const uint32_t full = smem_u32(bars), empty = full + 8 * kMostStages, acc_full = empty + 8 * kMostStages, acc_empty = acc_full + 16;
   const uint32_t sums_full = acc_empty + 16, sums_empty = sums_full + 8, in_full = sums_empty + 8;  // kHidden
   const int rank = (int)cluster_rank(), pair = (int)blockIdx.x >> 1, pairs = (int)gridDim.x >> 1;
 
   if (tid == 0) {
-    for (int s = 0; s < kStages; ++s) {
+    for (int s = 0; s < kMostStages; ++s) {
       mbar_init(full + 8 * s, 1);
       mbar_init(empty + 8 * s, 1);
     }
@@ -160,6 +161,7 @@ __global__ void __launch_bounds__(Form<EPI>::kThreads, 1) train_umma_kernel(cons
     if constexpr (EPI == kEpiHidden) asm volatile("setmaxnreg.dec.sync.aligned.u32 56;");
     auto wait_all = [&](uint32_t bar, uint32_t parity) { return __all_sync(0xffffffffu, mbar_wait(bar, parity, abort_flag, p.status, p.budget)) != 0; };
     if (warp == 0) {
+      const uint32_t a_bytes = p.a_rows * kDeep * 2;
       int s = 0, phase = 0, left_out = blockIdx.x == 0 ? p.drop : -1;
       bool ok = true;
       while (ok && walk.step(p, it)) {
@@ -173,9 +175,9 @@ __global__ void __launch_bounds__(Form<EPI>::kThreads, 1) train_umma_kernel(cons
             const int part = u >= p.blocks ? 1 : 0, k0 = (u - part * p.blocks) * kDeep, which = p.batch > 1 ? at.batch : part;
             const CUtensorMap* ma = &maps.a[EPI == kEpiGateUp ? 0 : which];
             const CUtensorMap* mb = &maps.b[EPI == kEpiGateUp ? rank : which];
-            const uint32_t bar = map_rank(full + 8 * s, 0), da = ring + s * F::kStageBytes;
-            if (rank == 0) mbar_expect_tx(full + 8 * s, 2 * (1 + halves) * kHalfBytes);
-            if (left_out-- == 0) {
+            const uint32_t bar = map_rank(full + 8 * s, 0), da = ring + s * p.stage_bytes;
+            if (rank == 0) mbar_expect_tx(full + 8 * s, 2 * halves * kHalfBytes + (a_bytes < kHalfBytes ? 1 : 2) * a_bytes);
+            if (left_out-- == 0 || (rank == 1 && a_bytes < kHalfBytes)) {
             } else if (p.a_mn) {
               tma_tile_3d(da, ma, m0, k0, 0, bar);
               tma_tile_3d(da + kHalfBytes / 2, ma, m0 + 64, k0, 0, bar);
@@ -183,7 +185,7 @@ __global__ void __launch_bounds__(Form<EPI>::kThreads, 1) train_umma_kernel(cons
               tma_tile_3d(da, ma, k0, m0, 0, bar);
             }
             for (int h = 0; h < halves; ++h) {
-              const uint32_t db = da + (1 + h) * kHalfBytes;
+              const uint32_t db = da + a_bytes + h * kHalfBytes;
               const int n = n0 + 256 * h;
               if (p.b_mn) {
                 tma_tile_3d(db, mb, n, k0, 0, bar);
@@ -194,18 +196,19 @@ __global__ void __launch_bounds__(Form<EPI>::kThreads, 1) train_umma_kernel(cons
             }
           }
           __syncwarp();
-          if (++s == kStages) { s = 0; phase ^= 1; }
+          if (++s == p.stages) { s = 0; phase ^= 1; }
         }
       }
     } else if (warp == 1 && rank == 0) {
       const uint32_t idesc = idesc_bf16(kPairRows, 256, p.a_mn, p.b_mn);
       const uint64_t a0 = p.a_mn ? desc_mn_major(ring, kHalfBytes / 2) : desc_k_major(ring);
-      const uint64_t b0 = p.b_mn ? desc_mn_major(ring + kHalfBytes, kHalfBytes / 2) : desc_k_major(ring + kHalfBytes);
+      const uint32_t ring_b = ring + p.a_rows * kDeep * 2;
+      const uint64_t b0 = p.b_mn ? desc_mn_major(ring_b, kHalfBytes / 2) : desc_k_major(ring_b);
       const uint32_t a_step = p.a_mn ? 2048 >> 4 : 32 >> 4, b_step = p.b_mn ? 2048 >> 4 : 32 >> 4;  // sixteen k
       int s = 0, phase = 0, b = 0, acc_phase[2] = {1, 1};
       // the MMAs of a K block into one accumulator
       auto multiply = [&](int buffer, int h, uint32_t more) {
-        const uint32_t off = (uint32_t)(s * F::kStageBytes) >> 4;
+        const uint32_t off = (uint32_t)(s * p.stage_bytes) >> 4;
 #pragma unroll
         for (int k = 0; k < kDeep / 16; ++k)
           umma_pair(tmem + buffer * 256, a0 + off + k * a_step, b0 + off + h * (kHalfBytes >> 4) + k * b_step, idesc, k > 0 ? 1u : more);
@@ -233,7 +236,7 @@ __global__ void __launch_bounds__(Form<EPI>::kThreads, 1) train_umma_kernel(cons
             __syncwarp();
           }
           if (!ok) break;
-          if (++s == kStages) { s = 0; phase ^= 1; }
+          if (++s == p.stages) { s = 0; phase ^= 1; }
           for (int n = u + 1; n < end; ++n) {
             ok = wait_all(full + 8 * s, phase);
             if (!ok) break;
@@ -248,7 +251,7 @@ __global__ void __launch_bounds__(Form<EPI>::kThreads, 1) train_umma_kernel(cons
               }
             }
             __syncwarp();
-            if (++s == kStages) { s = 0; phase ^= 1; }
+            if (++s == p.stages) { s = 0; phase ^= 1; }
           }
           if (!ok) break;
           if (EPI == kEpiGateUp) b ^= 1;
@@ -532,8 +535,16 @@ cudaError_t launch_one(const TrainUmma& t, int pairs, cudaStream_t s) {
   UmmaParams p{};
   pairs = plan_umma(t, F::kTileCols, p, pairs);
   p.piece = (size_t)kPairRows * 256 * F::kWide;
+  // Few tokens: a CTA copies those rows of A in steps of 32 (what the epilogue's warps look at), and the ring holds more K blocks.  The
+  // MMAs read 128 rows all the same: what lies behind, the same stage's rows of B, goes into rows of the accumulator that nobody reads.
+  // bf16, without / with it: 1 and 5 tokens, 4096 x 14336, forward 107 / 92, 96 / 89 us, dh 58 / 43, 53 / 44; 16 tokens, 2048 x 8192,
+  // forward 41 / 37; 60 tokens, 4096 x 14336, dh 49 / 46.  Plain products lose (8 tokens, 8192 x 20000, dx 118 / 141).
+  p.a_rows = EPI != kEpiStore && g.a_major_k && g.M <= kFewRows ? (g.M + 31) & ~31 : 128;
+  p.stage_bytes = F::kStageBytes - kHalfBytes + p.a_rows * kDeep * 2;
+  p.stages = kStages * F::kStageBytes / p.stage_bytes;
+  static_assert(kStages * F::kStageBytes / (F::kStageBytes - kHalfBytes + 32 * kDeep * 2) <= kMostStages);
   Maps maps;
-  bool fine = pairs > 0 && make_operand_maps(t, maps.a, maps.b);
+  bool fine = pairs > 0 && make_operand_maps(t, p.a_rows, maps.a, maps.b);
   const TrainEpilogue& e = g.epi;
   void* const out[3] = {EPI == kEpiStore ? e.out[0] : EPI == kEpiGateUp ? e.z : e.dz, EPI == kEpiStore ? e.out[1] : EPI == kEpiGateUp ? e.u : e.du,
                         EPI == kEpiStore ? e.out[2] : e.h};
@@ -562,13 +573,13 @@ bool make_train_map(CUtensorMap* m, const void* base, int64_t width, int64_t row
             CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-bool make_operand_maps(const TrainUmma& t, CUtensorMap* a, CUtensorMap* b) {
+bool make_operand_maps(const TrainUmma& t, int a_rows, CUtensorMap* a, CUtensorMap* b) {
   const TrainGemm& g = t.g;
   const int na = g.epilogue == kEpiGateUp ? 1 : g.batch > 1 ? g.batch : g.parts, nb = g.batch > 1 ? g.batch : g.parts;
   const int terms = t.f32 ? 3 : 1;
   for (int i = 0; i < 3; ++i) {  // the first one again where there are fewer
     if (i >= na) a[i] = a[0];
-    else if (!(g.a_major_k ? make_train_map(&a[i], g.a[i].data, g.K, g.M, g.a[i].ld, terms, t.limb_a[i], 128)
+    else if (!(g.a_major_k ? make_train_map(&a[i], g.a[i].data, g.K, g.M, g.a[i].ld, terms, t.limb_a[i], a_rows)
                            : make_train_map(&a[i], g.a[i].data, g.M, g.K, g.a[i].ld, terms, t.limb_a[i], 64))) return false;
     if (i >= nb) b[i] = b[0];
     else if (!(g.b_major_k ? make_train_map(&b[i], g.b[i].data, g.K, g.N, g.b[i].ld, terms, t.limb_b[i], 128)
@@ -599,7 +610,9 @@ int plan_umma(const TrainUmma& t, int cols, UmmaParams& p, int pairs) {
   // Whole rounds of tiles, then the rest: whole too, or cut along K into `split` equal pieces a tile, dealt in rounds of their own.  What
   // is shortest, counted in K blocks of a product (half a microsecond): a piece's rows are written to the workspace (8 for 256 rows of
   // 256 columns), and a kernel of its own joins the pieces (5, and a half for each of a tile's).
-  // PLANFIGURES
+  // 4096 x 14336, bf16: z and u of 1000 tokens, 448 tiles on 74 pairs, whole 213 us, cut 181 and 13 for the join; backward pass of 1000, 1500
+  // and 2048 tokens with all pairs an equal share of the rest, wherever in K that starts, 689, 999, 1290 us, with equal pieces 650, 912,
+  // 1164 (dx of 2048 tokens then reads 2.3 GB from memory, its operands six times over); 5 tokens 190 / 195.
   const int rest = p.tiles % pairs;
   p.whole = p.tiles;
   if (t.partial && rest > 0) {

@@ -24,6 +24,7 @@ struct UmmaParams {
   int split;                          // into so many pieces each
   int batch, tile_cols;
   int a_mn, b_mn;
+  int a_rows, stages, stage_bytes;    // bf16: rows of A that a CTA copies; the ring
   float* partial;
   size_t piece;                       // floats of a piece
   int32_t* status;
@@ -146,8 +147,8 @@ __device__ __forceinline__ float column_sum(float* v, int lane) {
 
 // `terms` bf16 matrices [rows, width], rows `ld` elements apart, in boxes of 64 elements x `box` rows, 128-byte swizzle.
 bool make_train_map(CUtensorMap* m, const void* base, int64_t width, int64_t rows, int64_t ld, int terms, int64_t limb, int box);
-// The maps of a product's operands, three of each (the last one repeated where there are fewer).
-bool make_operand_maps(const TrainUmma& t, CUtensorMap* a, CUtensorMap* b);
+// The maps of a product's operands, three of each (the first one again where there are fewer); a_rows: of a box of a K-major A.
+bool make_operand_maps(const TrainUmma& t, int a_rows, CUtensorMap* a, CUtensorMap* b);
 // Fills in what follows from the product: tiles of `cols` columns, K in units, which tiles are cut for `pairs` pairs of CTAs
 // (returned: the pairs that have work).
 int plan_umma(const TrainUmma& t, int cols, UmmaParams& p, int pairs);

@@ -437,7 +437,7 @@ cudaError_t launch_train_umma_f32(const TrainUmma& t, int pairs, cudaStream_t s)
   pairs = plan_umma(t, t.g.epilogue == kEpiGateUp ? kCols / 2 : kCols, p, pairs);
   p.piece = (size_t)kPairRows * kCols;
   Maps maps;
-  if (pairs <= 0 || !make_operand_maps(t, maps.a, maps.b)) return cudaErrorInvalidValue;
+  if (pairs <= 0 || !make_operand_maps(t, 128, maps.a, maps.b)) return cudaErrorInvalidValue;
   if (t.g.epilogue == kEpiStore) return launch_one<kEpiStore>(p, maps, pairs, s);
   if (t.g.epilogue == kEpiGateUp) return launch_one<kEpiGateUp>(p, maps, pairs, s);
   return launch_one<kEpiHidden>(p, maps, pairs, s);
