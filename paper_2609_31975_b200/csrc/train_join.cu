@@ -2,8 +2,8 @@
 //
 // A CTA has 32 rows x 64 output columns of a tile, a thread four columns of four rows, or 8 rows and one where there are few such CTAs
 // (kHidden, which sums 32 rows at a time: 32, and one); sixteen loads of a thread are under way at once.  Bound by the pieces' bytes,
-// which are still in L2, and by latency where few tiles have many pieces (1000 tokens, 4096 x 14336: 54 MB of y's pieces 13 us, 19 MB
-// of z's and u's, 18 a tile, 15 us).
+// which are still in L2, and by latency where few tiles have many pieces (1000 tokens, 4096 x 14336: 33 MB of y's pieces, two a tile,
+// 10.6 us; 19 MB of z's and u's, 18 a tile, 9.2 us).
 #include "train_umma.cuh"
 
 namespace sffn {

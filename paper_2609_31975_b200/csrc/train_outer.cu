@@ -2,7 +2,7 @@
 //
 // Such a product is its own output: 4096 x 14336, one token, writes 352 MB (bf16) for half a flop a byte.  A thread keeps its 16 bytes
 // of every row of B in registers and goes down the rows, eight at a time, with the next eight entries of A's rows under way.
-// 4096 x 14336, backward pass of 1 / 4 tokens in bf16 162 / 180 us (the tensor-core product: 194, from 5 tokens on no slower);
+// 4096 x 14336, backward pass of 1 / 4 tokens in bf16 155 / 180 us (the tensor-core product: 190, from 5 tokens on no slower);
 // 4096 x 8192, 8 / 16 tokens in fp32 276 / 418 us (tiles of FMAs 504 / 654; split for the tensor cores 492 / 495).
 #include "train_kernels.cuh"
 
