@@ -10,7 +10,7 @@
 // to nearest.  Relative error of y (800 tokens, 512 x 1536, squared RELU) / time of a backward pass (500 tokens, 3840 x 14230): 6.2e-7
 // / 1.84 ms, fp32 FMAs 8.0e-7; each block's six products in turn 1.6e-6 / 1.83, runs of one block 2.8e-7 / 1.96, both blocks'
 // a0 b0 at the end 4.0e-7 / 1.87 (their places come back too late for the next run).
-// Three products of 278, 433 and 659 us there, 1.2 to 1.5 PFLOP/s of bf16, and 305 us for the terms of the weights.
+// Three products of 273, 460 and 664 us there, 1.2 to 1.5 PFLOP/s of bf16, and 295 us for the terms of weights and tokens.
 #include "fused_kernel.cuh"
 #include "train_umma.cuh"
 
