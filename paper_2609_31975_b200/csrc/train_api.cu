@@ -21,7 +21,7 @@ namespace {
   } while (0)
 
 constexpr double kSplitProducts = 1.5e8;  // T D H
-constexpr int kFewTokens = 16;
+constexpr int kFewForward = 32, kFewBackward = 16;  // tokens
 constexpr int kMaxRows = 1 << 22;  // tokens, and neurons: the kernels' grids and tensor maps have room for so many
 
 inline bool aligned(const void* p, uintptr_t a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) == 0; }
@@ -41,8 +41,12 @@ int sm_count(int* n) {
 // Which kernels serve a call: tensor cores for bf16, and for fp32 from the size on at which splitting every operand into three
 // terms and multiplying them six times is faster than fp32 FMAs.  Forward / backward in us, FMAs against terms: T D H = 1.3e8 44 / 89
 // against 58 / 80, 1.5e8 64 / 120 against 62 / 107, 2.7e8 78 / 149 against 65 / 91.  Few tokens read the weights once and split them for
-// nothing: 4096 x 8192, 16 tokens 259 / 418 against 349 / 495, 32 tokens 337 / 675 against 352 / 497.
-bool on_tensor_cores(int T, int D, int H, int dtype) { return dtype == SFFN_BF16 || (T > kFewTokens && (double)T * D * H >= kSplitProducts); }
+// nothing, which a backward pass, with more products, outweighs sooner: 4096 x 8192, 16 tokens 259 / 418 against 349 / 495; 3840 x 14230, 20
+// tokens 523 / 1224 against 611 / 817, 32 tokens 530 / 1347 against 614 / 820, 48 tokens 968 against 618; 8192 x 20000, 32 tokens 1315
+// against 1751.
+bool on_tensor_cores(int T, int D, int H, int dtype, bool backward) {
+  return dtype == SFFN_BF16 || (T > (backward ? kFewBackward : kFewForward) && (double)T * D * H >= kSplitProducts);
+}
 
 struct TrainLayout {
   bool umma, split;         // split: operands in three bf16 terms
@@ -59,7 +63,7 @@ TrainLayout train_layout(int T, int D, int H, int dtype, bool backward) {
     off += up256(bytes);
     return o;
   };
-  L.umma = on_tensor_cores(T, D, H, dtype);
+  L.umma = on_tensor_cores(T, D, H, dtype, backward);
   L.split = L.umma && dtype == SFFN_F32;
   L.ld_h = hidden_ld(H);
   L.ld_d = hidden_ld(D);
