@@ -41,9 +41,9 @@ int sm_count(int* n) {
 // Which kernels serve a call: tensor cores for bf16, and for fp32 from the size on at which splitting every operand into three
 // terms and multiplying them six times is faster than fp32 FMAs.  Forward / backward in us, FMAs against terms: T D H = 1.3e8 44 / 89
 // against 58 / 80, 1.5e8 64 / 120 against 62 / 107, 2.7e8 78 / 149 against 65 / 91.  Few tokens read the weights once and split them for
-// nothing, which a backward pass, with more products, outweighs sooner: 4096 x 8192, 16 tokens 259 / 418 against 349 / 495; 3840 x 14230, 20
-// tokens 523 / 1224 against 611 / 817, 32 tokens 530 / 1347 against 614 / 820, 48 tokens 968 against 618; 8192 x 20000, 32 tokens 1315
-// against 1751.
+// nothing, which a backward pass, with more products, outweighs sooner: 4096 x 8192, 16 tokens 264 / 401 against 349 / 495; 32 tokens forward
+// 2048 x 4096 86 against 119, 4096 x 14336 476 against 649; 48 tokens, 3840 x 14230, 968 against 618; backward of 20 tokens there 1224
+// against 817.
 bool on_tensor_cores(int T, int D, int H, int dtype, bool backward) {
   return dtype == SFFN_BF16 || (T > (backward ? kFewBackward : kFewForward) && (double)T * D * H >= kSplitProducts);
 }

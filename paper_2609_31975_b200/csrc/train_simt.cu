@@ -1,12 +1,13 @@
 // Products of small training calls in fp32 FMAs (fp32 storage; larger calls split their operands for the tensor cores).
 //
-// A CTA owns a 32 x 64 tile of C, or z and u of 32 tokens x 32 neurons; two threads 4 x 4 of it, a half of a piece's k each.  For up
-// to 16 rows: 8 x 64 tiles, eight threads an eighth of the k each.  Pieces of 64 k go through registers into [k][m] and [k][n]
-// arrays, whichever way an operand lies in memory, the next piece under way while one is multiplied.  Such a call has few tiles and
-// is bound by latency, so K is cut among up to eight CTAs of a cluster: each
-// leaves its sums in shared memory and takes a share of the tile's rows, which it adds up over all of them, in order.
-// 64 tokens, 256 x 1024: forward 16 us, backward 29 us as a graph, of which launches 4 and 6, FMAs 4 and 10, the clusters' exchange 4 and
-// 2 (59 and 114 us without clusters); with few tokens bound by the weights' bytes: 1 token, 4096 x 14336, forward 264 us for 705 MB.
+// A CTA owns a 32 x 64 tile of C, or z and u of 32 tokens x 32 neurons; four threads 8 x 4 of it, a quarter of a piece's k each, in packed
+// FMAs.  For up to 16 rows: 8 x 64 tiles, eight threads 4 x 4, an eighth of the k each.  Pieces of 64 k go through registers into
+// [k][m] and [k][n] arrays, whichever way an operand lies in memory, the next piece under way while one is multiplied.  Such a call has
+// few tiles and is bound by latency, so K is cut among up to eight CTAs of a cluster: each leaves its sums in shared memory and takes
+// a share of the tile's rows, which it adds up over all of them, in order.
+// 64 tokens, 256 x 1024, in a loop: forward 17 us, backward 31, of which launches 4 and 6 (20 and 33 with 4 x 4 a thread, 59 and 114 without
+// clusters); 32 tokens, 4096 x 14336, forward 476 us (577), three times the FMAs' time: loads of a piece wait for their stores.  1 token:
+// 264 us for 705 MB.
 #include "train_kernels.cuh"
 
 namespace sffn {
@@ -107,17 +108,18 @@ __global__ void __launch_bounds__(kThreads) train_simt_kernel(const __grid_const
   float(*const sa)[kRows + 4] = reinterpret_cast<float(*)[kRows + 4]>(pool);
   float(*const sb)[kCols + 4] = reinterpret_cast<float(*)[kCols + 4]>(pool + kDepth * (kRows + 4));  // kDual: columns of W_g, then of W_up
   __shared__ __align__(16) float tile[kRows][kCols + 4];
-  constexpr int kSide = 16 * (kRows / 4), kParts = kThreads / kSide, kShare = kDepth / kParts;  // threads of a tile; parts of a piece's k
+  constexpr int kMine = kRows < 32 ? 4 : 8;  // rows of a thread
+  constexpr int kSide = 16 * (kRows / kMine), kParts = kThreads / kSide, kShare = kDepth / kParts;  // threads of a tile; parts of a piece's k
   pdl_launch_dependents();
   pdl_wait();
-  const int tx = threadIdx.x & 15, ty = threadIdx.x / 16 % (kRows / 4), part_k = threadIdx.x / kSide;
+  const int tx = threadIdx.x & 15, ty = threadIdx.x / 16 % (kRows / kMine), part_k = threadIdx.x / kSide;
   const int m_tiles = (g.M + kRows - 1) / kRows, n_tiles = (g.N + kNeurons - 1) / kNeurons;
   const int at_tile = blockIdx.x / splits, split = blockIdx.x - at_tile * splits, at_col = at_tile / m_tiles, z = at_col / n_tiles;
   const int m0 = (at_tile - at_col * m_tiles) * kRows, n0 = (at_col - z * n_tiles) * kNeurons;
   // K of all parts in a row, in pieces
   const int parts = kDual ? 1 : g.parts, per = (g.K + kDepth - 1) / kDepth, pieces = parts * per;
   const int first = (int)((long long)pieces * split / splits), last = (int)((long long)pieces * (split + 1) / splits);
-  float acc[4][4] = {};
+  float2 acc[kMine][2] = {};
   Piece<kRows> pa;
   Piece<kDual ? kNeurons : kCols> pb;
   Piece<kDual ? kNeurons : kRows> pu;  // kDual: of W_up
@@ -149,12 +151,15 @@ __global__ void __launch_bounds__(kThreads) train_simt_kernel(const __grid_const
 #pragma unroll 8
     for (int q = 0; q < k_end; ++q) {
       const int k = part_k * kShare + q;
-      const float4 a = *reinterpret_cast<const float4*>(&sa[k][4 * ty]), b = *reinterpret_cast<const float4*>(&sb[k][4 * tx]);
-      const float av[4] = {a.x, a.y, a.z, a.w}, bv[4] = {b.x, b.y, b.z, b.w};
+      const float4 b = *reinterpret_cast<const float4*>(&sb[k][4 * tx]);
+      alignas(16) float av[kMine];
 #pragma unroll
-      for (int i = 0; i < 4; ++i)
+      for (int i = 0; i < kMine; i += 4) *reinterpret_cast<float4*>(av + i) = *reinterpret_cast<const float4*>(&sa[k][kMine * ty + i]);
 #pragma unroll
-        for (int j = 0; j < 4; ++j) acc[i][j] = fmaf(av[i], bv[j], acc[i][j]);
+      for (int i = 0; i < kMine; ++i) {
+        acc[i][0] = fma2(make_float2(av[i], av[i]), make_float2(b.x, b.y), acc[i][0]);
+        acc[i][1] = fma2(make_float2(av[i], av[i]), make_float2(b.z, b.w), acc[i][1]);
+      }
     }
     __syncthreads();
   }
@@ -162,18 +167,19 @@ __global__ void __launch_bounds__(kThreads) train_simt_kernel(const __grid_const
   static_assert((kParts - 1) * kRows * (kCols + 4) <= kDepth * (kRows + 4 + kCols + 4), "the parts' sums fit the operands' arrays");
   if (part_k > 0) {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) *reinterpret_cast<float4*>(&other[part_k - 1][4 * ty + i][4 * tx]) = make_float4(acc[i][0], acc[i][1], acc[i][2], acc[i][3]);
+    for (int i = 0; i < kMine; ++i) *reinterpret_cast<float4*>(&other[part_k - 1][kMine * ty + i][4 * tx]) = make_float4(acc[i][0].x, acc[i][0].y, acc[i][1].x, acc[i][1].y);
   }
   __syncthreads();
   if (part_k == 0) {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
+    for (int i = 0; i < kMine; ++i) {
+      float4 sum = make_float4(acc[i][0].x, acc[i][0].y, acc[i][1].x, acc[i][1].y);
 #pragma unroll
       for (int q = 0; q < kParts - 1; ++q) {
-        const float4 o = *reinterpret_cast<const float4*>(&other[q][4 * ty + i][4 * tx]);
-        acc[i][0] += o.x; acc[i][1] += o.y; acc[i][2] += o.z; acc[i][3] += o.w;
+        const float4 o = *reinterpret_cast<const float4*>(&other[q][kMine * ty + i][4 * tx]);
+        sum.x += o.x; sum.y += o.y; sum.z += o.z; sum.w += o.w;
       }
-      *reinterpret_cast<float4*>(&tile[4 * ty + i][4 * tx]) = make_float4(acc[i][0], acc[i][1], acc[i][2], acc[i][3]);
+      *reinterpret_cast<float4*>(&tile[kMine * ty + i][4 * tx]) = sum;
     }
   }
   if (splits > 1) cluster_meet();
