@@ -42,7 +42,7 @@ int sm_count(int* n) {
 // terms and multiplying them six times is faster than fp32 FMAs.  Forward / backward in us, FMAs against terms: T D H = 1.3e8 44 / 89
 // against 58 / 80, 1.5e8 64 / 120 against 62 / 107, 2.7e8 78 / 149 against 65 / 91.  Few tokens read the weights once and split them for
 // nothing, which a backward pass, with more products, outweighs sooner: 4096 x 8192, 16 tokens 264 / 401 against 349 / 495; 32 tokens forward
-// 2048 x 4096 86 against 119, 4096 x 14336 476 against 649; 48 tokens, 3840 x 14230, 968 against 618; backward of 20 tokens there 1224
+// 2048 x 4096 86 against 119, 4096 x 14336 476 against 649; 48 tokens, 3840 x 14230, 968 against 615; backward of 20 tokens there 1224
 // against 817.
 bool on_tensor_cores(int T, int D, int H, int dtype, bool backward) {
   return dtype == SFFN_BF16 || (T > (backward ? kFewBackward : kFewForward) && (double)T * D * H >= kSplitProducts);
