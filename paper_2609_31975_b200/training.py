@@ -116,7 +116,8 @@ def gated_ffn_backward(dy, x, z, u, W_g, W_up, W_down, act="relu", act_up=None, 
 
 
 class GatedFFNFunction(torch.autograd.Function):
-    """The pair as a node of torch's graph: ``GatedFFNFunction.apply(x, W_g, b_g, W_up, W_down, act, act_up)``, x [..., D]."""
+    """The pair as a node of torch's graph: ``GatedFFNFunction.apply(x, W_g, b_g, W_up, W_down, act, act_up)``, x [..., D].
+    First derivatives only: a second differentiation (``create_graph=True``, then through the gradients) raises."""
 
     @staticmethod
     def forward(ctx, x, W_g, b_g, W_up, W_down, act="relu", act_up=None):
@@ -129,6 +130,7 @@ class GatedFFNFunction(torch.autograd.Function):
         return y.view(x.shape)
 
     @staticmethod
+    @torch.autograd.function.once_differentiable
     def backward(ctx, dy):
         rows, z, u, W_g, W_up, W_down = ctx.saved_tensors
         names = ("dx", "dW_g", "db_g", "dW_up", "dW_down")
