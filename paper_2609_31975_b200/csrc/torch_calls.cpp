@@ -82,6 +82,11 @@ Tensor make_hidden(int64_t T, int64_t H, at::ScalarType dtype, const at::Device&
   Tensor t = make({T, ld}, dtype, dev);
   return ld == H ? t : t.narrow(1, 0, H);
 }
+// Torch's graph is to know of what a call has written into a caller's tensor, as of its own operations in place: a backward pass that
+// saved it before then raises.  (Tensors made in inference mode are not in any graph, and count nothing.)
+void written(const Tensor& t) {
+  if (!t.is_inference()) t.unsafeGetTensorImpl()->bump_version();
+}
 void* current_stream(const at::Device& dev) { return c10::cuda::getCurrentCUDAStream(dev.index()).stream(); }
 
 // What both passes hand over; the workspace in `ws`.
@@ -126,6 +131,7 @@ py::tuple ffn_forward(const Tensor& x, const Tensor& W_g, const OptTensor& b_g, 
   const int64_t ld_y = rows("y", y, c.T, c.D, dtype, dev);
   if (!save) {
     if (rc == SFFN_OK) rc = entry.forward(&c, y.data_ptr(), ld_y, current_stream(dev));
+    if (rc == SFFN_OK && y_out) written(y);
     return py::make_tuple(rc, y, py::none(), py::none());
   }
   const Tensor z = z_out ? *z_out : make_hidden(c.T, c.H, dtype, dev), u = u_out ? *u_out : make_hidden(c.T, c.H, dtype, dev);
@@ -134,6 +140,11 @@ py::tuple ffn_forward(const Tensor& x, const Tensor& W_g, const OptTensor& b_g, 
   c.z = z.data_ptr();
   c.u = u.data_ptr();
   if (rc == SFFN_OK) rc = entry.forward(&c, y.data_ptr(), ld_y, current_stream(dev));
+  if (rc == SFFN_OK) {
+    if (y_out) written(y);
+    if (z_out) written(z);
+    if (u_out) written(u);
+  }
   return py::make_tuple(rc, y, z, u);
 }
 
@@ -168,6 +179,8 @@ py::tuple ffn_backward(const Tensor& dy, const Tensor& x, const Tensor& z, const
   if (need & 8) g.dW_down = whole("dW_down", take(3, {c.H, c.D}, dtype), {c.H, c.D}, dtype, dev);
   if (need & 16) g.db_g = static_cast<float*>(whole("db_g", take(4, {c.H}, at::kFloat), {c.H}, at::kFloat, dev));
   if (rc == SFFN_OK) rc = entry.backward(&c, dy.data_ptr(), ld_dy, &g, current_stream(dev));
+  for (size_t i = 0; rc == SFFN_OK && i < 5 && i < out.size(); ++i)
+    if (got[i] && out[i]) written(*got[i]);
   return py::make_tuple(rc, got[0], got[1], got[2], got[3], got[4]);
 }
 
@@ -202,6 +215,7 @@ py::tuple grad_norm(const py::object& tensors, const OptTensor& norm_out, const 
   const Tensor norm = norm_out ? *norm_out : make({}, at::kFloat, dev);
   float* out = static_cast<float*>(whole("norm", norm, {}, at::kFloat, dev));
   const int rc = entry.grad_norm(t.data(), (int)list.n, out, ws.data_ptr(), (size_t)ws.numel(), current_stream(dev));
+  if (rc == SFFN_OK && norm_out) written(norm);
   return py::make_tuple(rc, norm);
 }
 
@@ -264,7 +278,15 @@ int adamw_step(const py::object& params, const py::object& grads, const py::obje
   c.beta1 = beta1; c.beta2 = beta2; c.eps = eps; c.step = step; c.max_norm = max_norm;
   if (grad_norm) c.grad_norm = static_cast<const float*>(whole("grad_norm", *grad_norm, {}, at::kFloat, dev));
   const c10::cuda::CUDAGuard guard(dev);
-  return entry.adamw_step(t.data(), (int)p.n, &c, current_stream(dev));
+  const int rc = entry.adamw_step(t.data(), (int)p.n, &c, current_stream(dev));
+  for (Py_ssize_t i = 0; rc == SFFN_OK && i < p.n; ++i) {
+    written(THPVariable_Unpack(p[i]));
+    if (t[i].master) written(THPVariable_Unpack(w[i]));
+    for (const char* name : {"m", "v"}) written(THPVariable_Unpack(PyDict_GetItemString(s[i], name)));
+    if (t[i].state_bits != 8) continue;
+    for (const char* name : {"m_scale", "v_scale"}) written(THPVariable_Unpack(PyDict_GetItemString(s[i], name)));
+  }
+  return rc;
 }
 
 int adamw_state_values(const py::object& states, const py::object& out) {
@@ -285,7 +307,10 @@ int adamw_state_values(const py::object& states, const py::object& out) {
     v[i] = static_cast<float*>(whole("v", tensor_of(PyDict_GetItemString(o[i], "v"), "v"), mi.sizes(), at::kFloat, dev));
   }
   const c10::cuda::CUDAGuard guard(dev);
-  return entry.adamw_state_values(t.data(), (int)s.n, m.data(), v.data(), current_stream(dev));
+  const int rc = entry.adamw_state_values(t.data(), (int)s.n, m.data(), v.data(), current_stream(dev));
+  for (Py_ssize_t i = 0; rc == SFFN_OK && i < s.n; ++i)
+    for (const char* name : {"m", "v"}) written(THPVariable_Unpack(PyDict_GetItemString(o[i], name)));
+  return rc;
 }
 
 }  // namespace

@@ -1,6 +1,7 @@
 """Training of the gated FFN: forward and backward pass, the norm of the gradients and the AdamW step, as functions over torch
 tensors (the "training" section of sparse_ffn.h).  Every step runs in the library's kernels; torch owns the memory.  Arguments are
-checked and marshalled in C++ (csrc/torch_calls.cpp)."""
+checked and marshalled in C++ (csrc/torch_calls.cpp).  A call that writes into a caller's tensor counts as an operation in place: a
+backward pass of torch's graph that saved the tensor before raises."""
 from __future__ import annotations
 
 import ctypes
