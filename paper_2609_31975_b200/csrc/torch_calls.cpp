@@ -5,6 +5,7 @@
 //
 // The C entry points come in as addresses (`bind`), from the library that the binding has loaded.
 #include <ATen/ATen.h>
+#include <c10/cuda/CUDAGraphsC10Utils.h>
 #include <c10/cuda/CUDAGuard.h>
 #include <c10/cuda/CUDAStream.h>
 #include <torch/csrc/autograd/python_variable.h>
@@ -88,6 +89,8 @@ void written(const Tensor& t) {
   if (!t.is_inference()) t.unsafeGetTensorImpl()->bump_version();
 }
 void* current_stream(const at::Device& dev) { return c10::cuda::getCurrentCUDAStream(dev.index()).stream(); }
+
+bool capturing() { return c10::cuda::currentStreamCaptureStatusMayInitCtx() != c10::cuda::CaptureStatus::None; }
 
 // What both passes hand over; the workspace in `ws`.
 sffn_train_call make_call(const Tensor& x, const Tensor& W_g, const Tensor& W_up, const Tensor& W_down, int act, int act_up, const Tensor& status, bool backward,
@@ -212,9 +215,12 @@ py::tuple grad_norm(const py::object& tensors, const OptTensor& norm_out, const 
     t[i].dtype = dtype_code(g.scalar_type(), "gradients");
   }
   const c10::cuda::CUDAGuard guard(dev);
+  // `ws` is this stream's, whose calls run one after another.  A graph may be replayed beside them: each captured call has its own,
+  // zeroed by every replay.
+  const Tensor own = capturing() ? at::zeros({ws.numel()}, ws.options()) : ws;
   const Tensor norm = norm_out ? *norm_out : make({}, at::kFloat, dev);
   float* out = static_cast<float*>(whole("norm", norm, {}, at::kFloat, dev));
-  const int rc = entry.grad_norm(t.data(), (int)list.n, out, ws.data_ptr(), (size_t)ws.numel(), current_stream(dev));
+  const int rc = entry.grad_norm(t.data(), (int)list.n, out, own.data_ptr(), (size_t)own.numel(), current_stream(dev));
   if (rc == SFFN_OK && norm_out) written(norm);
   return py::make_tuple(rc, norm);
 }
