@@ -92,6 +92,21 @@ void* current_stream(const at::Device& dev) { return c10::cuda::getCurrentCUDASt
 
 bool capturing() { return c10::cuda::currentStreamCaptureStatusMayInitCtx() != c10::cuda::CaptureStatus::None; }
 
+// A zeroed buffer that outlives a call.  It comes from a stream of its own, and is there, zeroed, when this returns: the calls that use it
+// may be on any stream, and one that is being captured leaves neither the buffer nor its zeros to the graph.
+Tensor kept(int64_t bytes, int index) {
+  const c10::cuda::CUDAGuard guard((c10::DeviceIndex)index);
+  const c10::cuda::CUDAStreamCaptureModeGuard relaxed(cudaStreamCaptureModeRelaxed);
+  for (int i = 0; i < 64; ++i) {  // torch hands out its streams in turn: not one that is being captured
+    const c10::cuda::CUDAStreamGuard on(c10::cuda::getStreamFromPool(false, (c10::DeviceIndex)index));
+    if (capturing()) continue;
+    const Tensor t = at::zeros({bytes}, at::TensorOptions().dtype(at::kByte).device(at::kCUDA, index));
+    on.current_stream().synchronize();
+    return t;
+  }
+  throw std::runtime_error("every stream is being captured");
+}
+
 // What both passes hand over; the workspace in `ws`.
 sffn_train_call make_call(const Tensor& x, const Tensor& W_g, const Tensor& W_up, const Tensor& W_down, int act, int act_up, const Tensor& status, bool backward,
                           Tensor& ws, int* rc) {
@@ -323,6 +338,7 @@ int adamw_state_values(const py::object& states, const py::object& out) {
 
 PYBIND11_MODULE(_training, m) {
   m.def("bind", &bind);
+  m.def("kept", &kept);
   m.def("ffn_forward", &ffn_forward);
   m.def("ffn_backward", &ffn_backward);
   m.def("grad_norm", &grad_norm);

@@ -45,9 +45,7 @@ def _keep(index, stream, what, nbytes):
     if t is None:
         if index < 0:
             raise TypeError("tensors must be on a CUDA device")
-        t = torch.zeros(nbytes, dtype=torch.uint8, device=torch.device("cuda", index))
-        if not torch.cuda.is_current_stream_capturing():  # one made while capturing is zeroed by every replay, and that graph's
-            _kept[index, stream, what] = t
+        t = _kept[index, stream, what] = _calls().kept(nbytes, index)
     return t
 
 
