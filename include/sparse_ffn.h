@@ -333,7 +333,10 @@ int sffn_lopa_residual(const float* W, const int32_t* g_idx, const int8_t* g_sig
  * than 3.38e38 do not fit bf16 terms.
  * Rows: D a multiple of 16 bytes; x, dy, y, dx [T, D] and z, u [T, H] have row strides `ld_*` in elements, a multiple
  * of 16 bytes and at least the width; H may be any number (columns of z and u past H are neither read nor written).
- * T = 0 is a call like any other: gradients of the weights come out as zeros. */
+ * T = 0 is a call like any other: gradients of the weights come out as zeros.
+ * Overlaps: y may lie over x, and dx over x, dy, z and u (they are read before).  Any other overlap of an output's rows
+ * with an input's, with the workspace or with another output's is SFFN_ERR_INVALID_ARG; what lies between rows does not
+ * count, so that matrices may be columns of one. */
 typedef struct {
   int32_t T, D, H;            /* tokens, model width, hidden width                                                */
   int32_t dtype, act, act_up; /* sffn_dtype, sffn_act, sffn_act                                                   */

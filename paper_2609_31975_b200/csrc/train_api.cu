@@ -140,6 +140,41 @@ int check_rows(const void* p, int64_t ld, int64_t width, size_t esz) {
   return aligned(p, 16) && (ld * esz) % 16 == 0 && ld <= (1ll << 31) ? SFFN_OK : SFFN_ERR_UNSUPPORTED;
 }
 
+// A matrix's rows in memory, and whether any of them meets any row of another matrix's (what lies between rows does not count: two
+// matrices may be columns of one).
+struct Span {
+  const void* p;
+  int64_t rows, width, ld;  // bytes
+};
+bool meet(const Span& a, const Span& b) {
+  if (!a.p || !b.p || a.rows <= 0 || b.rows <= 0 || a.width <= 0 || b.width <= 0) return false;
+  const int64_t d = (int64_t)(reinterpret_cast<uintptr_t>(b.p) - reinterpret_cast<uintptr_t>(a.p));  // b's first byte, from a's
+  if (d >= (a.rows - 1) * a.ld + a.width || -d >= (b.rows - 1) * b.ld + b.width) return false;
+  if (a.ld == b.ld) {  // rows i of a and j of b meet where d - a.width < (i - j) ld < d + b.width
+    const auto below = [](int64_t v, int64_t n) { return v >= 0 ? v / n : -((-v + n - 1) / n); };
+    const int64_t least = below(d - a.width, a.ld) + 1, most = -below(-(d + b.width), a.ld) - 1;
+    return (least > 1 - b.rows ? least : 1 - b.rows) <= (most < a.rows - 1 ? most : a.rows - 1);
+  }
+  for (int64_t i = 0, j = 0; i < a.rows && j < b.rows;) {
+    if (i * a.ld + a.width <= d + j * b.ld) ++i;
+    else if (d + j * b.ld + b.width <= i * a.ld) ++j;
+    else return true;
+  }
+  return false;
+}
+// Whether an output of a call meets one of these inputs, or another output.
+template <size_t kIn, size_t kOut>
+bool outputs_meet(const Span (&in)[kIn], const Span (&out)[kOut]) {
+  for (size_t o = 0; o < kOut; ++o) {
+    for (const Span& i : in)
+      if (meet(out[o], i)) return true;
+    for (size_t q = o + 1; q < kOut; ++q)
+      if (meet(out[o], out[q])) return true;
+  }
+  return false;
+}
+Span whole(const void* p, int64_t bytes) { return {p, 1, bytes, bytes}; }
+
 int check_call(const sffn_train_call* c, bool backward) {
   if (!c) return SFFN_ERR_INVALID_ARG;
   const int shape = check_shape(c->T, c->D, c->H, c->dtype);
@@ -186,6 +221,12 @@ int gated_ffn_forward(const sffn_train_call* c, void* y, int64_t ld_y, void* str
   if (rc != SFFN_OK) return rc;
   const Products p(c, false, static_cast<cudaStream_t>(stream));
   const TrainLayout& L = p.L;
+  const int64_t esz = (int64_t)element(c->dtype), matrix = esz * c->H * c->D;
+  const Span x = {c->x, c->T, esz * c->D, esz * c->ld_x}, own = whole(c->workspace, (int64_t)L.total);
+  const Span out = {y, c->T, esz * c->D, esz * ld_y}, z = {c->z, c->T, esz * c->H, esz * c->ld_hidden}, u = {c->u, c->T, esz * c->H, esz * c->ld_hidden};
+  const Span W[3] = {whole(c->W_g, matrix), whole(c->W_up, matrix), whole(c->W_down, matrix)}, bias = whole(c->b_g, 4ll * c->H);
+  // y is written when x has been read for the last time
+  if (outputs_meet({W[0], W[1], W[2], bias, own}, {out, z, u}) || meet(x, z) || meet(x, u)) return SFFN_ERR_INVALID_ARG;
   const int64_t tokens[3] = {L.limb_t, L.limb_t, L.limb_t}, weights[3] = {L.limb_w, L.limb_w, L.limb_w}, hidden[3] = {L.limb_h, L.limb_h, L.limb_h};
   SFFN_CUDA(p.split(c->x, c->ld_x, c->T, L.x, L.limb_t));
   SFFN_CUDA(p.split(c->W_g, c->D, c->H, L.w[0], L.limb_w));
@@ -244,6 +285,15 @@ int gated_ffn_backward(const sffn_train_call* c, const void* dy, int64_t ld_dy, 
   const TrainLayout& L = p.L;
   const bool want_dz = g->dx || g->dW_g, want_du = g->dx || g->dW_up, want_dh = want_dz || want_du || g->db_g;
   if (!want_dh && !g->dW_down) return SFFN_OK;
+  {
+    const int64_t e = (int64_t)esz, T = c->T, D = c->D, H = c->H, matrix = e * H * D;
+    const Span x = {c->x, T, e * D, e * c->ld_x}, dys = {dy, T, e * D, e * ld_dy}, z = {c->z, T, e * H, e * c->ld_hidden}, u = {c->u, T, e * H, e * c->ld_hidden};
+    const Span W[3] = {whole(c->W_g, matrix), whole(c->W_up, matrix), whole(c->W_down, matrix)}, own = whole(c->workspace, (int64_t)L.total);
+    const Span dx = {g->dx, T, e * D, e * g->ld_dx}, w[3] = {whole(g->dW_g, matrix), whole(g->dW_up, matrix), whole(g->dW_down, matrix)};
+    const Span db = whole(g->db_g, 4 * H);
+    // dx is written last: what it may lie over has been read by then
+    if (outputs_meet({W[0], W[1], W[2], own}, {dx, w[0], w[1], w[2], db}) || outputs_meet({x, dys, z, u}, {w[0], w[1], w[2], db})) return SFFN_ERR_INVALID_ARG;
+  }
   const int64_t tokens[3] = {L.limb_t, L.limb_t, L.limb_t}, weights[3] = {L.limb_w, L.limb_w, L.limb_w}, hidden[3] = {L.limb_h, L.limb_h, L.limb_h};
   void* const values[3] = {p.hidden(L.dz), p.hidden(L.du), p.hidden(L.h)};
   float* const lines = reinterpret_cast<float*>(p.ws + L.db);
@@ -273,6 +323,20 @@ int gated_ffn_backward(const sffn_train_call* c, const void* dy, int64_t ld_dy, 
   SFFN_CUDA(p.run(dh, tokens, weights, &n_lines));
   if (g->db_g) SFFN_CUDA(sffn::launch_train_column_sums(lines, n_lines, L.ld_h, c->H, g->db_g, s));
 
+  sffn::TrainGemm dw{};
+  dw.M = c->H; dw.N = c->D; dw.K = c->T;
+  dw.parts = 1;
+  for (int i = 0; i < 3; ++i) {
+    if (!dW[i]) continue;
+    dw.a[dw.batch] = {values[i], L.ld_h};
+    dw.b[dw.batch] = i < 2 ? p.operand(c->x, c->ld_x, L.x) : p.operand(dy, ld_dy, L.dy);
+    dw.epi.out[dw.batch++] = dW[i];
+  }
+  dw.a_major_k = dw.b_major_k = false;
+  dw.epilogue = sffn::kEpiStore;
+  dw.epi.M = c->H; dw.epi.N = c->D; dw.epi.ld_out = c->D;
+  if (dw.batch > 0) SFFN_CUDA(p.run(dw, hidden, tokens));
+
   if (g->dx) {
     sffn::TrainGemm dx{};
     dx.M = c->T; dx.N = c->D; dx.K = c->H;
@@ -287,20 +351,6 @@ int gated_ffn_backward(const sffn_train_call* c, const void* dy, int64_t ld_dy, 
     dx.epi.out[0] = g->dx; dx.epi.ld_out = g->ld_dx;
     SFFN_CUDA(p.run(dx, hidden, weights));
   }
-  sffn::TrainGemm dw{};
-  dw.M = c->H; dw.N = c->D; dw.K = c->T;
-  dw.parts = 1;
-  for (int i = 0; i < 3; ++i) {
-    if (!dW[i]) continue;
-    dw.a[dw.batch] = {values[i], L.ld_h};
-    dw.b[dw.batch] = i < 2 ? p.operand(c->x, c->ld_x, L.x) : p.operand(dy, ld_dy, L.dy);
-    dw.epi.out[dw.batch++] = dW[i];
-  }
-  if (dw.batch == 0) return SFFN_OK;
-  dw.a_major_k = dw.b_major_k = false;
-  dw.epilogue = sffn::kEpiStore;
-  dw.epi.M = c->H; dw.epi.N = c->D; dw.epi.ld_out = c->D;
-  SFFN_CUDA(p.run(dw, hidden, tokens));
   return SFFN_OK;
 }
 

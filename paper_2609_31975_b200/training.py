@@ -82,7 +82,8 @@ def gated_ffn_forward(x, W_g, b_g, W_up, W_down, act="relu", act_up=None, *, sav
 
     Returns (y, z, u): the pre-activations z, u [T, H] are what :func:`gated_ffn_backward` needs; ``save=False`` leaves them out
     (None).  Types: x, weights, y, z, u all fp32 or all bf16, b_g fp32 or None.  ``act`` / ``act_up``: relu, sqrelu, rsplus, silu,
-    none (``act_up=None``: none).  Rows of x, y, z, u may be strided (a multiple of 16 bytes)."""
+    none (``act_up=None``: none).  Rows of x, y, z, u may be strided (a multiple of 16 bytes).  y may be x; no other output may
+    share memory with an input or another output."""
     if stream is not None:
         with torch.cuda.stream(stream):
             return gated_ffn_forward(x, W_g, b_g, W_up, W_down, act, act_up, save=save, y=y, z=z, u=u)
@@ -98,7 +99,8 @@ GRADS = ("dx", "dW_g", "dW_up", "dW_down", "db_g")
 
 def gated_ffn_backward(dy, x, z, u, W_g, W_up, W_down, act="relu", act_up=None, *, need=GRADS, out=None, stream=None):
     """Gradients of :func:`gated_ffn_forward` from dy [T, D] and what the forward pass saved: a dict of those named in ``need``
-    (dx [T, D], dW_g, dW_up, dW_down [H, D] in the weights' type, db_g [H] fp32).  ``out``: a dict of tensors to write to."""
+    (dx [T, D], dW_g, dW_up, dW_down [H, D] in the weights' type, db_g [H] fp32).  ``out``: a dict of tensors to write to; dx may be
+    dy, x, z or u, no other one may share memory with an input or another output."""
     if stream is not None:
         with torch.cuda.stream(stream):
             return gated_ffn_backward(dy, x, z, u, W_g, W_up, W_down, act, act_up, need=need, out=out)
