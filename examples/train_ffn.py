@@ -39,7 +39,7 @@ def main(steps=200, bits=8, tokens=4096, width=1024, hidden=4096, bias=-0.5, lr=
             losses.append((error.square().mean() / want.float().square().mean()).item())
             if not quiet:
                 print(f"step {step:5d}: error {losses[-1]:.4f} of the teacher's energy, gradient norm {norm.item():.2e}")
-    assert ffn.training_status(device) == 0                  # synchronises: the weights may go to the decode path now
+    assert ffn.training_status(device) == 0
     # decode: one token at a time through the sparse path, which reads the rows of the neurons that fire
     served = ffn.SparseFFN(width, hidden, torch.bfloat16, device=device)
     x = normal(8, width).bfloat16()

@@ -35,7 +35,7 @@
  * g_sign, rms_gain) are treated as parameters: the kernels may start reading them while the work queued
  * just before the call is still running (that is how back-to-back calls overlap), so they must not be
  * written by device work queued immediately before a call on the same stream -- put a stream or event
- * synchronisation between an update of the weights and the next call.
+ * synchronisation between an update of the weights and the next call (sffn_adamw_step needs none).
  * A single-token call runs one CTA on every SM, and its CTAs wait for one another (LoPA: for the rank-r vector;
  * always: the first CTAs to finish stay and wait for the partial results of the rest, which they sum; every wait is bounded).
  * Calls of different handles are therefore meant to run one after another -- one stream, or streams ordered by
@@ -311,8 +311,8 @@ int sffn_lopa_residual(const float* W, const int32_t* g_idx, const int8_t* g_sig
  * The same FFN with its gradients, and the optimiser step of its weights.  These calls take no handle: what a call
  * needs is in its arguments, and the caller owns every buffer, the workspace too.  They are ordinary stream work:
  * nothing is read before the work queued earlier on `stream` has finished (weights included, so a forward pass may
- * follow the step that wrote them) -- but the inference calls above may start reading weights early, so put a stream
- * or event synchronisation between sffn_adamw_step and the next sparse_ffn_forward on the same weights.
+ * follow the step that wrote them), and nothing queued after sffn_adamw_step starts before the step has ended: an
+ * inference call above, which may start reading weights early, may follow it on the same stream as it is.
  * `status` (device int32, zeroed by the caller once) receives SFFN_ERR_TIMEOUT if a bounded wait inside a kernel runs
  * out; it is never cleared by the library.  Results are bitwise the same on every call with the same inputs
  * and the same outputs asked for.

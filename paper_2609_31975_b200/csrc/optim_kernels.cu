@@ -534,8 +534,7 @@ template <int N, int WHAT>
 __global__ void __launch_bounds__(kStepThreads, WHAT == kHalfCodes ? 5 : 6) adamw_kernel(const __grid_constant__ StepList<N> list) {
   const int lane = threadIdx.x & 31;
   const uint32_t warps = gridDim.x * (kStepThreads / 32);
-  pdl_launch_dependents();
-  pdl_wait();
+  pdl_wait();  // and no launch_dependents: what follows may be an inference call, which reads weights before its own wait
   float coef = 1.f;
   if (list.grad_norm) {
     const float norm = *list.grad_norm;

@@ -177,7 +177,8 @@ def adamw_step(params, grads, states, step, *, lr, betas=(0.9, 0.999), eps=1e-8,
 
     ``lr`` and ``weight_decay``: one number, or one for each tensor.  ``masters``: for bf16 parameters, fp32 copies that take the
     step (a list with None where there is none).  ``grad_norm``: the device scalar of :func:`grad_norm`; gradients are scaled by
-    min(1, max_norm / (grad_norm + 1e-6)), and a norm that is not finite leaves everything as it was."""
+    min(1, max_norm / (grad_norm + 1e-6)), and a norm that is not finite leaves everything as it was.  Calls that read the parameters,
+    :meth:`SparseFFN.sparse_ffn_forward` too, may follow on the same stream without a synchronisation."""
     if max_norm is not None and grad_norm is None:
         raise ValueError("max_norm needs grad_norm")
     if stream is not None:
