@@ -380,8 +380,10 @@ int sffn_grad_norm(const sffn_tensor* tensors, int n, float* norm, void* workspa
  *     g' = g min(1, max_norm / (grad_norm + 1e-6))                     (grad_norm given; else g' = g)
  *     m = beta1 m + (1 - beta1) g',   v = beta2 v + (1 - beta2) g'^2
  *     p = p (1 - lr weight_decay) - lr / (1 - beta1^step) m / (sqrt(v / (1 - beta2^step)) + eps)
- * in fp32.  grad_norm is a device word, as sffn_grad_norm leaves it; where it is not finite the whole step is left out
- * (parameters and moments keep their bits), without the host having to look.
+ * in fp32, so that a v below 2^-149 is zero; with eps = 0 an entry whose m and v are zero is 0 / 0.  Moments in 8 bits need
+ * an eps of 2^-50 (8.9e-16) at least, the root of what is stored as zero.  grad_norm is a device word, as sffn_grad_norm
+ * leaves it; where it is not finite the whole step is left out (parameters and moments keep their bits), without the host
+ * having to look.
  * p: fp32 or bf16; g: fp32 or bf16; master (bf16 p only, or NULL): fp32 copy of p that takes the step, p = bf16(master).
  * Moments with state_bits 32: m, v fp32.  With state_bits 8: m int8, v uint8 codes and one fp32 scale of each for every
  * 256 consecutive entries (the last group may be shorter; ceil(n / 256) scales),

@@ -337,8 +337,9 @@ __device__ __forceinline__ uint32_t two_bf16(f2 v) {
 }
 
 // Eight entries of a lane as four pairs.  Entry j of a lane: 8 lane + j where vectors are used (WIDE), 32 j + lane otherwise.
-// CODES: the moments are held in codes.  HALF: bf16 parameters without copies, which the kernel then need not look up.
-template <bool CODES, bool WIDE, bool HALF, typename List>
+// CODES: the moments are held in codes.  HALF: bf16 parameters without copies, which the kernel then need not look up.  FULL: roots and
+// quotients over all of fp32 (see fast_roots).
+template <bool CODES, bool WIDE, bool HALF, bool FULL, typename List>
 __device__ __forceinline__ void finish_group(const List& c, const StepEntry& t, uint32_t group, float coef, int lane, f2* w, f2* g, f2* m, f2* v) {
   const uint32_t kind = t.kind;
   const long long first = (long long)group * kGroup;
@@ -353,9 +354,10 @@ __device__ __forceinline__ void finish_group(const List& c, const StepEntry& t, 
     g[q] = mul2(g[q], both(coef));
     m[q] = add_apart(mul2(m[q], both(c.beta1)), mul2(g[q], both(c.one_beta1)));
     v[q] = add_apart(mul2(v[q], both(c.beta2)), mul2(mul2(g[q], g[q]), both(c.one_beta2)));
-    root[q] = pack2(sqrt_approx(low(v[q])), sqrt_approx(high(v[q])));
+    root[q] = FULL ? pack2(__fsqrt_rn(low(v[q])), __fsqrt_rn(high(v[q]))) : pack2(sqrt_approx(low(v[q])), sqrt_approx(high(v[q])));
     const f2 below = fma2_b64(root[q], both(c.root_bc2), both(c.eps));
-    const f2 part = mul2(m[q], pack2(rcp_approx(low(below)), rcp_approx(high(below))));
+    const f2 part = FULL ? pack2(__fdiv_rn(low(m[q]), low(below)), __fdiv_rn(high(m[q]), high(below)))
+                         : mul2(m[q], pack2(rcp_approx(low(below)), rcp_approx(high(below))));
     w[q] = fma2_b64(part, both(-t.rate), mul2(w[q], both(t.decay)));
     if (CODES) {  // entries past the end are zeros, of weight zero
       most_m = max_nan(most_m, max_nan(fabsf(low(m[q])), fabsf(high(m[q]))));
@@ -437,7 +439,7 @@ __device__ __forceinline__ void finish_group(const List& c, const StepEntry& t, 
   }
 }
 
-template <bool CODES, bool WIDE, typename List>
+template <bool CODES, bool WIDE, bool FULL, typename List>
 __device__ __forceinline__ void step_group(const List& c, const StepEntry& t, uint32_t group, float coef, int lane) {
   const uint32_t kind = t.kind;
   const long long first = (long long)group * kGroup;
@@ -496,7 +498,7 @@ __device__ __forceinline__ void step_group(const List& c, const StepEntry& t, ui
       w[q] = pack2(e[0][0], e[0][1]); g[q] = pack2(e[1][0], e[1][1]); m[q] = pack2(e[2][0], e[2][1]); v[q] = pack2(e[3][0], e[3][1]);
     }
   }
-  finish_group<CODES, WIDE, false>(c, t, group, coef, lane, w, g, m, v);
+  finish_group<CODES, WIDE, false, FULL>(c, t, group, coef, lane, w, g, m, v);
 }
 
 // bf16 parameters and gradients, moments in codes: a group's 24 bytes a lane.
@@ -513,7 +515,7 @@ struct HalfGroup {
     sm = t.m_scale[group];
     sv = t.v_scale[group];
   }
-  template <typename List>
+  template <bool FULL, typename List>
   __device__ __forceinline__ void step(const List& c, const StepEntry& t, uint32_t group, float coef, int lane) const {
     f2 pw[4], pg[4], pm[4], pv[4];
     pairs_of(reinterpret_cast<const uint32_t*>(&w), true, pw);
@@ -521,7 +523,7 @@ struct HalfGroup {
     const f2 um = both(unit_m(sm)), uv = both(unit_v(sv));
     codes_m(m.x, um, pm); codes_m(m.y, um, pm + 2);
     codes_v(v.x, uv, pv); codes_v(v.y, uv, pv + 2);
-    finish_group<true, true, true>(c, t, group, coef, lane, pw, pg, pm, pv);
+    finish_group<true, true, true, FULL>(c, t, group, coef, lane, pw, pg, pm, pv);
   }
 };
 
@@ -530,7 +532,7 @@ enum { kWords = 0, kAnyCodes = 1, kHalfCodes = 2 };
 
 // A warp's piece is `run` groups in a row.  The step of a group in codes is some 450 instructions a warp and its loads take as long:
 // kHalfCodes has the next group's under way meanwhile (705 M entries: 2.14 -> 1.70 ms).
-template <int N, int WHAT>
+template <int N, int WHAT, bool FULL>
 __global__ void __launch_bounds__(kStepThreads, WHAT == kHalfCodes ? 5 : 6) adamw_kernel(const __grid_constant__ StepList<N> list) {
   const int lane = threadIdx.x & 31;
   const uint32_t warps = gridDim.x * (kStepThreads / 32);
@@ -554,15 +556,15 @@ __global__ void __launch_bounds__(kStepThreads, WHAT == kHalfCodes ? 5 : 6) adam
 #pragma unroll 1
       for (; group < wide_end; ++group) {
         if (group + 1 < wide_end) next.load(t, group + 1, lane);
-        now.step(list, t, group, coef, lane);
+        now.template step<FULL>(list, t, group, coef, lane);
         now = next;
       }
     } else {
 #pragma unroll 1
-      for (; group < wide_end; ++group) step_group<WHAT != kWords, true>(list, t, group, coef, lane);
+      for (; group < wide_end; ++group) step_group<WHAT != kWords, true, FULL>(list, t, group, coef, lane);
     }
 #pragma unroll 1
-    for (; group < end; ++group) step_group<WHAT != kWords, false>(list, t, group, coef, lane);
+    for (; group < end; ++group) step_group<WHAT != kWords, false, FULL>(list, t, group, coef, lane);
   }
 }
 
@@ -607,7 +609,11 @@ inline uint32_t run_of(const sffn_adamw_tensor* t, int n, int sm_count, uint32_t
   return groups > 256ll * most * sm_count ? most : 1;
 }
 
-template <int N>
+// The fast root takes a v below 2^-126 for zero, which is up to 2^-63 / sqrt(1 - beta2^step) less to divide by: nothing, in fp32, beside an
+// eps 2^25 times that, as all but the smallest are.
+inline bool fast_roots(const sffn_adamw_config& c) { return c.eps * sqrt(1.0 - pow(c.beta2, (double)c.step)) >= 0x1p-38; }
+
+template <int N, bool FULL>
 cudaError_t adamw_launches(const sffn_adamw_tensor* t, int n, const sffn_adamw_config& c, int sm_count, cudaStream_t s) {
   StepList<N> list;
   list.grad_norm = c.grad_norm;
@@ -631,13 +637,13 @@ cudaError_t adamw_launches(const sffn_adamw_tensor* t, int n, const sffn_adamw_c
     e.rate = (float)(a.lr / bc1);
   };
   list.run = 1;
-  cudaError_t err = list_launches<N>(list, adamw_kernel<N, kWords>, n, t, sm_count, s, [](const sffn_adamw_tensor& a) { return what_of(a) == kWords; }, fill);
+  cudaError_t err = list_launches<N>(list, adamw_kernel<N, kWords, FULL>, n, t, sm_count, s, [](const sffn_adamw_tensor& a) { return what_of(a) == kWords; }, fill);
   if (err != cudaSuccess) return err;
   list.run = run_of(t, n, sm_count, 16);
-  err = list_launches<N>(list, adamw_kernel<N, kHalfCodes>, n, t, sm_count, s, [](const sffn_adamw_tensor& a) { return what_of(a) == kHalfCodes; }, fill);
+  err = list_launches<N>(list, adamw_kernel<N, kHalfCodes, FULL>, n, t, sm_count, s, [](const sffn_adamw_tensor& a) { return what_of(a) == kHalfCodes; }, fill);
   if (err != cudaSuccess) return err;
   list.run = 1;
-  return list_launches<N>(list, adamw_kernel<N, kAnyCodes>, n, t, sm_count, s, [](const sffn_adamw_tensor& a) { return what_of(a) == kAnyCodes; }, fill);
+  return list_launches<N>(list, adamw_kernel<N, kAnyCodes, FULL>, n, t, sm_count, s, [](const sffn_adamw_tensor& a) { return what_of(a) == kAnyCodes; }, fill);
 }
 
 // ---- values of 8-bit moments -----------------------------------------------------------------------------------------
@@ -734,7 +740,8 @@ cudaError_t launch_grad_norm(const sffn_tensor* t, int n, float* norm, void* wor
 }
 
 cudaError_t launch_adamw(const sffn_adamw_tensor* t, int n, const sffn_adamw_config& c, int sm_count, cudaStream_t s) {
-  return n <= kShort ? adamw_launches<kShort>(t, n, c, sm_count, s) : adamw_launches<kLongStep>(t, n, c, sm_count, s);
+  if (fast_roots(c)) return n <= kShort ? adamw_launches<kShort, false>(t, n, c, sm_count, s) : adamw_launches<kLongStep, false>(t, n, c, sm_count, s);
+  return adamw_launches<kLongStep, true>(t, n, c, sm_count, s);
 }
 
 cudaError_t launch_adamw_values(const sffn_adamw_tensor* t, int n, float* const* m_out, float* const* v_out, int sm_count, cudaStream_t s) {

@@ -395,6 +395,9 @@ int sffn_adamw_step(const sffn_adamw_tensor* t, int n, const sffn_adamw_config* 
   if (!c || c->step < 1 || !(c->beta1 >= 0 && c->beta1 < 1) || !(c->beta2 >= 0 && c->beta2 < 1) || !(c->eps >= 0) || std::isinf(c->eps)) return SFFN_ERR_INVALID_ARG;
   if (c->grad_norm && !(c->max_norm > 0)) return SFFN_ERR_INVALID_ARG;
   if (!aligned(c->grad_norm, 4)) return SFFN_ERR_UNSUPPORTED;
+  // 2^-50 is the root of the largest v that codes hold as zero: with a smaller eps there would be next to nothing to divide by
+  for (int i = 0; i < n; ++i)
+    if (t[i].state_bits == 8 && c->eps < 0x1p-50) return SFFN_ERR_UNSUPPORTED;
   int sms = 0;
   rc = sm_count(&sms);
   if (rc != SFFN_OK) return rc;

@@ -175,7 +175,7 @@ def adamw_step(params, grads, states, step, *, lr, betas=(0.9, 0.999), eps=1e-8,
     """One AdamW step over a list of tensors, in place (sffn_adamw_step): params fp32 or bf16, grads fp32 or bf16, states as
     :func:`adamw_state` makes them (updated), ``step`` = 1, 2, ...
 
-    ``lr`` and ``weight_decay``: one number, or one for each tensor.  ``masters``: for bf16 parameters, fp32 copies that take the
+    ``eps`` may be 0, with 8-bit moments 8.9e-16 at least.  ``lr`` and ``weight_decay``: one number, or one for each tensor.  ``masters``: for bf16 parameters, fp32 copies that take the
     step (a list with None where there is none).  ``grad_norm``: the device scalar of :func:`grad_norm`; gradients are scaled by
     min(1, max_norm / (grad_norm + 1e-6)), and a norm that is not finite leaves everything as it was.  Calls that read the parameters,
     :meth:`SparseFFN.sparse_ffn_forward` too, may follow on the same stream without a synchronisation."""
