@@ -1,4 +1,5 @@
 // Host side of the training calls of the C ABI: argument checks, workspace layout, and the order of the kernels.
+#include <algorithm>
 #include <cmath>
 
 #include "optim_kernels.cuh"
@@ -70,8 +71,12 @@ TrainLayout train_layout(int T, int D, int H, int dtype, bool backward) {
   L.limb_h = T * L.ld_h;
   L.limb_t = T * L.ld_d;
   L.limb_w = H * L.ld_d;
-  if (L.umma) {
-    L.partial = take(sffn::kTrainPartialBytes);
+  if (L.umma) {  // what the largest of the call's products may leave in pieces
+    const long long of_d = (D + 63) / 64, of_h = (H + 63) / 64, of_t = (T + 63) / 64;
+    const size_t room[3] = {sffn::train_umma_partial_bytes(backward ? sffn::kEpiHidden : sffn::kEpiGateUp, L.split, T, H, of_d, 1),
+                            sffn::train_umma_partial_bytes(sffn::kEpiStore, L.split, T, D, (backward ? 2 : 1) * of_h, 1),
+                            backward ? sffn::train_umma_partial_bytes(sffn::kEpiStore, L.split, H, D, of_t, 3) : 0};
+    L.partial = take(std::max({room[0], room[1], room[2]}));
   }
   const size_t hidden = (size_t)T * L.ld_h * (L.split ? 6 : element(dtype));
   L.h = take(hidden);

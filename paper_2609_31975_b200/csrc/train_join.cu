@@ -158,7 +158,7 @@ __global__ void __launch_bounds__(join_threads(EPI)) train_join_kernel(const __g
 
 template <int EPI, typename T, int kEach>
 cudaError_t launch(const UmmaParams& p, cudaStream_t s) {
-  const int across = (p.tile_cols + kJoinCols - 1) / kJoinCols, cols = (int)(p.piece / kPairRows), rows = join_threads(EPI) / (kJoinCols / 4) * kEach;
+  const int across = (p.tile_cols + kJoinCols - 1) / kJoinCols, cols = piece_cols(EPI, sizeof(T) == 4), rows = join_threads(EPI) / (kJoinCols / 4) * kEach;
   const int tall = p.m_tiles > 1 || p.epi.M > kPairRows ? kPairRows : p.epi.M, groups = (tall + rows - 1) / rows;
   return launch_pdl(train_join_kernel<EPI, T, kEach>, dim3((unsigned)((p.tiles - p.whole) * across * groups)), dim3(join_threads(EPI)), 0, s, p, cols, groups);
 }

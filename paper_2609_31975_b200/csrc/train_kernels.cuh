@@ -91,13 +91,13 @@ struct TrainUmma {
   TrainGemm g;
   bool f32;                // storage type of the outputs, and three terms an operand
   int64_t limb_a[3], limb_b[3];
-  float* partial;          // room for the pieces of tiles that several pairs of CTAs share (kTrainPartialBytes)
+  float* partial;          // room for the pieces of tiles that several pairs of CTAs share (train_umma_partial_bytes)
   int32_t* status;
 };
 constexpr int kTrainUmmaPairs = 80;    // pairs of CTAs at most
-constexpr size_t kTrainPieceBytes = 256 * 512 * 4;
 constexpr int kTrainPieces = 2 * kTrainUmmaPairs;  // of tiles that are cut, at most
-constexpr size_t kTrainPartialBytes = kTrainPieces * kTrainPieceBytes;
+// The most that the pieces of a product M x N may take, on any device: `blocks` of K, in 64s, of all parts.
+size_t train_umma_partial_bytes(int epilogue, bool f32, int M, int N, long long blocks, int batch);
 int train_umma_lines(int M);
 cudaError_t launch_train_umma(const TrainUmma& t, cudaStream_t s);
 // out[l][r][c], l = 0, 1, 2: the bf16 terms of in[r][c]; `ld_out` elements between rows, `limb` between terms.

@@ -534,7 +534,7 @@ cudaError_t launch_one(const TrainUmma& t, int pairs, cudaStream_t s) {
   const TrainGemm& g = t.g;
   UmmaParams p{};
   pairs = plan_umma(t, F::kTileCols, p, pairs);
-  p.piece = (size_t)kPairRows * 256 * F::kWide;
+  static_assert(piece_cols(EPI, false) == 256 * F::kWide);
   // Few tokens: a CTA copies those rows of A in steps of 32 (what the epilogue's warps look at), and the ring holds more K blocks.  The
   // MMAs read 128 rows all the same: what lies behind, the same stage's rows of B, goes into rows of the accumulator that nobody reads.
   // bf16, without / with it: 1 and 5 tokens, 4096 x 14336, forward 107 / 92, 96 / 89 us, dh 58 / 43, 53 / 44; 16 tokens, 2048 x 8192,
@@ -604,6 +604,7 @@ int plan_umma(const TrainUmma& t, int cols, UmmaParams& p, int pairs) {
   p.a_mn = !g.a_major_k;
   p.b_mn = !g.b_major_k;
   p.partial = t.partial;
+  p.piece = (size_t)piece_rows(g.M) * piece_cols(g.epilogue, t.f32);
   p.status = t.status;
   p.budget = fused_test_knobs().wait_cycles;
   p.drop = fused_test_knobs().drop_stage;
@@ -631,6 +632,14 @@ int plan_umma(const TrainUmma& t, int cols, UmmaParams& p, int pairs) {
   const int pieces = (p.tiles - p.whole) * p.split, most = p.whole > pieces ? p.whole : pieces;
   if (most < pairs) pairs = most;
   return pairs;
+}
+
+// (A product has fewer tiles to cut than it has tiles, and a tile a piece for every block at most.)
+size_t train_umma_partial_bytes(int epilogue, bool f32, int M, int N, long long blocks, int batch) {
+  const int cols = epilogue == kEpiGateUp ? 128 : piece_cols(epilogue, f32);
+  const long long tiles = (long long)((M + kPairRows - 1) / kPairRows) * ((N + cols - 1) / cols) * batch;
+  const long long pieces = blocks < 2 ? 0 : tiles < kTrainPieces && tiles * blocks < kTrainPieces ? tiles * blocks : kTrainPieces;
+  return (size_t)pieces * piece_rows(M) * piece_cols(epilogue, f32) * 4;
 }
 
 int train_umma_lines(int M) { return (M + 31) / 32; }

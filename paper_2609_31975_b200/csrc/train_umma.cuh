@@ -79,7 +79,10 @@ __device__ __forceinline__ Place place_of(const UmmaParams& p, int tile) {
   return at;
 }
 
-// A piece, [256][columns of the accumulators] fp32: part `part` of the t-th tile that is cut is number t + part * (tiles that are cut).
+// Rows and columns of a tile's accumulators that a piece holds: the rows that there are, in 32s (what the epilogue's warps look at).
+__host__ __device__ constexpr int piece_rows(int M) { return M < kPairRows ? (M + 31) / 32 * 32 : kPairRows; }
+__host__ __device__ constexpr int piece_cols(int epilogue, bool f32) { return epilogue == kEpiStore && !f32 ? 512 : 256; }
+// A piece, [rows][columns of the accumulators] fp32: part `part` of the t-th tile that is cut is number t + part * (tiles that are cut).
 __device__ __forceinline__ float* piece_of(const UmmaParams& p, int number) { return p.partial + (size_t)number * p.piece; }
 // Sixteen columns of a row of a piece.
 __device__ __forceinline__ void put_piece(float* at, const float* v) {

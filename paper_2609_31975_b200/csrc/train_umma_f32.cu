@@ -435,7 +435,7 @@ cudaError_t launch_train_split(const float* in, int64_t ld_in, int rows, int col
 cudaError_t launch_train_umma_f32(const TrainUmma& t, int pairs, cudaStream_t s) {
   UmmaParams p{};
   pairs = plan_umma(t, t.g.epilogue == kEpiGateUp ? kCols / 2 : kCols, p, pairs);
-  p.piece = (size_t)kPairRows * kCols;
+  static_assert(piece_cols(kEpiStore, true) == kCols && piece_cols(kEpiGateUp, true) == kCols && piece_cols(kEpiHidden, true) == kCols);
   Maps maps;
   if (pairs <= 0 || !make_operand_maps(t, 128, maps.a, maps.b)) return cudaErrorInvalidValue;
   if (t.g.epilogue == kEpiStore) return launch_one<kEpiStore>(p, maps, pairs, s);
