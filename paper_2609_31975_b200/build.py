@@ -9,9 +9,11 @@ with the environment variable SFFN_LIBRARY."""
 from __future__ import annotations
 
 import os
+import shutil
 import subprocess
 import sys
 import sysconfig
+import warnings
 from concurrent.futures import ThreadPoolExecutor
 from pathlib import Path
 
@@ -30,19 +32,27 @@ def _headers_mtime() -> float:
     return max(d.stat().st_mtime for d in deps)
 
 
-def build_calls(force: bool = False) -> Path:
-    """Compiles the module that checks and marshals the training calls' tensors, against the torch that is installed."""
-    src = CSRC / "torch_calls.cpp"
-    newest = max(src.stat().st_mtime, (ROOT / "include" / "sparse_ffn.h").stat().st_mtime)
-    if not force and CALLS.exists() and CALLS.stat().st_mtime >= newest:
-        return CALLS
+def build_calls(force: bool = False) -> Path | None:
+    """Compiles the module that checks and marshals the training calls' tensors, against the torch that is installed; again when that
+    changes.  Where a compiler or headers for it are missing, which the C library does without, says so and leaves it out: the
+    training calls from Python then raise."""
     import torch
 
-    at = Path(torch.__file__).resolve().parent
-    includes = [at / "include", at / "include" / "torch" / "csrc" / "api" / "include", Path(sysconfig.get_paths()["include"]),
-                Path(os.environ.get("CUDA_HOME", "/usr/local/cuda")) / "include"]
+    src = CSRC / "torch_calls.cpp"
+    at, python, cxx = Path(torch.__file__).resolve().parent, Path(sysconfig.get_paths()["include"]), os.environ.get("CXX", "g++")
+    made_for = f"torch {torch.__version__}, Python {sysconfig.get_python_version()}"
+    stamp = OBJ / "_training.made_for"
+    newest = max(src.stat().st_mtime, (ROOT / "include" / "sparse_ffn.h").stat().st_mtime)
+    if not force and CALLS.exists() and CALLS.stat().st_mtime >= newest and stamp.exists() and stamp.read_text() == made_for:
+        return CALLS
+    missing = [str(f) for f in (python / "Python.h", at / "include" / "ATen" / "ATen.h") if not f.exists()] + ([] if shutil.which(cxx) else [cxx])
+    if missing:
+        CALLS.unlink(missing_ok=True)  # one made from other sources, or for another torch
+        warnings.warn(f"{CALLS.name} is left out, and with it the training calls from Python: no {', '.join(missing)}")
+        return None
+    includes = [at / "include", at / "include" / "torch" / "csrc" / "api" / "include", python, Path(os.environ.get("CUDA_HOME", "/usr/local/cuda")) / "include"]
     tmp = CALLS.with_suffix(f".{os.getpid()}.tmp")
-    cmd = [os.environ.get("CXX", "g++"), "-O2", "-std=c++17", "-fPIC", "-shared", "-fvisibility=hidden",
+    cmd = [cxx, "-O2", "-std=c++17", "-fPIC", "-shared", "-fvisibility=hidden", f'-DSFFN_TORCH="{torch.__version__}"',
            f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}", "-I", str(ROOT / "include")]
     for p in includes:
         cmd += ["-isystem", str(p)]
@@ -51,11 +61,18 @@ def build_calls(force: bool = False) -> Path:
     if r.returncode != 0:
         raise RuntimeError(f"{src.name}:\n{r.stdout}\n{r.stderr}")
     os.replace(tmp, CALLS)
+    OBJ.mkdir(parents=True, exist_ok=True)
+    stamp.write_text(made_for)
     return CALLS
 
 
 def build(force: bool = False, verbose: bool = False, trace: bool = False, debug: bool = False) -> Path:
+    lib = build_library(force, verbose, trace, debug)
     build_calls(force)
+    return lib
+
+
+def build_library(force: bool = False, verbose: bool = False, trace: bool = False, debug: bool = False) -> Path:
     lib = PKG / "libsparse_ffn_trace.so" if trace else PKG / "libsparse_ffn_debug.so" if debug else LIB
     newest = max(_headers_mtime(), max((CSRC / s).stat().st_mtime for s in SOURCES))
     if not force and lib.exists() and lib.stat().st_mtime >= newest:

@@ -337,6 +337,7 @@ int adamw_state_values(const py::object& states, const py::object& out) {
 }  // namespace
 
 PYBIND11_MODULE(_training, m) {
+  m.attr("torch_version") = SFFN_TORCH;  // what it was compiled against
   m.def("bind", &bind);
   m.def("kept", &kept);
   m.def("ffn_forward", &ffn_forward);

@@ -30,6 +30,8 @@ def _calls():
             from . import _training
         except ImportError as e:
             raise RuntimeError("_training.so is missing or does not load: build it with `python -m paper_2609_31975_b200.build`") from e
+        if _training.torch_version != torch.__version__:
+            raise RuntimeError(f"_training.so was built for torch {_training.torch_version}: build it with `python -m paper_2609_31975_b200.build`")
         _training.bind([ctypes.cast(getattr(lib, name), ctypes.c_void_p).value for name in _ENTRIES])
         _bound = _training
     return _bound
