@@ -101,11 +101,13 @@ GRADS = ("dx", "dW_g", "dW_up", "dW_down", "db_g")
 
 def gated_ffn_backward(dy, x, z, u, W_g, W_up, W_down, act="relu", act_up=None, *, need=GRADS, out=None, stream=None):
     """Gradients of :func:`gated_ffn_forward` from dy [T, D] and what the forward pass saved: a dict of those named in ``need``
-    (dx [T, D], dW_g, dW_up, dW_down [H, D] in the weights' type, db_g [H] fp32).  ``out``: a dict of tensors to write to; dx may be
-    dy, x, z or u, no other one may share memory with an input or another output."""
+    (dx [T, D], dW_g, dW_up, dW_down [H, D] in the weights' type, db_g [H] fp32).  ``out``: a dict of tensors to write to (those
+    not in ``need`` are left alone); dx may be dy, x, z or u, no other one may share memory with an input or another output."""
     if stream is not None:
         with torch.cuda.stream(stream):
             return gated_ffn_backward(dy, x, z, u, W_g, W_up, W_down, act, act_up, need=need, out=out)
+    if out and set(out) - set(GRADS):
+        raise ValueError(f"no such gradient: {sorted(set(out) - set(GRADS))}")
     bits = 31
     if need is not GRADS:
         bits = sum(1 << GRADS.index(name) for name in set(need) if name in GRADS)

@@ -1,5 +1,5 @@
-"""The autograd node of the gated FFN by itself, without a device: its two calls are replaced by their formulas, so what is tested is
-which gradients it asks for, what it hands back, and what it refuses."""
+"""The backward pass and the autograd node of the gated FFN without a device: the two calls are replaced by their formulas, so what is tested
+is which gradients the node asks for, what it hands back, and what is refused."""
 import pytest
 import torch
 
@@ -67,3 +67,10 @@ def test_gradients_that_are_expanded(node):
     apply(*t, "silu", None).sum().backward()          # dy is one number, expanded
     want = torch.autograd.grad(plain(*t).sum(), t)
     assert all(torch.allclose(x.grad, w, atol=1e-12) for x, w in zip(t, want))
+
+
+def test_outputs_by_a_wrong_name_are_refused():
+    """A misspelt output would be made anew, and the caller's tensor stay as it was."""
+    w = torch.zeros(8, 8)
+    with pytest.raises(ValueError, match="dWg"):
+        training.gated_ffn_backward(w, w, w, w, w, w, w, out=dict(dWg=w))
