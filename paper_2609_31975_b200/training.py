@@ -140,7 +140,10 @@ class GatedFFNFunction(torch.autograd.Function):
         rows, z, u, W_g, W_up, W_down = ctx.saved_tensors
         names = ("dx", "dW_g", "db_g", "dW_up", "dW_down")
         need = [n for n, wanted in zip(names, ctx.needs_input_grad) if wanted]
-        got = gated_ffn_backward(dy.reshape(rows.shape).contiguous(), rows, z, u, W_g, W_up, W_down, *ctx.acts, need=need)
+        dy = dy.reshape(rows.shape).contiguous()
+        if dy.data_ptr() % 16:  # a slice of something longer
+            dy = dy.clone()
+        got = gated_ffn_backward(dy, rows, z, u, W_g, W_up, W_down, *ctx.acts, need=need)
         if "dx" in got:
             got["dx"] = got["dx"].view(ctx.shape)
         return (*[got.get(n) for n in names], None, None)

@@ -17,7 +17,7 @@ def node(monkeypatch):
 
     def backward(dy, x, z, u, W_g, W_up, W_down, act="relu", act_up=None, *, need):
         asked.append(sorted(need))
-        assert dy.is_contiguous() and dy.shape == x.shape
+        assert dy.is_contiguous() and dy.shape == x.shape and dy.data_ptr() % 16 == 0   # as the kernels take it
         return {k: v for k, v in ref.backward(dy, x, z, u, W_g, W_up, W_down, act, act_up).items() if k in need}
 
     monkeypatch.setattr(training, "gated_ffn_forward", forward)
@@ -66,6 +66,17 @@ def test_gradients_that_are_expanded(node):
     t = leaves()
     apply(*t, "silu", None).sum().backward()          # dy is one number, expanded
     want = torch.autograd.grad(plain(*t).sum(), t)
+    assert all(torch.allclose(x.grad, w, atol=1e-12) for x, w in zip(t, want))
+
+
+def test_gradients_that_are_slices(node):
+    """dy comes from torch, as whatever it is: here the tail of a longer vector, which does not start on 16 bytes."""
+    apply, _ = node
+    t = leaves()
+    weights = torch.linspace(-1, 1, 1 + 2 * 3 * 8, dtype=torch.float64)
+    head = torch.zeros(1, dtype=torch.float64)
+    (torch.cat([head, apply(*t, "silu", None).flatten()]) * weights).sum().backward()
+    want = torch.autograd.grad((torch.cat([head, plain(*t).flatten()]) * weights).sum(), t)
     assert all(torch.allclose(x.grad, w, atol=1e-12) for x, w in zip(t, want))
 
 
