@@ -6,9 +6,9 @@
 //   adamw_values_kernel  8-bit moments as the fp32 values they stand for
 //
 // Bound by the bytes they move, the step with 8-bit moments also by its instructions (about 55 an entry, half of them on the ALU).
-// B200, copies at 6.45 TB/s: norm of 704 M bf16 entries 200 us (7.0 TB/s); step of 164 M entries with fp32 moments and copies 745 us
-// (6.2 TB/s), of 64 tensors of 12.6 M entries in all 50 us (7 TB/s); 235 M bf16 entries in 8 bits 489 us (4.8 TB/s), their values
-// 405 us (5.8 TB/s).
+// B200, copies at 6.45 TB/s, calls in a loop: norm of 704 M bf16 entries 202 us (7.0 TB/s); step of 164 M entries with fp32 moments and
+// copies 758 us (6.1 TB/s), of 64 tensors of 12.6 M entries in all 60 us (5.9 TB/s; 59 where the next launch may start under its tail); 235 M
+// bf16 entries in 8 bits 489 us (4.8 TB/s), their values 405 us (5.8 TB/s).
 #include "optim_kernels.cuh"
 
 #include <math.h>

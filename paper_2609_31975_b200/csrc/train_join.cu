@@ -31,8 +31,8 @@ __device__ __forceinline__ void load4(const __nv_bfloat16* p, float* v, int n) {
     for (int i = 0; i < 4; ++i) v[i] = i < n ? __bfloat162float(p[i]) : 0.f;
   }
 }
-// Steps known to the compiler, here and below: as loops to n, inlined three times, nvcc 12.9 left the first bf16 term of du's last
-// columns unstored where four does not divide H.
+// Steps known to the compiler, here and below: of loops to n, inlined three times, nvcc 12.9 drops one, and the first bf16 term of du's
+// last columns stayed unstored where four does not divide H (the three calls alone, in a kernel of 20 lines, do the same).
 __device__ __forceinline__ void store4(float* p, const float* v, int n) {
   if (n == 4) {
     *reinterpret_cast<float4*>(p) = make_float4(v[0], v[1], v[2], v[3]);

@@ -5,7 +5,7 @@
 // [k][m] and [k][n] arrays, whichever way an operand lies in memory, the next piece under way while one is multiplied.  Such a call has
 // few tiles and is bound by latency, so K is cut among up to eight CTAs of a cluster: each leaves its sums in shared memory and takes
 // a share of the tile's rows, which it adds up over all of them, in order.
-// 64 tokens, 256 x 1024, in a loop: forward 17 us, backward 31, of which launches 4 and 6 (20 and 33 with 4 x 4 a thread, 59 and 114 without
+// 64 tokens, 256 x 1024, in a loop: forward 17 us, backward 29, of which launches 4 and 6 (20 and 33 with 4 x 4 a thread, 59 and 114 without
 // clusters); 32 tokens, 4096 x 14336, forward 476 us (577), three times the FMAs' time: loads of a piece wait for their stores.  1 token:
 // 264 us for 705 MB.
 #include "train_kernels.cuh"

@@ -1,7 +1,7 @@
 // Products of the training calls in bf16 on the 5th-generation tensor cores (tcgen05.mma, accumulators in tensor memory).
 //
 // A pair of CTAs (cta_group::2) owns 256 rows of C = A B^T: each holds 128 rows of A and half of B's rows of a 64-deep K block
-// in each of four stages.  Both operands may lie K-major or MN-major in memory (the tensor core takes either from the
+// in each of four stages (z and u, and dh, of up to 64 tokens: the rows of A that there are, in up to six).  Both operands may lie K-major or MN-major in memory (the tensor core takes either from the
 // 128-byte-swizzled boxes that the tensor-map copies leave), so none of the six products of a training step needs a transposed copy.
 //
 //   kStore   512 columns: two accumulators of 256 fill tensor memory, and share A.  The copies into shared memory run at 10 TB/s at
