@@ -531,7 +531,8 @@ struct HalfGroup {
 enum { kWords = 0, kAnyCodes = 1, kHalfCodes = 2 };
 
 // A warp's piece is `run` groups in a row.  The step of a group in codes is some 450 instructions a warp and its loads take as long:
-// kHalfCodes has the next group's under way meanwhile (705 M entries: 2.14 -> 1.70 ms).
+// kHalfCodes has the next group's under way meanwhile (705 M entries: 2.14 -> 1.70 ms).  176 M entries: kHalfCodes 367 us (4.8 TB/s), kAnyCodes with
+// copies 554 (5.1), of fp32 583 (4.9), of bf16 with fp32 gradients 541 (3.9).
 template <int N, int WHAT, bool FULL>
 __global__ void __launch_bounds__(kStepThreads, WHAT == kHalfCodes ? 5 : 6) adamw_kernel(const __grid_constant__ StepList<N> list) {
   const int lane = threadIdx.x & 31;
