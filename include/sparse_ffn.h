@@ -413,6 +413,64 @@ int sffn_adamw_step(const sffn_adamw_tensor* tensors, int n, const sffn_adamw_co
  * either array of pointers may be NULL). */
 int sffn_adamw_state_values(const sffn_adamw_tensor* tensors, int n, float* const* m_out, float* const* v_out, void* stream);
 
+/* ---- the block around the FFN -----------------------------------------------------------------------------------
+ * The norms before and after an FFN (or any block of a residual stream) with its gate, its residual scale and the sum:
+ *     h = resid + scale gate . N(y; post_gain),   n = N(h; pre_gain),   N(v; g) = v / sqrt(mean_k v_k^2 + eps) . g
+ * y [T, D]: the block's output; n: what the next block reads.  Without post_gain (NULL) y is taken as it is; without pre_gain there is
+ * no n; without resid h is the second term; without y (NULL) h is resid, nothing is written to h, and n is its norm.  One call serves
+ * training and decoding: a row is one token, its types are free (an FFN's fp32 y onto a bf16 stream, say), and T may be 1.
+ * Like the training calls it takes no handle and is ordinary stream work: nothing is read before the work queued earlier has finished.
+ * Sums and statistics are fp32; h and n are each rounded once (n is the norm of the unrounded h).
+ * Types: y, h (and resid, with it) and n are each fp32 or bf16; gains, a gate of channels or tokens, and their gradients fp32; a full
+ * gate has h's type.  D: up to SFFN_BLOCK_MAX_D, a multiple of 4, of 8 where anything is bf16.  Rows have strides in elements, a
+ * multiple of 16 bytes; pointers are 16-byte aligned, those of a gate of tokens and of stats 4-byte.  T = 0 is a call like any other.
+ * h may be resid (the same rows); other overlaps of an output with an input or output are SFFN_ERR_INVALID_ARG. */
+#define SFFN_BLOCK_MAX_D 32768
+typedef enum { SFFN_BLOCK_GATE_NONE = 0, SFFN_BLOCK_GATE_CHANNEL = 1 /* [D] */, SFFN_BLOCK_GATE_TOKEN = 2 /* [T] */,
+               SFFN_BLOCK_GATE_FULL = 3 /* [T, D] */ } sffn_block_gate;
+typedef struct {
+  int32_t T, D;
+  int32_t y_dtype, h_dtype, n_dtype;  /* sffn_dtype */
+  int32_t gate_kind;                  /* sffn_block_gate */
+  const void* y;                      /* [T, D] or NULL */
+  int64_t ld_y;
+  const void* resid;                  /* [T, D] or NULL; only the forward call reads it */
+  int64_t ld_resid;
+  const float *post_gain, *pre_gain;  /* [D] or NULL */
+  const void* gate;
+  int64_t ld_gate;                    /* of a full gate */
+  float scale, eps;                   /* eps >= 0 */
+  void* h;                            /* [T, D]: forward: written; backward: read (as the forward call left it; without y: resid) */
+  int64_t ld_h;
+  void* n;                            /* [T, D]: forward: written */
+  int64_t ld_n;
+  float* stats;                       /* [2, T]: 1 / sqrt(mean + eps) of y's rows, of h's; forward: written, or NULL; backward: read */
+} sffn_block_norm;
+int sffn_block_norm_forward(const sffn_block_norm* call, void* stream);
+
+/* Gradients, from dh and dn (either may be NULL: zero).  With t = pre_gain . dn, rho = stats[1], r = stats[0], w = scale post_gain . gate:
+ *     dresid = g = dh + rho t - h rho^3 / D sum_k(t h),   dy = r w . g - y r^3 / D sum_k(w y g)      (without post_gain: dy = w . g)
+ *     dpre_gain = sum_t dn . h rho,   dpost_gain = scale sum_t gate . g . y r,   dgate = scale g . post_gain . y r
+ * dgate being summed over what the gate was broadcast along.  Any output may be NULL (not wanted).  dresid may be dh (the same rows).
+ * Results are bitwise the same on every call with the same inputs. */
+typedef struct {
+  const void* dh;                     /* [T, D], h_dtype */
+  int64_t ld_dh;
+  const void* dn;                     /* [T, D], n_dtype */
+  int64_t ld_dn;
+  void* dy;                           /* [T, D], y_dtype */
+  int64_t ld_dy;
+  void* dresid;                       /* [T, D], h_dtype */
+  int64_t ld_dresid;
+  float *dpost_gain, *dpre_gain;      /* [D] */
+  void* dgate;                        /* as the gate */
+  int64_t ld_dgate;
+  void* workspace;                    /* 16-byte aligned; needed where a gradient of a gain or of a gate of channels is wanted */
+  size_t workspace_bytes;
+} sffn_block_grads;
+int sffn_block_norm_workspace_bytes(int D, size_t* bytes);
+int sffn_block_norm_backward(const sffn_block_norm* call, const sffn_block_grads* grads, void* stream);
+
 /* Static string for a status code. */
 const char* sffn_status_string(int status);
 

@@ -15,6 +15,7 @@ from .binding import (  # noqa: F401
     sparse_ffn_forward_static,
     test_set_knob,
 )
+from .block import BlockNormFunction, block_norm_backward, block_norm_forward  # noqa: F401
 from .lopa import g_diagonal, g_tiled, touched_bytes, dense_bytes, lopa_approximation  # noqa: F401
 from .training import (  # noqa: F401
     GatedFFNFunction,

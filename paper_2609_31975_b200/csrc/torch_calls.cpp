@@ -8,6 +8,7 @@
 #include <c10/cuda/CUDAGraphsC10Utils.h>
 #include <c10/cuda/CUDAGuard.h>
 #include <c10/cuda/CUDAStream.h>
+#include <torch/csrc/Dtype.h>
 #include <torch/csrc/autograd/python_variable.h>
 #include <torch/csrc/utils/pybind.h>
 
@@ -30,16 +31,22 @@ struct Entry {
   decltype(&sffn_grad_norm) grad_norm;
   decltype(&sffn_adamw_step) adamw_step;
   decltype(&sffn_adamw_state_values) adamw_state_values;
+  decltype(&sffn_block_norm_forward) block_forward;
+  decltype(&sffn_block_norm_workspace_bytes) block_workspace_bytes;
+  decltype(&sffn_block_norm_backward) block_backward;
 } entry;
 
 void bind(const std::vector<uintptr_t>& a) {
-  if (a.size() != 6) throw py::value_error("six addresses");
+  if (a.size() != 9) throw py::value_error("nine addresses");
   entry.workspace_bytes = reinterpret_cast<decltype(entry.workspace_bytes)>(a[0]);
   entry.forward = reinterpret_cast<decltype(entry.forward)>(a[1]);
   entry.backward = reinterpret_cast<decltype(entry.backward)>(a[2]);
   entry.grad_norm = reinterpret_cast<decltype(entry.grad_norm)>(a[3]);
   entry.adamw_step = reinterpret_cast<decltype(entry.adamw_step)>(a[4]);
   entry.adamw_state_values = reinterpret_cast<decltype(entry.adamw_state_values)>(a[5]);
+  entry.block_forward = reinterpret_cast<decltype(entry.block_forward)>(a[6]);
+  entry.block_workspace_bytes = reinterpret_cast<decltype(entry.block_workspace_bytes)>(a[7]);
+  entry.block_backward = reinterpret_cast<decltype(entry.block_backward)>(a[8]);
 }
 
 [[noreturn]] void type_error(const std::string& what) { throw py::type_error(what); }
@@ -334,6 +341,154 @@ int adamw_state_values(const py::object& states, const py::object& out) {
   return rc;
 }
 
+// What both passes of the norms around a block hand over, but for resid, h, n and their statistics.
+sffn_block_norm make_block(const OptTensor& y, const Tensor& like, const OptTensor& post_gain, const OptTensor& pre_gain, const OptTensor& gate, double scale,
+                           double eps) {
+  on_cuda(like);
+  if (like.dim() != 2) type_error("y, resid and h are [T, D]");
+  const at::Device dev = like.device();
+  const int64_t T = like.size(0), D = like.size(1);
+  if (T > INT32_MAX || D > INT32_MAX) type_error("sizes beyond 32 bits");
+  sffn_block_norm c{};
+  c.T = (int32_t)T; c.D = (int32_t)D;
+  c.scale = (float)scale; c.eps = (float)eps;
+  if (y) {
+    c.y_dtype = dtype_code(y->scalar_type(), "y");
+    c.ld_y = rows("y", *y, T, D, y->scalar_type(), dev);
+    c.y = y->data_ptr();
+  }
+  if (post_gain) c.post_gain = static_cast<const float*>(whole("post_gain", *post_gain, {D}, at::kFloat, dev));
+  if (pre_gain) c.pre_gain = static_cast<const float*>(whole("pre_gain", *pre_gain, {D}, at::kFloat, dev));
+  if (gate && gate->dim() == 1) {
+    c.gate_kind = SFFN_BLOCK_GATE_CHANNEL;
+    c.gate = whole("gate", *gate, {D}, at::kFloat, dev);
+  } else if (gate && gate->dim() == 2 && gate->size(1) == 1 && D != 1) {
+    c.gate_kind = SFFN_BLOCK_GATE_TOKEN;
+    c.gate = whole("gate", *gate, {T, 1}, at::kFloat, dev);
+  } else if (gate) {
+    c.gate_kind = SFFN_BLOCK_GATE_FULL;  // its type is h's: checked once that is known
+    c.ld_gate = rows("gate", *gate, T, D, gate->scalar_type(), dev);
+    c.gate = gate->data_ptr();
+  }
+  return c;
+}
+void check_full_gate(const sffn_block_norm& c, const OptTensor& gate, at::ScalarType h_dtype) {
+  if (c.gate_kind == SFFN_BLOCK_GATE_FULL) check_plain("gate", *gate, {c.T, c.D}, h_dtype, gate->device());
+}
+
+// (status, h, n, stats): h None without y, n None without pre_gain.
+py::tuple block_forward(const OptTensor& y, const OptTensor& resid, const OptTensor& post_gain, const OptTensor& pre_gain, const OptTensor& gate, double scale,
+                        double eps, bool save, const py::object& h_dtype, const py::object& n_dtype, const OptTensor& h_out, const OptTensor& n_out) {
+  if (!y && !resid) type_error("y or resid is needed");
+  const Tensor& like = resid ? *resid : *y;
+  sffn_block_norm c = make_block(y, like, post_gain, pre_gain, gate, scale, eps);
+  const at::Device dev = like.device();
+  const c10::cuda::CUDAGuard guard(dev);
+  auto asked = [](const py::object& o) { return reinterpret_cast<THPDtype*>(o.ptr())->scalar_type; };
+  for (const py::object* o : {&h_dtype, &n_dtype})
+    if (!o->is_none() && !THPDtype_Check(o->ptr())) type_error("h_dtype and n_dtype are torch types");
+  const at::ScalarType th = resid ? resid->scalar_type() : h_out ? h_out->scalar_type() : h_dtype.is_none() ? y->scalar_type() : asked(h_dtype);
+  if (!h_dtype.is_none() && asked(h_dtype) != th) type_error("h has resid's type, or that of the tensor given for it");
+  const at::ScalarType tn = n_out ? n_out->scalar_type() : n_dtype.is_none() ? th : asked(n_dtype);
+  if (!n_dtype.is_none() && asked(n_dtype) != tn) type_error("n has the type of the tensor given for it");
+  c.h_dtype = dtype_code(th, "the residual stream");
+  c.n_dtype = dtype_code(tn, "n");
+  if (!y) c.y_dtype = c.h_dtype;
+  check_full_gate(c, gate, th);
+  if (resid) {
+    c.ld_resid = rows("resid", *resid, c.T, c.D, th, dev);
+    c.resid = resid->data_ptr();
+  }
+  OptTensor h, n, stats;
+  if (y) {
+    h = h_out ? *h_out : make({c.T, c.D}, th, dev);
+    c.ld_h = rows("h", *h, c.T, c.D, th, dev);
+    c.h = h->data_ptr();
+  } else if (h_out) {
+    type_error("without y, h is resid: nothing is written to it");
+  }
+  if (pre_gain) {
+    n = n_out ? *n_out : make({c.T, c.D}, tn, dev);
+    c.ld_n = rows("n", *n, c.T, c.D, tn, dev);
+    c.n = n->data_ptr();
+  } else if (n_out) {
+    type_error("n needs pre_gain");
+  }
+  if (save) {
+    stats = make({2, c.T}, at::kFloat, dev);
+    c.stats = static_cast<float*>(stats->data_ptr());
+  }
+  const int rc = entry.block_forward(&c, current_stream(dev));
+  if (rc == SFFN_OK) {
+    if (y && h_out) written(*h);
+    if (n_out) written(*n);
+  }
+  return py::make_tuple(rc, h, n, stats);
+}
+
+// need: bits dy, dresid, dpost_gain, dpre_gain, dgate; out: those five, None where they are made here.
+py::tuple block_backward(const OptTensor& dh, const OptTensor& dn, const OptTensor& y, const Tensor& h, const OptTensor& stats, const OptTensor& post_gain,
+                         const OptTensor& pre_gain, const OptTensor& gate, double scale, int need, const std::vector<OptTensor>& out) {
+  sffn_block_norm c = make_block(y, h, post_gain, pre_gain, gate, scale, 0.0);
+  const at::Device dev = h.device();
+  const c10::cuda::CUDAGuard guard(dev);
+  const at::ScalarType th = h.scalar_type();
+  c.h_dtype = dtype_code(th, "the residual stream");
+  c.n_dtype = dn ? dtype_code(dn->scalar_type(), "dn") : c.h_dtype;
+  if (!y) c.y_dtype = c.h_dtype;
+  check_full_gate(c, gate, th);
+  c.ld_h = rows("h", h, c.T, c.D, th, dev);
+  c.h = h.data_ptr();
+  if (stats) c.stats = static_cast<float*>(whole("stats", *stats, {2, c.T}, at::kFloat, dev));
+  sffn_block_grads g{};
+  if (dh) {
+    g.ld_dh = rows("dh", *dh, c.T, c.D, th, dev);
+    g.dh = dh->data_ptr();
+  }
+  if (dn) {
+    g.ld_dn = rows("dn", *dn, c.T, c.D, dn->scalar_type(), dev);
+    g.dn = dn->data_ptr();
+  }
+  OptTensor got[5];
+  auto take = [&](int i, at::IntArrayRef shape, at::ScalarType t) -> const Tensor& {
+    got[i] = (size_t)i < out.size() && out[i] ? *out[i] : make(shape, t, dev);
+    return *got[i];
+  };
+  if (need & 1 && y) {
+    const Tensor& t = take(0, {c.T, c.D}, y->scalar_type());
+    g.ld_dy = rows("dy", t, c.T, c.D, y->scalar_type(), dev);
+    g.dy = t.data_ptr();
+  }
+  if (need & 2) {
+    const Tensor& t = take(1, {c.T, c.D}, th);
+    g.ld_dresid = rows("dresid", t, c.T, c.D, th, dev);
+    g.dresid = t.data_ptr();
+  }
+  if (need & 4 && post_gain) g.dpost_gain = static_cast<float*>(whole("dpost_gain", take(2, {c.D}, at::kFloat), {c.D}, at::kFloat, dev));
+  if (need & 8 && pre_gain) g.dpre_gain = static_cast<float*>(whole("dpre_gain", take(3, {c.D}, at::kFloat), {c.D}, at::kFloat, dev));
+  if (need & 16 && gate) {
+    const Tensor& t = take(4, gate->sizes(), gate->scalar_type());
+    if (c.gate_kind == SFFN_BLOCK_GATE_FULL) g.ld_dgate = rows("dgate", t, c.T, c.D, th, dev);
+    else whole("dgate", t, gate->sizes(), at::kFloat, dev);
+    g.dgate = t.data_ptr();
+  }
+  Tensor ws;
+  int rc = SFFN_OK;
+  if (g.dpost_gain || g.dpre_gain || (g.dgate && c.gate_kind == SFFN_BLOCK_GATE_CHANNEL)) {
+    size_t bytes = 0;
+    rc = entry.block_workspace_bytes(c.D, &bytes);
+    if (rc == SFFN_OK) {
+      ws = make({(int64_t)bytes}, at::kByte, dev);
+      g.workspace = ws.data_ptr();
+      g.workspace_bytes = bytes;
+    }
+  }
+  if (rc == SFFN_OK) rc = entry.block_backward(&c, &g, current_stream(dev));
+  for (size_t i = 0; rc == SFFN_OK && i < 5 && i < out.size(); ++i)
+    if (got[i] && out[i]) written(*got[i]);
+  return py::make_tuple(rc, got[0], got[1], got[2], got[3], got[4]);
+}
+
 }  // namespace
 
 PYBIND11_MODULE(_training, m) {
@@ -345,4 +500,6 @@ PYBIND11_MODULE(_training, m) {
   m.def("grad_norm", &grad_norm);
   m.def("adamw_step", &adamw_step);
   m.def("adamw_state_values", &adamw_state_values);
+  m.def("block_forward", &block_forward);
+  m.def("block_backward", &block_backward);
 }

@@ -2,42 +2,22 @@
 #include <algorithm>
 #include <cmath>
 
+#define SFFN_FILE "train_api.cu"
+#include "host_checks.cuh"
 #include "optim_kernels.cuh"
 #include "sparse_ffn.h"
 #include "train_kernels.cuh"
 
-namespace sffn {
-void note_cuda_error(cudaError_t e, const char* file, int line);  // api.cu
-}
+using namespace sffn::host;
 
 namespace {
-
-#define SFFN_CUDA(expr)                                   \
-  do {                                                    \
-    const cudaError_t e_ = (expr);                        \
-    if (e_ != cudaSuccess) {                              \
-      sffn::note_cuda_error(e_, "train_api.cu", __LINE__); \
-      return SFFN_ERR_CUDA;                               \
-    }                                                     \
-  } while (0)
 
 constexpr double kSplitProducts = 1.5e8;  // T D H
 constexpr int kFewForward = 32, kFewBackward = 16;  // tokens
 constexpr int kMaxRows = 1 << 22;  // tokens, and neurons: the kernels' grids and tensor maps have room for so many
 
-inline bool aligned(const void* p, uintptr_t a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) == 0; }
-inline size_t up256(size_t v) { return (v + 255) / 256 * 256; }
-inline size_t element(int dtype) { return dtype == SFFN_BF16 ? 2 : 4; }
 inline int64_t hidden_ld(int H) { return ((int64_t)H + 7) / 8 * 8; }
-inline bool storage_type(int dtype) { return dtype == SFFN_F32 || dtype == SFFN_BF16; }
 inline bool any_act(int act) { return act >= SFFN_ACT_RELU && act <= SFFN_ACT_SILU; }
-
-int sm_count(int* n) {
-  int dev = 0;
-  SFFN_CUDA(cudaGetDevice(&dev));
-  SFFN_CUDA(cudaDeviceGetAttribute(n, cudaDevAttrMultiProcessorCount, dev));
-  return SFFN_OK;
-}
 
 // Which kernels serve a call: tensor cores for bf16, and for fp32 from the size on at which splitting every operand into three
 // terms and multiplying them six times is faster than fp32 FMAs.  Forward / backward in us, FMAs against terms: T D H = 1.3e8 44 / 89
@@ -139,46 +119,6 @@ int check_shape(int T, int D, int H, int dtype) {
   if ((D * element(dtype)) % 16 || T > kMaxRows || H > kMaxRows || D > kMaxRows) return SFFN_ERR_UNSUPPORTED;
   return SFFN_OK;
 }
-
-int check_rows(const void* p, int64_t ld, int64_t width, size_t esz) {
-  if (ld < width) return SFFN_ERR_INVALID_ARG;
-  return aligned(p, 16) && (ld * esz) % 16 == 0 && ld <= (1ll << 31) ? SFFN_OK : SFFN_ERR_UNSUPPORTED;
-}
-
-// A matrix's rows in memory, and whether any of them meets any row of another matrix's (what lies between rows does not count: two
-// matrices may be columns of one).
-struct Span {
-  const void* p;
-  int64_t rows, width, ld;  // bytes
-};
-bool meet(const Span& a, const Span& b) {
-  if (!a.p || !b.p || a.rows <= 0 || b.rows <= 0 || a.width <= 0 || b.width <= 0) return false;
-  const int64_t d = (int64_t)(reinterpret_cast<uintptr_t>(b.p) - reinterpret_cast<uintptr_t>(a.p));  // b's first byte, from a's
-  if (d >= (a.rows - 1) * a.ld + a.width || -d >= (b.rows - 1) * b.ld + b.width) return false;
-  if (a.ld == b.ld) {  // rows i of a and j of b meet where d - a.width < (i - j) ld < d + b.width
-    const auto below = [](int64_t v, int64_t n) { return v >= 0 ? v / n : -((-v + n - 1) / n); };
-    const int64_t least = below(d - a.width, a.ld) + 1, most = -below(-(d + b.width), a.ld) - 1;
-    return (least > 1 - b.rows ? least : 1 - b.rows) <= (most < a.rows - 1 ? most : a.rows - 1);
-  }
-  for (int64_t i = 0, j = 0; i < a.rows && j < b.rows;) {
-    if (i * a.ld + a.width <= d + j * b.ld) ++i;
-    else if (d + j * b.ld + b.width <= i * a.ld) ++j;
-    else return true;
-  }
-  return false;
-}
-// Whether an output of a call meets one of these inputs, or another output.
-template <size_t kIn, size_t kOut>
-bool outputs_meet(const Span (&in)[kIn], const Span (&out)[kOut]) {
-  for (size_t o = 0; o < kOut; ++o) {
-    for (const Span& i : in)
-      if (meet(out[o], i)) return true;
-    for (size_t q = o + 1; q < kOut; ++q)
-      if (meet(out[o], out[q])) return true;
-  }
-  return false;
-}
-Span whole(const void* p, int64_t bytes) { return {p, 1, bytes, bytes}; }
 
 int check_call(const sffn_train_call* c, bool backward) {
   if (!c) return SFFN_ERR_INVALID_ARG;
