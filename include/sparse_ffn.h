@@ -413,6 +413,60 @@ int sffn_adamw_step(const sffn_adamw_tensor* tensors, int n, const sffn_adamw_co
  * either array of pointers may be NULL). */
 int sffn_adamw_state_values(const sffn_adamw_tensor* tensors, int n, float* const* m_out, float* const* v_out, void* stream);
 
+/* ---- Muon ---------------------------------------------------------------------------------------------------------
+ * An update made orthogonal by Newton-Schulz products, for n matrices U [rows, cols] at once:
+ *     X = U / (|U|_F + eps),   then for every step, with its coefficients a, b, c:   X = a X + (b P + c P^2) X,  P = X X^T
+ * (on the shorter side: P = X^T X where rows > cols, from the right), O = X.  Singular values of U above about a^-steps of its norm come
+ * out near 1 with the usual coefficients (3.4445, -4.7750, 2.0315), smaller ones are multiplied by a^steps.
+ * `bits` of the products: 16: one fp16 term an operand (O within about 1e-3 of its norm; singular values far below the largest are as exact
+ * as the others); 32: two (within 1e-5), three products for one; 0: by what is written, 32 where that has 32 bits, else 16.  Sums
+ * are fp32, the norm 64-bit.  A NaN or infinity in U makes all of its O NaN; zeros give zeros; no rows or columns: nothing is done.
+ * U and O: fp32 or bf16, rows at any stride >= cols, aligned as their type.  o may lie over its own u; other overlaps of an output with
+ * anything of the call are SFFN_ERR_INVALID_ARG, as are coefficients under which singular values grow beyond 2^30.
+ * Sides: up to 65536 and 2^22.  Matrices of one shape and type are multiplied together.  Results repeat bit for bit with the same list.
+ * Stream order, `status` and the workspace (256-byte aligned) are as for the training calls above. */
+#define SFFN_NS_MAX_STEPS 32
+typedef struct {
+  int32_t steps, bits;
+  const double* coefficients;  /* host, [steps][3] */
+  double eps;
+} sffn_newton_schulz;
+typedef struct {
+  const void* u;
+  int64_t ld_u;
+  void* o;
+  int64_t ld_o;
+  int32_t rows, cols, dtype;   /* sffn_dtype of u and o */
+} sffn_orthogonal;
+int sffn_orthogonalize_workspace_bytes(const sffn_orthogonal* matrices, int n, const sffn_newton_schulz* ns, size_t* bytes);
+int sffn_orthogonalize(const sffn_orthogonal* matrices, int n, const sffn_newton_schulz* ns, void* workspace, size_t workspace_bytes,
+                       int32_t* status, void* stream);
+
+/* One Muon step over n matrices, in place:
+ *     g' = g min(1, max_norm / (grad_norm + 1e-6))      (grad_norm given; else g' = g)
+ *     m = momentum m + (1 - momentum) g',   U = (1 - momentum) g' + momentum m   (nesterov; else U = m)
+ *     p = p (1 - lr weight_decay) - lr scale O(U)
+ * p: fp32 or bf16, [rows, cols] without gaps, as g (fp32 or bf16) and m (fp32); master (bf16 p only, or NULL): fp32 copy of p that takes
+ * the step, p = bf16(master).  A grad_norm that is not finite leaves the whole step out, as in sffn_adamw_step, and as there nothing
+ * queued after the call starts before it has ended.  No tensor may lie over another. */
+typedef struct {
+  void* p;
+  const void* g;
+  float *master, *m;
+  int32_t rows, cols, p_dtype, g_dtype;
+  double lr, weight_decay, scale;
+} sffn_muon_tensor;
+typedef struct {
+  sffn_newton_schulz newton_schulz;
+  double momentum;             /* 0 <= momentum < 1 */
+  int32_t nesterov;
+  const float* grad_norm;      /* device, or NULL */
+  double max_norm;             /* read where grad_norm is given; infinity: no clipping, only the test for finite */
+} sffn_muon_config;
+int sffn_muon_workspace_bytes(const sffn_muon_tensor* tensors, int n, const sffn_newton_schulz* ns, size_t* bytes);
+int sffn_muon_step(const sffn_muon_tensor* tensors, int n, const sffn_muon_config* config, void* workspace, size_t workspace_bytes,
+                   int32_t* status, void* stream);
+
 /* ---- the block around the FFN -----------------------------------------------------------------------------------
  * The norms before and after an FFN (or any block of a residual stream) with its gate, its residual scale and the sum:
  *     h = resid + scale gate . N(y; post_gain),   n = N(h; pre_gain),   N(v; g) = v / sqrt(mean_k v_k^2 + eps) . g

@@ -17,6 +17,7 @@ from .binding import (  # noqa: F401
 )
 from .block import BlockNormFunction, block_norm_backward, block_norm_forward  # noqa: F401
 from .lopa import g_diagonal, g_tiled, touched_bytes, dense_bytes, lopa_approximation  # noqa: F401
+from .muon import MUON_COEFFICIENTS, muon_state, muon_step, orthogonalize  # noqa: F401
 from .training import (  # noqa: F401
     GatedFFNFunction,
     adamw_state,

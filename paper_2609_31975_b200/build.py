@@ -25,7 +25,7 @@ CALLS = PKG / "_training.so"  # the training calls' Python side (csrc/torch_call
 OBJ = PKG / "build"
 SOURCES = ["api.cu", "general_kernels.cu", "fused_kernel.cu", "fused_tc_kernel.cu", "static_entry.cu",
            "batched_kernels.cu", "umma_kernels.cu", "cast_kernels.cu", "optim_kernels.cu", "train_simt.cu", "train_umma.cu", "train_umma_f32.cu", "train_join.cu", "train_outer.cu", "train_api.cu",
-           "block_kernels.cu", "block_api.cu"]
+           "block_kernels.cu", "block_api.cu", "muon_kernels.cu", "muon_umma.cu", "muon_api.cu"]
 
 
 def _headers_mtime() -> float:

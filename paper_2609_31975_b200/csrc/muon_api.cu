@@ -1,0 +1,334 @@
+// Host side of the orthogonalised update and the Muon step: argument checks, batches of matrices of one shape, workspace layout, the order of
+// the kernels, and the powers of two that everything in sixteen bits is stored with.
+#include <algorithm>
+#include <cmath>
+#include <vector>
+
+#define SFFN_FILE "muon_api.cu"
+#include "host_checks.cuh"
+#include "muon_kernels.cuh"
+#include "sparse_ffn.h"
+
+using namespace sffn::host;
+using sffn::MuonBatch;
+using sffn::MuonItem;
+
+namespace {
+
+constexpr int kMaxShort = 1 << 16, kMaxLong = 1 << 22;  // sides of a matrix: tiles' numbers and tensor maps have room for so many
+// Entries of a batch, but for a matrix that has more by itself: matrices of which one fills the device take turns in one workspace.
+constexpr int64_t kBatchEntries = 1ll << 26;
+constexpr double kLargestBound = 1 << 30;
+
+struct Matrix {
+  MuonItem item;
+  int R, C;
+  bool src_bf16, out_bf16;
+  int terms;
+};
+
+// ---- powers of two ----------------------------------------------------------------------------------------------------
+// A matrix whose singular values are at most `bound` is stored with 2^e: entries stay below 2^14, a quarter of what fp16 holds.
+int exponent(double bound) { return sffn::kMuonExponent - (int)std::ceil(std::log2(std::max(bound, 0x1p-20))); }
+
+struct Plan {
+  float a, b, c;
+  int ex, ep, eq;
+};
+// The largest |f| on [0, end], f smooth: looked up at 2048 points, with 2 % for what lies between and for roundings.
+template <typename F>
+double most(double end, F f) {
+  double m = 0;
+  for (int i = 0; i <= 2048; ++i) m = std::max(m, std::fabs(f(end * i / 2048)));
+  return 1.02 * m;
+}
+// false: coefficients under which singular values leave every bound.
+bool make_plans(const sffn_newton_schulz& ns, std::vector<Plan>& plans) {
+  double bound = 1.0;  // of X's singular values: the first X has norm 1
+  for (int k = 0; k < ns.steps; ++k) {
+    const double a = ns.coefficients[3 * k], b = ns.coefficients[3 * k + 1], c = ns.coefficients[3 * k + 2];
+    if (!std::isfinite(a) || !std::isfinite(b) || !std::isfinite(c)) return false;
+    const double square = bound * bound, q = most(square, [&](double l) { return b * l + c * l * l; });
+    // The first X is stored up to a factor 1 < g <= 2 smaller than its norm says: P's entries are smaller for it, Q's larger.
+    plans.push_back({(float)a, (float)b, (float)c, exponent(bound), exponent(square), exponent(k == 0 ? 2 * q : q)});
+    bound = most(bound, [&](double x) { return x * (a + x * x * (b + x * x * c)); });
+    if (!(bound <= kLargestBound) || !(q <= kLargestBound)) return false;
+  }
+  return true;
+}
+
+int check_ns(const sffn_newton_schulz* ns, std::vector<Plan>& plans) {
+  if (!ns || ns->steps < 1 || ns->steps > SFFN_NS_MAX_STEPS || !ns->coefficients || !(ns->eps >= 0) || std::isinf(ns->eps)) return SFFN_ERR_INVALID_ARG;
+  if (ns->bits != 0 && ns->bits != 16 && ns->bits != 32) return SFFN_ERR_INVALID_ARG;
+  return make_plans(*ns, plans) ? SFFN_OK : SFFN_ERR_INVALID_ARG;
+}
+
+int check_shape(int rows, int cols) {
+  if (rows < 0 || cols < 0) return SFFN_ERR_INVALID_ARG;
+  return std::min(rows, cols) > kMaxShort || std::max(rows, cols) > kMaxLong ? SFFN_ERR_UNSUPPORTED : SFFN_OK;
+}
+
+// ---- batches ----------------------------------------------------------------------------------------------------------
+
+// Matrices of one shape and kind, in the order that the caller has them, as many at a time as a batch takes.
+std::vector<std::vector<const Matrix*>> batches_of(const std::vector<Matrix>& all) {
+  std::vector<const Matrix*> left;
+  for (const Matrix& m : all)
+    if (m.R > 0 && m.C > 0) left.push_back(&m);
+  std::stable_sort(left.begin(), left.end(), [](const Matrix* a, const Matrix* b) {
+    const int64_t x[5] = {a->R, a->C, a->src_bf16, a->out_bf16, a->terms}, y[5] = {b->R, b->C, b->src_bf16, b->out_bf16, b->terms};
+    return std::lexicographical_compare(x, x + 5, y, y + 5);
+  });
+  std::vector<std::vector<const Matrix*>> out;
+  for (const Matrix* m : left) {
+    const bool joins = !out.empty() && [&] {
+      const Matrix* f = out.back()[0];
+      const int64_t with = (int64_t)out.back().size() + 1;
+      return f->R == m->R && f->C == m->C && f->src_bf16 == m->src_bf16 && f->out_bf16 == m->out_bf16 && f->terms == m->terms && with <= sffn::kMuonBatch &&
+             with * m->R * m->C <= kBatchEntries;
+    }();
+    if (!joins) out.emplace_back();
+    out.back().push_back(m);
+  }
+  return out;
+}
+
+// The workspace of a batch; `base` NULL: only its size.
+size_t layout(MuonBatch& b, int n, const Matrix& like, char* base) {
+  b.n = n;
+  b.R = like.R; b.C = like.C;
+  b.tall = like.R > like.C;
+  b.S = std::min(like.R, like.C);
+  b.L = std::max(like.R, like.C);
+  b.src_bf16 = like.src_bf16;
+  b.out_bf16 = like.out_bf16;
+  b.terms = like.terms;
+  b.ld_x = ((int64_t)b.C + 15) / 16 * 16;
+  b.ld_p = ((int64_t)b.S + 15) / 16 * 16;
+  b.x_matrix = b.R * b.ld_x;
+  b.p_matrix = b.S * b.ld_p;
+  b.x_term = n * b.x_matrix;
+  b.p_term = n * b.p_matrix;
+  size_t off = 0;
+  auto take = [&](size_t bytes) {
+    char* const at = base + off;
+    off += up256(bytes);
+    return base ? at : nullptr;
+  };
+  for (uint16_t*& x : b.x) x = reinterpret_cast<uint16_t*>(take((size_t)b.x_term * 4));
+  b.P = reinterpret_cast<uint16_t*>(take((size_t)b.p_term * 2 * b.terms));
+  b.Q = reinterpret_cast<uint16_t*>(take((size_t)b.p_term * 2 * b.terms));
+  b.diag = reinterpret_cast<float*>(take((size_t)n * b.S * 4));
+  b.first = reinterpret_cast<float*>(take((size_t)n * 16));
+  b.squares = reinterpret_cast<double*>(take((size_t)n * sffn::kMuonPartials * 8));
+  b.partial = reinterpret_cast<float*>(take(sffn::muon_partial_floats(b.S, b.R, b.C, n, b.terms) * 4));
+  return off;
+}
+
+size_t workspace_of(const std::vector<Matrix>& all) {
+  size_t need = 256;
+  for (const auto& batch : batches_of(all)) {
+    MuonBatch b{};
+    need = std::max(need, layout(b, (int)batch.size(), *batch[0], nullptr));
+  }
+  return need;
+}
+
+// Everything that a call writes, and what it reads of others: whether any of the first meets anything else but its own source.
+struct Range {
+  Span span;
+  int owner, source;  // source: what may lie under this output (an index of a matrix), or -1
+  bool output;
+  uintptr_t first() const { return reinterpret_cast<uintptr_t>(span.p); }
+  uintptr_t end() const { return first() + (uintptr_t)((span.rows - 1) * span.ld + span.width); }
+};
+bool any_meet(std::vector<Range>& all) {
+  all.erase(std::remove_if(all.begin(), all.end(), [](const Range& r) { return !r.span.p || r.span.rows <= 0 || r.span.width <= 0; }), all.end());
+  std::sort(all.begin(), all.end(), [](const Range& a, const Range& b) { return a.first() < b.first(); });
+  std::vector<const Range*> open;
+  for (const Range& r : all) {
+    open.erase(std::remove_if(open.begin(), open.end(), [&](const Range* o) { return o->end() <= r.first(); }), open.end());
+    for (const Range* o : open) {
+      if (!r.output && !o->output) continue;
+      const bool own = (r.output && !o->output && r.source == o->owner) || (o->output && !r.output && o->source == r.owner);
+      if (!own && meet(r.span, o->span)) return true;
+    }
+    open.push_back(&r);
+  }
+  return false;
+}
+
+int run(const std::vector<Matrix>& all, const std::vector<Plan>& plans, const MuonBatch& common, void* workspace, cudaStream_t s) {
+  int sms = 0;
+  const int rc = sm_count(&sms);
+  if (rc != SFFN_OK) return rc;
+  for (const auto& batch : batches_of(all)) {
+    MuonBatch b = common;
+    layout(b, (int)batch.size(), *batch[0], static_cast<char*>(workspace));
+    for (size_t i = 0; i < batch.size(); ++i) b.item[i] = batch[i]->item;
+    SFFN_CUDA(sffn::launch_muon_moments(b, sms, s));
+    SFFN_CUDA(sffn::launch_muon_scale(b, sms, s));
+    for (size_t k = 0; k < plans.size(); ++k) {
+      const Plan& now = plans[k];
+      sffn::MuonProduct p{};
+      p.from = (int)(k & 1);
+      p.first = k == 0;
+      p.last = k + 1 == plans.size();
+      p.a = now.a; p.b = now.b; p.c = now.c;
+      p.ex = now.ex; p.ep = now.ep; p.eq = now.eq;
+      p.ey = p.last ? 0 : plans[k + 1].ex;
+      for (int kind : {sffn::kGram, sffn::kPoly, sffn::kApply}) {
+        p.kind = kind;
+        SFFN_CUDA(sffn::launch_muon_product(b, p, sms, s));
+      }
+    }
+  }
+  return SFFN_OK;
+}
+
+int matrices_of(const sffn_orthogonal* t, int n, const sffn_newton_schulz* ns, std::vector<Matrix>& out, bool pointers) {
+  if (n < 0 || (n > 0 && !t)) return SFFN_ERR_INVALID_ARG;
+  for (int i = 0; i < n; ++i) {
+    const sffn_orthogonal& a = t[i];
+    if (!storage_type(a.dtype)) return SFFN_ERR_INVALID_ARG;
+    const int shape = check_shape(a.rows, a.cols);
+    if (shape != SFFN_OK) return shape;
+    if (pointers && a.rows > 0 && a.cols > 0) {
+      if (!a.u || !a.o || a.ld_u < a.cols || a.ld_o < a.cols) return SFFN_ERR_INVALID_ARG;
+      if (!aligned(a.u, element(a.dtype)) || !aligned(a.o, element(a.dtype)) || a.ld_u > (1ll << 40) || a.ld_o > (1ll << 40)) return SFFN_ERR_UNSUPPORTED;
+    }
+    Matrix m{};
+    m.item.src = a.u; m.item.ld_src = a.ld_u;
+    m.item.out = a.o; m.item.ld_out = a.ld_o;
+    m.R = a.rows; m.C = a.cols;
+    m.src_bf16 = m.out_bf16 = a.dtype == SFFN_BF16;
+    m.terms = ns->bits == 32 || (ns->bits == 0 && a.dtype == SFFN_F32) ? 2 : 1;
+    out.push_back(m);
+  }
+  return SFFN_OK;
+}
+
+int matrices_of(const sffn_muon_tensor* t, int n, const sffn_newton_schulz* ns, std::vector<Matrix>& out, bool pointers) {
+  if (n < 0 || (n > 0 && !t)) return SFFN_ERR_INVALID_ARG;
+  for (int i = 0; i < n; ++i) {
+    const sffn_muon_tensor& a = t[i];
+    if (!storage_type(a.p_dtype) || !storage_type(a.g_dtype) || (a.master && a.p_dtype != SFFN_BF16)) return SFFN_ERR_INVALID_ARG;
+    const int shape = check_shape(a.rows, a.cols);
+    if (shape != SFFN_OK) return shape;
+    if (pointers) {
+      if (!std::isfinite(a.lr) || !std::isfinite(a.weight_decay) || !std::isfinite(a.scale)) return SFFN_ERR_INVALID_ARG;
+      if (a.rows > 0 && a.cols > 0) {
+        if (!a.p || !a.g || !a.m) return SFFN_ERR_INVALID_ARG;
+        if (!aligned(a.p, element(a.p_dtype)) || !aligned(a.g, element(a.g_dtype)) || !aligned(a.m, 4) || !aligned(a.master, 4)) return SFFN_ERR_UNSUPPORTED;
+      }
+    }
+    Matrix m{};
+    m.item.src = a.g; m.item.ld_src = a.cols;
+    m.item.out = a.p; m.item.ld_out = a.cols;
+    m.item.m = a.m; m.item.master = a.master;
+    m.item.decay = (float)(1.0 - a.lr * a.weight_decay);
+    m.item.rate = (float)(a.lr * a.scale);
+    m.R = a.rows; m.C = a.cols;
+    m.src_bf16 = a.g_dtype == SFFN_BF16;
+    m.out_bf16 = a.p_dtype == SFFN_BF16;
+    m.terms = ns->bits == 32 || (ns->bits == 0 && (a.p_dtype == SFFN_F32 || a.master)) ? 2 : 1;
+    out.push_back(m);
+  }
+  return SFFN_OK;
+}
+
+template <typename T>
+int workspace_bytes(const T* t, int n, const sffn_newton_schulz* ns, size_t* bytes) {
+  if (!bytes) return SFFN_ERR_INVALID_ARG;
+  std::vector<Plan> plans;
+  std::vector<Matrix> all;
+  int rc = check_ns(ns, plans);
+  if (rc == SFFN_OK) rc = matrices_of(t, n, ns, all, false);
+  if (rc == SFFN_OK) *bytes = workspace_of(all);
+  return rc;
+}
+
+int check_workspace(const std::vector<Matrix>& all, const void* workspace, size_t bytes, const int32_t* status) {
+  if (!status) return SFFN_ERR_INVALID_ARG;
+  if (!aligned(status, 4)) return SFFN_ERR_UNSUPPORTED;
+  return workspace && aligned(workspace, 256) && bytes >= workspace_of(all) ? SFFN_OK : SFFN_ERR_WORKSPACE;
+}
+
+// No exception leaves a C call: what the lists here need is little, but it is memory.
+template <typename F>
+int guarded(F f) {
+  try {
+    return f();
+  } catch (...) {
+    return SFFN_ERR_INVALID_ARG;
+  }
+}
+
+}  // namespace
+
+extern "C" {
+
+int sffn_orthogonalize_workspace_bytes(const sffn_orthogonal* t, int n, const sffn_newton_schulz* ns, size_t* bytes) {
+  return guarded([&] { return workspace_bytes(t, n, ns, bytes); });
+}
+int sffn_muon_workspace_bytes(const sffn_muon_tensor* t, int n, const sffn_newton_schulz* ns, size_t* bytes) {
+  return guarded([&] { return workspace_bytes(t, n, ns, bytes); });
+}
+
+int sffn_orthogonalize(const sffn_orthogonal* t, int n, const sffn_newton_schulz* ns, void* workspace, size_t workspace_bytes, int32_t* status, void* stream) {
+  return guarded([&]() -> int {
+    std::vector<Plan> plans;
+    std::vector<Matrix> all;
+    int rc = check_ns(ns, plans);
+    if (rc == SFFN_OK) rc = matrices_of(t, n, ns, all, true);
+    if (rc == SFFN_OK) rc = check_workspace(all, workspace, workspace_bytes, status);
+    if (rc != SFFN_OK) return rc;
+    std::vector<Range> ranges = {{whole(workspace, (int64_t)workspace_of(all)), -2, -1, true}, {whole(status, 4), -3, -1, true}};
+    for (int i = 0; i < n; ++i) {
+      const int64_t e = (int64_t)element(t[i].dtype), rows = t[i].rows, width = e * t[i].cols;
+      ranges.push_back({{t[i].u, rows, width, e * t[i].ld_u}, i, -1, false});
+      ranges.push_back({{t[i].o, rows, width, e * t[i].ld_o}, i, i, true});
+    }
+    if (any_meet(ranges)) return SFFN_ERR_INVALID_ARG;
+    MuonBatch common{};
+    common.eps = (float)ns->eps;
+    common.status = status;
+    return run(all, plans, common, workspace, static_cast<cudaStream_t>(stream));
+  });
+}
+
+int sffn_muon_step(const sffn_muon_tensor* t, int n, const sffn_muon_config* c, void* workspace, size_t workspace_bytes, int32_t* status, void* stream) {
+  return guarded([&]() -> int {
+    if (!c) return SFFN_ERR_INVALID_ARG;
+    std::vector<Plan> plans;
+    std::vector<Matrix> all;
+    int rc = check_ns(&c->newton_schulz, plans);
+    if (rc != SFFN_OK) return rc;
+    if (!(c->momentum >= 0 && c->momentum < 1) || (c->grad_norm && !(c->max_norm > 0))) return SFFN_ERR_INVALID_ARG;
+    if (!aligned(c->grad_norm, 4)) return SFFN_ERR_UNSUPPORTED;
+    rc = matrices_of(t, n, &c->newton_schulz, all, true);
+    if (rc == SFFN_OK) rc = check_workspace(all, workspace, workspace_bytes, status);
+    if (rc != SFFN_OK) return rc;
+    std::vector<Range> ranges = {{whole(workspace, (int64_t)workspace_of(all)), -2, -1, true}, {whole(status, 4), -3, -1, true}, {whole(c->grad_norm, 4), -4, -1, false}};
+    for (int i = 0; i < n; ++i) {
+      const int64_t entries = (int64_t)t[i].rows * t[i].cols;
+      ranges.push_back({whole(t[i].g, entries * (int64_t)element(t[i].g_dtype)), i, -1, false});
+      ranges.push_back({whole(t[i].p, entries * (int64_t)element(t[i].p_dtype)), i, -1, true});
+      ranges.push_back({whole(t[i].m, entries * 4), i, -1, true});
+      ranges.push_back({whole(t[i].master, entries * 4), i, -1, true});
+    }
+    if (any_meet(ranges)) return SFFN_ERR_INVALID_ARG;
+    MuonBatch common{};
+    common.step = true;
+    common.nesterov = c->nesterov != 0;
+    common.momentum = (float)c->momentum;
+    common.one_momentum = (float)(1.0 - c->momentum);
+    common.eps = (float)c->newton_schulz.eps;
+    common.grad_norm = c->grad_norm;
+    common.max_norm = (float)c->max_norm;
+    common.status = status;
+    return run(all, plans, common, workspace, static_cast<cudaStream_t>(stream));
+  });
+}
+
+}  // extern "C"

@@ -1,0 +1,70 @@
+// The orthogonalised update and the Muon step: what the host side (muon_api.cu) hands to the kernels.
+#pragma once
+
+#include <cuda_runtime.h>
+#include <stdint.h>
+
+#include "sparse_ffn.h"
+
+namespace sffn {
+
+constexpr int kMuonBatch = 64;     // matrices of a launch, at most
+constexpr int kMuonPartials = 256; // partial sums of a matrix's squares, at most
+constexpr int kMuonPairs = 80;     // pairs of CTAs at most
+constexpr int kMuonPieces = 2 * kMuonPairs;  // of tiles that are cut along K, at most
+
+// A matrix as the caller has it.
+struct MuonItem {
+  const void* src;      // the update, or the gradient
+  int64_t ld_src;
+  void* out;            // the orthogonal matrix, or the parameter
+  int64_t ld_out;
+  float *m, *master;    // step: moments, copy in 32 bits or NULL
+  float decay, rate;    // step: p = decay p - rate O
+};
+
+// A batch of matrices of one shape and the workspace that they share.  X, P and Q are fp16, a value v standing as v 2^e, in one or two
+// terms (hi and what it leaves): X [R, C], P = X X^T (or X^T X) and Q, polynomials of it, [S, S].
+struct MuonBatch {
+  MuonItem item[kMuonBatch];
+  int n;                // matrices
+  int R, C, S, L;       // rows, columns, shorter and longer side
+  bool tall;            // R > C: P = X^T X
+  bool step, nesterov, src_bf16, out_bf16;
+  int terms;            // of the products' operands
+  float momentum, one_momentum, eps;
+  const float* grad_norm;
+  float max_norm;
+  // workspace
+  int64_t ld_x, ld_p;   // elements
+  int64_t x_matrix, p_matrix, x_term, p_term;  // elements between matrices of a batch, and between terms
+  uint16_t *x[2], *P, *Q;
+  float* diag;          // [n, S]: Q's diagonal, which is not in Q
+  float* first;         // [n][4]: what the first step's coefficients are multiplied by: g, g^3, g^5 (X = g times what is stored)
+  double* squares;      // [n][kMuonPartials]
+  float* partial;       // pieces of tiles that are cut
+  int32_t* status;
+};
+
+// A product and its epilogue.
+//   kGram   P = X X^T (X^T X)
+//   kPoly   Q = b P + c P P, its diagonal apart
+//   kApply  X' = (a + diag) X + Q X (X Q); the last one ends in the caller's matrix
+enum { kGram = 0, kPoly = 1, kApply = 2 };
+struct MuonProduct {
+  int kind, from;       // from: which of x is X (the other one receives X')
+  bool first, last;
+  float a, b, c;
+  int ex, ep, eq, ey;   // exponents that X, P, Q and X' are stored with
+};
+
+cudaError_t launch_muon_product(const MuonBatch& b, const MuonProduct& p, int sm_count, cudaStream_t s);
+// Floats that the pieces of a batch's products may take, on any device.
+size_t muon_partial_floats(int S, int R, int C, int n, int terms);
+
+// Moments (step), and the squares' sums; then X = U 2^k in two terms, with its factor.
+cudaError_t launch_muon_moments(const MuonBatch& b, int sm_count, cudaStream_t s);
+cudaError_t launch_muon_scale(const MuonBatch& b, int sm_count, cudaStream_t s);
+constexpr int kMuonExponent = 14;  // X before the first step: norm 2^13 to 2^14 as stored
+
+}  // namespace sffn

@@ -11,6 +11,7 @@
 #include <torch/csrc/Dtype.h>
 #include <torch/csrc/autograd/python_variable.h>
 #include <torch/csrc/utils/pybind.h>
+#include <pybind11/stl.h>
 
 #include <cmath>
 #include <string>
@@ -34,10 +35,14 @@ struct Entry {
   decltype(&sffn_block_norm_forward) block_forward;
   decltype(&sffn_block_norm_workspace_bytes) block_workspace_bytes;
   decltype(&sffn_block_norm_backward) block_backward;
+  decltype(&sffn_orthogonalize_workspace_bytes) orthogonalize_workspace_bytes;
+  decltype(&sffn_orthogonalize) orthogonalize;
+  decltype(&sffn_muon_workspace_bytes) muon_workspace_bytes;
+  decltype(&sffn_muon_step) muon_step;
 } entry;
 
 void bind(const std::vector<uintptr_t>& a) {
-  if (a.size() != 9) throw py::value_error("nine addresses");
+  if (a.size() != 13) throw py::value_error("thirteen addresses");
   entry.workspace_bytes = reinterpret_cast<decltype(entry.workspace_bytes)>(a[0]);
   entry.forward = reinterpret_cast<decltype(entry.forward)>(a[1]);
   entry.backward = reinterpret_cast<decltype(entry.backward)>(a[2]);
@@ -47,6 +52,10 @@ void bind(const std::vector<uintptr_t>& a) {
   entry.block_forward = reinterpret_cast<decltype(entry.block_forward)>(a[6]);
   entry.block_workspace_bytes = reinterpret_cast<decltype(entry.block_workspace_bytes)>(a[7]);
   entry.block_backward = reinterpret_cast<decltype(entry.block_backward)>(a[8]);
+  entry.orthogonalize_workspace_bytes = reinterpret_cast<decltype(entry.orthogonalize_workspace_bytes)>(a[9]);
+  entry.orthogonalize = reinterpret_cast<decltype(entry.orthogonalize)>(a[10]);
+  entry.muon_workspace_bytes = reinterpret_cast<decltype(entry.muon_workspace_bytes)>(a[11]);
+  entry.muon_step = reinterpret_cast<decltype(entry.muon_step)>(a[12]);
 }
 
 [[noreturn]] void type_error(const std::string& what) { throw py::type_error(what); }
@@ -341,6 +350,102 @@ int adamw_state_values(const py::object& states, const py::object& out) {
   return rc;
 }
 
+// Steps of (a, b, c), one after another.
+sffn_newton_schulz newton_schulz(const std::vector<double>& coefficients, double eps, int bits) {
+  if (coefficients.empty() || coefficients.size() % 3) throw py::value_error("coefficients: three for every step");
+  sffn_newton_schulz ns{};
+  ns.steps = (int32_t)(coefficients.size() / 3);
+  ns.bits = bits;
+  ns.coefficients = coefficients.data();
+  ns.eps = eps;
+  return ns;
+}
+// rows x cols of a tensor of a matrix.
+void matrix_of(const char* name, const Tensor& t, int32_t* r, int32_t* c) {
+  if (t.dim() != 2) type_error(std::string(name) + ": a matrix expected, got " + shape_text(t.sizes()));
+  if (t.size(0) > INT32_MAX || t.size(1) > INT32_MAX) type_error("sizes beyond 32 bits");
+  *r = (int32_t)t.size(0);
+  *c = (int32_t)t.size(1);
+}
+
+// (status, list of O): out: None, or a list of tensors to write to.
+py::tuple orthogonalize(const py::object& updates, const py::object& out, const std::vector<double>& coefficients, double eps, int bits, const Tensor& status) {
+  const Items u(updates);
+  const bool given = !out.is_none();
+  const Items o(given ? out : updates);
+  if (o.n != u.n) throw py::value_error("updates and out must be lists of one length");
+  const sffn_newton_schulz ns = newton_schulz(coefficients, eps, bits);
+  std::vector<sffn_orthogonal> t((size_t)u.n);
+  std::vector<Tensor> made((size_t)u.n);
+  const at::Device dev = status.device();
+  const c10::cuda::CUDAGuard guard(dev);
+  for (Py_ssize_t i = 0; i < u.n; ++i) {
+    const Tensor& ui = tensor_of(u[i], "update");
+    sffn_orthogonal& a = t[i];
+    a.dtype = dtype_code(ui.scalar_type(), "updates");
+    matrix_of("update", ui, &a.rows, &a.cols);
+    a.ld_u = rows("update", ui, a.rows, a.cols, ui.scalar_type(), dev);
+    a.u = ui.data_ptr();
+    made[i] = given ? tensor_of(o[i], "out") : make({a.rows, a.cols}, ui.scalar_type(), dev);
+    a.ld_o = rows("out", made[i], a.rows, a.cols, ui.scalar_type(), dev);
+    a.o = made[i].data_ptr();
+  }
+  size_t bytes = 0;
+  int rc = entry.orthogonalize_workspace_bytes(t.data(), (int)u.n, &ns, &bytes);
+  if (rc == SFFN_OK) {
+    const Tensor ws = make({(int64_t)bytes}, at::kByte, dev);
+    rc = entry.orthogonalize(t.data(), (int)u.n, &ns, ws.data_ptr(), bytes, static_cast<int32_t*>(status.data_ptr()), current_stream(dev));
+  }
+  if (rc == SFFN_OK && given)
+    for (const Tensor& m : made) written(m);
+  return py::make_tuple(rc, made);
+}
+
+int muon_step(const py::object& params, const py::object& grads, const py::object& states, const py::object& masters, const py::object& lr, double momentum,
+              bool nesterov, const py::object& weight_decay, const py::object& scale, const std::vector<double>& coefficients, double eps, int bits,
+              const OptTensor& grad_norm, double max_norm, const Tensor& status) {
+  const Items p(params), g(grads), s(states);
+  const bool copies = !masters.is_none();
+  const Items w(copies ? masters : params);
+  if (g.n != p.n || s.n != p.n || w.n != p.n) throw py::value_error("params, grads, states and masters must be lists of one length");
+  const Numbers rates(lr, p.n, "lr"), decays(weight_decay, p.n, "weight_decay"), scales(scale, p.n, "scale");
+  std::vector<sffn_muon_tensor> t((size_t)p.n);
+  const at::Device dev = status.device();
+  for (Py_ssize_t i = 0; i < p.n; ++i) {
+    const Tensor &pi = tensor_of(p[i], "parameter"), &gi = tensor_of(g[i], "gradient");
+    sffn_muon_tensor& a = t[i];
+    a.p_dtype = dtype_code(pi.scalar_type(), "parameters");
+    a.g_dtype = dtype_code(gi.scalar_type(), "gradients");
+    matrix_of("parameter", pi, &a.rows, &a.cols);
+    a.p = whole("parameter", pi, pi.sizes(), pi.scalar_type(), dev);
+    a.g = whole("gradient", gi, pi.sizes(), gi.scalar_type(), dev);
+    if (copies && w[i] != Py_None) a.master = static_cast<float*>(whole("master", tensor_of(w[i], "master"), pi.sizes(), at::kFloat, dev));
+    if (!PyDict_Check(s[i])) type_error("a state is a dict of m");
+    a.m = static_cast<float*>(whole("m", tensor_of(PyDict_GetItemString(s[i], "m"), "m"), pi.sizes(), at::kFloat, dev));
+    a.lr = rates[i];
+    a.weight_decay = decays[i];
+    a.scale = scales[i];
+  }
+  sffn_muon_config c{};
+  c.newton_schulz = newton_schulz(coefficients, eps, bits);
+  c.momentum = momentum;
+  c.nesterov = nesterov;
+  c.max_norm = max_norm;
+  if (grad_norm) c.grad_norm = static_cast<const float*>(whole("grad_norm", *grad_norm, {}, at::kFloat, dev));
+  const c10::cuda::CUDAGuard guard(dev);
+  size_t bytes = 0;
+  int rc = entry.muon_workspace_bytes(t.data(), (int)p.n, &c.newton_schulz, &bytes);
+  if (rc != SFFN_OK) return rc;
+  const Tensor ws = make({(int64_t)bytes}, at::kByte, dev);
+  rc = entry.muon_step(t.data(), (int)p.n, &c, ws.data_ptr(), bytes, static_cast<int32_t*>(status.data_ptr()), current_stream(dev));
+  for (Py_ssize_t i = 0; rc == SFFN_OK && i < p.n; ++i) {
+    written(THPVariable_Unpack(p[i]));
+    if (t[i].master) written(THPVariable_Unpack(w[i]));
+    written(THPVariable_Unpack(PyDict_GetItemString(s[i], "m")));
+  }
+  return rc;
+}
+
 // What both passes of the norms around a block hand over, but for resid, h, n and their statistics.
 sffn_block_norm make_block(const OptTensor& y, const Tensor& like, const OptTensor& post_gain, const OptTensor& pre_gain, const OptTensor& gate, double scale,
                            double eps) {
@@ -500,6 +605,8 @@ PYBIND11_MODULE(_training, m) {
   m.def("grad_norm", &grad_norm);
   m.def("adamw_step", &adamw_step);
   m.def("adamw_state_values", &adamw_state_values);
+  m.def("orthogonalize", &orthogonalize);
+  m.def("muon_step", &muon_step);
   m.def("block_forward", &block_forward);
   m.def("block_backward", &block_backward);
 }

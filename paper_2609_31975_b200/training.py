@@ -16,7 +16,8 @@ ACT_TRAIN = dict(ACT_UP, none=3)  # activations of either branch in training
 ACT_TRAIN[None] = 3
 GROUP = 256                       # entries that share the scales of their 8-bit moments
 _ENTRIES = ("sffn_train_workspace_bytes", "gated_ffn_forward", "gated_ffn_backward", "sffn_grad_norm", "sffn_adamw_step",
-            "sffn_adamw_state_values", "sffn_block_norm_forward", "sffn_block_norm_workspace_bytes", "sffn_block_norm_backward")
+            "sffn_adamw_state_values", "sffn_block_norm_forward", "sffn_block_norm_workspace_bytes", "sffn_block_norm_backward",
+            "sffn_orthogonalize_workspace_bytes", "sffn_orthogonalize", "sffn_muon_workspace_bytes", "sffn_muon_step")
 
 _bound = None
 
