@@ -204,61 +204,124 @@ __device__ __forceinline__ void row_sums(float (&v)[4], float* room) {
   }
 }
 
+// Rows of up to 8192 entries: W warps, two pieces of eight entries a thread (one where W is 1: eight rows a CTA).  Wider ones: 32 warps of up
+// to four, whose sums of columns do not fit registers beside the rest.
 template <int W, int V>
 struct BackShape {
   static constexpr int kRows = W == 1 ? 8 : 1, kThreads = 32 * W * kRows;
+  static constexpr int kPerSm = kThreads >= 512 ? 1 : 512 / kThreads;
+  static constexpr bool kRing = W < 32;  // rows come through shared memory, which has no room for wider ones
 };
+constexpr int kBackStages = 4;  // rows under way, at most
 
-template <int W, int V>
-__global__ void __launch_bounds__(BackShape<W, V>::kThreads, W * V <= 16 && W > 1 ? 1024 / BackShape<W, V>::kThreads : 1)
-    block_backward_kernel(const __grid_constant__ BlockParams p) {
-  constexpr int kRows = BackShape<W, V>::kRows;
+__device__ __forceinline__ void copy16(uint32_t to, const char* from) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to), "l"(from) : "memory");
+}
+__device__ __forceinline__ uint4 shared16(uint32_t from) {
+  uint4 v;
+  asm volatile("ld.shared.v4.b32 {%0,%1,%2,%3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(from) : "memory");
+  return v;
+}
+
+// Every thread copies what it will read itself into shared memory, `stages` rows ahead: its own copies are all that it waits for.
+// ALL_BF16: y, h and n are bf16, else each is what the call says.
+template <int W, int V, bool ALL_BF16>
+__global__ void __launch_bounds__(BackShape<W, V>::kThreads, BackShape<W, V>::kPerSm)
+    block_backward_kernel(const __grid_constant__ BlockParams p, int stages) {
+  constexpr int kRows = BackShape<W, V>::kRows, kThreads = BackShape<W, V>::kThreads;
+  extern __shared__ __align__(16) uint8_t ring_raw[];
   __shared__ __align__(16) float room[2][4 * W];
   __shared__ float lines[W == 1 ? kRows : 1][W == 1 ? 256 * V : 1];
   const int in_row = threadIdx.x % (32 * W);
+  const bool y_bf16 = ALL_BF16 || p.y_bf16, h_bf16 = ALL_BF16 || p.h_bf16, n_bf16 = ALL_BF16 || p.n_bf16;
+  const bool post = p.post_gain != nullptr, full = p.gate_kind == SFFN_BLOCK_GATE_FULL, channel = p.gate_kind == SFFN_BLOCK_GATE_CHANNEL;
+  const bool has_dh = p.dh != nullptr, has_n = p.dn != nullptr, has_y = p.y != nullptr;
+  // The ring: for every stage, array and piece (and half of an fp32 piece) a plane of 16 bytes a thread.
+  const int wide_h = h_bf16 ? 1 : 2, wide_n = n_bf16 ? 1 : 2, wide_y = y_bf16 ? 1 : 2;
+  struct Array {
+    const char* p;
+    int64_t ld;
+    int plane;
+    bool bf16;
+  };
+  const Array dh = {p.dh, p.ld_dh, 0, h_bf16}, dn = {p.dn, p.ld_dn, has_dh ? wide_h : 0, n_bf16}, h = {p.h, p.ld_h, dn.plane + (has_n ? wide_n : 0), h_bf16};
+  const Array y = {p.y, p.ld_y, h.plane + (has_n ? wide_h : 0), y_bf16}, gate = {p.gate, p.ld_gate, y.plane + (has_y ? wide_y : 0), h_bf16};
+  const int stage_bytes = (gate.plane + (full ? wide_h : 0)) * V * kThreads * 16;
+  const uint32_t ring = static_cast<uint32_t>(__cvta_generic_to_shared(ring_raw)) + threadIdx.x * 16;
+  auto plane = [&](int stage, const Array& a, int i) { return ring + stage * stage_bytes + (a.plane * V + (a.bf16 ? i : 2 * i)) * (kThreads * 16); };
+
   pdl_launch_dependents();
   pdl_wait();
-  const bool post = p.post_gain != nullptr, full = p.gate_kind == SFFN_BLOCK_GATE_FULL, channel = p.gate_kind == SFFN_BLOCK_GATE_CHANNEL;
-  const bool has_n = p.dn != nullptr, has_y = p.y != nullptr;
-  float acc_pre[V][8], acc_c[V][8];
+  auto copy_piece = [&](int stage, const Array& a, int t, int i, int c) {
+    const uint32_t to = plane(stage, a, i);
+    const char* from = a.p + t * a.ld + ((int64_t)c << (a.bf16 ? 1 : 2));
+    copy16(to, from);
+    if (!a.bf16 && c + 4 < p.D) copy16(to + kThreads * 16, from + 16);
+  };
+  auto fetch = [&](int stage, int t) {
+    if constexpr (!BackShape<W, V>::kRing) return;
+    if (t < p.T) {
 #pragma unroll
-  for (int i = 0; i < V; ++i)
-#pragma unroll
-    for (int j = 0; j < 8; ++j) acc_pre[i][j] = acc_c[i][j] = 0.f;
-  int turn = 0;
-  for (int t = blockIdx.x * kRows + threadIdx.x / (32 * W); t < p.T; t += gridDim.x * kRows, turn ^= 1) {
-    Raw dh[V], dn[V], h[V], y[V], gate[V];
-#pragma unroll
-    for (int i = 0; i < V; ++i) {
-      const int c = 8 * (in_row + 32 * W * i);
-      if (c >= p.D) continue;
-      if (p.dh) dh[i] = load_raw(p.dh + t * p.ld_dh, p.h_bf16, c, p.D);
-      if (has_n) {
-        dn[i] = load_raw(p.dn + t * p.ld_dn, p.n_bf16, c, p.D);
-        h[i] = load_raw(p.h + t * p.ld_h, p.h_bf16, c, p.D);
+      for (int i = 0; i < V; ++i) {
+        const int c = 8 * (in_row + 32 * W * i);
+        if (c >= p.D) continue;
+        if (has_dh) copy_piece(stage, dh, t, i, c);
+        if (has_n) {
+          copy_piece(stage, dn, t, i, c);
+          copy_piece(stage, h, t, i, c);
+        }
+        if (has_y) copy_piece(stage, y, t, i, c);
+        if (full) copy_piece(stage, gate, t, i, c);
       }
-      if (has_y) y[i] = load_raw(p.y + t * p.ld_y, p.y_bf16, c, p.D);
-      if (full) gate[i] = load_raw(p.gate + t * p.ld_gate, p.h_bf16, c, p.D);
     }
+    asm volatile("cp.async.commit_group;" ::: "memory");  // a group a row, empty or not
+  };
+  auto get = [&](int stage, const Array& a, int t, int i, int c, float* f) {
+    Raw r;
+    if constexpr (BackShape<W, V>::kRing) {
+      const uint32_t from = plane(stage, a, i);
+      r.a = shared16(from);
+      if (!a.bf16) r.b = c + 4 < p.D ? shared16(from + kThreads * 16) : make_uint4(0, 0, 0, 0);
+    } else {
+      r = load_raw(a.p + t * a.ld, a.bf16, c, p.D);
+    }
+    unpack(r, a.bf16, f);
+  };
+
+  const int first = blockIdx.x * kRows + threadIdx.x / (32 * W), step = gridDim.x * kRows;
+  for (int q = 0; q < stages; ++q) fetch(q, first + q * step);  // (not more than 2^30 rows and a grid's: no overflow)
+  // This thread's columns: n's gains, and what multiplies y's entries but for r and a gate of a token's or an entry's.
+  float pre[V][8], w[V][8], acc_pre[V][8], acc_c[V][8];
+#pragma unroll
+  for (int i = 0; i < V; ++i) {
+    const int c = 8 * (in_row + 32 * W * i);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      acc_pre[i][j] = acc_c[i][j] = pre[i][j] = 0.f;
+      w[i][j] = p.scale;
+    }
+    if (c >= p.D) continue;
+    if (has_n) load_gain(p.pre_gain, c, p.D, pre[i]);
+    float f[8];
+    if (post) {
+      load_gain(p.post_gain, c, p.D, f);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) w[i][j] *= f[j];
+    }
+    if (channel) {
+      load_gain(reinterpret_cast<const float*>(p.gate), c, p.D, f);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) w[i][j] *= f[j];
+    }
+  }
+  int turn = 0, stage = 0;
+  for (int t = first; t < p.T; t += step, turn ^= 1) {
+    if (stages >= 4) asm volatile("cp.async.wait_group 3;" ::: "memory");
+    else if (stages == 3) asm volatile("cp.async.wait_group 2;" ::: "memory");
+    else if (stages == 2) asm volatile("cp.async.wait_group 1;" ::: "memory");
+    else asm volatile("cp.async.wait_group 0;" ::: "memory");
     const float r = post ? p.stats[t] : 1.f, rho = has_n ? p.stats[p.T + t] : 0.f;
     const float token = p.gate_kind == SFFN_BLOCK_GATE_TOKEN ? reinterpret_cast<const float*>(p.gate)[t] : 1.f;
-    // what multiplies y's entries, but for r and a token's gate
-    auto weights = [&](int i, int c, float* w) {
-#pragma unroll
-      for (int j = 0; j < 8; ++j) w[j] = p.scale;
-      float f[8];
-      if (post) {
-        load_gain(p.post_gain, c, p.D, f);
-#pragma unroll
-        for (int j = 0; j < 8; ++j) w[j] *= f[j];
-      }
-      if (channel) load_gain(reinterpret_cast<const float*>(p.gate), c, p.D, f);
-      else if (full) unpack(gate[i], p.h_bf16, f);
-      if (channel || full) {
-#pragma unroll
-        for (int j = 0; j < 8; ++j) w[j] *= f[j];
-      }
-    };
     float sums[4] = {0.f, 0.f, 0.f, 0.f};  // of t h, w y dh, w y t, w y h
 #pragma unroll
     for (int i = 0; i < V; ++i) {
@@ -266,21 +329,24 @@ __global__ void __launch_bounds__(BackShape<W, V>::kThreads, W * V <= 16 && W > 
       if (c >= p.D) continue;
       float a[8], b[8], e[8];
       if (has_n) {
-        load_gain(p.pre_gain, c, p.D, e);
-        unpack(dn[i], p.n_bf16, a);
-        unpack(h[i], p.h_bf16, b);
+        get(stage, dn, t, i, c, a);
+        get(stage, h, t, i, c, b);
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
-          a[j] *= e[j];
+          a[j] *= pre[i][j];
           sums[0] = fmaf(a[j], b[j], sums[0]);
         }
       }
       if (has_y) {
-        float f[8];
-        unpack(y[i], p.y_bf16, f);
-        weights(i, c, e);
+        get(stage, y, t, i, c, e);
 #pragma unroll
-        for (int j = 0; j < 8; ++j) e[j] *= f[j];
+        for (int j = 0; j < 8; ++j) e[j] *= w[i][j];
+        if (full) {
+          float f[8];
+          get(stage, gate, t, i, c, f);
+#pragma unroll
+          for (int j = 0; j < 8; ++j) e[j] *= f[j];
+        }
         if (has_n) {
 #pragma unroll
           for (int j = 0; j < 8; ++j) {
@@ -288,10 +354,10 @@ __global__ void __launch_bounds__(BackShape<W, V>::kThreads, W * V <= 16 && W > 
             sums[3] = fmaf(e[j], b[j], sums[3]);
           }
         }
-        if (p.dh) {
-          unpack(dh[i], p.h_bf16, f);
+        if (has_dh) {
+          get(stage, dh, t, i, c, a);
 #pragma unroll
-          for (int j = 0; j < 8; ++j) sums[1] = fmaf(e[j], f[j], sums[1]);
+          for (int j = 0; j < 8; ++j) sums[1] = fmaf(e[j], a[j], sums[1]);
         }
       }
     }
@@ -305,56 +371,45 @@ __global__ void __launch_bounds__(BackShape<W, V>::kThreads, W * V <= 16 && W > 
       const int c = 8 * (in_row + 32 * W * i);
       if (c >= p.D) continue;
       float g[8], f[8], e[8];
-      if (p.dh) unpack(dh[i], p.h_bf16, g);
+      if (has_dh) get(stage, dh, t, i, c, g);
       else
 #pragma unroll
         for (int j = 0; j < 8; ++j) g[j] = 0.f;
       if (has_n) {
-        load_gain(p.pre_gain, c, p.D, e);
-        unpack(dn[i], p.n_bf16, f);
+        get(stage, dn, t, i, c, f);
+        get(stage, h, t, i, c, e);
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
           f[j] *= rho;
-          g[j] = fmaf(f[j], e[j], g[j]);
-        }
-        unpack(h[i], p.h_bf16, e);
-#pragma unroll
-        for (int j = 0; j < 8; ++j) {
-          g[j] = fmaf(-k1, e[j], g[j]);
+          g[j] = fmaf(-k1, e[j], fmaf(f[j], pre[i][j], g[j]));
           acc_pre[i][j] = fmaf(f[j], e[j], acc_pre[i][j]);
         }
       }
-      if (p.dresid) store8(p.dresid + t * p.ld_dresid, p.h_bf16, c, p.D, g);
+      if (p.dresid) store8(p.dresid + t * p.ld_dresid, h_bf16, c, p.D, g);
       if (has_y) {
-        unpack(y[i], p.y_bf16, f);
+        get(stage, y, t, i, c, f);
         if (full) {
-          unpack(gate[i], p.h_bf16, e);
+          get(stage, gate, t, i, c, e);
           if (p.dgate) {
             float d[8];
 #pragma unroll
-            for (int j = 0; j < 8; ++j) d[j] = own * g[j] * f[j];
-            float gain[8];
-            if (post) {
-              load_gain(p.post_gain, c, p.D, gain);
-#pragma unroll
-              for (int j = 0; j < 8; ++j) d[j] *= gain[j];
-            }
-            store8(p.dgate + t * p.ld_dgate, p.h_bf16, c, p.D, d);
+            for (int j = 0; j < 8; ++j) d[j] = up * w[i][j] * g[j] * f[j];
+            store8(p.dgate + t * p.ld_dgate, h_bf16, c, p.D, d);
           }
 #pragma unroll
-          for (int j = 0; j < 8; ++j) acc_c[i][j] = fmaf(own * e[j] * g[j], f[j], acc_c[i][j]);
-        } else {
-#pragma unroll
-          for (int j = 0; j < 8; ++j) acc_c[i][j] = fmaf(own * g[j], f[j], acc_c[i][j]);
+          for (int j = 0; j < 8; ++j) g[j] *= e[j];
         }
-        if (p.dy) {
-          weights(i, c, e);
 #pragma unroll
-          for (int j = 0; j < 8; ++j) f[j] = up * e[j] * g[j] - k2 * f[j];
-          store8(p.dy + t * p.ld_dy, p.y_bf16, c, p.D, f);
+        for (int j = 0; j < 8; ++j) acc_c[i][j] = fmaf(own * g[j], f[j], acc_c[i][j]);
+        if (p.dy) {
+#pragma unroll
+          for (int j = 0; j < 8; ++j) f[j] = fmaf(up * w[i][j], g[j], -k2 * f[j]);
+          store8(p.dy + t * p.ld_dy, y_bf16, c, p.D, f);
         }
       }
     }
+    fetch(stage, t + stages * step);  // what was in this stage has been used
+    if (++stage == stages) stage = 0;
   }
   // This CTA's line of column sums.
   float* const line = p.partial + (int64_t)blockIdx.x * p.D;
@@ -372,10 +427,10 @@ __global__ void __launch_bounds__(BackShape<W, V>::kThreads, W * V <= 16 && W > 
 #pragma unroll
         for (int j = 0; j < 8; ++j) lines[threadIdx.x >> 5][256 * i + 8 * in_row + j] = acc[i][j];
       __syncthreads();
-      for (int c = threadIdx.x; c < p.D; c += BackShape<W, V>::kThreads) {
+      for (int c = threadIdx.x; c < p.D; c += kThreads) {
         float s = 0.f;
 #pragma unroll
-        for (int w = 0; w < kRows; ++w) s += lines[w][c];
+        for (int q = 0; q < kRows; ++q) s += lines[q][c];
         to[c] = s;
       }
     }
@@ -438,16 +493,28 @@ cudaError_t forward(const BlockParams& p, cudaStream_t s) {
   using S = Shape<W, V>;
   return launch_pdl(block_forward_kernel<W, V>, dim3((p.T + S::kRows - 1) / S::kRows), dim3(S::kThreads), 0, s, p);
 }
-template <int W, int V>
+constexpr int kSmShared = 200 * 1024;  // of an SM, for the rings of the CTAs on it (up to eight, with up to 9 KB more each)
+
+template <int W, int V, bool ALL_BF16>
 cudaError_t backward(const BlockParams& p, int sm_count, int* lines, cudaStream_t s) {
   using S = BackShape<W, V>;
-  int per_sm = 0;
-  const cudaError_t e = cudaOccupancyMaxActiveBlocksPerMultiprocessor(&per_sm, block_backward_kernel<W, V>, S::kThreads, 0);
+  static unsigned long long configured = 0;
+  cudaError_t e = allow_dynamic_smem(block_backward_kernel<W, V, ALL_BF16>, kSmShared, configured);
   if (e != cudaSuccess) return e;
-  const int rows = (p.T + S::kRows - 1) / S::kRows, room = (per_sm > 0 ? per_sm : 1) * sm_count;
+  const int h = p.h_bf16 ? 1 : 2, n = p.n_bf16 ? 1 : 2, y = p.y_bf16 ? 1 : 2;
+  const int planes = (p.dh ? h : 0) + (p.dn ? n + h : 0) + (p.y ? y : 0) + (p.gate_kind == SFFN_BLOCK_GATE_FULL ? h : 0);
+  const int stage = S::kRing ? planes * V * S::kThreads * 16 : 0, rows = (p.T + S::kRows - 1) / S::kRows;
+  // At most five arrays of fp32, two pieces of 512 threads of an SM: 160 KB.
+  int stages = stage > 0 ? kSmShared / S::kPerSm / stage : 1;
+  stages = stages > kBackStages ? kBackStages : stages;
+  const int room = S::kPerSm * sm_count;
   *lines = rows < room ? rows : room;
   if (*lines > p.lines) *lines = p.lines;
-  return launch_pdl(block_backward_kernel<W, V>, dim3(*lines), dim3(S::kThreads), 0, s, p);
+  return launch_pdl(block_backward_kernel<W, V, ALL_BF16>, dim3(*lines), dim3(S::kThreads), (size_t)stages * stage, s, p, stages);
+}
+template <int W, int V>
+cudaError_t backward(const BlockParams& p, int sm_count, int* lines, cudaStream_t s) {
+  return p.y_bf16 && p.h_bf16 && p.n_bf16 ? backward<W, V, true>(p, sm_count, lines, s) : backward<W, V, false>(p, sm_count, lines, s);
 }
 
 }  // namespace
@@ -483,11 +550,11 @@ cudaError_t launch_block_backward(const sffn_block_norm& b, const sffn_block_gra
   int lines = 0;
   cudaError_t e;
   if (p.D <= 256) e = backward<1, 1>(p, sm_count, &lines, s);
-  else if (p.D <= 512) e = backward<1, 2>(p, sm_count, &lines, s);
-  else if (p.D <= 1024) e = backward<4, 1>(p, sm_count, &lines, s);
-  else if (p.D <= 2048) e = backward<8, 1>(p, sm_count, &lines, s);
-  else if (p.D <= 4096) e = backward<16, 1>(p, sm_count, &lines, s);
-  else if (p.D <= 8192) e = backward<32, 1>(p, sm_count, &lines, s);
+  else if (p.D <= 512) e = backward<2, 1>(p, sm_count, &lines, s);
+  else if (p.D <= 1024) e = backward<2, 2>(p, sm_count, &lines, s);
+  else if (p.D <= 2048) e = backward<4, 2>(p, sm_count, &lines, s);
+  else if (p.D <= 4096) e = backward<8, 2>(p, sm_count, &lines, s);
+  else if (p.D <= 8192) e = backward<16, 2>(p, sm_count, &lines, s);
   else if (p.D <= 16384) e = backward<32, 2>(p, sm_count, &lines, s);
   else e = backward<32, 4>(p, sm_count, &lines, s);
   if (e != cudaSuccess || (!p.want_pre && !p.want_c)) return e;
