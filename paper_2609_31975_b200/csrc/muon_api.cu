@@ -2,6 +2,7 @@
 // the kernels, and the powers of two that everything in sixteen bits is stored with.
 #include <algorithm>
 #include <cmath>
+#include <cstring>
 #include <vector>
 
 #define SFFN_FILE "muon_api.cu"
@@ -31,36 +32,121 @@ struct Matrix {
 // A matrix whose singular values are at most `bound` is stored with 2^e: entries stay below 2^14, a quarter of what fp16 holds.
 int exponent(double bound) { return sffn::kMuonExponent - (int)std::ceil(std::log2(std::max(bound, 0x1p-20))); }
 
-struct Plan {
-  float a, b, c;
-  int ex, ep, eq;
-};
-// The largest |f| on [0, end], f smooth: looked up at 2048 points, with 2 % for what lies between and for roundings.
-template <typename F>
-double most(double end, F f) {
+
+// What a call launches for every batch (muon_umma.cu has the forms).  Singular values are followed at 2049 points of what they can be, with
+// 2 % for what lies between and for roundings: what X and the polynomials of A reach gives the powers of two.
+using Products = std::vector<sffn::MuonProduct>;
+constexpr int kPoints = 2049;
+double most(const std::vector<double>& v) {
   double m = 0;
-  for (int i = 0; i <= 2048; ++i) m = std::max(m, std::fabs(f(end * i / 2048)));
+  for (double x : v) m = std::max(m, std::fabs(x));
   return 1.02 * m;
 }
-// false: coefficients under which singular values leave every bound.
-bool make_plans(const sffn_newton_schulz& ns, std::vector<Plan>& plans) {
+
+// `group` steps at a time.  false: coefficients under which singular values leave every bound.
+bool make_products(const sffn_newton_schulz& ns, int group, Products& out) {
+  using sffn::MuonTerm;
+  struct Held {  // a matrix: where, with which exponent
+    int which, e;
+  };
+  const MuonTerm none = {-1, 0, 0.f, -1};
+  auto with = [](const Held& h, double c, int factor) { return MuonTerm{h.which, h.e, (float)c, factor}; };
+  auto only = [](double c, int factor) { return MuonTerm{-1, 0, (float)c, factor}; };
   double bound = 1.0;  // of X's singular values: the first X has norm 1
-  for (int k = 0; k < ns.steps; ++k) {
-    const double a = ns.coefficients[3 * k], b = ns.coefficients[3 * k + 1], c = ns.coefficients[3 * k + 2];
-    if (!std::isfinite(a) || !std::isfinite(b) || !std::isfinite(c)) return false;
-    const double square = bound * bound, q = most(square, [&](double l) { return b * l + c * l * l; });
-    // The first X is stored up to a factor 1 < g <= 2 smaller than its norm says: P's entries are smaller for it, Q's larger.
-    plans.push_back({(float)a, (float)b, (float)c, exponent(bound), exponent(square), exponent(k == 0 ? 2 * q : q)});
-    bound = most(bound, [&](double x) { return x * (a + x * x * (b + x * x * c)); });
-    if (!(bound <= kLargestBound) || !(q <= kLargestBound)) return false;
+  for (int k = 0, from = 0; k < ns.steps; from ^= 1) {
+    const int steps = std::min(group, ns.steps - k), ex = exponent(bound);
+    const bool first = k == 0;
+    // The first X is stored up to a factor 1 < g <= 2 smaller than it is: A's entries are smaller for it, those with a factor g larger.
+    const double g = first ? 2.0 : 1.0;
+    auto factor = [&](int which) { return first ? which : -1; };  // of g: its first, second, third and fifth power
+    std::vector<double> x(kPoints), poly(kPoints), rest(kPoints), now(kPoints);  // singular values, what B, R and a result have for them
+    for (int i = 0; i < kPoints; ++i) x[i] = bound * i / (kPoints - 1);
+    bool bounded = true;
+    auto result = [&](int which, double scale) {
+      const double m = scale * most(now);
+      bounded = bounded && m <= kLargestBound;
+      return Held{which, exponent(m)};
+    };
+    auto push = [&](int kind, const Held& r, MuonTerm m, MuonTerm n, MuonTerm coefficient) {
+      out.push_back({kind, from, r.which, first, m, n, coefficient, ex, r.e});
+    };
+    for (int i = 0; i < kPoints; ++i) now[i] = x[i] * x[i];
+    Held A = result(0, 1.0), B{}, R{};
+    push(sffn::kGram, A, none, none, none);
+    double q = 0;
+    for (int j = 0; j < steps; ++j) {
+      const double *const c = ns.coefficients + 3 * (k + j), *const before = c - 3;
+      for (int i = 0; i < 3; ++i)
+        if (!std::isfinite(c[i])) return false;
+      const bool scaled = first && j == 0, was = first && j == 1;  // the coefficients of the very first step come with powers of g
+      if (j > 0) {  // A of the step before to this one's: D = a A + A B, A = a D + D B
+        for (int i = 0; i < kPoints; ++i) now[i] = x[i] * x[i] * (before[0] + poly[i]);
+        const int free = 6 - A.which - B.which - R.which;
+        const Held D = result(j == 1 ? 2 : free, 1.0);
+        push(sffn::kForm, D, with(A, before[0], was ? 0 : -1), with(B, 0, -1), only(1, -1));
+        for (int i = 0; i < kPoints; ++i) {
+          x[i] *= before[0] + poly[i];
+          now[i] = x[i] * x[i];
+        }
+        A = result(A.which, 1.0);
+        push(sffn::kForm, A, with(D, before[0], was ? 0 : -1), with(B, 0, -1), only(1, -1));
+        for (int i = 0; i < kPoints; ++i) now[i] = poly[i] = x[i] * x[i] * (c[1] + x[i] * x[i] * c[2]);
+        B = result(D.which, 1.0);
+      } else {
+        for (int i = 0; i < kPoints; ++i) now[i] = poly[i] = x[i] * x[i] * (c[1] + x[i] * x[i] * c[2]);
+        B = result(1, g);
+      }
+      push(sffn::kForm, B, with(A, c[1], scaled ? 2 : -1), with(A, 0, -1), only(c[2], scaled ? 3 : -1));
+      if (j == 0) {
+        R = B;
+        rest = poly;
+        q = c[0];
+      } else {  // R = q B + a R + R B
+        for (int i = 0; i < kPoints; ++i) now[i] = rest[i] = q * poly[i] + c[0] * rest[i] + rest[i] * poly[i];
+        const Held last = R;
+        R = result(6 - A.which - B.which - R.which, g);
+        push(sffn::kForm, R, with(last, c[0], -1), with(B, q, factor(0)), only(1, -1));
+        q *= c[0];
+      }
+    }
+    const double* const c = ns.coefficients + 3 * (k + steps - 1);
+    for (int i = 0; i < kPoints; ++i) now[i] = x[i] *= c[0] + poly[i];
+    bound = most(now);
+    k += steps;
+    const bool last = k == ns.steps;
+    push(last ? sffn::kLast : sffn::kApply, Held{0, last ? 0 : exponent(bound)}, with(R, 0, -1), none, only(q, factor(0)));
+    if (!bounded || !(bound <= kLargestBound)) return false;
   }
   return true;
 }
 
-int check_ns(const sffn_newton_schulz* ns, std::vector<Plan>& plans) {
+// Steps at a time: one, two, three.  Where the longer side of X is longer than the shorter one, a step in the company of others is four products
+// of S x S instead of two, and saves a Gram matrix and a product with X: 14336 x 4096, bf16, one / two at a time ? / ? us.  Roundings in
+// between are not made good again by the next Gram matrix, and grow: in 16 bits two steps are as exact as one by one but for a factor of
+// two where singular values are far apart, three are not; with operands in two terms three are (2^-11 of the errors).
+struct Plans {
+  Products of[3];
+};
+// What follows from coefficients alone takes half a millisecond: a thread keeps what its last ones gave.
+int check_ns(const sffn_newton_schulz* ns, const Plans** plans) {
   if (!ns || ns->steps < 1 || ns->steps > SFFN_NS_MAX_STEPS || !ns->coefficients || !(ns->eps >= 0) || std::isinf(ns->eps)) return SFFN_ERR_INVALID_ARG;
   if (ns->bits != 0 && ns->bits != 16 && ns->bits != 32) return SFFN_ERR_INVALID_ARG;
-  return make_plans(*ns, plans) ? SFFN_OK : SFFN_ERR_INVALID_ARG;
+  struct Last {
+    std::vector<double> coefficients;
+    Plans plans;
+  };
+  static thread_local Last last;
+  const size_t n = (size_t)3 * ns->steps;
+  if (last.coefficients.size() != n || std::memcmp(last.coefficients.data(), ns->coefficients, n * sizeof(double)) != 0) {
+    last.coefficients.clear();  // (until the plans are there)
+    for (int i = 0; i < 3; ++i) {
+      last.plans.of[i].clear();
+      if (!make_products(*ns, i + 1, last.plans.of[i])) return SFFN_ERR_INVALID_ARG;
+    }
+    last.coefficients.assign(ns->coefficients, ns->coefficients + n);
+  }
+  *plans = &last.plans;
+  return SFFN_OK;
 }
 
 int check_shape(int rows, int cols) {
@@ -116,9 +202,8 @@ size_t layout(MuonBatch& b, int n, const Matrix& like, char* base) {
     return base ? at : nullptr;
   };
   for (uint16_t*& x : b.x) x = reinterpret_cast<uint16_t*>(take((size_t)b.x_term * 4));
-  b.P = reinterpret_cast<uint16_t*>(take((size_t)b.p_term * 2 * b.terms));
-  b.Q = reinterpret_cast<uint16_t*>(take((size_t)b.p_term * 2 * b.terms));
-  b.diag = reinterpret_cast<float*>(take((size_t)n * b.S * 4));
+  for (uint16_t*& m : b.sym) m = reinterpret_cast<uint16_t*>(take((size_t)b.p_term * 2 * b.terms));
+  b.diag = reinterpret_cast<float*>(take((size_t)4 * n * ((b.S + 15) / 16 * 16) * 4));
   b.first = reinterpret_cast<float*>(take((size_t)n * 16));
   b.squares = reinterpret_cast<double*>(take((size_t)n * sffn::kMuonPartials * 8));
   b.partial = reinterpret_cast<float*>(take(sffn::muon_partial_floats(b.S, b.R, b.C, n, b.terms) * 4));
@@ -158,7 +243,9 @@ bool any_meet(std::vector<Range>& all) {
   return false;
 }
 
-int run(const std::vector<Matrix>& all, const std::vector<Plan>& plans, const MuonBatch& common, void* workspace, cudaStream_t s) {
+int steps_at_a_time(const MuonBatch& b) { return 4 * (int64_t)b.L < 5 * (int64_t)b.S ? 1 : b.terms == 2 ? 3 : 2; }
+
+int run(const std::vector<Matrix>& all, const Plans& plans, const MuonBatch& common, void* workspace, cudaStream_t s) {
   int sms = 0;
   const int rc = sm_count(&sms);
   if (rc != SFFN_OK) return rc;
@@ -168,20 +255,7 @@ int run(const std::vector<Matrix>& all, const std::vector<Plan>& plans, const Mu
     for (size_t i = 0; i < batch.size(); ++i) b.item[i] = batch[i]->item;
     SFFN_CUDA(sffn::launch_muon_moments(b, sms, s));
     SFFN_CUDA(sffn::launch_muon_scale(b, sms, s));
-    for (size_t k = 0; k < plans.size(); ++k) {
-      const Plan& now = plans[k];
-      sffn::MuonProduct p{};
-      p.from = (int)(k & 1);
-      p.first = k == 0;
-      p.last = k + 1 == plans.size();
-      p.a = now.a; p.b = now.b; p.c = now.c;
-      p.ex = now.ex; p.ep = now.ep; p.eq = now.eq;
-      p.ey = p.last ? 0 : plans[k + 1].ex;
-      for (int kind : {sffn::kGram, sffn::kPoly, sffn::kApply}) {
-        p.kind = kind;
-        SFFN_CUDA(sffn::launch_muon_product(b, p, sms, s));
-      }
-    }
+    for (const sffn::MuonProduct& p : plans.of[steps_at_a_time(b) - 1]) SFFN_CUDA(sffn::launch_muon_product(b, p, sms, s));
   }
   return SFFN_OK;
 }
@@ -240,9 +314,9 @@ int matrices_of(const sffn_muon_tensor* t, int n, const sffn_newton_schulz* ns, 
 template <typename T>
 int workspace_bytes(const T* t, int n, const sffn_newton_schulz* ns, size_t* bytes) {
   if (!bytes) return SFFN_ERR_INVALID_ARG;
-  std::vector<Plan> plans;
+  const Plans* plans = nullptr;
   std::vector<Matrix> all;
-  int rc = check_ns(ns, plans);
+  int rc = check_ns(ns, &plans);
   if (rc == SFFN_OK) rc = matrices_of(t, n, ns, all, false);
   if (rc == SFFN_OK) *bytes = workspace_of(all);
   return rc;
@@ -277,9 +351,9 @@ int sffn_muon_workspace_bytes(const sffn_muon_tensor* t, int n, const sffn_newto
 
 int sffn_orthogonalize(const sffn_orthogonal* t, int n, const sffn_newton_schulz* ns, void* workspace, size_t workspace_bytes, int32_t* status, void* stream) {
   return guarded([&]() -> int {
-    std::vector<Plan> plans;
+    const Plans* plans = nullptr;
     std::vector<Matrix> all;
-    int rc = check_ns(ns, plans);
+    int rc = check_ns(ns, &plans);
     if (rc == SFFN_OK) rc = matrices_of(t, n, ns, all, true);
     if (rc == SFFN_OK) rc = check_workspace(all, workspace, workspace_bytes, status);
     if (rc != SFFN_OK) return rc;
@@ -293,16 +367,16 @@ int sffn_orthogonalize(const sffn_orthogonal* t, int n, const sffn_newton_schulz
     MuonBatch common{};
     common.eps = (float)ns->eps;
     common.status = status;
-    return run(all, plans, common, workspace, static_cast<cudaStream_t>(stream));
+    return run(all, *plans, common, workspace, static_cast<cudaStream_t>(stream));
   });
 }
 
 int sffn_muon_step(const sffn_muon_tensor* t, int n, const sffn_muon_config* c, void* workspace, size_t workspace_bytes, int32_t* status, void* stream) {
   return guarded([&]() -> int {
     if (!c) return SFFN_ERR_INVALID_ARG;
-    std::vector<Plan> plans;
+    const Plans* plans = nullptr;
     std::vector<Matrix> all;
-    int rc = check_ns(&c->newton_schulz, plans);
+    int rc = check_ns(&c->newton_schulz, &plans);
     if (rc != SFFN_OK) return rc;
     if (!(c->momentum >= 0 && c->momentum < 1) || (c->grad_norm && !(c->max_norm > 0))) return SFFN_ERR_INVALID_ARG;
     if (!aligned(c->grad_norm, 4)) return SFFN_ERR_UNSUPPORTED;
@@ -327,7 +401,7 @@ int sffn_muon_step(const sffn_muon_tensor* t, int n, const sffn_muon_config* c, 
     common.grad_norm = c->grad_norm;
     common.max_norm = (float)c->max_norm;
     common.status = status;
-    return run(all, plans, common, workspace, static_cast<cudaStream_t>(stream));
+    return run(all, *plans, common, workspace, static_cast<cudaStream_t>(stream));
   });
 }
 

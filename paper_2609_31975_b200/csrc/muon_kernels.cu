@@ -132,8 +132,9 @@ __global__ void __launch_bounds__(kThreads) muon_scale_kernel(const __grid_const
     const double g = some ? scalbn(1.0, kMuonExponent - k) / (norm + (double)b.eps) : norm == 0.0 ? 0.0 : (double)NAN;
     float* const to = b.first + 4 * blockIdx.y;
     to[0] = (float)g;
-    to[1] = (float)(g * g * g);
-    to[2] = (float)(g * g * g * g * g);
+    to[1] = (float)(g * g);
+    to[2] = (float)(g * g * g);
+    to[3] = (float)(g * g * g * g * g);
   }
   const double scale = scalbn(1.0, k);
   bool fine;

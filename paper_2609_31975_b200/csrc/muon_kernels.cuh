@@ -23,8 +23,8 @@ struct MuonItem {
   float decay, rate;    // step: p = decay p - rate O
 };
 
-// A batch of matrices of one shape and the workspace that they share.  X, P and Q are fp16, a value v standing as v 2^e, in one or two
-// terms (hi and what it leaves): X [R, C], P = X X^T (or X^T X) and Q, polynomials of it, [S, S].
+// A batch of matrices of one shape and the workspace that they share.  Matrices are fp16, a value v standing as v 2^e: X [R, C] in two
+// terms (hi and what it leaves), A = X X^T (or X^T X) and polynomials of it [S, S] in `terms`, without their diagonals, which are fp32.
 struct MuonBatch {
   MuonItem item[kMuonBatch];
   int n;                // matrices
@@ -38,24 +38,32 @@ struct MuonBatch {
   // workspace
   int64_t ld_x, ld_p;   // elements
   int64_t x_matrix, p_matrix, x_term, p_term;  // elements between matrices of a batch, and between terms
-  uint16_t *x[2], *P, *Q;
-  float* diag;          // [n, S]: Q's diagonal, which is not in Q
-  float* first;         // [n][4]: what the first step's coefficients are multiplied by: g, g^3, g^5 (X = g times what is stored)
+  uint16_t *x[2], *sym[4];
+  float* diag;          // [4][n, S up to a multiple of 16]: the diagonals of sym
+  float* first;         // [n][4]: g, g^2, g^3, g^5: the first X is g times what is stored
   double* squares;      // [n][kMuonPartials]
   float* partial;       // pieces of tiles that are cut
   int32_t* status;
 };
 
 // A product and its epilogue.
-//   kGram   P = X X^T (X^T X)
-//   kPoly   Q = b P + c P P, its diagonal apart
-//   kApply  X' = (a + diag) X + Q X (X Q); the last one ends in the caller's matrix
-enum { kGram = 0, kPoly = 1, kApply = 2 };
+//   kGram   A = X X^T (X^T X) into sym[out]
+//   kForm   sym[out] = m M + n N + k M N, polynomials of A; out is neither M nor N
+//   kApply  X' = k X + M X (X M); X is x[from], X' the other one
+//   kLast   the same into the caller's matrix
+enum { kGram = 0, kForm = 1, kApply = 2, kLast = 3 };
+__host__ __device__ constexpr bool symmetric(int kind) { return kind == kGram || kind == kForm; }
+struct MuonTerm {
+  int which;            // of sym
+  int e;                // the exponent that it is stored with
+  float c;              // coefficient,
+  int factor;           // and which of the first step's factors multiplies it (-1: none)
+};
 struct MuonProduct {
-  int kind, from;       // from: which of x is X (the other one receives X')
-  bool first, last;
-  float a, b, c;
-  int ex, ep, eq, ey;   // exponents that X, P, Q and X' are stored with
+  int kind, from, out;
+  bool first;           // factors are to be looked at
+  MuonTerm m, n, k;
+  int ex, e_out;        // exponents that X, and the result, are stored with
 };
 
 cudaError_t launch_muon_product(const MuonBatch& b, const MuonProduct& p, int sm_count, cudaStream_t s);

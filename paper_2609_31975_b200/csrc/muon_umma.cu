@@ -1,20 +1,26 @@
 // Products of the Newton-Schulz steps on the 5th-generation tensor cores (tcgen05.mma kind::f16, accumulators in tensor memory).
 //
-// A step is X' = a X + (b P + c P^2) X with P = X X^T on the shorter side: three products, of which P and P^2 are symmetric: their tiles
-// at and below the diagonal are computed, and what lies below it is stored twice.
+// A step is X' = a X + (b A + c A^2) X with A = X X^T on the shorter side S.  Steps in company go on from A instead of X:
+//     B = b A + c A^2,   D = a A + A B,   A' = a D + D B  (= X' X'^T),   B' = b' A' + c' A'^2,   R = a B' + a' B + B B',   X'' = a a' X + R X
+// one product with X for all of them and one Gram matrix, for four products of S x S a step.  All of these are polynomials of A, so
+// symmetric, and each is one form m M + n N + k M N: tiles at and below the diagonal are computed, and what lies below it is stored
+// twice.  (A' = a^2 A + 2 a A B + A B B would lose four bits: its terms are 20 times as large as what is left of them.)
 //
-// Operands are fp16, not bf16: the matrices are scaled (powers of two; a bound on every one's entries follows from the coefficients), so
+// Operands are fp16, not bf16: matrices are scaled (powers of two; a bound on every one's entries follows from the coefficients), so
 // the exponent range is not needed, and eleven bits are eight times as exact at the same rate.  What would be amplified is kept out
 // of sixteen bits: singular values far below the largest grow by a in every step, 485 times in five, and with them the rounding of a X.
-// So X is held in two terms, hi + lo, and only the products take hi; and Q's diagonal, its largest entries, goes with a X, in fp32.
-// (64-bit model, 1344 x 384, error against exact, norm by norm: Gaussian 7.6e-4, of rank 16 1.0e-3, dying singular values 2e-4 to 5e-4; with
-// a X from one term rank 16 2.9e-2, with bf16 operands 1.2e-2 and 0.24.)  Where results are wanted in 32 bits, every operand enters in two
-// terms: hi hi in runs of eight K blocks, which are added up in registers because the tensor cores truncate when they add onto an
-// accumulator, and hi lo + lo hi in an accumulator of their own.
+// So X is held in two terms, hi + lo, and only the products take hi.  And every symmetric matrix is held as its diagonal, in fp32, and the
+// rest: diagonals are the largest entries by far, and what they contribute to a product is added in the epilogue.
+// (64-bit model, 1344 x 384, error against exact, norm by norm, steps one by one / in pairs: Gaussian 6e-4 / 5e-4, of rank 16 1.2e-3 / 2.2e-3,
+// singular values dying away 3e-4 to 5e-4 / 6e-4 to 8e-4, half of them small 2e-3 / 3.6e-3; with a X from one term rank 16 2.9e-2, with bf16 operands 1.2e-2 and 0.24.)
+// Where results are wanted in 32 bits, every operand enters in two terms: hi hi in runs of eight K blocks, which are added up in registers
+// because the tensor cores truncate when they add onto an accumulator, and hi lo + lo hi in an accumulator of their own.
 //
-// A pair of CTAs (cta_group::2) owns 256 rows; one term: 512 columns, two accumulators, 48 KB a K block of 64 in four stages; two terms: 256
-// columns, 64 KB in three.  X is used as it lies: X^T X takes MN-major boxes, X X^T K-major ones.  Epilogues go from tensor memory through
-// registers straight to memory, a lane a row, sixteen columns (32 bytes) at a time; what they read is under way one step ahead.
+// A pair of CTAs (cta_group::2) owns 256 rows; one term: 512 columns, two accumulators, 48 KB a K block of 64 in four stages, and eight
+// epilogue warps for each accumulator, as both hold the next tile up; two terms: 256 columns, 64 KB in three stages, eight epilogue warps
+// that add up the runs and finish the tile from their registers under the next one.  X is used as it lies: X^T X takes MN-major boxes,
+// X X^T K-major ones.  Epilogues go from tensor memory through registers straight to memory, a lane a row, sixteen columns (32 bytes)
+// at a time.
 //
 // Tiles are dealt to the pairs round robin; what is left for a last, partly idle round is cut along K where that is shorter, and
 // muon_join_kernel adds up the pieces in their order and does the epilogue.  Every wait is bounded by a cycle budget; on expiry the status
@@ -36,8 +42,7 @@ using namespace tc;
 constexpr int kRows = 256;                   // of a pair's tile
 constexpr int kDeep = 64;                    // fp16 elements of a 128-byte swizzle row: a K block
 constexpr int kBlockBytes = 128 * kDeep * 2; // 128 rows of a K block
-constexpr int kThreads = 384;
-constexpr int kEpilogueWarps = 8;            // warps 4-11
+constexpr int kEpilogueWarps = 8;            // of an accumulator
 constexpr int kRun = 8;                      // two terms: K blocks of a run
 
 template <int TERMS>
@@ -47,6 +52,7 @@ struct Form {
   static constexpr int kStages = TERMS == 1 ? 4 : 3;
   static constexpr int kStageBytes = TERMS == 1 ? 3 * kBlockBytes : 4 * kBlockBytes;
   static constexpr int kSmemBytes = kStages * kStageBytes + 1024;
+  static constexpr int kThreads = 128 + 32 * kEpilogueWarps * kWide;  // warps 4 and on: epilogue
 };
 
 struct Maps {
@@ -64,17 +70,24 @@ struct Params {
   long long budget;
   int drop;                       // test hook: a K block whose rows of A CTA 0 leaves out (-1: none)
   // epilogue
-  int tall, first, last;
-  float a, b, c;                  // of what is stored: alpha for kGram in c
-  const float* factors;           // first step: [n][4]
-  float x_scale, acc_scale;       // kApply: of a X, and of the accumulator
-  float diag_scale;               // kPoly: from Q as stored to Q
-  const uint16_t* in;             // kPoly: P; kApply: X
-  uint16_t* out;                  // kGram: P; kPoly: Q; kApply: X'
-  int64_t ld, matrix, term;       // of both
-  float* diag;
+  int tall, first;
+  const float* factors;           // first step: [n][4], powers of g: 1, 2, 3, 5
   int S;
-  // last step
+  uint16_t* out;                  // symmetric: the result; kApply: X'
+  float* out_diag;
+  int64_t ld, matrix, term;       // of X, or of the symmetric matrices
+  // symmetric: off the diagonal out = (m + k_m d_N[j]) M + (n + k_n d_M[i]) N + k acc (coefficients as values are stored)
+  const uint16_t *M_, *N_;        // N NULL where it is M
+  const float *M_diag, *N_diag;
+  float m, nn, k_m, k_n, k;
+  float dm, dn, dk, dacc;         // the diagonal (as it is): dm d_M + dn d_N + dk (d_M d_N + dacc acc)
+  int fm, fn, fk;                 // first step: which factor the terms in m, n, k take (-1: none)
+  // kApply, kLast: X' = (q + d) x_scale X + acc_scale acc
+  const uint16_t* X;
+  const float* diag;
+  float q, x_scale, acc_scale;
+  int fq;
+  // kLast
   int step, out_bf16;
   const float* grad_norm;
   MuonItem item[kMuonBatch];
@@ -90,7 +103,7 @@ __device__ __forceinline__ Place place_of(const Params& p, int tile) {
   Place at;
   at.batch = tile / p.per;
   tile -= at.batch * p.per;
-  if constexpr (KIND != kApply) {
+  if constexpr (symmetric(KIND)) {
     if constexpr (WIDE == 1) {
       int m = (int)((sqrtf(8.f * tile + 1.f) - 1.f) * 0.5f);
       while (m * (m + 1) / 2 > tile) --m;
@@ -118,7 +131,7 @@ __device__ __forceinline__ Place place_of(const Params& p, int tile) {
 template <int KIND, int WIDE>
 __device__ __forceinline__ int halves_of(const Params& p, const Place& at) {
   if (WIDE == 1) return 1;
-  if (KIND != kApply) return 2 * at.n + 1 <= at.m ? 2 : 1;
+  if (symmetric(KIND)) return 2 * at.n + 1 <= at.m ? 2 : 1;
   return at.n * 512 + 256 < p.N ? 2 : 1;
 }
 
@@ -152,98 +165,118 @@ struct Walk {
 
 // ---- epilogue: sixteen columns from n0 on of the row m = row0 + lane ------------------------------------------------
 
-__device__ __forceinline__ void half8(const uint4& w, float* f) {
-  const uint32_t u[4] = {w.x, w.y, w.z, w.w};
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const float2 v = __half22float2(*reinterpret_cast<const __half2*>(&u[i]));
-    f[2 * i] = v.x;
-    f[2 * i + 1] = v.y;
-  }
-}
+// Two fp16 in a word, and sixteen of them in two vectors.
 __device__ __forceinline__ uint32_t two_halves(float lo, float hi) {
   const __half2 v = __floats2half2_rn(lo, hi);
   return *reinterpret_cast<const uint32_t*>(&v);
 }
-__device__ __forceinline__ float rest_of_half(float v) { return v - __half2float(__float2half_rn(v)); }
-__device__ __forceinline__ void put16(uint16_t* to, const float* v) {  // 32 bytes
+__device__ __forceinline__ float2 from_halves(uint32_t w) { return __half22float2(*reinterpret_cast<const __half2*>(&w)); }
+struct Sixteen {
   uint32_t w[8];
+  __device__ __forceinline__ void load(const uint16_t* from) {  // 32 bytes
+    asm volatile("ld.global.v8.b32 {%0,%1,%2,%3,%4,%5,%6,%7}, [%8];"
+                 : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]), "=r"(w[4]), "=r"(w[5]), "=r"(w[6]), "=r"(w[7])
+                 : "l"(from)
+                 : "memory");
+  }
+  __device__ __forceinline__ void store(uint16_t* to) const {
+    asm volatile("st.global.v8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};" ::"l"(to), "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3]), "r"(w[4]), "r"(w[5]), "r"(w[6]), "r"(w[7])
+                 : "memory");
+  }
+  __device__ __forceinline__ void pack(const float* v) {
 #pragma unroll
-  for (int i = 0; i < 8; ++i) w[i] = two_halves(v[2 * i], v[2 * i + 1]);
-  asm volatile("st.global.v8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};" ::"l"(to), "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3]), "r"(w[4]), "r"(w[5]), "r"(w[6]),
-               "r"(w[7])
-               : "memory");
-}
-__device__ __forceinline__ void get32(const void* from, uint4* w) {  // 32 bytes
-  asm volatile("ld.global.v8.b32 {%0,%1,%2,%3,%4,%5,%6,%7}, [%8];"
-               : "=r"(w[0].x), "=r"(w[0].y), "=r"(w[0].z), "=r"(w[0].w), "=r"(w[1].x), "=r"(w[1].y), "=r"(w[1].z), "=r"(w[1].w)
-               : "l"(from)
-               : "memory");
-}
-
-// What a chunk's epilogue reads, under way while the one before is worked on.
-struct Ahead {
-  uint4 hi[2], lo[2];
-  uint4 w[4];      // last step: the parameter, sixteen fp32 or bf16
-  float d;         // the diagonal: lane l has column n0 + l's (tall), or its row's
+    for (int i = 0; i < 8; ++i) w[i] = two_halves(v[2 * i], v[2 * i + 1]);
+  }
+  // v - what this holds
+  __device__ __forceinline__ void rest(const float* v, float* r) const {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const float2 f = from_halves(w[i]);
+      r[2 * i] = v[2 * i] - f.x;
+      r[2 * i + 1] = v[2 * i + 1] - f.y;
+    }
+  }
 };
-// Whether a row of the caller's can be read and written sixteen columns at a time.
-__device__ __forceinline__ bool wide_row(const void* p, int bytes) { return (reinterpret_cast<uintptr_t>(p) & (bytes - 1)) == 0; }
-
-template <int KIND, int TERMS>
-__device__ __forceinline__ void load_ahead(const Params& p, int batch, int m, int n0, int lane, Ahead& t) {
-  if constexpr (KIND == kGram) return;
-  const bool row = m < p.M && n0 < p.N;
-  if (row) {
-    const uint16_t* from = p.in + batch * p.matrix + (int64_t)m * p.ld + n0;
-    get32(from, t.hi);
-    if (KIND == kApply || TERMS == 2) get32(from + p.term, t.lo);
-  }
-  if constexpr (KIND == kApply) {
-    const float* d = p.diag + (int64_t)batch * p.S;
-    t.d = 0.f;
-    if (p.tall) {
-      if (lane < 16 && n0 + lane < p.N) t.d = d[n0 + lane];
-    } else if (m < p.M) {
-      t.d = d[m];
-    }
-    if (p.last && p.step && row && n0 + 16 <= p.N) {
-      const MuonItem& it = p.item[batch];
-      const int64_t at = (int64_t)m * it.ld_out + n0;
-      if (it.master || !p.out_bf16) {
-        const float* w = (it.master ? it.master : static_cast<float*>(it.out)) + at;
-        if (wide_row(w, 32)) {
-          get32(w, t.w);
-          get32(w + 8, t.w + 2);
-        }
-      } else {
-        const uint16_t* w = static_cast<uint16_t*>(it.out) + at;
-        if (wide_row(w, 32)) get32(w, t.w);
-      }
-    }
+// Sixteen numbers of a vector, from n0 on; past its end anything.  (All lanes read the same: the diagonal is padded to a multiple of 16.)
+__device__ __forceinline__ void columns16(const float* from, float* d) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const float4 f = __ldcg(reinterpret_cast<const float4*>(from) + i);
+    d[4 * i] = f.x; d[4 * i + 1] = f.y; d[4 * i + 2] = f.z; d[4 * i + 3] = f.w;
   }
 }
+__device__ __forceinline__ int64_t diag_ld(int S) { return (S + 15) / 16 * 16; }
+__device__ __forceinline__ float factor(const Params& p, int batch, int which) { return p.first && which >= 0 ? p.factors[4 * batch + which] : 1.f; }
 
+// What a chunk's epilogue reads of the matrices in sixteen bits.
+template <int KIND, int TERMS>
+struct Ahead {
+  static constexpr int kTiles = KIND == kForm ? 2 * TERMS : symmetric(KIND) ? 1 : 2;
+  Sixteen t[kTiles];
+  __device__ __forceinline__ void load(const Params& p, int batch, int m, int n0) {
+    if (KIND == kGram || m >= p.M || n0 >= p.N) return;
+    const int64_t at = batch * p.matrix + (int64_t)m * p.ld + n0;
+    if constexpr (KIND == kForm) {
+#pragma unroll
+      for (int q = 0; q < TERMS; ++q) {
+        t[q].load(p.M_ + at + q * p.term);
+        if (p.N_) t[TERMS + q].load(p.N_ + at + q * p.term);
+      }
+    } else {
+      t[0].load(p.X + at);
+      t[1].load(p.X + at + p.term);
+    }
+  }
+};
+
+// Whether a row of the caller's can be read and written sixteen columns at a time.
+__device__ __forceinline__ bool wide_row(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 31) == 0; }
 __device__ __forceinline__ uint32_t two_bf16(float lo, float hi) {
   const __nv_bfloat162 v = __floats2bfloat162_rn(lo, hi);
   return *reinterpret_cast<const uint32_t*>(&v);
 }
-__device__ __forceinline__ void out_bf16(uint16_t* to, const float* v, int count) {
-  if (count == 16 && wide_row(to, 32)) {
-    uint32_t w[8];
+__device__ __forceinline__ void row_in(const float* from, float* v, int count) {
+  if (count == 16 && wide_row(from)) {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) w[i] = two_bf16(v[2 * i], v[2 * i + 1]);
-    asm volatile("st.global.v8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};" ::"l"(to), "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3]), "r"(w[4]), "r"(w[5]), "r"(w[6]),
-                 "r"(w[7])
-                 : "memory");
+    for (int h = 0; h < 2; ++h)
+      asm volatile("ld.global.v8.f32 {%0,%1,%2,%3,%4,%5,%6,%7}, [%8];"
+                   : "=f"(v[8 * h]), "=f"(v[8 * h + 1]), "=f"(v[8 * h + 2]), "=f"(v[8 * h + 3]), "=f"(v[8 * h + 4]), "=f"(v[8 * h + 5]), "=f"(v[8 * h + 6]),
+                     "=f"(v[8 * h + 7])
+                   : "l"(from + 8 * h)
+                   : "memory");
+  } else {
+#pragma unroll
+    for (int i = 0; i < 16; ++i) v[i] = i < count ? from[i] : 0.f;
+  }
+}
+__device__ __forceinline__ void row_in(const uint16_t* from, float* v, int count) {  // bf16
+  if (count == 16 && wide_row(from)) {
+    Sixteen t;
+    t.load(from);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      v[2 * i] = __uint_as_float(t.w[i] << 16);
+      v[2 * i + 1] = __uint_as_float(t.w[i] & 0xffff0000u);
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < 16; ++i) v[i] = i < count ? __uint_as_float((uint32_t)from[i] << 16) : 0.f;
+  }
+}
+__device__ __forceinline__ void row_out(uint16_t* to, const float* v, int count) {  // bf16
+  if (count == 16 && wide_row(to)) {
+    Sixteen t;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) t.w[i] = two_bf16(v[2 * i], v[2 * i + 1]);
+    t.store(to);
   } else {
 #pragma unroll
     for (int i = 0; i < 16; ++i)
       if (i < count) to[i] = __bfloat16_as_ushort(__float2bfloat16_rn(v[i]));
   }
 }
-__device__ __forceinline__ void out_f32(float* to, const float* v, int count) {
-  if (count == 16 && wide_row(to, 32)) {
+__device__ __forceinline__ void row_out(float* to, const float* v, int count) {
+  if (count == 16 && wide_row(to)) {
 #pragma unroll
     for (int h = 0; h < 2; ++h)
       asm volatile("st.global.v8.f32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};" ::"l"(to + 8 * h), "f"(v[8 * h]), "f"(v[8 * h + 1]), "f"(v[8 * h + 2]),
@@ -255,119 +288,149 @@ __device__ __forceinline__ void out_f32(float* to, const float* v, int count) {
       if (i < count) to[i] = v[i];
   }
 }
-
 // The caller's sixteen entries: O itself, or p = decay p - rate O.
-__device__ __forceinline__ void finish_last(const Params& p, int batch, int m, int n0, float* v, const Ahead& t) {
+__device__ __forceinline__ void finish_last(const Params& p, int batch, int m, int n0, float* v) {
   const MuonItem& it = p.item[batch];
   const int count = min(16, p.N - n0);
   const int64_t at = (int64_t)m * it.ld_out + n0;
   if (p.step) {
     if (p.grad_norm && !isfinite(*p.grad_norm)) return;
     float w[16];
-    const bool f32 = it.master || !p.out_bf16;
-    float* const wide = (it.master ? it.master : static_cast<float*>(it.out)) + at;
-    uint16_t* const narrow = static_cast<uint16_t*>(it.out) + at;
-    const bool had = count == 16 && wide_row(f32 ? static_cast<const void*>(wide) : narrow, 32);
-    if (f32) {
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        w[4 * i] = __uint_as_float(t.w[i].x); w[4 * i + 1] = __uint_as_float(t.w[i].y);
-        w[4 * i + 2] = __uint_as_float(t.w[i].z); w[4 * i + 3] = __uint_as_float(t.w[i].w);
-      }
-    } else {
-      Elem<__nv_bfloat16>::unpack(t.w[0], w);
-      Elem<__nv_bfloat16>::unpack(t.w[1], w + 8);
-    }
-    if (!had) {
-#pragma unroll
-      for (int i = 0; i < 16; ++i)
-        if (i < count) w[i] = f32 ? wide[i] : __uint_as_float((uint32_t)narrow[i] << 16);
-    }
+    if (it.master) row_in(it.master + at, w, count);
+    else if (p.out_bf16) row_in(static_cast<const uint16_t*>(it.out) + at, w, count);
+    else row_in(static_cast<const float*>(it.out) + at, w, count);
 #pragma unroll
     for (int i = 0; i < 16; ++i) v[i] = fmaf(-it.rate, v[i], it.decay * w[i]);
-    if (it.master) out_f32(it.master + at, v, count);
+    if (it.master) row_out(it.master + at, v, count);
   }
-  if (p.out_bf16) out_bf16(static_cast<uint16_t*>(it.out) + at, v, count);
-  else out_f32(static_cast<float*>(it.out) + at, v, count);
+  if (p.out_bf16) row_out(static_cast<uint16_t*>(it.out) + at, v, count);
+  else row_out(static_cast<float*>(it.out) + at, v, count);
+}
+
+// Sixteen entries of row m, columns n0 and on, once more where they mirror: rows n0 + i, column m.  Lanes in pairs put two rows' entries of a
+// column together.  All lanes of a warp come here.
+__device__ __forceinline__ void mirror(const Params& p, uint16_t* out, int m, int n0, int lane, const Sixteen& t) {
+  const bool odd = lane & 1, two = (m | 1) < p.M, one = m < p.M;  // (of a last, single row its lane stores both columns alone)
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    const uint32_t other = __shfl_xor_sync(0xffffffffu, t.w[i], 1);
+    const int n = n0 + 2 * i + odd;
+    if (two) {
+      if (n < p.N) *reinterpret_cast<uint32_t*>(out + (int64_t)n * p.ld + (m & ~1)) = odd ? __byte_perm(other, t.w[i], 0x7632) : __byte_perm(t.w[i], other, 0x5410);
+    } else if (one) {
+      if (n < p.N) out[(int64_t)n * p.ld + m] = (uint16_t)t.w[i];
+      if (n + 1 < p.N) out[(int64_t)(n + 1) * p.ld + m] = (uint16_t)(t.w[i] >> 16);
+    }
+  }
 }
 
 // v: the accumulators of these sixteen columns.  All lanes of a warp come here together.
 template <int KIND, int TERMS>
-__device__ __forceinline__ void finish(const Params& p, int batch, int row0, int n0, int lane, float* v, const Ahead& t) {
+__device__ __forceinline__ void finish(const Params& p, int batch, int row0, int n0, int lane, float* v, const Ahead<KIND, TERMS>& a) {
   const int m = row0 + lane;
   const bool row = m < p.M;
-  if constexpr (KIND == kApply) {
-    const float a = p.first ? p.a * p.factors[4 * batch] : p.a;
-    float hi[16], lo[16];
-    half8(t.hi[0], hi);
-    half8(t.hi[1], hi + 8);
-    half8(t.lo[0], lo);
-    half8(t.lo[1], lo + 8);
+  if constexpr (!symmetric(KIND)) {
+    const float q = p.q * factor(p, batch, p.fq);
+    const float* const diag = p.diag + batch * diag_ld(p.S);
+    float d[16];
+    if (p.tall) {
+      columns16(diag + n0, d);
+    } else {
+      const float own = row ? __ldcg(diag + m) : 0.f;
 #pragma unroll
-    for (int i = 0; i < 16; ++i) {
-      const float d = p.tall ? __shfl_sync(0xffffffffu, t.d, i) : t.d;
-      v[i] = fmaf((a + d) * p.x_scale, hi[i] + lo[i], v[i] * p.acc_scale);
+      for (int i = 0; i < 16; ++i) d[i] = own;
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const float2 hi = from_halves(a.t[0].w[i]), lo = from_halves(a.t[1].w[i]);
+      v[2 * i] = fmaf((q + d[2 * i]) * p.x_scale, hi.x + lo.x, v[2 * i] * p.acc_scale);
+      v[2 * i + 1] = fmaf((q + d[2 * i + 1]) * p.x_scale, hi.y + lo.y, v[2 * i + 1] * p.acc_scale);
     }
     if (!row) return;
-    if (p.last) {
-      finish_last(p, batch, m, n0, v, t);
-      return;
+    if constexpr (KIND == kLast) {
+      finish_last(p, batch, m, n0, v);
+    } else {
+      uint16_t* const out = p.out + batch * p.matrix + (int64_t)m * p.ld + n0;
+      Sixteen t;
+      float r[16];
+      t.pack(v);
+      t.rest(v, r);
+      t.store(out);
+      t.pack(r);
+      t.store(out + p.term);
     }
   } else {
-    float scale = p.c, linear = p.b;
-    if (KIND == kPoly && p.first) {
-      linear *= p.factors[4 * batch + 1];
-      scale *= p.factors[4 * batch + 2];
-    }
-#pragma unroll
-    for (int i = 0; i < 16; ++i) v[i] *= scale;
-    if constexpr (KIND == kPoly) {
-      float f[16];
-      half8(t.hi[0], f);
-      half8(t.hi[1], f + 8);
-      if constexpr (TERMS == 2) {
-        float lo[16];
-        half8(t.lo[0], lo);
-        half8(t.lo[1], lo + 8);
-#pragma unroll
-        for (int i = 0; i < 16; ++i) f[i] += lo[i];
-      }
-#pragma unroll
-      for (int i = 0; i < 16; ++i) v[i] = fmaf(linear, f[i], v[i]);
+    const bool on_diagonal = (n0 >> 5) == (row0 >> 5);
+    float own = 0.f;  // of the diagonal: this row's accumulator
+    if (on_diagonal) {
 #pragma unroll
       for (int i = 0; i < 16; ++i)
-        if (n0 + i == m && row) {
-          p.diag[(int64_t)batch * p.S + m] = v[i] * p.diag_scale;
-          v[i] = 0.f;
-        }
+        if (n0 + i == m) own = v[i];
     }
-  }
-  uint16_t* const out = p.out + batch * p.matrix;
-  if (row) {
-    put16(out + (int64_t)m * p.ld + n0, v);
-    if (KIND == kApply || TERMS == 2) {
-      float r[16];
+    if constexpr (KIND == kGram) {
+      if (on_diagonal && row && m >= n0 && m < n0 + 16) p.out_diag[batch * diag_ld(p.S) + m] = own * p.dacc;
 #pragma unroll
-      for (int i = 0; i < 16; ++i) r[i] = rest_of_half(v[i]);
-      put16(out + p.term + (int64_t)m * p.ld + n0, r);
-    }
-  }
-  if constexpr (KIND != kApply) {
-    if (row && (n0 >> 5) < (row0 >> 5)) {  // below the diagonal: the same above it
+      for (int i = 0; i < 16; ++i) v[i] *= p.k;
+    } else {
+      const int64_t line = batch * diag_ld(p.S);
+      const float fm = factor(p, batch, p.fm), fk = factor(p, batch, p.fk);
+      const float d_m = row ? __ldcg(p.M_diag + line + m) : 0.f;
+      if (on_diagonal && row && m >= n0 && m < n0 + 16) {
+        const float d_n = __ldcg(p.N_diag + line + m);
+        p.out_diag[line + m] = p.dm * fm * d_m + p.dn * factor(p, batch, p.fn) * d_n + p.dk * fk * fmaf(own, p.dacc, d_m * d_n);
+      }
+      // M = N: their entry once, times m + k (d_M[i] + d_M[j])
+      const float fixed = p.m * fm, by_row = p.k_n * fk * d_m, each = p.k_m * fk, scale = p.k * fk;
+      const float mm = p.N_ ? fixed : fixed + by_row, nn = p.nn * factor(p, batch, p.fn) + by_row;
+      float d[16];
+      columns16(p.N_diag + line + n0, d);
 #pragma unroll
       for (int i = 0; i < 16; ++i) {
-        if (n0 + i >= p.N) continue;
-        uint16_t* const to = out + (int64_t)(n0 + i) * p.ld + m;
-        *to = __half_as_ushort(__float2half_rn(v[i]));
-        if (TERMS == 2) to[p.term] = __half_as_ushort(__float2half_rn(rest_of_half(v[i])));
+        v[i] *= scale;
+        d[i] = fmaf(each, d[i], mm);
       }
+#pragma unroll
+      for (int q = 0; q < TERMS; ++q) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          const float2 f = from_halves(a.t[q].w[i]);
+          v[2 * i] = fmaf(d[2 * i], f.x, v[2 * i]);
+          v[2 * i + 1] = fmaf(d[2 * i + 1], f.y, v[2 * i + 1]);
+        }
+        if (p.N_) {
+#pragma unroll
+          for (int i = 0; i < 8; ++i) {
+            const float2 f = from_halves(a.t[TERMS + q].w[i]);
+            v[2 * i] = fmaf(nn, f.x, v[2 * i]);
+            v[2 * i + 1] = fmaf(nn, f.y, v[2 * i + 1]);
+          }
+        }
+      }
+    }
+    if (on_diagonal) {
+#pragma unroll
+      for (int i = 0; i < 16; ++i)
+        if (n0 + i == m) v[i] = 0.f;
+    }
+    uint16_t* const out = p.out + batch * p.matrix;
+    const bool twice = (n0 >> 5) < (row0 >> 5);
+    Sixteen t;
+    t.pack(v);
+    if (row) t.store(out + (int64_t)m * p.ld + n0);
+    if (twice) mirror(p, out, m, n0, lane, t);
+    if constexpr (TERMS == 2) {
+      float r[16];
+      t.rest(v, r);
+      t.pack(r);
+      if (row) t.store(out + p.term + (int64_t)m * p.ld + n0);
+      if (twice) mirror(p, out + p.term, m, n0, lane, t);
     }
   }
 }
 // Whether a chunk is there to be computed.
 template <int KIND>
 __device__ __forceinline__ bool wanted(const Params& p, int row0, int n0) {
-  return n0 < p.N && (KIND == kApply || (n0 >> 5) <= (row0 >> 5));
+  return n0 < p.N && (!symmetric(KIND) || (n0 >> 5) <= (row0 >> 5));
 }
 
 __device__ __forceinline__ void put_piece(float* at, const float* v) {
@@ -383,7 +446,7 @@ __device__ __forceinline__ uint32_t idesc_f16(int m, int n, bool a_mn, bool b_mn
 }
 
 template <int KIND, int TERMS>
-__global__ void __launch_bounds__(kThreads, 1) muon_umma_kernel(const __grid_constant__ Params p, const __grid_constant__ Maps maps) {
+__global__ void __launch_bounds__(Form<TERMS>::kThreads, 1) muon_umma_kernel(const __grid_constant__ Params p, const __grid_constant__ Maps maps) {
   using F = Form<TERMS>;
   constexpr int kStages = F::kStages;
   extern __shared__ uint8_t smem_raw[];
@@ -417,13 +480,14 @@ __global__ void __launch_bounds__(kThreads, 1) muon_umma_kernel(const __grid_con
   fence_after();
   const uint32_t tmem = tmem_slot;
   // a step's last launch writes parameters, which calls of the inference side read before they wait: nothing starts early behind it
-  if (!(p.last && p.step && p.whole == p.tiles)) pdl_launch_dependents();
+  if (!(KIND == kLast && p.step && p.whole == p.tiles)) pdl_launch_dependents();
   pdl_wait();
 
   Walk walk(pairs, pair);
   Item it;
   auto wait_all = [&](uint32_t bar, uint32_t parity) { return __all_sync(0xffffffffu, mbar_wait(bar, parity, abort_flag, p.status, p.budget)) != 0; };
 
+  if (TERMS == 2 && warp < 4) asm volatile("setmaxnreg.dec.sync.aligned.u32 56;");  // 4 x 56 + 8 x 224 = 12 x 168, as launched
   if (warp == 0) {
     int s = 0, phase = 0, left_out = blockIdx.x == 0 ? p.drop : -1;
     bool ok = true;
@@ -532,16 +596,16 @@ __global__ void __launch_bounds__(kThreads, 1) muon_umma_kernel(const __grid_con
       }
     }
   } else if (warp >= 4) {
-    const int quad = warp & 3, half = (warp - 4) >> 2;
+    if constexpr (TERMS == 2) asm volatile("setmaxnreg.inc.sync.aligned.u32 224;");
+    const int quad = warp & 3, part = ((warp - 4) >> 2) & 1, own = (warp - 4) >> 3;  // lanes, columns, accumulator
     const uint32_t lanes = (uint32_t)(32 * quad) << 16;
-    constexpr int kChunks = 8;  // of sixteen columns, of a warp and accumulator
-    const uint32_t empty0 = map_rank(acc_empty, 0);
-    int full_phase[2] = {0, 0};
+    constexpr int kChunks = 8;  // of sixteen columns, of a warp
+    const uint32_t empty0 = map_rank(acc_empty, 0), acc = tmem + lanes + own * 256 + 128 * part;
+    int full_phase = 0;
     bool ok = true;
-    auto wait_full = [&](int buffer) {
-      const bool there = wait_all(acc_full + 8 * buffer, buffer ? full_phase[1] : full_phase[0]);
-      if (buffer) full_phase[1] ^= 1;
-      else full_phase[0] ^= 1;
+    auto wait_full = [&]() {
+      const bool there = wait_all(acc_full + 8 * own, full_phase);
+      full_phase ^= 1;
       fence_after();
       return there;
     };
@@ -552,78 +616,87 @@ __global__ void __launch_bounds__(kThreads, 1) muon_umma_kernel(const __grid_con
     };
     while (ok && walk.step(p, it)) {
       const Place at = place_of<KIND, F::kWide>(p, it.tile);
+      if (own >= halves_of<KIND, F::kWide>(p, at)) continue;
       const int row0 = at.m * kRows + rank * 128 + 32 * quad;  // this warp's first row
       const bool rows = row0 < p.M;                            // has any: the others only keep step
-      float* const piece = it.piece < 0 ? nullptr : p.partial + (size_t)it.piece * p.piece + (size_t)(rank * 128 + 32 * quad + lane) * F::kCols;
-      const int halves = halves_of<KIND, F::kWide>(p, at);
+      const int n_base = at.n * F::kCols + 256 * own + 128 * part;
+      float* const piece = it.piece < 0 ? nullptr
+                                        : p.partial + (size_t)it.piece * p.piece + (size_t)(rank * 128 + 32 * quad + lane) * F::kCols + 256 * own + 128 * part;
       if constexpr (TERMS == 2) {
-        float acc[16 * kChunks];
+        float sum[16 * kChunks];
 #pragma unroll
-        for (int i = 0; i < 16 * kChunks; ++i) acc[i] = 0.f;
+        for (int i = 0; i < 16 * kChunks; ++i) sum[i] = 0.f;
 #pragma unroll 1
         for (int u = it.u0; u < it.u1; u += kRun) {
-          ok = wait_full(0);
+          ok = wait_full();
           if (!ok) break;
           if (rows) {
 #pragma unroll
             for (int c = 0; c < kChunks; ++c) {
               float v[16];
-              tmem_ld16(tmem + lanes + 128 * half + 16 * c, v);
+              tmem_ld16(acc + 16 * c, v);
               tmem_arrived(v);
 #pragma unroll
-              for (int i = 0; i < 16; ++i) acc[16 * c + i] += v[i];
+              for (int i = 0; i < 16; ++i) sum[16 * c + i] += v[i];
             }
           }
-          if (u + kRun < it.u1) give_back(0);
+          give_back(0);
         }
         if (!ok) break;
-        // the last run's commit stands for all products of the tile: the small ones are there too.  The sums go back to where the
-        // runs were, as a loop over chunks needs.
+        // the last run's commit stands for all products of the tile: the small ones are there too
         if (rows) {
 #pragma unroll
           for (int c = 0; c < kChunks; ++c) {
             float v[16];
-            tmem_ld16(tmem + 256 + lanes + 128 * half + 16 * c, v);
+            tmem_ld16(acc + 256 + 16 * c, v);
             tmem_arrived(v);
 #pragma unroll
-            for (int i = 0; i < 16; ++i) acc[16 * c + i] += v[i];
-            tmem_st16(tmem + lanes + 128 * half + 16 * c, acc + 16 * c);
+            for (int i = 0; i < 16; ++i) sum[16 * c + i] += v[i];
           }
-          tmem_stored();
         }
         give_back(1);
-      }
-      for (int h = 0; h < halves; ++h) {
-        const int n_base = at.n * F::kCols + 256 * h + 128 * half;
-        Ahead next;
-        if (rows && !piece && wanted<KIND>(p, row0, n_base)) load_ahead<KIND, TERMS>(p, at.batch, row0 + lane, n_base, lane, next);
-        if constexpr (TERMS == 1) {
-          ok = wait_full(h);
-          if (!ok) break;
+        if (!rows) continue;
+        // One copy of the epilogue's code, which takes the first sixteen sums; the others move up.  (Eight copies, each run once a tile, wait
+        // for their instructions: 65 us a tile.)
+#pragma unroll 1
+        for (int c = 0; c < kChunks; ++c) {
+          if (piece) {
+            put_piece(piece + 16 * c, sum);
+          } else if (wanted<KIND>(p, row0, n_base + 16 * c)) {
+            Ahead<KIND, TERMS> a;
+            a.load(p, at.batch, row0 + lane, n_base + 16 * c);
+            finish<KIND, TERMS>(p, at.batch, row0, n_base + 16 * c, lane, sum, a);
+          }
+#pragma unroll
+          for (int i = 0; i < 16 * (kChunks - 1); ++i) sum[i] = sum[i + 16];
         }
-        const uint32_t acc = tmem + lanes + h * 256 + 128 * half;
+      } else {
+        Ahead<KIND, TERMS> next;
+        if (rows && !piece && wanted<KIND>(p, row0, n_base)) next.load(p, at.batch, row0 + lane, n_base);
+        ok = wait_full();
+        if (!ok) break;
         if (rows && piece) {
 #pragma unroll 2
           for (int c = 0; c < kChunks; ++c) {
             float v[16];
             tmem_ld16(acc + 16 * c, v);
             tmem_arrived(v);
-            put_piece(piece + 256 * h + 128 * half + 16 * c, v);
+            put_piece(piece + 16 * c, v);
           }
         } else if (rows) {
 #pragma unroll 1
           for (int c = 0; c < kChunks; ++c) {
             const int n0 = n_base + 16 * c;
             if (!wanted<KIND>(p, row0, n0)) break;  // nor is any further one
-            const Ahead now = next;
+            const Ahead<KIND, TERMS> now = next;
             float v[16];
             tmem_ld16(acc + 16 * c, v);
-            if (c + 1 < kChunks && wanted<KIND>(p, row0, n0 + 16)) load_ahead<KIND, TERMS>(p, at.batch, row0 + lane, n0 + 16, lane, next);
+            if (c + 1 < kChunks && wanted<KIND>(p, row0, n0 + 16)) next.load(p, at.batch, row0 + lane, n0 + 16);
             tmem_arrived(v);
             finish<KIND, TERMS>(p, at.batch, row0, n0, lane, v, now);
           }
         }
-        give_back(h);
+        give_back(own);
       }
     }
   }
@@ -646,7 +719,7 @@ template <int KIND, int TERMS>
 __global__ void __launch_bounds__(32 * kJoinWarps) muon_join_kernel(const __grid_constant__ Params p) {
   using F = Form<TERMS>;
   const int lane = threadIdx.x & 31, number = blockIdx.x * kJoinWarps + (threadIdx.x >> 5);
-  if (!(p.last && p.step)) pdl_launch_dependents();
+  if (!(KIND == kLast && p.step)) pdl_launch_dependents();
   pdl_wait();
   constexpr int kAcross = F::kCols / 16, kPer = kAcross * (kRows / 32);
   const int t = number / kPer, in = number % kPer, r0 = in / kAcross * 32, c0 = in % kAcross * 16;
@@ -654,8 +727,8 @@ __global__ void __launch_bounds__(32 * kJoinWarps) muon_join_kernel(const __grid
   const Place at = place_of<KIND, F::kWide>(p, p.whole + t);
   const int row0 = at.m * kRows + r0, n0 = at.n * F::kCols + c0;
   if (row0 >= p.M || !wanted<KIND>(p, row0, n0)) return;
-  Ahead now;
-  load_ahead<KIND, TERMS>(p, at.batch, row0 + lane, n0, lane, now);
+  Ahead<KIND, TERMS> now;
+  now.load(p, at.batch, row0 + lane, n0);
   float v[16] = {};
   const float* from = p.partial + (size_t)t * p.piece + (size_t)(r0 + lane) * F::kCols + c0;
   const size_t next = (size_t)(p.tiles - p.whole) * p.piece;
@@ -702,7 +775,7 @@ int tiles_of(int kind, int wide, int M, int N, int* m_tiles, int* n_tiles) {
   const int m = (M + kRows - 1) / kRows, n = (N + 256 * wide - 1) / (256 * wide);
   if (m_tiles) *m_tiles = m;
   if (n_tiles) *n_tiles = n;
-  if (kind == kApply) return m * n;
+  if (!symmetric(kind)) return m * n;
   if (wide == 1) return m * (m + 1) / 2;
   return m / 2 * (m / 2 + 1) + (m & 1 ? m / 2 + 1 : 0);
 }
@@ -743,7 +816,14 @@ cudaError_t launch(const MuonBatch& b, Params& p, const Maps& maps, int sm_count
   static unsigned long long configured = 0;
   cudaError_t e = allow_dynamic_smem(muon_umma_kernel<KIND, TERMS>, F::kSmemBytes, configured);
   if (e != cudaSuccess) return e;
-  e = launch_clusters(2, muon_umma_kernel<KIND, TERMS>, dim3(2 * pairs), dim3(kThreads), F::kSmemBytes, s, p, maps);
+  if constexpr (TERMS == 2) {  // the registers that the roles share out have to be there: a warp that asks for more than there are waits for ever
+    static const bool enough = [] {
+      cudaFuncAttributes a;
+      return cudaFuncGetAttributes(&a, muon_umma_kernel<KIND, TERMS>) == cudaSuccess && a.numRegs >= 168;
+    }();
+    if (!enough) return cudaErrorInvalidConfiguration;
+  }
+  e = launch_clusters(2, muon_umma_kernel<KIND, TERMS>, dim3(2 * pairs), dim3(F::kThreads), F::kSmemBytes, s, p, maps);
   if (e != cudaSuccess || p.whole == p.tiles) return e;
   const int warps = (p.tiles - p.whole) * (F::kCols / 16) * (kRows / 32);
   return launch_pdl(muon_join_kernel<KIND, TERMS>, dim3((warps + kJoinWarps - 1) / kJoinWarps), dim3(32 * kJoinWarps), 0, s, p);
@@ -754,7 +834,7 @@ cudaError_t launch(const MuonBatch& b, Params& p, const Maps& maps, int sm_count
 size_t muon_partial_floats(int S, int R, int C, int n, int terms) {
   size_t most = 0;
   const int wide = terms == 1 ? 2 : 1;
-  for (int kind : {kGram, kPoly, kApply}) {
+  for (int kind : {kGram, kForm, kApply}) {
     const long long K = kind == kGram ? (R > C ? R : C) : S, blocks = (K + kDeep - 1) / kDeep;
     const long long tiles = (long long)tiles_of(kind, wide, kind == kApply ? R : S, kind == kApply ? C : S, nullptr, nullptr) * n;
     const long long pieces = blocks < 2 ? 0 : tiles < kMuonPieces && tiles * blocks < kMuonPieces ? tiles * blocks : kMuonPieces;
@@ -769,8 +849,9 @@ cudaError_t launch_muon_product(const MuonBatch& b, const MuonProduct& q, int sm
   p.kind = q.kind;
   p.n = b.n;
   p.S = b.S;
-  p.M = q.kind == kApply ? b.R : b.S;
-  p.N = q.kind == kApply ? b.C : b.S;
+  const bool sym = symmetric(q.kind);
+  p.M = sym ? b.S : b.R;
+  p.N = sym ? b.S : b.C;
   p.K = q.kind == kGram ? b.L : b.S;
   p.partial = b.partial;
   p.status = b.status;
@@ -778,59 +859,74 @@ cudaError_t launch_muon_product(const MuonBatch& b, const MuonProduct& q, int sm
   p.drop = fused_test_knobs().drop_stage;
   p.tall = b.tall;
   p.first = q.first;
-  p.last = q.last;
   p.factors = b.first;
-  p.diag = b.diag;
-  const uint16_t *const X = b.x[q.from];
-  uint16_t* const Y = b.x[q.from ^ 1];
+  p.ld = sym ? b.ld_p : b.ld_x;
+  p.matrix = sym ? b.p_matrix : b.x_matrix;
+  p.term = sym ? b.p_term : b.x_term;
   auto two = [](int e) { return (float)std::ldexp(1.0, e); };
+  auto diag = [&](int i) { return b.diag + (size_t)i * b.n * ((b.S + 15) / 16 * 16); };
+  const uint16_t* const X = b.x[q.from];
   Maps maps;
   bool fine = true;
   for (int t = 0; t < b.terms && fine; ++t) {
-    const uint16_t *const x = X + t * b.x_term, *const P = b.P + t * b.p_term, *const Q = b.Q + t * b.p_term;
+    const uint16_t* const x = X + t * b.x_term;
+    auto square = [&](CUtensorMap* m, int i) { return make_map(m, b.sym[i] + t * b.p_term, b.S, b.S, b.ld_p, b.n, b.p_matrix, 128); };
     if (q.kind == kGram) {  // rows of X are k where it is tall
       fine = make_map(&maps.a[t], x, b.C, b.R, b.ld_x, b.n, b.x_matrix, b.tall ? 64 : 128);
       maps.b[t] = maps.a[t];
       p.a_mn = p.b_mn = b.tall;
-    } else if (q.kind == kPoly) {
-      fine = make_map(&maps.a[t], P, b.S, b.S, b.ld_p, b.n, b.p_matrix, 128);
-      maps.b[t] = maps.a[t];
+    } else if (q.kind == kForm) {
+      fine = square(&maps.a[t], q.m.which) && square(&maps.b[t], q.n.which);
     } else if (b.tall) {
-      fine = make_map(&maps.a[t], x, b.C, b.R, b.ld_x, b.n, b.x_matrix, 128) && make_map(&maps.b[t], Q, b.S, b.S, b.ld_p, b.n, b.p_matrix, 128);
+      fine = make_map(&maps.a[t], x, b.C, b.R, b.ld_x, b.n, b.x_matrix, 128) && square(&maps.b[t], q.m.which);
     } else {
-      fine = make_map(&maps.a[t], Q, b.S, b.S, b.ld_p, b.n, b.p_matrix, 128) && make_map(&maps.b[t], x, b.C, b.R, b.ld_x, b.n, b.x_matrix, 64);
+      fine = square(&maps.a[t], q.m.which) && make_map(&maps.b[t], x, b.C, b.R, b.ld_x, b.n, b.x_matrix, 64);
       p.b_mn = 1;
     }
   }
   if (!fine) return cudaErrorInvalidValue;
   if (b.terms == 1) maps.a[1] = maps.a[0], maps.b[1] = maps.b[0];
   if (q.kind == kGram) {
-    p.c = two(q.ep - 2 * q.ex);
-    p.out = b.P;
-    p.ld = b.ld_p; p.matrix = b.p_matrix; p.term = b.p_term;
+    p.k = two(q.e_out - 2 * q.ex);
+    p.dacc = two(-2 * q.ex);
+    p.out = b.sym[q.out];
+    p.out_diag = diag(q.out);
     return b.terms == 1 ? launch<kGram, 1>(b, p, maps, sm_count, s) : launch<kGram, 2>(b, p, maps, sm_count, s);
   }
-  if (q.kind == kPoly) {
-    p.b = q.b * two(q.eq - q.ep);
-    p.c = q.c * two(q.eq - 2 * q.ep);
-    p.diag_scale = two(-q.eq);
-    p.in = b.P;
-    p.out = b.Q;
-    p.ld = b.ld_p; p.matrix = b.p_matrix; p.term = b.p_term;
-    return b.terms == 1 ? launch<kPoly, 1>(b, p, maps, sm_count, s) : launch<kPoly, 2>(b, p, maps, sm_count, s);
+  if (q.kind == kForm) {
+    const bool same = q.m.which == q.n.which;
+    p.out = b.sym[q.out];
+    p.out_diag = diag(q.out);
+    p.M_ = b.sym[q.m.which];
+    p.M_diag = diag(q.m.which);
+    p.N_ = same ? nullptr : b.sym[q.n.which];
+    p.N_diag = diag(q.n.which);
+    p.m = q.m.c * two(q.e_out - q.m.e);
+    p.nn = q.n.c * two(q.e_out - q.n.e);
+    p.k_m = q.k.c * two(q.e_out - q.m.e);
+    p.k_n = q.k.c * two(q.e_out - q.n.e);
+    p.k = q.k.c * two(q.e_out - q.m.e - q.n.e);
+    p.dm = q.m.c; p.dn = q.n.c; p.dk = q.k.c;
+    p.dacc = two(-q.m.e - q.n.e);
+    p.fm = q.m.factor; p.fn = q.n.factor; p.fk = q.k.factor;
+    return b.terms == 1 ? launch<kForm, 1>(b, p, maps, sm_count, s) : launch<kForm, 2>(b, p, maps, sm_count, s);
   }
-  p.a = q.a;
-  p.x_scale = two((q.last ? 0 : q.ey) - q.ex);
-  p.acc_scale = two((q.last ? 0 : q.ey) - q.ex - q.eq);
-  p.in = X;
-  p.out = Y;
-  p.ld = b.ld_x; p.matrix = b.x_matrix; p.term = b.x_term;
+  const bool last = q.kind == kLast;
+  p.q = q.k.c;
+  p.fq = q.k.factor;
+  p.x_scale = two((last ? 0 : q.e_out) - q.ex);
+  p.acc_scale = two((last ? 0 : q.e_out) - q.ex - q.m.e);
+  p.diag = diag(q.m.which);
+  p.X = X;
+  if (!last) {
+    p.out = b.x[q.from ^ 1];
+    return b.terms == 1 ? launch<kApply, 1>(b, p, maps, sm_count, s) : launch<kApply, 2>(b, p, maps, sm_count, s);
+  }
   p.step = b.step;
   p.out_bf16 = b.out_bf16;
   p.grad_norm = b.grad_norm;
-  if (q.last)
-    for (int i = 0; i < b.n; ++i) p.item[i] = b.item[i];
-  return b.terms == 1 ? launch<kApply, 1>(b, p, maps, sm_count, s) : launch<kApply, 2>(b, p, maps, sm_count, s);
+  for (int i = 0; i < b.n; ++i) p.item[i] = b.item[i];
+  return b.terms == 1 ? launch<kLast, 1>(b, p, maps, sm_count, s) : launch<kLast, 2>(b, p, maps, sm_count, s);
 }
 
 }  // namespace sffn
