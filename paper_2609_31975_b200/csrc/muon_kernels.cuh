@@ -11,7 +11,6 @@ namespace sffn {
 constexpr int kMuonBatch = 64;     // matrices of a launch, at most
 constexpr int kMuonPartials = 256; // partial sums of a matrix's squares, at most
 constexpr int kMuonPairs = 80;     // pairs of CTAs at most
-constexpr int kMuonPieces = 2 * kMuonPairs;  // of tiles that are cut along K, at most
 
 // A matrix as the caller has it.
 struct MuonItem {

@@ -27,6 +27,7 @@
 // word is set, all roles wind down and tensor memory is given back.
 #include <cuda_fp16.h>
 
+#include <algorithm>
 #include <cmath>
 
 #include "common.cuh"
@@ -42,17 +43,24 @@ using namespace tc;
 constexpr int kRows = 256;                   // of a pair's tile
 constexpr int kDeep = 64;                    // fp16 elements of a 128-byte swizzle row: a K block
 constexpr int kBlockBytes = 128 * kDeep * 2; // 128 rows of a K block
-constexpr int kEpilogueWarps = 8;            // of an accumulator
 constexpr int kRun = 8;                      // two terms: K blocks of a run
 
-template <int TERMS>
+// Tiles: 512 columns of one term, 256 of two; NARROW: 128 of either, for products of few tiles: four times the CTAs, a quarter of the
+// epilogue each, and room for the next launch's CTAs beside these.
+template <int TERMS, bool NARROW>
 struct Form {
-  static constexpr int kWide = TERMS == 1 ? 2 : 1;         // accumulators side by side
-  static constexpr int kCols = 256 * kWide;
-  static constexpr int kStages = TERMS == 1 ? 4 : 3;
-  static constexpr int kStageBytes = TERMS == 1 ? 3 * kBlockBytes : 4 * kBlockBytes;
+  static constexpr int kAcc = NARROW ? 128 : 256;                    // columns of an accumulator
+  static constexpr int kWide = TERMS == 1 && !NARROW ? 2 : 1;        // accumulators side by side
+  static constexpr int kCols = kAcc * kWide;
+  static constexpr int kStages = TERMS == 1 ? 4 : NARROW ? 2 : 3;
+  static constexpr int kBBytes = kAcc / 2 * kDeep * 2;               // a CTA's half of an accumulator's columns
+  static constexpr int kStageBytes = TERMS * (kBlockBytes + kWide * kBBytes);
   static constexpr int kSmemBytes = kStages * kStageBytes + 1024;
-  static constexpr int kThreads = 128 + 32 * kEpilogueWarps * kWide;  // warps 4 and on: epilogue
+  static constexpr int kWarps = NARROW ? 16 : 8;                     // epilogue warps of an accumulator,
+  static constexpr int kPart = kAcc / (kWarps / 4);                  // their columns
+  static constexpr int kThreads = 128 + 32 * kWarps * kWide;
+  static constexpr int kTmem = NARROW ? 256 : 512;
+  static constexpr bool kSplitRegisters = TERMS == 2 && !NARROW;
 };
 
 struct Maps {
@@ -98,18 +106,19 @@ struct Place {
 };
 // Where a tile lies.  Symmetric products: tiles that reach the diagonal or lie below it, two rows of tiles by two (by one, with one
 // accumulator a tile).  Others: groups of eight tile rows, column by column, so that what runs at one time shares rows and columns in L2.
-template <int KIND, int WIDE>
+template <int KIND, int COLS>
 __device__ __forceinline__ Place place_of(const Params& p, int tile) {
   Place at;
   at.batch = tile / p.per;
   tile -= at.batch * p.per;
   if constexpr (symmetric(KIND)) {
-    if constexpr (WIDE == 1) {
-      int m = (int)((sqrtf(8.f * tile + 1.f) - 1.f) * 0.5f);
-      while (m * (m + 1) / 2 > tile) --m;
-      while ((m + 1) * (m + 2) / 2 <= tile) ++m;
+    if constexpr (COLS <= kRows) {  // row m: its kRows / COLS (m + 1) tiles
+      constexpr int kEach = kRows / COLS;
+      int m = (int)((sqrtf(8.f / kEach * tile + 1.f) - 1.f) * 0.5f);
+      while (kEach * (m * (m + 1) / 2) > tile) --m;
+      while (kEach * ((m + 1) * (m + 2) / 2) <= tile) ++m;
       at.m = m;
-      at.n = tile - m * (m + 1) / 2;
+      at.n = tile - kEach * (m * (m + 1) / 2);
     } else {
       int q = (int)((sqrtf(4.f * tile + 1.f) - 1.f) * 0.5f);
       while (q * (q + 1) > tile) --q;
@@ -128,9 +137,9 @@ __device__ __forceinline__ Place place_of(const Params& p, int tile) {
   return at;
 }
 // Accumulators of a tile that have columns to compute.
-template <int KIND, int WIDE>
+template <int KIND, int COLS>
 __device__ __forceinline__ int halves_of(const Params& p, const Place& at) {
-  if (WIDE == 1) return 1;
+  if (COLS <= kRows) return 1;
   if (symmetric(KIND)) return 2 * at.n + 1 <= at.m ? 2 : 1;
   return at.n * 512 + 256 < p.N ? 2 : 1;
 }
@@ -207,6 +216,45 @@ __device__ __forceinline__ void columns16(const float* from, float* d) {
 }
 __device__ __forceinline__ int64_t diag_ld(int S) { return (S + 15) / 16 * 16; }
 __device__ __forceinline__ float factor(const Params& p, int batch, int which) { return p.first && which >= 0 ? p.factors[4 * batch + which] : 1.f; }
+
+// What all chunks of a warp's row share.
+template <int KIND>
+struct Shared {
+  float d, f_m, f_n, f_k;  // this row's diagonal (kForm: of M; X M: none), and the first step's factors
+  __device__ __forceinline__ Shared(const Params& p, int batch, int m) : d(0.f), f_m(1.f), f_n(1.f), f_k(1.f) {
+    const bool row = m < p.M;
+    if constexpr (KIND == kForm) {
+      if (row) d = __ldcg(p.M_diag + batch * diag_ld(p.S) + m);
+      if (p.first) {
+        f_m = factor(p, batch, p.fm);
+        f_n = factor(p, batch, p.fn);
+        f_k = factor(p, batch, p.fk);
+      }
+    } else if constexpr (!symmetric(KIND)) {
+      if (row && !p.tall) d = __ldcg(p.diag + batch * diag_ld(p.S) + m);
+      f_k = p.q * factor(p, batch, p.fq);
+    }
+  }
+};
+// A row's lines on their way into L2: `bytes` from n0's column on.
+__device__ __forceinline__ void prefetch_row(const char* from, int bytes) {
+  for (int i = 0; i < bytes; i += 128) asm volatile("prefetch.global.L2 [%0];" ::"l"(from + i));
+}
+// What a warp's epilogue of a tile will read that its products do not: under way while they are computed.
+template <int KIND, int COLUMNS>
+__device__ __forceinline__ void prefetch(const Params& p, int batch, int m, int n0) {
+  if (symmetric(KIND) || m >= p.M || n0 >= p.N) return;  // (symmetric: operands of these products)
+  const int64_t at = batch * p.matrix + (int64_t)m * p.ld + n0;
+  const int columns = min(COLUMNS, p.N - n0);
+  prefetch_row(reinterpret_cast<const char*>(p.X + at), 2 * columns);
+  prefetch_row(reinterpret_cast<const char*>(p.X + at + p.term), 2 * columns);
+  if (KIND == kLast && p.step) {
+    const MuonItem& it = p.item[batch];
+    const int64_t to = (int64_t)m * it.ld_out + n0;
+    if (it.master) prefetch_row(reinterpret_cast<const char*>(it.master + to), 4 * columns);
+    else prefetch_row(static_cast<const char*>(it.out) + to * (p.out_bf16 ? 2 : 4), (p.out_bf16 ? 2 : 4) * columns);
+  }
+}
 
 // What a chunk's epilogue reads of the matrices in sixteen bits.
 template <int KIND, int TERMS>
@@ -326,19 +374,17 @@ __device__ __forceinline__ void mirror(const Params& p, uint16_t* out, int m, in
 
 // v: the accumulators of these sixteen columns.  All lanes of a warp come here together.
 template <int KIND, int TERMS>
-__device__ __forceinline__ void finish(const Params& p, int batch, int row0, int n0, int lane, float* v, const Ahead<KIND, TERMS>& a) {
+__device__ __forceinline__ void finish(const Params& p, const Shared<KIND>& all, int batch, int row0, int n0, int lane, float* v, const Ahead<KIND, TERMS>& a) {
   const int m = row0 + lane;
   const bool row = m < p.M;
   if constexpr (!symmetric(KIND)) {
-    const float q = p.q * factor(p, batch, p.fq);
-    const float* const diag = p.diag + batch * diag_ld(p.S);
+    const float q = all.f_k + all.d;
     float d[16];
     if (p.tall) {
-      columns16(diag + n0, d);
+      columns16(p.diag + batch * diag_ld(p.S) + n0, d);
     } else {
-      const float own = row ? __ldcg(diag + m) : 0.f;
 #pragma unroll
-      for (int i = 0; i < 16; ++i) d[i] = own;
+      for (int i = 0; i < 16; ++i) d[i] = 0.f;
     }
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
@@ -373,15 +419,14 @@ __device__ __forceinline__ void finish(const Params& p, int batch, int row0, int
       for (int i = 0; i < 16; ++i) v[i] *= p.k;
     } else {
       const int64_t line = batch * diag_ld(p.S);
-      const float fm = factor(p, batch, p.fm), fk = factor(p, batch, p.fk);
-      const float d_m = row ? __ldcg(p.M_diag + line + m) : 0.f;
+      const float fm = all.f_m, fk = all.f_k, d_m = all.d;
       if (on_diagonal && row && m >= n0 && m < n0 + 16) {
         const float d_n = __ldcg(p.N_diag + line + m);
-        p.out_diag[line + m] = p.dm * fm * d_m + p.dn * factor(p, batch, p.fn) * d_n + p.dk * fk * fmaf(own, p.dacc, d_m * d_n);
+        p.out_diag[line + m] = p.dm * fm * d_m + p.dn * all.f_n * d_n + p.dk * fk * fmaf(own, p.dacc, d_m * d_n);
       }
       // M = N: their entry once, times m + k (d_M[i] + d_M[j])
       const float fixed = p.m * fm, by_row = p.k_n * fk * d_m, each = p.k_m * fk, scale = p.k * fk;
-      const float mm = p.N_ ? fixed : fixed + by_row, nn = p.nn * factor(p, batch, p.fn) + by_row;
+      const float mm = p.N_ ? fixed : fixed + by_row, nn = p.nn * all.f_n + by_row;
       float d[16];
       columns16(p.N_diag + line + n0, d);
 #pragma unroll
@@ -445,9 +490,9 @@ __device__ __forceinline__ uint32_t idesc_f16(int m, int n, bool a_mn, bool b_mn
   return (1u << 4) | (a_mn ? 1u << 15 : 0u) | (b_mn ? 1u << 16 : 0u) | ((uint32_t)(n >> 3) << 17) | ((uint32_t)(m >> 4) << 24);
 }
 
-template <int KIND, int TERMS>
-__global__ void __launch_bounds__(Form<TERMS>::kThreads, 1) muon_umma_kernel(const __grid_constant__ Params p, const __grid_constant__ Maps maps) {
-  using F = Form<TERMS>;
+template <int KIND, int TERMS, bool NARROW>
+__global__ void __launch_bounds__(Form<TERMS, NARROW>::kThreads, 1) muon_umma_kernel(const __grid_constant__ Params p, const __grid_constant__ Maps maps) {
+  using F = Form<TERMS, NARROW>;
   constexpr int kStages = F::kStages;
   extern __shared__ uint8_t smem_raw[];
   __shared__ int abort_word;
@@ -466,13 +511,13 @@ __global__ void __launch_bounds__(Form<TERMS>::kThreads, 1) muon_umma_kernel(con
     }
     for (int b = 0; b < 2; ++b) {
       mbar_init(acc_full + 8 * b, 1);
-      mbar_init(acc_empty + 8 * b, 2 * kEpilogueWarps);
+      mbar_init(acc_empty + 8 * b, 2 * F::kWarps);
     }
     abort_word = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
   if (warp == 2) {
-    asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&tmem_slot)), "r"(512) : "memory");
+    asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&tmem_slot)), "r"(F::kTmem) : "memory");
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
   }
   fence_before();
@@ -487,20 +532,20 @@ __global__ void __launch_bounds__(Form<TERMS>::kThreads, 1) muon_umma_kernel(con
   Item it;
   auto wait_all = [&](uint32_t bar, uint32_t parity) { return __all_sync(0xffffffffu, mbar_wait(bar, parity, abort_flag, p.status, p.budget)) != 0; };
 
-  if (TERMS == 2 && warp < 4) asm volatile("setmaxnreg.dec.sync.aligned.u32 56;");  // 4 x 56 + 8 x 224 = 12 x 168, as launched
+  if (F::kSplitRegisters && warp < 4) asm volatile("setmaxnreg.dec.sync.aligned.u32 56;");  // 4 x 56 + 8 x 224 = 12 x 168, as launched
   if (warp == 0) {
     int s = 0, phase = 0, left_out = blockIdx.x == 0 ? p.drop : -1;
     bool ok = true;
     while (ok && walk.step(p, it)) {
-      const Place at = place_of<KIND, F::kWide>(p, it.tile);
-      const int m0 = at.m * kRows + rank * 128, n0 = at.n * F::kCols + rank * 128, halves = halves_of<KIND, F::kWide>(p, at);
+      const Place at = place_of<KIND, F::kCols>(p, it.tile);
+      const int m0 = at.m * kRows + rank * 128, n0 = at.n * F::kCols + rank * (F::kAcc / 2), halves = halves_of<KIND, F::kCols>(p, at);
       for (int u = it.u0; u < it.u1; ++u) {
         ok = wait_all(empty + 8 * s, phase ^ 1);
         if (!ok) break;
         if (elect_one()) {
           const int k0 = u * kDeep;
           const uint32_t bar = map_rank(full + 8 * s, 0), da = ring + s * F::kStageBytes;
-          if (rank == 0) mbar_expect_tx(full + 8 * s, 2 * TERMS * (1 + halves) * kBlockBytes);
+          if (rank == 0) mbar_expect_tx(full + 8 * s, 2 * TERMS * (kBlockBytes + halves * F::kBBytes));
           const bool leave = left_out-- == 0;
 #pragma unroll
           for (int q = 0; q < TERMS; ++q) {
@@ -514,12 +559,12 @@ __global__ void __launch_bounds__(Form<TERMS>::kThreads, 1) muon_umma_kernel(con
             }
           }
           for (int h = 0; h < TERMS * halves; ++h) {  // one term: halves of the columns; two: hi and lo
-            const uint32_t to = da + (TERMS + h) * kBlockBytes;
+            const uint32_t to = da + TERMS * kBlockBytes + h * F::kBBytes;
             const CUtensorMap* map = &maps.b[TERMS == 2 ? h : 0];
             const int n = TERMS == 2 ? n0 : n0 + 256 * h;
             if (p.b_mn) {
               tma_tile_3d(to, map, n, k0, at.batch, bar);
-              tma_tile_3d(to + kBlockBytes / 2, map, n + 64, k0, at.batch, bar);
+              if (!NARROW) tma_tile_3d(to + kBlockBytes / 2, map, n + 64, k0, at.batch, bar);
             } else {
               tma_tile_3d(to, map, k0, n, at.batch, bar);
             }
@@ -530,22 +575,22 @@ __global__ void __launch_bounds__(Form<TERMS>::kThreads, 1) muon_umma_kernel(con
       }
     }
   } else if (warp == 1 && rank == 0) {
-    const uint32_t idesc = idesc_f16(kRows, 256, p.a_mn, p.b_mn);
+    const uint32_t idesc = idesc_f16(kRows, F::kAcc, p.a_mn, p.b_mn);
     const uint64_t a0 = p.a_mn ? desc_mn_major(ring, kBlockBytes / 2) : desc_k_major(ring);
     const uint32_t ring_b = ring + TERMS * kBlockBytes;
     const uint64_t b0 = p.b_mn ? desc_mn_major(ring_b, kBlockBytes / 2) : desc_k_major(ring_b);
     const uint32_t a_step = p.a_mn ? 2048 >> 4 : 32 >> 4, b_step = p.b_mn ? 2048 >> 4 : 32 >> 4;  // sixteen k
-    constexpr uint32_t kNext = kBlockBytes >> 4;
+    constexpr uint32_t kNextA = kBlockBytes >> 4, kNextB = F::kBBytes >> 4;
     int s = 0, phase = 0, acc_phase[2] = {1, 1};
     auto multiply = [&](int buffer, int ta, int tb, uint32_t more) {  // terms (or halves) ta, tb of a K block
       const uint32_t off = (uint32_t)(s * F::kStageBytes) >> 4;
 #pragma unroll
       for (int k = 0; k < kDeep / 16; ++k)
-        umma_pair(tmem + buffer * 256, a0 + off + ta * kNext + k * a_step, b0 + off + tb * kNext + k * b_step, idesc, k > 0 ? 1u : more);
+        umma_pair(tmem + buffer * F::kAcc, a0 + off + ta * kNextA + k * a_step, b0 + off + tb * kNextB + k * b_step, idesc, k > 0 ? 1u : more);
     };
     bool ok = true;
     while (ok && walk.step(p, it)) {
-      const int halves = halves_of<KIND, F::kWide>(p, place_of<KIND, F::kWide>(p, it.tile));
+      const int halves = halves_of<KIND, F::kCols>(p, place_of<KIND, F::kCols>(p, it.tile));
       for (int u = it.u0; ok && u < it.u1;) {
         const int end = TERMS == 2 ? min(it.u1, u + kRun) : it.u1;
         for (int n = u; n < end; ++n) {
@@ -596,11 +641,11 @@ __global__ void __launch_bounds__(Form<TERMS>::kThreads, 1) muon_umma_kernel(con
       }
     }
   } else if (warp >= 4) {
-    if constexpr (TERMS == 2) asm volatile("setmaxnreg.inc.sync.aligned.u32 224;");
-    const int quad = warp & 3, part = ((warp - 4) >> 2) & 1, own = (warp - 4) >> 3;  // lanes, columns, accumulator
+    if constexpr (F::kSplitRegisters) asm volatile("setmaxnreg.inc.sync.aligned.u32 224;");
+    constexpr int kPart = F::kPart, kChunks = kPart / 16;  // a warp's columns
+    const int quad = warp & 3, part = ((warp - 4) >> 2) % (F::kWarps / 4), own = (warp - 4) / F::kWarps;  // lanes, columns, accumulator
     const uint32_t lanes = (uint32_t)(32 * quad) << 16;
-    constexpr int kChunks = 8;  // of sixteen columns, of a warp
-    const uint32_t empty0 = map_rank(acc_empty, 0), acc = tmem + lanes + own * 256 + 128 * part;
+    const uint32_t empty0 = map_rank(acc_empty, 0), acc = tmem + lanes + own * F::kAcc + kPart * part;
     int full_phase = 0;
     bool ok = true;
     auto wait_full = [&]() {
@@ -615,13 +660,15 @@ __global__ void __launch_bounds__(Form<TERMS>::kThreads, 1) muon_umma_kernel(con
       if (lane == 0) mbar_arrive_cluster(empty0 + 8 * buffer);
     };
     while (ok && walk.step(p, it)) {
-      const Place at = place_of<KIND, F::kWide>(p, it.tile);
-      if (own >= halves_of<KIND, F::kWide>(p, at)) continue;
+      const Place at = place_of<KIND, F::kCols>(p, it.tile);
+      if (own >= halves_of<KIND, F::kCols>(p, at)) continue;
       const int row0 = at.m * kRows + rank * 128 + 32 * quad;  // this warp's first row
       const bool rows = row0 < p.M;                            // has any: the others only keep step
-      const int n_base = at.n * F::kCols + 256 * own + 128 * part;
+      const int n_base = at.n * F::kCols + F::kAcc * own + kPart * part;
       float* const piece = it.piece < 0 ? nullptr
-                                        : p.partial + (size_t)it.piece * p.piece + (size_t)(rank * 128 + 32 * quad + lane) * F::kCols + 256 * own + 128 * part;
+                                        : p.partial + (size_t)it.piece * p.piece + (size_t)(rank * 128 + 32 * quad + lane) * F::kCols + F::kAcc * own + kPart * part;
+      if (rows && !piece) prefetch<KIND, kPart>(p, at.batch, row0 + lane, n_base);
+      const Shared<KIND> all(p, at.batch, row0 + lane);
       if constexpr (TERMS == 2) {
         float sum[16 * kChunks];
 #pragma unroll
@@ -648,7 +695,7 @@ __global__ void __launch_bounds__(Form<TERMS>::kThreads, 1) muon_umma_kernel(con
 #pragma unroll
           for (int c = 0; c < kChunks; ++c) {
             float v[16];
-            tmem_ld16(acc + 256 + 16 * c, v);
+            tmem_ld16(acc + F::kAcc + 16 * c, v);
             tmem_arrived(v);
 #pragma unroll
             for (int i = 0; i < 16; ++i) sum[16 * c + i] += v[i];
@@ -658,14 +705,19 @@ __global__ void __launch_bounds__(Form<TERMS>::kThreads, 1) muon_umma_kernel(con
         if (!rows) continue;
         // One copy of the epilogue's code, which takes the first sixteen sums; the others move up.  (Eight copies, each run once a tile, wait
         // for their instructions: 65 us a tile.)
+        constexpr bool kEarly = KIND != kForm;  // (four tiles in registers twice are too many)
+        Ahead<KIND, TERMS> next;
+        if (kEarly && !piece && wanted<KIND>(p, row0, n_base)) next.load(p, at.batch, row0 + lane, n_base);
 #pragma unroll 1
         for (int c = 0; c < kChunks; ++c) {
+          const int n0 = n_base + 16 * c;
           if (piece) {
             put_piece(piece + 16 * c, sum);
-          } else if (wanted<KIND>(p, row0, n_base + 16 * c)) {
-            Ahead<KIND, TERMS> a;
-            a.load(p, at.batch, row0 + lane, n_base + 16 * c);
-            finish<KIND, TERMS>(p, at.batch, row0, n_base + 16 * c, lane, sum, a);
+          } else if (wanted<KIND>(p, row0, n0)) {
+            if (!kEarly) next.load(p, at.batch, row0 + lane, n0);
+            const Ahead<KIND, TERMS> now = next;
+            if (kEarly && c + 1 < kChunks && wanted<KIND>(p, row0, n0 + 16)) next.load(p, at.batch, row0 + lane, n0 + 16);
+            finish<KIND, TERMS>(p, all, at.batch, row0, n0, lane, sum, now);
           }
 #pragma unroll
           for (int i = 0; i < 16 * (kChunks - 1); ++i) sum[i] = sum[i + 16];
@@ -693,7 +745,7 @@ __global__ void __launch_bounds__(Form<TERMS>::kThreads, 1) muon_umma_kernel(con
             tmem_ld16(acc + 16 * c, v);
             if (c + 1 < kChunks && wanted<KIND>(p, row0, n0 + 16)) next.load(p, at.batch, row0 + lane, n0 + 16);
             tmem_arrived(v);
-            finish<KIND, TERMS>(p, at.batch, row0, n0, lane, v, now);
+            finish<KIND, TERMS>(p, all, at.batch, row0, n0, lane, v, now);
           }
         }
         give_back(own);
@@ -709,26 +761,27 @@ __global__ void __launch_bounds__(Form<TERMS>::kThreads, 1) muon_umma_kernel(con
   cluster_sync();
   if (warp == 2) {
     fence_after();
-    asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512) : "memory");
+    asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(F::kTmem) : "memory");
   }
 }
 
 // The tiles that were cut along K: a warp has 32 rows x 16 columns, adds up their pieces in the order of K and does the epilogue.
 constexpr int kJoinWarps = 4;
-template <int KIND, int TERMS>
+template <int KIND, int TERMS, bool NARROW>
 __global__ void __launch_bounds__(32 * kJoinWarps) muon_join_kernel(const __grid_constant__ Params p) {
-  using F = Form<TERMS>;
+  using F = Form<TERMS, NARROW>;
   const int lane = threadIdx.x & 31, number = blockIdx.x * kJoinWarps + (threadIdx.x >> 5);
   if (!(KIND == kLast && p.step)) pdl_launch_dependents();
   pdl_wait();
   constexpr int kAcross = F::kCols / 16, kPer = kAcross * (kRows / 32);
   const int t = number / kPer, in = number % kPer, r0 = in / kAcross * 32, c0 = in % kAcross * 16;
   if (t >= p.tiles - p.whole) return;
-  const Place at = place_of<KIND, F::kWide>(p, p.whole + t);
+  const Place at = place_of<KIND, F::kCols>(p, p.whole + t);
   const int row0 = at.m * kRows + r0, n0 = at.n * F::kCols + c0;
   if (row0 >= p.M || !wanted<KIND>(p, row0, n0)) return;
   Ahead<KIND, TERMS> now;
   now.load(p, at.batch, row0 + lane, n0);
+  const Shared<KIND> all(p, at.batch, row0 + lane);
   float v[16] = {};
   const float* from = p.partial + (size_t)t * p.piece + (size_t)(r0 + lane) * F::kCols + c0;
   const size_t next = (size_t)(p.tiles - p.whole) * p.piece;
@@ -740,7 +793,7 @@ __global__ void __launch_bounds__(32 * kJoinWarps) muon_join_kernel(const __grid
       v[4 * i] += f.x; v[4 * i + 1] += f.y; v[4 * i + 2] += f.z; v[4 * i + 3] += f.w;
     }
   }
-  finish<KIND, TERMS>(p, at.batch, row0, n0, lane, v, now);
+  finish<KIND, TERMS>(p, all, at.batch, row0, n0, lane, v, now);
 }
 
 // ---- host ------------------------------------------------------------------------------------------------------------
@@ -771,75 +824,119 @@ bool make_map(CUtensorMap* m, const void* base, int64_t width, int64_t rows, int
 }
 
 // Tiles of a product of one matrix.
-int tiles_of(int kind, int wide, int M, int N, int* m_tiles, int* n_tiles) {
-  const int m = (M + kRows - 1) / kRows, n = (N + 256 * wide - 1) / (256 * wide);
+int tiles_of(int kind, int cols, int M, int N, int* m_tiles = nullptr, int* n_tiles = nullptr) {
+  const int m = (M + kRows - 1) / kRows, n = (N + cols - 1) / cols;
   if (m_tiles) *m_tiles = m;
   if (n_tiles) *n_tiles = n;
   if (!symmetric(kind)) return m * n;
-  if (wide == 1) return m * (m + 1) / 2;
+  if (cols <= kRows) return kRows / cols * (m * (m - 1) / 2) + n;
   return m / 2 * (m / 2 + 1) + (m & 1 ? m / 2 + 1 : 0);
 }
 
-// Whole rounds of tiles, then the rest: whole too, or cut along K into equal pieces, dealt in rounds of their own.  What is shortest, counted in
-// K blocks: a piece's rows are written to the workspace, and a kernel of its own joins the pieces.
-int plan(Params& p, int wide, int terms, int pairs) {
-  const int rest = p.tiles % pairs;
-  p.whole = p.tiles;
-  p.split = 1;
-  if (rest > 0) {
-    const double products = terms == 2 ? 3 : 1, piece = 1.0 + 8.0 * wide;
-    double best = p.blocks * products;
-    for (int split = 2; split <= p.blocks && rest * split <= kMuonPieces; ++split) {
-      const int rounds = (rest * split + pairs - 1) / pairs;
-      const double time = rounds * (std::ceil((double)p.blocks / split) * products + piece) + 5.0 + 0.5 * split;
-      if (time < best) {
-        best = time;
+struct Plan {
+  int per, m_tiles, n_tiles, tiles, whole, split, pairs;
+  double time;
+};
+// Pieces that the workspace has room for: 84 MB.
+constexpr size_t kPieceFloats = (size_t)160 * kRows * 512;
+long long most_pieces(int cols, long long tiles, long long blocks) {
+  const long long room = (long long)(kPieceFloats / ((size_t)kRows * cols));
+  return tiles < room && tiles * blocks < room ? tiles * blocks : room;
+}
+// Whole tiles in rounds, the last, partly idle one cut along K into equal pieces, or every tile left to the join, in one piece or several;
+// whatever is shortest, in microseconds: of a K block, of a tile's epilogue, which few warps do, of a piece's way to the workspace, and of
+// the launch that joins the pieces, where all warps of the device share the epilogues.
+template <int TERMS, bool NARROW>
+Plan plan_of(int kind, int M, int N, int K, int n, int pairs) {
+  using F = Form<TERMS, NARROW>;
+  Plan p{};
+  p.per = tiles_of(kind, F::kCols, M, N, &p.m_tiles, &p.n_tiles);
+  p.tiles = p.per * n;
+  const int blocks = (K + kDeep - 1) / kDeep, rest = p.tiles % pairs;
+  const double block = NARROW ? (TERMS == 1 ? 0.35 : 0.75) : TERMS == 1 ? 0.7 : 1.2, start = 3.0;
+  const double tail = TERMS == 1 ? (NARROW ? 4.0 : 10.0) : NARROW ? 6.0 : 24.0, piece = NARROW ? 1.0 : TERMS == 1 ? 3.0 : 2.0;
+  const long long room = most_pieces(F::kCols, p.tiles, blocks);
+  auto join = [&](int tiles, int split) { return 4.0 + 0.2 * split + (double)tiles * (split + 1) * kRows * F::kCols * 4 / 3e6; };
+  // two terms: a tile's epilogue runs under the next one's products
+  const double first = start + (double)(p.tiles / pairs) * (TERMS == 2 ? std::max(blocks * block, tail) : blocks * block + tail);
+  auto cut = [&](int whole, double before, int from) {
+    const int tiles = p.tiles - whole;
+    for (int split = from; tiles > 0 && split <= blocks && (long long)tiles * split <= room; ++split) {
+      const long long rounds = ((long long)tiles * split + pairs - 1) / pairs;
+      const double time = before + rounds * (std::ceil((double)blocks / split) * block + piece) + join(tiles, split);
+      if (time < p.time) {
+        p.time = time;
+        p.whole = whole;
         p.split = split;
       }
     }
-    if (p.split > 1) p.whole = p.tiles - rest;
-  }
+  };
+  p.whole = p.tiles;
+  p.split = 1;
+  p.time = first + (rest > 0 ? blocks * block + tail : TERMS == 2 ? tail : 0.0);
+  if (rest > 0) cut(p.tiles - rest, first, 1);
+  cut(0, start, 1);
   const int pieces = (p.tiles - p.whole) * p.split, most = p.whole > pieces ? p.whole : pieces;
-  return most < pairs ? most : pairs;
+  p.pairs = most < pairs ? most : pairs;
+  return p;
 }
 
-template <int KIND, int TERMS>
-cudaError_t launch(const MuonBatch& b, Params& p, const Maps& maps, int sm_count, cudaStream_t s) {
-  using F = Form<TERMS>;
-  const int per = tiles_of(KIND, F::kWide, p.M, p.N, &p.m_tiles, &p.n_tiles);
-  p.per = per;
-  p.tiles = per * b.n;
+template <int KIND, int TERMS, bool NARROW>
+cudaError_t launch_form(Params& p, const Plan& plan, const Maps& maps, cudaStream_t s) {
+  using F = Form<TERMS, NARROW>;
+  p.m_tiles = plan.m_tiles; p.n_tiles = plan.n_tiles; p.per = plan.per; p.tiles = plan.tiles; p.whole = plan.whole; p.split = plan.split;
   p.blocks = (p.K + kDeep - 1) / kDeep;
   p.piece = kRows * F::kCols;
-  const int most = sm_count / 2 < kMuonPairs ? sm_count / 2 : kMuonPairs;
-  const int pairs = plan(p, F::kWide, TERMS, most);
   static unsigned long long configured = 0;
-  cudaError_t e = allow_dynamic_smem(muon_umma_kernel<KIND, TERMS>, F::kSmemBytes, configured);
+  cudaError_t e = allow_dynamic_smem(muon_umma_kernel<KIND, TERMS, NARROW>, F::kSmemBytes, configured);
   if (e != cudaSuccess) return e;
-  if constexpr (TERMS == 2) {  // the registers that the roles share out have to be there: a warp that asks for more than there are waits for ever
+  if constexpr (F::kSplitRegisters) {  // the registers that the roles share out have to be there: a warp that asks for more than there are waits for ever
     static const bool enough = [] {
       cudaFuncAttributes a;
-      return cudaFuncGetAttributes(&a, muon_umma_kernel<KIND, TERMS>) == cudaSuccess && a.numRegs >= 168;
+      return cudaFuncGetAttributes(&a, muon_umma_kernel<KIND, TERMS, NARROW>) == cudaSuccess && a.numRegs >= 168;
     }();
     if (!enough) return cudaErrorInvalidConfiguration;
   }
-  e = launch_clusters(2, muon_umma_kernel<KIND, TERMS>, dim3(2 * pairs), dim3(F::kThreads), F::kSmemBytes, s, p, maps);
+  e = launch_clusters(2, muon_umma_kernel<KIND, TERMS, NARROW>, dim3(2 * plan.pairs), dim3(F::kThreads), F::kSmemBytes, s, p, maps);
   if (e != cudaSuccess || p.whole == p.tiles) return e;
   const int warps = (p.tiles - p.whole) * (F::kCols / 16) * (kRows / 32);
-  return launch_pdl(muon_join_kernel<KIND, TERMS>, dim3((warps + kJoinWarps - 1) / kJoinWarps), dim3(32 * kJoinWarps), 0, s, p);
+  return launch_pdl(muon_join_kernel<KIND, TERMS, NARROW>, dim3((warps + kJoinWarps - 1) / kJoinWarps), dim3(32 * kJoinWarps), 0, s, p);
+}
+
+// What a product's operands are, and how they lie: `k`: rows are k.
+struct Operand {
+  const uint16_t* data;
+  int64_t width, rows, ld, matrix, term;
+  bool k;
+};
+
+template <int KIND, int TERMS>
+cudaError_t launch(const MuonBatch& b, Params& p, const Operand& x, const Operand& y, int sm_count, cudaStream_t s) {
+  const int pairs = sm_count / 2 < kMuonPairs ? sm_count / 2 : kMuonPairs;
+  const Plan wide = plan_of<TERMS, false>(KIND, p.M, p.N, p.K, b.n, pairs), narrow = plan_of<TERMS, true>(KIND, p.M, p.N, p.K, b.n, pairs);
+  const bool few = narrow.time < wide.time;
+  Maps maps;
+  for (int t = 0; t < TERMS; ++t) {
+    auto make = [&](CUtensorMap* m, const Operand& o, int rows) { return make_map(m, o.data + t * o.term, o.width, o.rows, o.ld, b.n, o.matrix, o.k ? 64 : rows); };
+    if (!make(&maps.a[t], x, 128) || !make(&maps.b[t], y, few ? 64 : 128)) return cudaErrorInvalidValue;
+  }
+  if (TERMS == 1) maps.a[1] = maps.a[0], maps.b[1] = maps.b[0];
+  p.a_mn = x.k;
+  p.b_mn = y.k;
+  return few ? launch_form<KIND, TERMS, true>(p, narrow, maps, s) : launch_form<KIND, TERMS, false>(p, wide, maps, s);
 }
 
 }  // namespace
 
 size_t muon_partial_floats(int S, int R, int C, int n, int terms) {
   size_t most = 0;
-  const int wide = terms == 1 ? 2 : 1;
-  for (int kind : {kGram, kForm, kApply}) {
-    const long long K = kind == kGram ? (R > C ? R : C) : S, blocks = (K + kDeep - 1) / kDeep;
-    const long long tiles = (long long)tiles_of(kind, wide, kind == kApply ? R : S, kind == kApply ? C : S, nullptr, nullptr) * n;
-    const long long pieces = blocks < 2 ? 0 : tiles < kMuonPieces && tiles * blocks < kMuonPieces ? tiles * blocks : kMuonPieces;
-    const size_t floats = (size_t)pieces * kRows * 256 * wide;
-    if (floats > most) most = floats;
+  for (int cols : {terms == 1 ? Form<1, false>::kCols : Form<2, false>::kCols, Form<1, true>::kCols}) {
+    for (int kind : {kGram, kForm, kApply}) {
+      const long long K = kind == kGram ? (R > C ? R : C) : S, blocks = (K + kDeep - 1) / kDeep;
+      const long long tiles = (long long)tiles_of(kind, cols, kind == kApply ? R : S, kind == kApply ? C : S) * n;
+      const size_t floats = (size_t)most_pieces(cols, tiles, blocks) * kRows * cols;
+      if (floats > most) most = floats;
+    }
   }
   return most;
 }
@@ -866,32 +963,15 @@ cudaError_t launch_muon_product(const MuonBatch& b, const MuonProduct& q, int sm
   auto two = [](int e) { return (float)std::ldexp(1.0, e); };
   auto diag = [&](int i) { return b.diag + (size_t)i * b.n * ((b.S + 15) / 16 * 16); };
   const uint16_t* const X = b.x[q.from];
-  Maps maps;
-  bool fine = true;
-  for (int t = 0; t < b.terms && fine; ++t) {
-    const uint16_t* const x = X + t * b.x_term;
-    auto square = [&](CUtensorMap* m, int i) { return make_map(m, b.sym[i] + t * b.p_term, b.S, b.S, b.ld_p, b.n, b.p_matrix, 128); };
-    if (q.kind == kGram) {  // rows of X are k where it is tall
-      fine = make_map(&maps.a[t], x, b.C, b.R, b.ld_x, b.n, b.x_matrix, b.tall ? 64 : 128);
-      maps.b[t] = maps.a[t];
-      p.a_mn = p.b_mn = b.tall;
-    } else if (q.kind == kForm) {
-      fine = square(&maps.a[t], q.m.which) && square(&maps.b[t], q.n.which);
-    } else if (b.tall) {
-      fine = make_map(&maps.a[t], x, b.C, b.R, b.ld_x, b.n, b.x_matrix, 128) && square(&maps.b[t], q.m.which);
-    } else {
-      fine = square(&maps.a[t], q.m.which) && make_map(&maps.b[t], x, b.C, b.R, b.ld_x, b.n, b.x_matrix, 64);
-      p.b_mn = 1;
-    }
-  }
-  if (!fine) return cudaErrorInvalidValue;
-  if (b.terms == 1) maps.a[1] = maps.a[0], maps.b[1] = maps.b[0];
+  auto square = [&](int i) { return Operand{b.sym[i], b.S, b.S, b.ld_p, b.p_matrix, b.p_term, false}; };
+  auto long_side = [&](bool k) { return Operand{X, b.C, b.R, b.ld_x, b.x_matrix, b.x_term, k}; };
   if (q.kind == kGram) {
     p.k = two(q.e_out - 2 * q.ex);
     p.dacc = two(-2 * q.ex);
     p.out = b.sym[q.out];
     p.out_diag = diag(q.out);
-    return b.terms == 1 ? launch<kGram, 1>(b, p, maps, sm_count, s) : launch<kGram, 2>(b, p, maps, sm_count, s);
+    const Operand x = long_side(b.tall);  // rows of X are k where it is tall
+    return b.terms == 1 ? launch<kGram, 1>(b, p, x, x, sm_count, s) : launch<kGram, 2>(b, p, x, x, sm_count, s);
   }
   if (q.kind == kForm) {
     const bool same = q.m.which == q.n.which;
@@ -909,9 +989,11 @@ cudaError_t launch_muon_product(const MuonBatch& b, const MuonProduct& q, int sm
     p.dm = q.m.c; p.dn = q.n.c; p.dk = q.k.c;
     p.dacc = two(-q.m.e - q.n.e);
     p.fm = q.m.factor; p.fn = q.n.factor; p.fk = q.k.factor;
-    return b.terms == 1 ? launch<kForm, 1>(b, p, maps, sm_count, s) : launch<kForm, 2>(b, p, maps, sm_count, s);
+    const Operand m = square(q.m.which), n = square(q.n.which);
+    return b.terms == 1 ? launch<kForm, 1>(b, p, m, n, sm_count, s) : launch<kForm, 2>(b, p, m, n, sm_count, s);
   }
   const bool last = q.kind == kLast;
+  const Operand x = b.tall ? long_side(false) : square(q.m.which), y = b.tall ? square(q.m.which) : long_side(true);
   p.q = q.k.c;
   p.fq = q.k.factor;
   p.x_scale = two((last ? 0 : q.e_out) - q.ex);
@@ -920,13 +1002,13 @@ cudaError_t launch_muon_product(const MuonBatch& b, const MuonProduct& q, int sm
   p.X = X;
   if (!last) {
     p.out = b.x[q.from ^ 1];
-    return b.terms == 1 ? launch<kApply, 1>(b, p, maps, sm_count, s) : launch<kApply, 2>(b, p, maps, sm_count, s);
+    return b.terms == 1 ? launch<kApply, 1>(b, p, x, y, sm_count, s) : launch<kApply, 2>(b, p, x, y, sm_count, s);
   }
   p.step = b.step;
   p.out_bf16 = b.out_bf16;
   p.grad_norm = b.grad_norm;
   for (int i = 0; i < b.n; ++i) p.item[i] = b.item[i];
-  return b.terms == 1 ? launch<kLast, 1>(b, p, maps, sm_count, s) : launch<kLast, 2>(b, p, maps, sm_count, s);
+  return b.terms == 1 ? launch<kLast, 1>(b, p, x, y, sm_count, s) : launch<kLast, 2>(b, p, x, y, sm_count, s);
 }
 
 }  // namespace sffn
