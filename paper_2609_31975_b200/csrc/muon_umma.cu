@@ -40,27 +40,34 @@ namespace {
 
 using namespace tc;
 
-constexpr int kRows = 256;                   // of a pair's tile
 constexpr int kDeep = 64;                    // fp16 elements of a 128-byte swizzle row: a K block
 constexpr int kBlockBytes = 128 * kDeep * 2; // 128 rows of a K block
 constexpr int kRun = 8;                      // two terms: K blocks of a run
 
-// Tiles: 512 columns of one term, 256 of two; NARROW: 128 of either, for products of few tiles: four times the CTAs, a quarter of the
-// epilogue each, and room for the next launch's CTAs beside these.
-template <int TERMS, bool NARROW>
+// Pairs' tiles: 256 rows, 512 columns of one term, 256 of two.
+template <int TERMS>
 struct Form {
-  static constexpr int kAcc = NARROW ? 128 : 256;                    // columns of an accumulator
-  static constexpr int kWide = TERMS == 1 && !NARROW ? 2 : 1;        // accumulators side by side
-  static constexpr int kCols = kAcc * kWide;
-  static constexpr int kStages = TERMS == 1 ? 4 : NARROW ? 2 : 3;
-  static constexpr int kBBytes = kAcc / 2 * kDeep * 2;               // a CTA's half of an accumulator's columns
-  static constexpr int kStageBytes = TERMS * (kBlockBytes + kWide * kBBytes);
+  static constexpr int kRows = 256;
+  static constexpr int kWide = TERMS == 1 ? 2 : 1;                    // accumulators side by side, of 256 columns
+  static constexpr int kCols = 256 * kWide;
+  static constexpr int kStages = TERMS == 1 ? 4 : 3;
+  static constexpr int kStageBytes = TERMS * (1 + kWide) * kBlockBytes;
   static constexpr int kSmemBytes = kStages * kStageBytes + 1024;
-  static constexpr int kWarps = NARROW ? 16 : 8;                     // epilogue warps of an accumulator,
-  static constexpr int kPart = kAcc / (kWarps / 4);                  // their columns
+  static constexpr int kWarps = 8;                                   // epilogue warps of an accumulator
   static constexpr int kThreads = 128 + 32 * kWarps * kWide;
-  static constexpr int kTmem = NARROW ? 256 : 512;
-  static constexpr bool kSplitRegisters = TERMS == 2 && !NARROW;
+};
+// Small tiles: a CTA each, two at a time on an SM.
+template <int TERMS>
+struct Small {
+  static constexpr int kRows = 128, kCols = 64;
+  static constexpr int kBBytes = kCols * kDeep * 2;
+  static constexpr int kStages = TERMS == 1 ? 4 : 2;
+  static constexpr int kStageBytes = TERMS * (kBlockBytes + kBBytes);
+  static constexpr int kSmemBytes = kStages * kStageBytes + 1024;
+  static constexpr int kThreads = 256;
+  static constexpr int kRuns = 3;                                    // two terms: runs that have an accumulator
+  static constexpr int kTmem = TERMS == 1 ? kCols : (kRuns + 1) * kCols;
+  static constexpr int kMostBlocks = TERMS == 1 ? 1 << 20 : kRuns * kRun;  // K blocks of a piece
 };
 
 struct Maps {
@@ -106,14 +113,14 @@ struct Place {
 };
 // Where a tile lies.  Symmetric products: tiles that reach the diagonal or lie below it, two rows of tiles by two (by one, with one
 // accumulator a tile).  Others: groups of eight tile rows, column by column, so that what runs at one time shares rows and columns in L2.
-template <int KIND, int COLS>
+template <int KIND, typename FORM>
 __device__ __forceinline__ Place place_of(const Params& p, int tile) {
   Place at;
   at.batch = tile / p.per;
   tile -= at.batch * p.per;
   if constexpr (symmetric(KIND)) {
-    if constexpr (COLS <= kRows) {  // row m: its kRows / COLS (m + 1) tiles
-      constexpr int kEach = kRows / COLS;
+    if constexpr (FORM::kCols <= FORM::kRows) {  // row m: its kRows / kCols (m + 1) tiles
+      constexpr int kEach = FORM::kRows / FORM::kCols;
       int m = (int)((sqrtf(8.f / kEach * tile + 1.f) - 1.f) * 0.5f);
       while (kEach * (m * (m + 1) / 2) > tile) --m;
       while (kEach * ((m + 1) * (m + 2) / 2) <= tile) ++m;
@@ -136,10 +143,10 @@ __device__ __forceinline__ Place place_of(const Params& p, int tile) {
   }
   return at;
 }
-// Accumulators of a tile that have columns to compute.
-template <int KIND, int COLS>
+// Accumulators of a pair's tile that have columns to compute.
+template <int KIND, int WIDE>
 __device__ __forceinline__ int halves_of(const Params& p, const Place& at) {
-  if (COLS <= kRows) return 1;
+  if (WIDE == 1) return 1;
   if (symmetric(KIND)) return 2 * at.n + 1 <= at.m ? 2 : 1;
   return at.n * 512 + 256 < p.N ? 2 : 1;
 }
@@ -490,9 +497,9 @@ __device__ __forceinline__ uint32_t idesc_f16(int m, int n, bool a_mn, bool b_mn
   return (1u << 4) | (a_mn ? 1u << 15 : 0u) | (b_mn ? 1u << 16 : 0u) | ((uint32_t)(n >> 3) << 17) | ((uint32_t)(m >> 4) << 24);
 }
 
-template <int KIND, int TERMS, bool NARROW>
-__global__ void __launch_bounds__(Form<TERMS, NARROW>::kThreads, 1) muon_umma_kernel(const __grid_constant__ Params p, const __grid_constant__ Maps maps) {
-  using F = Form<TERMS, NARROW>;
+template <int KIND, int TERMS>
+__global__ void __launch_bounds__(Form<TERMS>::kThreads, 1) muon_umma_kernel(const __grid_constant__ Params p, const __grid_constant__ Maps maps) {
+  using F = Form<TERMS>;
   constexpr int kStages = F::kStages;
   extern __shared__ uint8_t smem_raw[];
   __shared__ int abort_word;
@@ -517,7 +524,7 @@ __global__ void __launch_bounds__(Form<TERMS, NARROW>::kThreads, 1) muon_umma_ke
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
   if (warp == 2) {
-    asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&tmem_slot)), "r"(F::kTmem) : "memory");
+    asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&tmem_slot)), "r"(512) : "memory");
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
   }
   fence_before();
@@ -532,20 +539,20 @@ __global__ void __launch_bounds__(Form<TERMS, NARROW>::kThreads, 1) muon_umma_ke
   Item it;
   auto wait_all = [&](uint32_t bar, uint32_t parity) { return __all_sync(0xffffffffu, mbar_wait(bar, parity, abort_flag, p.status, p.budget)) != 0; };
 
-  if (F::kSplitRegisters && warp < 4) asm volatile("setmaxnreg.dec.sync.aligned.u32 56;");  // 4 x 56 + 8 x 224 = 12 x 168, as launched
+  if (TERMS == 2 && warp < 4) asm volatile("setmaxnreg.dec.sync.aligned.u32 56;");  // 4 x 56 + 8 x 224 = 12 x 168, as launched
   if (warp == 0) {
     int s = 0, phase = 0, left_out = blockIdx.x == 0 ? p.drop : -1;
     bool ok = true;
     while (ok && walk.step(p, it)) {
-      const Place at = place_of<KIND, F::kCols>(p, it.tile);
-      const int m0 = at.m * kRows + rank * 128, n0 = at.n * F::kCols + rank * (F::kAcc / 2), halves = halves_of<KIND, F::kCols>(p, at);
+      const Place at = place_of<KIND, F>(p, it.tile);
+      const int m0 = at.m * F::kRows + rank * 128, n0 = at.n * F::kCols + rank * 128, halves = halves_of<KIND, F::kWide>(p, at);
       for (int u = it.u0; u < it.u1; ++u) {
         ok = wait_all(empty + 8 * s, phase ^ 1);
         if (!ok) break;
         if (elect_one()) {
           const int k0 = u * kDeep;
           const uint32_t bar = map_rank(full + 8 * s, 0), da = ring + s * F::kStageBytes;
-          if (rank == 0) mbar_expect_tx(full + 8 * s, 2 * TERMS * (kBlockBytes + halves * F::kBBytes));
+          if (rank == 0) mbar_expect_tx(full + 8 * s, 2 * TERMS * (1 + halves) * kBlockBytes);
           const bool leave = left_out-- == 0;
 #pragma unroll
           for (int q = 0; q < TERMS; ++q) {
@@ -559,12 +566,12 @@ __global__ void __launch_bounds__(Form<TERMS, NARROW>::kThreads, 1) muon_umma_ke
             }
           }
           for (int h = 0; h < TERMS * halves; ++h) {  // one term: halves of the columns; two: hi and lo
-            const uint32_t to = da + TERMS * kBlockBytes + h * F::kBBytes;
+            const uint32_t to = da + (TERMS + h) * kBlockBytes;
             const CUtensorMap* map = &maps.b[TERMS == 2 ? h : 0];
             const int n = TERMS == 2 ? n0 : n0 + 256 * h;
             if (p.b_mn) {
               tma_tile_3d(to, map, n, k0, at.batch, bar);
-              if (!NARROW) tma_tile_3d(to + kBlockBytes / 2, map, n + 64, k0, at.batch, bar);
+              tma_tile_3d(to + kBlockBytes / 2, map, n + 64, k0, at.batch, bar);
             } else {
               tma_tile_3d(to, map, k0, n, at.batch, bar);
             }
@@ -575,22 +582,22 @@ __global__ void __launch_bounds__(Form<TERMS, NARROW>::kThreads, 1) muon_umma_ke
       }
     }
   } else if (warp == 1 && rank == 0) {
-    const uint32_t idesc = idesc_f16(kRows, F::kAcc, p.a_mn, p.b_mn);
+    const uint32_t idesc = idesc_f16(F::kRows, 256, p.a_mn, p.b_mn);
     const uint64_t a0 = p.a_mn ? desc_mn_major(ring, kBlockBytes / 2) : desc_k_major(ring);
     const uint32_t ring_b = ring + TERMS * kBlockBytes;
     const uint64_t b0 = p.b_mn ? desc_mn_major(ring_b, kBlockBytes / 2) : desc_k_major(ring_b);
     const uint32_t a_step = p.a_mn ? 2048 >> 4 : 32 >> 4, b_step = p.b_mn ? 2048 >> 4 : 32 >> 4;  // sixteen k
-    constexpr uint32_t kNextA = kBlockBytes >> 4, kNextB = F::kBBytes >> 4;
+    constexpr uint32_t kNext = kBlockBytes >> 4;
     int s = 0, phase = 0, acc_phase[2] = {1, 1};
     auto multiply = [&](int buffer, int ta, int tb, uint32_t more) {  // terms (or halves) ta, tb of a K block
       const uint32_t off = (uint32_t)(s * F::kStageBytes) >> 4;
 #pragma unroll
       for (int k = 0; k < kDeep / 16; ++k)
-        umma_pair(tmem + buffer * F::kAcc, a0 + off + ta * kNextA + k * a_step, b0 + off + tb * kNextB + k * b_step, idesc, k > 0 ? 1u : more);
+        umma_pair(tmem + buffer * 256, a0 + off + ta * kNext + k * a_step, b0 + off + tb * kNext + k * b_step, idesc, k > 0 ? 1u : more);
     };
     bool ok = true;
     while (ok && walk.step(p, it)) {
-      const int halves = halves_of<KIND, F::kCols>(p, place_of<KIND, F::kCols>(p, it.tile));
+      const int halves = halves_of<KIND, F::kWide>(p, place_of<KIND, F>(p, it.tile));
       for (int u = it.u0; ok && u < it.u1;) {
         const int end = TERMS == 2 ? min(it.u1, u + kRun) : it.u1;
         for (int n = u; n < end; ++n) {
@@ -641,11 +648,11 @@ __global__ void __launch_bounds__(Form<TERMS, NARROW>::kThreads, 1) muon_umma_ke
       }
     }
   } else if (warp >= 4) {
-    if constexpr (F::kSplitRegisters) asm volatile("setmaxnreg.inc.sync.aligned.u32 224;");
-    constexpr int kPart = F::kPart, kChunks = kPart / 16;  // a warp's columns
-    const int quad = warp & 3, part = ((warp - 4) >> 2) % (F::kWarps / 4), own = (warp - 4) / F::kWarps;  // lanes, columns, accumulator
+    if constexpr (TERMS == 2) asm volatile("setmaxnreg.inc.sync.aligned.u32 224;");
+    constexpr int kPart = 128, kChunks = kPart / 16;  // a warp's columns
+    const int quad = warp & 3, part = ((warp - 4) >> 2) & 1, own = (warp - 4) >> 3;  // lanes, columns, accumulator
     const uint32_t lanes = (uint32_t)(32 * quad) << 16;
-    const uint32_t empty0 = map_rank(acc_empty, 0), acc = tmem + lanes + own * F::kAcc + kPart * part;
+    const uint32_t empty0 = map_rank(acc_empty, 0), acc = tmem + lanes + own * 256 + kPart * part;
     int full_phase = 0;
     bool ok = true;
     auto wait_full = [&]() {
@@ -660,13 +667,13 @@ __global__ void __launch_bounds__(Form<TERMS, NARROW>::kThreads, 1) muon_umma_ke
       if (lane == 0) mbar_arrive_cluster(empty0 + 8 * buffer);
     };
     while (ok && walk.step(p, it)) {
-      const Place at = place_of<KIND, F::kCols>(p, it.tile);
-      if (own >= halves_of<KIND, F::kCols>(p, at)) continue;
-      const int row0 = at.m * kRows + rank * 128 + 32 * quad;  // this warp's first row
+      const Place at = place_of<KIND, F>(p, it.tile);
+      if (own >= halves_of<KIND, F::kWide>(p, at)) continue;
+      const int row0 = at.m * F::kRows + rank * 128 + 32 * quad;  // this warp's first row
       const bool rows = row0 < p.M;                            // has any: the others only keep step
-      const int n_base = at.n * F::kCols + F::kAcc * own + kPart * part;
+      const int n_base = at.n * F::kCols + 256 * own + kPart * part;
       float* const piece = it.piece < 0 ? nullptr
-                                        : p.partial + (size_t)it.piece * p.piece + (size_t)(rank * 128 + 32 * quad + lane) * F::kCols + F::kAcc * own + kPart * part;
+                                        : p.partial + (size_t)it.piece * p.piece + (size_t)(rank * 128 + 32 * quad + lane) * F::kCols + 256 * own + kPart * part;
       if (rows && !piece) prefetch<KIND, kPart>(p, at.batch, row0 + lane, n_base);
       const Shared<KIND> all(p, at.batch, row0 + lane);
       if constexpr (TERMS == 2) {
@@ -695,7 +702,7 @@ __global__ void __launch_bounds__(Form<TERMS, NARROW>::kThreads, 1) muon_umma_ke
 #pragma unroll
           for (int c = 0; c < kChunks; ++c) {
             float v[16];
-            tmem_ld16(acc + F::kAcc + 16 * c, v);
+            tmem_ld16(acc + 256 + 16 * c, v);
             tmem_arrived(v);
 #pragma unroll
             for (int i = 0; i < 16; ++i) sum[16 * c + i] += v[i];
@@ -761,23 +768,179 @@ __global__ void __launch_bounds__(Form<TERMS, NARROW>::kThreads, 1) muon_umma_ke
   cluster_sync();
   if (warp == 2) {
     fence_after();
-    asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(F::kTmem) : "memory");
+    asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512) : "memory");
   }
 }
 
-// The tiles that were cut along K: a warp has 32 rows x 16 columns, adds up their pieces in the order of K and does the epilogue.
+// ---- small tiles -----------------------------------------------------------------------------------------------------
+// For products that do not fill the device with pairs' tiles: a CTA has one tile of 128 x 64 (or a piece of it along K), eight warps,
+// of which the first two issue the copies and the MMAs before they take their share of the epilogue.  Two CTAs an SM, and the next
+// launch's start beside these.  With two terms, every run of K blocks has an accumulator of its own, so a piece is at most three runs.
+__device__ __forceinline__ void tma_tile_alone(uint32_t dst, const CUtensorMap* map, int c0, int c1, int c2, uint32_t bar) {
+  asm volatile(
+      "cp.async.bulk.tensor.3d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];" ::"r"(dst), "l"(map), "r"(c0), "r"(c1),
+      "r"(c2), "r"(bar)
+      : "memory");
+}
+__device__ __forceinline__ void umma_alone(uint32_t tmem_d, uint64_t adesc, uint64_t bdesc, uint32_t idesc, uint32_t accumulate) {
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t"
+      "setp.ne.b32 p, %4, 0;\n\t"
+      "tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}" ::"r"(tmem_d),
+      "l"(adesc), "l"(bdesc), "r"(idesc), "r"(accumulate)
+      : "memory");
+}
+__device__ __forceinline__ void commit_alone(uint32_t bar) {
+  asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
+}
+
+template <int KIND, int TERMS>
+__global__ void __launch_bounds__(Small<TERMS>::kThreads, 2) muon_small_kernel(const __grid_constant__ Params p, const __grid_constant__ Maps maps) {
+  using F = Small<TERMS>;
+  constexpr int kStages = F::kStages;
+  extern __shared__ uint8_t smem_raw[];
+  __shared__ int abort_word;
+  __shared__ uint32_t tmem_slot;
+  __shared__ __align__(8) uint64_t bars[2 * kStages + 1];
+  volatile int* const abort_flag = &abort_word;
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  const uint32_t ring = (smem_u32(smem_raw) + 1023u) & ~1023u;
+  const uint32_t full = smem_u32(bars), empty = full + 8 * kStages, acc_full = empty + 8 * kStages;
+  if (tid == 0) {
+    for (int s = 0; s < 2 * kStages + 1; ++s) mbar_init(full + 8 * s, 1);
+    abort_word = 0;
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  }
+  if (warp == 2) {
+    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&tmem_slot)), "r"(F::kTmem) : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+  }
+  fence_before();
+  __syncthreads();
+  fence_after();
+  const uint32_t tmem = tmem_slot;
+  const bool pieces = p.whole < p.tiles;
+  if (!(KIND == kLast && p.step && !pieces)) pdl_launch_dependents();
+  pdl_wait();
+
+  const int number = blockIdx.x, part = number / p.tiles, tile = number - part * p.tiles;
+  const Place at = place_of<KIND, F>(p, tile);
+  const int u0 = (int)((long long)p.blocks * part / p.split), u1 = (int)((long long)p.blocks * (part + 1) / p.split);
+  auto wait_all = [&](uint32_t bar, uint32_t parity) { return __all_sync(0xffffffffu, mbar_wait(bar, parity, abort_flag, p.status, p.budget)) != 0; };
+  if (warp == 0) {
+    int s = 0, phase = 0;
+    for (int u = u0; u < u1; ++u) {
+      if (!wait_all(empty + 8 * s, phase ^ 1)) break;
+      if (elect_one()) {
+        const int k0 = u * kDeep, m0 = at.m * F::kRows, n0 = at.n * F::kCols;
+        const uint32_t bar = full + 8 * s, da = ring + s * F::kStageBytes, db = da + TERMS * kBlockBytes;
+        mbar_expect_tx(bar, F::kStageBytes);
+        const bool leave = number == 0 && u - u0 == p.drop;
+#pragma unroll
+        for (int q = 0; q < TERMS; ++q) {
+          if (!leave) {
+            const uint32_t to = da + q * kBlockBytes;
+            if (p.a_mn) {
+              tma_tile_alone(to, &maps.a[q], m0, k0, at.batch, bar);
+              tma_tile_alone(to + kBlockBytes / 2, &maps.a[q], m0 + 64, k0, at.batch, bar);
+            } else {
+              tma_tile_alone(to, &maps.a[q], k0, m0, at.batch, bar);
+            }
+          }
+          if (p.b_mn) tma_tile_alone(db + q * F::kBBytes, &maps.b[q], n0, k0, at.batch, bar);
+          else tma_tile_alone(db + q * F::kBBytes, &maps.b[q], k0, n0, at.batch, bar);
+        }
+      }
+      __syncwarp();
+      if (++s == kStages) { s = 0; phase ^= 1; }
+    }
+  } else if (warp == 1) {
+    const uint32_t idesc = idesc_f16(F::kRows, F::kCols, p.a_mn, p.b_mn);
+    const uint64_t a0 = p.a_mn ? desc_mn_major(ring, kBlockBytes / 2) : desc_k_major(ring);
+    const uint32_t ring_b = ring + TERMS * kBlockBytes;
+    const uint64_t b0 = p.b_mn ? desc_mn_major(ring_b, F::kBBytes) : desc_k_major(ring_b);
+    const uint32_t a_step = p.a_mn ? 2048 >> 4 : 32 >> 4, b_step = p.b_mn ? 2048 >> 4 : 32 >> 4;  // sixteen k
+    int s = 0, phase = 0;
+    for (int u = u0; u < u1; ++u) {
+      if (!wait_all(full + 8 * s, phase)) break;
+      fence_after();
+      if (elect_one()) {
+        const uint32_t off = (uint32_t)(s * F::kStageBytes) >> 4;
+        auto multiply = [&](int buffer, int ta, int tb, uint32_t more) {
+#pragma unroll
+          for (int k = 0; k < kDeep / 16; ++k)
+            umma_alone(tmem + buffer * F::kCols, a0 + off + ta * (kBlockBytes >> 4) + k * a_step, b0 + off + tb * (F::kBBytes >> 4) + k * b_step, idesc,
+                       k > 0 ? 1u : more);
+        };
+        if constexpr (TERMS == 2) {
+          multiply(0, 0, 1, u > u0);
+          multiply(0, 1, 0, 1);
+          multiply(1 + (u - u0) / kRun, 0, 0, (u - u0) % kRun != 0);
+        } else {
+          multiply(0, 0, 0, u > u0);
+        }
+        commit_alone(empty + 8 * s);
+        if (u + 1 == u1) commit_alone(acc_full);
+      }
+      __syncwarp();
+      if (++s == kStages) { s = 0; phase ^= 1; }
+    }
+  }
+  __syncwarp();
+
+  const int quad = warp & 3, n_base = at.n * F::kCols + 32 * (warp >> 2), row0 = at.m * F::kRows + 32 * quad;
+  const bool rows = row0 < p.M;
+  Ahead<KIND, TERMS> next;
+  if (rows && !pieces && wanted<KIND>(p, row0, n_base)) next.load(p, at.batch, row0 + lane, n_base);
+  const Shared<KIND> all(p, at.batch, row0 + lane);
+  if (wait_all(acc_full, 0) && rows) {
+    fence_after();
+    const uint32_t acc = tmem + ((uint32_t)(32 * quad) << 16) + 32 * (warp >> 2);
+    float* const piece = p.partial + (size_t)number * p.piece + (size_t)(32 * quad + lane) * F::kCols + 32 * (warp >> 2);
+#pragma unroll 1
+    for (int c = 0; c < 2; ++c) {
+      const int n0 = n_base + 16 * c;
+      if (!pieces && !wanted<KIND>(p, row0, n0)) break;
+      const Ahead<KIND, TERMS> now = next;
+      float v[16];
+      tmem_ld16(acc + 16 * c, v);
+      if (!pieces && c == 0 && wanted<KIND>(p, row0, n0 + 16)) next.load(p, at.batch, row0 + lane, n0 + 16);
+      tmem_arrived(v);
+      if constexpr (TERMS == 2) {  // the small products first
+        for (int run = 0; run * kRun < u1 - u0; ++run) {
+          float w[16];
+          tmem_ld16(acc + (1 + run) * F::kCols + 16 * c, w);
+          tmem_arrived(w);
+#pragma unroll
+          for (int i = 0; i < 16; ++i) v[i] += w[i];
+        }
+      }
+      if (pieces) put_piece(piece + 16 * c, v);
+      else finish<KIND, TERMS>(p, all, at.batch, row0, n0, lane, v, now);
+    }
+  }
+  if (*abort_flag)  // (copies and MMAs that may still be in flight end within microseconds)
+    for (int i = 0; i < 50; ++i) __nanosleep(1000);
+  fence_before();
+  __syncthreads();
+  if (warp == 2) {
+    fence_after();
+    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(F::kTmem) : "memory");
+  }
+}
+
+// The tiles that were left in pieces: a warp has 32 rows x 16 columns, adds up their pieces in the order of K and does the epilogue.
 constexpr int kJoinWarps = 4;
-template <int KIND, int TERMS, bool NARROW>
+template <int KIND, int TERMS, typename F>
 __global__ void __launch_bounds__(32 * kJoinWarps) muon_join_kernel(const __grid_constant__ Params p) {
-  using F = Form<TERMS, NARROW>;
   const int lane = threadIdx.x & 31, number = blockIdx.x * kJoinWarps + (threadIdx.x >> 5);
   if (!(KIND == kLast && p.step)) pdl_launch_dependents();
   pdl_wait();
-  constexpr int kAcross = F::kCols / 16, kPer = kAcross * (kRows / 32);
+  constexpr int kAcross = F::kCols / 16, kPer = kAcross * (F::kRows / 32);
   const int t = number / kPer, in = number % kPer, r0 = in / kAcross * 32, c0 = in % kAcross * 16;
   if (t >= p.tiles - p.whole) return;
-  const Place at = place_of<KIND, F::kCols>(p, p.whole + t);
-  const int row0 = at.m * kRows + r0, n0 = at.n * F::kCols + c0;
+  const Place at = place_of<KIND, F>(p, p.whole + t);
+  const int row0 = at.m * F::kRows + r0, n0 = at.n * F::kCols + c0;
   if (row0 >= p.M || !wanted<KIND>(p, row0, n0)) return;
   Ahead<KIND, TERMS> now;
   now.load(p, at.batch, row0 + lane, n0);
@@ -824,83 +987,120 @@ bool make_map(CUtensorMap* m, const void* base, int64_t width, int64_t rows, int
 }
 
 // Tiles of a product of one matrix.
-int tiles_of(int kind, int cols, int M, int N, int* m_tiles = nullptr, int* n_tiles = nullptr) {
-  const int m = (M + kRows - 1) / kRows, n = (N + cols - 1) / cols;
+int tiles_of(int kind, int rows, int cols, int M, int N, int* m_tiles = nullptr, int* n_tiles = nullptr) {
+  const int m = (M + rows - 1) / rows, n = (N + cols - 1) / cols;
   if (m_tiles) *m_tiles = m;
   if (n_tiles) *n_tiles = n;
   if (!symmetric(kind)) return m * n;
-  if (cols <= kRows) return kRows / cols * (m * (m - 1) / 2) + n;
+  if (cols <= rows) return rows / cols * (m * (m - 1) / 2) + n;
   return m / 2 * (m / 2 + 1) + (m & 1 ? m / 2 + 1 : 0);
 }
 
 struct Plan {
-  int per, m_tiles, n_tiles, tiles, whole, split, pairs;
+  int per, m_tiles, n_tiles, tiles, whole, split, ctas;
   double time;
 };
-// Pieces that the workspace has room for: 84 MB.
-constexpr size_t kPieceFloats = (size_t)160 * kRows * 512;
-long long most_pieces(int cols, long long tiles, long long blocks) {
-  const long long room = (long long)(kPieceFloats / ((size_t)kRows * cols));
+// Floats of the pieces that the workspace has room for: 84 MB.
+constexpr size_t kPieceFloats = (size_t)160 * 256 * 512;
+long long most_pieces(int rows, int cols, long long tiles, long long blocks) {
+  const long long room = (long long)(kPieceFloats / ((size_t)rows * cols));
   return tiles < room && tiles * blocks < room ? tiles * blocks : room;
 }
-// Whole tiles in rounds, the last, partly idle one cut along K into equal pieces, or every tile left to the join, in one piece or several;
-// whatever is shortest, in microseconds: of a K block, of a tile's epilogue, which few warps do, of a piece's way to the workspace, and of
-// the launch that joins the pieces, where all warps of the device share the epilogues.
-template <int TERMS, bool NARROW>
-Plan plan_of(int kind, int M, int N, int K, int n, int pairs) {
-  using F = Form<TERMS, NARROW>;
+// Microseconds of the launch that joins `split` pieces of each of so many tiles.
+double join_time(double tiles, int split, int rows, int cols) { return 4.0 + 0.2 * split + tiles * (split + 1) * rows * cols * 4 / 3e6; }
+
+// Pairs' tiles: whole ones in rounds, the last, partly idle one cut along K into equal pieces where that is shorter (times in microseconds: of
+// a K block, of a tile's epilogue, of a piece's way to the workspace).
+template <int TERMS>
+Plan plan_pairs(int kind, int M, int N, int K, int n, int pairs) {
+  using F = Form<TERMS>;
   Plan p{};
-  p.per = tiles_of(kind, F::kCols, M, N, &p.m_tiles, &p.n_tiles);
+  p.per = tiles_of(kind, F::kRows, F::kCols, M, N, &p.m_tiles, &p.n_tiles);
   p.tiles = p.per * n;
   const int blocks = (K + kDeep - 1) / kDeep, rest = p.tiles % pairs;
-  const double block = NARROW ? (TERMS == 1 ? 0.35 : 0.75) : TERMS == 1 ? 0.7 : 1.2, start = 3.0;
-  const double tail = TERMS == 1 ? (NARROW ? 4.0 : 10.0) : NARROW ? 6.0 : 24.0, piece = NARROW ? 1.0 : TERMS == 1 ? 3.0 : 2.0;
-  const long long room = most_pieces(F::kCols, p.tiles, blocks);
-  auto join = [&](int tiles, int split) { return 4.0 + 0.2 * split + (double)tiles * (split + 1) * kRows * F::kCols * 4 / 3e6; };
+  const double block = TERMS == 1 ? 0.7 : 1.2, start = 3.0, tail = TERMS == 1 ? 15.0 : 24.0, piece = TERMS == 1 ? 3.0 : 2.0;
+  const long long room = most_pieces(F::kRows, F::kCols, p.tiles, blocks);
   // two terms: a tile's epilogue runs under the next one's products
-  const double first = start + (double)(p.tiles / pairs) * (TERMS == 2 ? std::max(blocks * block, tail) : blocks * block + tail);
-  auto cut = [&](int whole, double before, int from) {
-    const int tiles = p.tiles - whole;
-    for (int split = from; tiles > 0 && split <= blocks && (long long)tiles * split <= room; ++split) {
-      const long long rounds = ((long long)tiles * split + pairs - 1) / pairs;
-      const double time = before + rounds * (std::ceil((double)blocks / split) * block + piece) + join(tiles, split);
-      if (time < p.time) {
-        p.time = time;
-        p.whole = whole;
-        p.split = split;
-      }
-    }
-  };
+  const double rounds = start + (double)(p.tiles / pairs) * (TERMS == 2 ? std::max(blocks * block, tail) : blocks * block + tail);
   p.whole = p.tiles;
   p.split = 1;
-  p.time = first + (rest > 0 ? blocks * block + tail : TERMS == 2 ? tail : 0.0);
-  if (rest > 0) cut(p.tiles - rest, first, 1);
-  cut(0, start, 1);
+  p.time = rounds + (rest > 0 ? blocks * block + tail : TERMS == 2 ? tail : 0.0);
+  for (int split = 1; rest > 0 && split <= blocks && (long long)rest * split <= room; ++split) {
+    const int turns = (rest * split + pairs - 1) / pairs;
+    const double time = rounds + turns * (std::ceil((double)blocks / split) * block + piece) + join_time(rest, split, F::kRows, F::kCols);
+    if (time < p.time) {
+      p.time = time;
+      p.whole = p.tiles - rest;
+      p.split = split;
+    }
+  }
   const int pieces = (p.tiles - p.whole) * p.split, most = p.whole > pieces ? p.whole : pieces;
-  p.pairs = most < pairs ? most : pairs;
+  p.ctas = 2 * (most < pairs ? most : pairs);
+  return p;
+}
+// Small tiles: whole, or all of them in pieces.
+template <int TERMS>
+Plan plan_small(int kind, int M, int N, int K, int n, int sms) {
+  using F = Small<TERMS>;
+  Plan p{};
+  p.per = tiles_of(kind, F::kRows, F::kCols, M, N, &p.m_tiles, &p.n_tiles);
+  p.tiles = p.per * n;
+  const int blocks = (K + kDeep - 1) / kDeep, fewest = (blocks + F::kMostBlocks - 1) / F::kMostBlocks;
+  const long long room = most_pieces(F::kRows, F::kCols, p.tiles, blocks);
+  p.time = 1e30;
+  for (int split = fewest; split <= blocks && (split == 1 || (long long)p.tiles * split <= room); ++split) {
+    const long long ctas = (long long)p.tiles * split, rounds = (ctas + 2 * sms - 1) / (2 * sms);
+    if (ctas > (1 << 30)) break;
+    const double block = (TERMS == 1 ? 0.35 : 0.7) * (ctas > sms ? 2 : 1);  // two CTAs share an SM's copies
+    const double time = 3.0 + rounds * (2.0 + std::ceil((double)blocks / split) * block + (split > 1 ? 1.0 : 3.0)) +
+                        (split > 1 ? join_time(p.tiles, split, F::kRows, F::kCols) : 0.0);
+    if (time < p.time) {
+      p.time = time;
+      p.split = split;
+    }
+  }
+  p.whole = p.split > 1 ? 0 : p.tiles;
+  p.ctas = p.tiles * p.split;
   return p;
 }
 
-template <int KIND, int TERMS, bool NARROW>
-cudaError_t launch_form(Params& p, const Plan& plan, const Maps& maps, cudaStream_t s) {
-  using F = Form<TERMS, NARROW>;
+template <int KIND, int TERMS, typename F>
+cudaError_t launch_join(const Params& p, cudaStream_t s) {
+  const int warps = (p.tiles - p.whole) * (F::kCols / 16) * (F::kRows / 32);
+  return launch_pdl(muon_join_kernel<KIND, TERMS, F>, dim3((warps + kJoinWarps - 1) / kJoinWarps), dim3(32 * kJoinWarps), 0, s, p);
+}
+template <typename F>
+void take_plan(Params& p, const Plan& plan) {
   p.m_tiles = plan.m_tiles; p.n_tiles = plan.n_tiles; p.per = plan.per; p.tiles = plan.tiles; p.whole = plan.whole; p.split = plan.split;
   p.blocks = (p.K + kDeep - 1) / kDeep;
-  p.piece = kRows * F::kCols;
+  p.piece = F::kRows * F::kCols;
+}
+template <int KIND, int TERMS>
+cudaError_t launch_pairs(Params& p, const Plan& plan, const Maps& maps, cudaStream_t s) {
+  using F = Form<TERMS>;
+  take_plan<F>(p, plan);
   static unsigned long long configured = 0;
-  cudaError_t e = allow_dynamic_smem(muon_umma_kernel<KIND, TERMS, NARROW>, F::kSmemBytes, configured);
+  cudaError_t e = allow_dynamic_smem(muon_umma_kernel<KIND, TERMS>, F::kSmemBytes, configured);
   if (e != cudaSuccess) return e;
-  if constexpr (F::kSplitRegisters) {  // the registers that the roles share out have to be there: a warp that asks for more than there are waits for ever
+  if constexpr (TERMS == 2) {  // the registers that the roles share out have to be there: a warp that asks for more than there are waits for ever
     static const bool enough = [] {
       cudaFuncAttributes a;
-      return cudaFuncGetAttributes(&a, muon_umma_kernel<KIND, TERMS, NARROW>) == cudaSuccess && a.numRegs >= 168;
+      return cudaFuncGetAttributes(&a, muon_umma_kernel<KIND, TERMS>) == cudaSuccess && a.numRegs >= 168;
     }();
     if (!enough) return cudaErrorInvalidConfiguration;
   }
-  e = launch_clusters(2, muon_umma_kernel<KIND, TERMS, NARROW>, dim3(2 * plan.pairs), dim3(F::kThreads), F::kSmemBytes, s, p, maps);
-  if (e != cudaSuccess || p.whole == p.tiles) return e;
-  const int warps = (p.tiles - p.whole) * (F::kCols / 16) * (kRows / 32);
-  return launch_pdl(muon_join_kernel<KIND, TERMS, NARROW>, dim3((warps + kJoinWarps - 1) / kJoinWarps), dim3(32 * kJoinWarps), 0, s, p);
+  e = launch_clusters(2, muon_umma_kernel<KIND, TERMS>, dim3(plan.ctas), dim3(F::kThreads), F::kSmemBytes, s, p, maps);
+  return e != cudaSuccess || p.whole == p.tiles ? e : launch_join<KIND, TERMS, F>(p, s);
+}
+template <int KIND, int TERMS>
+cudaError_t launch_small(Params& p, const Plan& plan, const Maps& maps, cudaStream_t s) {
+  using F = Small<TERMS>;
+  take_plan<F>(p, plan);
+  static unsigned long long configured = 0;
+  cudaError_t e = allow_dynamic_smem(muon_small_kernel<KIND, TERMS>, F::kSmemBytes, configured);
+  if (e != cudaSuccess) return e;
+  e = launch_pdl(muon_small_kernel<KIND, TERMS>, dim3(plan.ctas), dim3(F::kThreads), F::kSmemBytes, s, p, maps);
+  return e != cudaSuccess || p.whole == p.tiles ? e : launch_join<KIND, TERMS, F>(p, s);
 }
 
 // What a product's operands are, and how they lie: `k`: rows are k.
@@ -912,9 +1112,9 @@ struct Operand {
 
 template <int KIND, int TERMS>
 cudaError_t launch(const MuonBatch& b, Params& p, const Operand& x, const Operand& y, int sm_count, cudaStream_t s) {
-  const int pairs = sm_count / 2 < kMuonPairs ? sm_count / 2 : kMuonPairs;
-  const Plan wide = plan_of<TERMS, false>(KIND, p.M, p.N, p.K, b.n, pairs), narrow = plan_of<TERMS, true>(KIND, p.M, p.N, p.K, b.n, pairs);
-  const bool few = narrow.time < wide.time;
+  const Plan pairs = plan_pairs<TERMS>(KIND, p.M, p.N, p.K, b.n, sm_count / 2 < kMuonPairs ? sm_count / 2 : kMuonPairs);
+  const Plan alone = plan_small<TERMS>(KIND, p.M, p.N, p.K, b.n, sm_count);
+  const bool few = alone.time < pairs.time;
   Maps maps;
   for (int t = 0; t < TERMS; ++t) {
     auto make = [&](CUtensorMap* m, const Operand& o, int rows) { return make_map(m, o.data + t * o.term, o.width, o.rows, o.ld, b.n, o.matrix, o.k ? 64 : rows); };
@@ -923,18 +1123,19 @@ cudaError_t launch(const MuonBatch& b, Params& p, const Operand& x, const Operan
   if (TERMS == 1) maps.a[1] = maps.a[0], maps.b[1] = maps.b[0];
   p.a_mn = x.k;
   p.b_mn = y.k;
-  return few ? launch_form<KIND, TERMS, true>(p, narrow, maps, s) : launch_form<KIND, TERMS, false>(p, wide, maps, s);
+  return few ? launch_small<KIND, TERMS>(p, alone, maps, s) : launch_pairs<KIND, TERMS>(p, pairs, maps, s);
 }
 
 }  // namespace
 
 size_t muon_partial_floats(int S, int R, int C, int n, int terms) {
   size_t most = 0;
-  for (int cols : {terms == 1 ? Form<1, false>::kCols : Form<2, false>::kCols, Form<1, true>::kCols}) {
+  const int sizes[2][2] = {{Form<1>::kRows, terms == 1 ? Form<1>::kCols : Form<2>::kCols}, {Small<1>::kRows, Small<1>::kCols}};
+  for (const auto& size : sizes) {
     for (int kind : {kGram, kForm, kApply}) {
       const long long K = kind == kGram ? (R > C ? R : C) : S, blocks = (K + kDeep - 1) / kDeep;
-      const long long tiles = (long long)tiles_of(kind, cols, kind == kApply ? R : S, kind == kApply ? C : S) * n;
-      const size_t floats = (size_t)most_pieces(cols, tiles, blocks) * kRows * cols;
+      const long long tiles = (long long)tiles_of(kind, size[0], size[1], kind == kApply ? R : S, kind == kApply ? C : S) * n;
+      const size_t floats = (size_t)most_pieces(size[0], size[1], tiles, blocks) * size[0] * size[1];
       if (floats > most) most = floats;
     }
   }
