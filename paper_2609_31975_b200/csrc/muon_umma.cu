@@ -61,10 +61,10 @@ template <int TERMS>
 struct Small {
   static constexpr int kRows = 128, kCols = 64;
   static constexpr int kBBytes = kCols * kDeep * 2;
-  static constexpr int kStages = TERMS == 1 ? 4 : 2;
+  static constexpr int kStages = 8 / TERMS;                          // half of them where two CTAs share an SM
   static constexpr int kStageBytes = TERMS * (kBlockBytes + kBBytes);
-  static constexpr int kSmemBytes = kStages * kStageBytes + 1024;
-  static constexpr int kThreads = 256;
+  static constexpr int smem_bytes(int stages) { return stages * kStageBytes + 1024; }
+  static constexpr int kThreads = 64 + 256;
   static constexpr int kRuns = 3;                                    // two terms: runs that have an accumulator
   static constexpr int kTmem = TERMS == 1 ? kCols : (kRuns + 1) * kCols;
   static constexpr int kMostBlocks = TERMS == 1 ? 1 << 20 : kRuns * kRun;  // K blocks of a piece
@@ -78,6 +78,7 @@ struct Params {
   int kind, M, N, K, n;           // n: matrices
   int m_tiles, n_tiles, per, tiles, blocks;
   int whole, split;               // tiles dealt whole; pieces of each of the others
+  int stages;                     // small tiles: of the ring
   int a_mn, b_mn;
   float* partial;
   int piece;                      // floats of a piece
@@ -379,12 +380,34 @@ __device__ __forceinline__ void mirror(const Params& p, uint16_t* out, int m, in
   }
 }
 
-// v: the accumulators of these sixteen columns.  All lanes of a warp come here together.
+// What the result has besides the accumulators, of sixteen columns.
 template <int KIND, int TERMS>
-__device__ __forceinline__ void finish(const Params& p, const Shared<KIND>& all, int batch, int row0, int n0, int lane, float* v, const Ahead<KIND, TERMS>& a) {
-  const int m = row0 + lane;
-  const bool row = m < p.M;
-  if constexpr (!symmetric(KIND)) {
+__device__ __forceinline__ void beside(const Params& p, const Shared<KIND>& all, int batch, int n0, const Ahead<KIND, TERMS>& a, float* v) {
+  if constexpr (KIND == kForm) {
+    // M = N: their entry once, times m + k (d_M[i] + d_M[j])
+    const float by_row = p.k_n * all.f_k * all.d, each = p.k_m * all.f_k, mm = p.N_ ? p.m * all.f_m : p.m * all.f_m + by_row, nn = p.nn * all.f_n + by_row;
+    float d[16];
+    columns16(p.N_diag + batch * diag_ld(p.S) + n0, d);
+#pragma unroll
+    for (int i = 0; i < 16; ++i) d[i] = fmaf(each, d[i], mm);
+#pragma unroll
+    for (int q = 0; q < TERMS; ++q) {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const float2 f = from_halves(a.t[q].w[i]);
+        v[2 * i] = q ? fmaf(d[2 * i], f.x, v[2 * i]) : d[2 * i] * f.x;
+        v[2 * i + 1] = q ? fmaf(d[2 * i + 1], f.y, v[2 * i + 1]) : d[2 * i + 1] * f.y;
+      }
+      if (p.N_) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          const float2 f = from_halves(a.t[TERMS + q].w[i]);
+          v[2 * i] = fmaf(nn, f.x, v[2 * i]);
+          v[2 * i + 1] = fmaf(nn, f.y, v[2 * i + 1]);
+        }
+      }
+    }
+  } else if constexpr (!symmetric(KIND)) {
     const float q = all.f_k + all.d;
     float d[16];
     if (p.tall) {
@@ -396,9 +419,21 @@ __device__ __forceinline__ void finish(const Params& p, const Shared<KIND>& all,
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
       const float2 hi = from_halves(a.t[0].w[i]), lo = from_halves(a.t[1].w[i]);
-      v[2 * i] = fmaf((q + d[2 * i]) * p.x_scale, hi.x + lo.x, v[2 * i] * p.acc_scale);
-      v[2 * i + 1] = fmaf((q + d[2 * i + 1]) * p.x_scale, hi.y + lo.y, v[2 * i + 1] * p.acc_scale);
+      v[2 * i] = (q + d[2 * i]) * p.x_scale * (hi.x + lo.x);
+      v[2 * i + 1] = (q + d[2 * i + 1]) * p.x_scale * (hi.y + lo.y);
     }
+  }
+}
+
+// acc: the accumulators of these sixteen columns, more: what is beside them.  All lanes of a warp come here together.
+template <int KIND, int TERMS>
+__device__ __forceinline__ void finish(const Params& p, const Shared<KIND>& all, int batch, int row0, int n0, int lane, const float* acc, const float* more) {
+  const int m = row0 + lane;
+  const bool row = m < p.M;
+  float v[16];
+  if constexpr (!symmetric(KIND)) {
+#pragma unroll
+    for (int i = 0; i < 16; ++i) v[i] = fmaf(acc[i], p.acc_scale, more[i]);
     if (!row) return;
     if constexpr (KIND == kLast) {
       finish_last(p, batch, m, n0, v);
@@ -413,56 +448,26 @@ __device__ __forceinline__ void finish(const Params& p, const Shared<KIND>& all,
       t.store(out + p.term);
     }
   } else {
-    const bool on_diagonal = (n0 >> 5) == (row0 >> 5);
-    float own = 0.f;  // of the diagonal: this row's accumulator
-    if (on_diagonal) {
+    const float scale = p.k * all.f_k;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) v[i] = KIND == kGram ? acc[i] * scale : fmaf(acc[i], scale, more[i]);
+    if ((n0 >> 5) == (row0 >> 5)) {  // the diagonal goes apart
+      float own = 0.f;
 #pragma unroll
       for (int i = 0; i < 16; ++i)
-        if (n0 + i == m) own = v[i];
-    }
-    if constexpr (KIND == kGram) {
-      if (on_diagonal && row && m >= n0 && m < n0 + 16) p.out_diag[batch * diag_ld(p.S) + m] = own * p.dacc;
-#pragma unroll
-      for (int i = 0; i < 16; ++i) v[i] *= p.k;
-    } else {
-      const int64_t line = batch * diag_ld(p.S);
-      const float fm = all.f_m, fk = all.f_k, d_m = all.d;
-      if (on_diagonal && row && m >= n0 && m < n0 + 16) {
-        const float d_n = __ldcg(p.N_diag + line + m);
-        p.out_diag[line + m] = p.dm * fm * d_m + p.dn * all.f_n * d_n + p.dk * fk * fmaf(own, p.dacc, d_m * d_n);
-      }
-      // M = N: their entry once, times m + k (d_M[i] + d_M[j])
-      const float fixed = p.m * fm, by_row = p.k_n * fk * d_m, each = p.k_m * fk, scale = p.k * fk;
-      const float mm = p.N_ ? fixed : fixed + by_row, nn = p.nn * all.f_n + by_row;
-      float d[16];
-      columns16(p.N_diag + line + n0, d);
-#pragma unroll
-      for (int i = 0; i < 16; ++i) {
-        v[i] *= scale;
-        d[i] = fmaf(each, d[i], mm);
-      }
-#pragma unroll
-      for (int q = 0; q < TERMS; ++q) {
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          const float2 f = from_halves(a.t[q].w[i]);
-          v[2 * i] = fmaf(d[2 * i], f.x, v[2 * i]);
-          v[2 * i + 1] = fmaf(d[2 * i + 1], f.y, v[2 * i + 1]);
+        if (n0 + i == m) {
+          own = acc[i];
+          v[i] = 0.f;
         }
-        if (p.N_) {
-#pragma unroll
-          for (int i = 0; i < 8; ++i) {
-            const float2 f = from_halves(a.t[TERMS + q].w[i]);
-            v[2 * i] = fmaf(nn, f.x, v[2 * i]);
-            v[2 * i + 1] = fmaf(nn, f.y, v[2 * i + 1]);
-          }
+      if (row && m >= n0 && m < n0 + 16) {
+        const int64_t at = batch * diag_ld(p.S) + m;
+        if constexpr (KIND == kGram) {
+          p.out_diag[at] = own * p.dacc;
+        } else {
+          const float d_n = __ldcg(p.N_diag + at);
+          p.out_diag[at] = p.dm * all.f_m * all.d + p.dn * all.f_n * d_n + p.dk * all.f_k * fmaf(own, p.dacc, all.d * d_n);
         }
       }
-    }
-    if (on_diagonal) {
-#pragma unroll
-      for (int i = 0; i < 16; ++i)
-        if (n0 + i == m) v[i] = 0.f;
     }
     uint16_t* const out = p.out + batch * p.matrix;
     const bool twice = (n0 >> 5) < (row0 >> 5);
@@ -724,7 +729,9 @@ __global__ void __launch_bounds__(Form<TERMS>::kThreads, 1) muon_umma_kernel(con
             if (!kEarly) next.load(p, at.batch, row0 + lane, n0);
             const Ahead<KIND, TERMS> now = next;
             if (kEarly && c + 1 < kChunks && wanted<KIND>(p, row0, n0 + 16)) next.load(p, at.batch, row0 + lane, n0 + 16);
-            finish<KIND, TERMS>(p, all, at.batch, row0, n0, lane, sum, now);
+            float more[16];
+            beside<KIND, TERMS>(p, all, at.batch, n0, now, more);
+            finish<KIND, TERMS>(p, all, at.batch, row0, n0, lane, sum, more);
           }
 #pragma unroll
           for (int i = 0; i < 16 * (kChunks - 1); ++i) sum[i] = sum[i + 16];
@@ -751,8 +758,10 @@ __global__ void __launch_bounds__(Form<TERMS>::kThreads, 1) muon_umma_kernel(con
             float v[16];
             tmem_ld16(acc + 16 * c, v);
             if (c + 1 < kChunks && wanted<KIND>(p, row0, n0 + 16)) next.load(p, at.batch, row0 + lane, n0 + 16);
+            float more[16];
+            beside<KIND, TERMS>(p, all, at.batch, n0, now, more);
             tmem_arrived(v);
-            finish<KIND, TERMS>(p, all, at.batch, row0, n0, lane, v, now);
+            finish<KIND, TERMS>(p, all, at.batch, row0, n0, lane, v, more);
           }
         }
         give_back(own);
@@ -773,9 +782,11 @@ __global__ void __launch_bounds__(Form<TERMS>::kThreads, 1) muon_umma_kernel(con
 }
 
 // ---- small tiles -----------------------------------------------------------------------------------------------------
-// For products that do not fill the device with pairs' tiles: a CTA has one tile of 128 x 64 (or a piece of it along K), eight warps,
-// of which the first two issue the copies and the MMAs before they take their share of the epilogue.  Two CTAs an SM, and the next
-// launch's start beside these.  With two terms, every run of K blocks has an accumulator of its own, so a piece is at most three runs.
+// For products that do not fill the device with pairs' tiles: a CTA has one tile of 128 x 64 (or a piece of it along K).  A chain of
+// such launches is a chain of latencies (1024 x 256, fp32: 1.8 us from a launch's end to the next one's start, 1.3 to the first K block): the
+// eight warps of the epilogue read and multiply what is beside the accumulators while these are made, and where the launch leaves SMs
+// idle, all K blocks of a short K are under way at once.  With two terms, every run of K blocks has an accumulator of its own, so a piece is
+// at most three runs.
 __device__ __forceinline__ void tma_tile_alone(uint32_t dst, const CUtensorMap* map, int c0, int c1, int c2, uint32_t bar) {
   asm volatile(
       "cp.async.bulk.tensor.3d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];" ::"r"(dst), "l"(map), "r"(c0), "r"(c1),
@@ -811,6 +822,7 @@ __global__ void __launch_bounds__(Small<TERMS>::kThreads, 2) muon_small_kernel(c
     abort_word = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
+  if (warp == 0 && lane < 2 * TERMS) asm volatile("prefetch.tensormap [%0];" ::"l"(lane < TERMS ? &maps.a[lane] : &maps.b[lane - TERMS]) : "memory");
   if (warp == 2) {
     asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&tmem_slot)), "r"(F::kTmem) : "memory");
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
@@ -852,7 +864,7 @@ __global__ void __launch_bounds__(Small<TERMS>::kThreads, 2) muon_small_kernel(c
         }
       }
       __syncwarp();
-      if (++s == kStages) { s = 0; phase ^= 1; }
+      if (++s == p.stages) { s = 0; phase ^= 1; }
     }
   } else if (warp == 1) {
     const uint32_t idesc = idesc_f16(F::kRows, F::kCols, p.a_mn, p.b_mn);
@@ -883,40 +895,47 @@ __global__ void __launch_bounds__(Small<TERMS>::kThreads, 2) muon_small_kernel(c
         if (u + 1 == u1) commit_alone(acc_full);
       }
       __syncwarp();
-      if (++s == kStages) { s = 0; phase ^= 1; }
+      if (++s == p.stages) { s = 0; phase ^= 1; }
     }
-  }
-  __syncwarp();
-
-  const int quad = warp & 3, n_base = at.n * F::kCols + 32 * (warp >> 2), row0 = at.m * F::kRows + 32 * quad;
-  const bool rows = row0 < p.M;
-  Ahead<KIND, TERMS> next;
-  if (rows && !pieces && wanted<KIND>(p, row0, n_base)) next.load(p, at.batch, row0 + lane, n_base);
-  const Shared<KIND> all(p, at.batch, row0 + lane);
-  if (wait_all(acc_full, 0) && rows) {
-    fence_after();
-    const uint32_t acc = tmem + ((uint32_t)(32 * quad) << 16) + 32 * (warp >> 2);
-    float* const piece = p.partial + (size_t)number * p.piece + (size_t)(32 * quad + lane) * F::kCols + 32 * (warp >> 2);
-#pragma unroll 1
-    for (int c = 0; c < 2; ++c) {
-      const int n0 = n_base + 16 * c;
-      if (!pieces && !wanted<KIND>(p, row0, n0)) break;
-      const Ahead<KIND, TERMS> now = next;
-      float v[16];
-      tmem_ld16(acc + 16 * c, v);
-      if (!pieces && c == 0 && wanted<KIND>(p, row0, n0 + 16)) next.load(p, at.batch, row0 + lane, n0 + 16);
-      tmem_arrived(v);
-      if constexpr (TERMS == 2) {  // the small products first
-        for (int run = 0; run * kRun < u1 - u0; ++run) {
-          float w[16];
-          tmem_ld16(acc + (1 + run) * F::kCols + 16 * c, w);
-          tmem_arrived(w);
+  } else {
+    const int quad = warp & 3, across = 32 * ((warp - 2) >> 2), n_base = at.n * F::kCols + across, row0 = at.m * F::kRows + 32 * quad;
+    const bool rows = row0 < p.M;
+    float more[2][16];
+    const Shared<KIND> all(p, at.batch, row0 + lane);
+    if (rows && !pieces) {
 #pragma unroll
-          for (int i = 0; i < 16; ++i) v[i] += w[i];
-        }
+      for (int c = 0; c < 2; ++c) {
+        if (!wanted<KIND>(p, row0, n_base + 16 * c)) break;
+        Ahead<KIND, TERMS> a;
+        a.load(p, at.batch, row0 + lane, n_base + 16 * c);
+        beside<KIND, TERMS>(p, all, at.batch, n_base + 16 * c, a, more[c]);
       }
-      if (pieces) put_piece(piece + 16 * c, v);
-      else finish<KIND, TERMS>(p, all, at.batch, row0, n0, lane, v, now);
+    }
+    if (wait_all(acc_full, 0) && rows) {
+      fence_after();
+      const uint32_t acc = tmem + ((uint32_t)(32 * quad) << 16) + across;
+      float* const piece = p.partial + (size_t)number * p.piece + (size_t)(32 * quad + lane) * F::kCols + across;
+#pragma unroll 1
+      for (int c = 0; c < 2; ++c) {
+        const int n0 = n_base + 16 * c;
+        if (!pieces && !wanted<KIND>(p, row0, n0)) break;
+        float v[16];
+        tmem_ld16(acc + 16 * c, v);
+        tmem_arrived(v);
+        if constexpr (TERMS == 2) {  // the small products first
+          for (int run = 0; run * kRun < u1 - u0; ++run) {
+            float w[16];
+            tmem_ld16(acc + (1 + run) * F::kCols + 16 * c, w);
+            tmem_arrived(w);
+#pragma unroll
+            for (int i = 0; i < 16; ++i) v[i] += w[i];
+          }
+        }
+        if (pieces) put_piece(piece + 16 * c, v);
+        else finish<KIND, TERMS>(p, all, at.batch, row0, n0, lane, v, more[0]);
+#pragma unroll
+        for (int i = 0; i < 16; ++i) more[0][i] = more[1][i];
+      }
     }
   }
   if (*abort_flag)  // (copies and MMAs that may still be in flight end within microseconds)
@@ -945,7 +964,7 @@ __global__ void __launch_bounds__(32 * kJoinWarps) muon_join_kernel(const __grid
   Ahead<KIND, TERMS> now;
   now.load(p, at.batch, row0 + lane, n0);
   const Shared<KIND> all(p, at.batch, row0 + lane);
-  float v[16] = {};
+  float v[16] = {}, more[16];
   const float* from = p.partial + (size_t)t * p.piece + (size_t)(r0 + lane) * F::kCols + c0;
   const size_t next = (size_t)(p.tiles - p.whole) * p.piece;
 #pragma unroll 4
@@ -956,7 +975,8 @@ __global__ void __launch_bounds__(32 * kJoinWarps) muon_join_kernel(const __grid
       v[4 * i] += f.x; v[4 * i + 1] += f.y; v[4 * i + 2] += f.z; v[4 * i + 3] += f.w;
     }
   }
-  finish<KIND, TERMS>(p, all, at.batch, row0, n0, lane, v, now);
+  beside<KIND, TERMS>(p, all, at.batch, n0, now, more);
+  finish<KIND, TERMS>(p, all, at.batch, row0, n0, lane, v, more);
 }
 
 // ---- host ------------------------------------------------------------------------------------------------------------
@@ -997,7 +1017,7 @@ int tiles_of(int kind, int rows, int cols, int M, int N, int* m_tiles = nullptr,
 }
 
 struct Plan {
-  int per, m_tiles, n_tiles, tiles, whole, split, ctas;
+  int per, m_tiles, n_tiles, tiles, whole, split, ctas, stages;
   double time;
 };
 // Floats of the pieces that the workspace has room for: 84 MB.
@@ -1061,6 +1081,7 @@ Plan plan_small(int kind, int M, int N, int K, int n, int sms) {
   }
   p.whole = p.split > 1 ? 0 : p.tiles;
   p.ctas = p.tiles * p.split;
+  p.stages = p.ctas > sms ? F::kStages / 2 : F::kStages;
   return p;
 }
 
@@ -1072,6 +1093,7 @@ cudaError_t launch_join(const Params& p, cudaStream_t s) {
 template <typename F>
 void take_plan(Params& p, const Plan& plan) {
   p.m_tiles = plan.m_tiles; p.n_tiles = plan.n_tiles; p.per = plan.per; p.tiles = plan.tiles; p.whole = plan.whole; p.split = plan.split;
+  p.stages = plan.stages;
   p.blocks = (p.K + kDeep - 1) / kDeep;
   p.piece = F::kRows * F::kCols;
 }
@@ -1097,9 +1119,9 @@ cudaError_t launch_small(Params& p, const Plan& plan, const Maps& maps, cudaStre
   using F = Small<TERMS>;
   take_plan<F>(p, plan);
   static unsigned long long configured = 0;
-  cudaError_t e = allow_dynamic_smem(muon_small_kernel<KIND, TERMS>, F::kSmemBytes, configured);
+  cudaError_t e = allow_dynamic_smem(muon_small_kernel<KIND, TERMS>, F::smem_bytes(F::kStages), configured);
   if (e != cudaSuccess) return e;
-  e = launch_pdl(muon_small_kernel<KIND, TERMS>, dim3(plan.ctas), dim3(F::kThreads), F::kSmemBytes, s, p, maps);
+  e = launch_pdl(muon_small_kernel<KIND, TERMS>, dim3(plan.ctas), dim3(F::kThreads), F::smem_bytes(plan.stages), s, p, maps);
   return e != cudaSuccess || p.whole == p.tiles ? e : launch_join<KIND, TERMS, F>(p, s);
 }
 
