@@ -43,9 +43,12 @@ def block_norm_backward(dh, dn, y, h, stats, post_gain=None, pre_gain=None, gate
     if stream is not None:
         with torch.cuda.stream(stream):
             return block_norm_backward(dh, dn, y, h, stats, post_gain, pre_gain, gate, scale=scale, need=need, out=out)
-    for name in (*need, *(out or ())):
-        if name not in BLOCK_GRADS:
-            raise ValueError(f"no such gradient: {name!r}")
+    bits = 31
+    if need is not BLOCK_GRADS or out:
+        for name in (*need, *(out or ())):
+            if name not in BLOCK_GRADS:
+                raise ValueError(f"no such gradient: {name!r}")
+        bits = sum(1 << BLOCK_GRADS.index(name) for name in set(need))
     if dh is None and dn is None:
         raise ValueError("dh or dn is needed")
     if h.dim() == 1:  # one token
@@ -53,7 +56,6 @@ def block_norm_backward(dh, dn, y, h, stats, post_gain=None, pre_gain=None, gate
         rows = {k: t[None] if k in ("dy", "dresid") else t for k, t in (out or {}).items()}
         got = block_norm_backward(one(dh), one(dn), one(y), h[None], stats, post_gain, pre_gain, gate, scale=scale, need=need, out=rows)
         return {k: t[0] if k in ("dy", "dresid") else t for k, t in got.items()}
-    bits = sum(1 << BLOCK_GRADS.index(name) for name in set(need))
     rc, *got = _calls().block_backward(dh, dn, y, h, stats, post_gain, pre_gain, gate, scale, bits, [out.get(name) for name in BLOCK_GRADS] if out else [])
     if rc:
         raise SFFNError("sffn_block_norm_backward", rc)

@@ -65,7 +65,10 @@ int sffn_block_norm_forward(const sffn_block_norm* c, void* stream) {
   if (outputs_meet({y, gate_of(c, c->gate, c->ld_gate), whole(c->post_gain, 4ll * c->D), whole(c->pre_gain, 4ll * c->D)}, {h, n, stats}) || meet(n, resid) ||
       meet(stats, resid) || (meet(h, resid) && !same(h, resid)))
     return SFFN_ERR_INVALID_ARG;
-  SFFN_CUDA(sffn::launch_block_forward(*c, static_cast<cudaStream_t>(stream)));
+  int sms = 0;
+  const int count = sm_count(&sms);
+  if (count != SFFN_OK) return count;
+  SFFN_CUDA(sffn::launch_block_forward(*c, sms, static_cast<cudaStream_t>(stream)));
   return SFFN_OK;
 }
 

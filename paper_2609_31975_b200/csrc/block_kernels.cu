@@ -21,6 +21,21 @@
 namespace sffn {
 namespace {
 
+// What becomes of the sums of columns.  The second array holds sum g y (r, scale, and a gate that is not one of the channels in it): times the
+// channel gate it is the post gain's gradient, times the post gain the gate's.
+struct ColumnSums {
+  const float *post_gain, *gate;  // gate: of channels, or NULL
+  float *dpre, *dpost, *dgate;    // NULL: not wanted
+};
+__device__ __forceinline__ void column_out(const ColumnSums& o, int which, int c, float s) {
+  if (which == 0) {
+    o.dpre[c] = s;
+  } else {
+    if (o.dpost) o.dpost[c] = s * (o.gate ? o.gate[c] : 1.f);
+    if (o.dgate) o.dgate[c] = s * (o.post_gain ? o.post_gain[c] : 1.f);
+  }
+}
+
 struct BlockParams {
   int T, D;
   int y_bf16, h_bf16, n_bf16, gate_kind;
@@ -37,15 +52,25 @@ struct BlockParams {
   int64_t ld_dh, ld_dn, ld_dy, ld_dresid, ld_dgate;
   float* partial;                         // [2][lines][D], or NULL
   int lines, want_pre, want_c;
+  int wide;                               // fp32 rows start on 32 bytes, all of them
+  int together;                           // the launch is one cluster
+  ColumnSums sums;
 };
 
 // Eight entries as they lie in memory (16 bytes of bf16, 32 of fp32; fp32 rows may end after four), and as fp32.
 struct Raw {
   uint4 a, b;
 };
-__device__ __forceinline__ Raw load_raw(const char* row, int bf16, int c, int D) {
+__device__ __forceinline__ Raw load_raw(const char* row, int bf16, int wide, int c, int D) {
   Raw r;
   const char* p = row + ((int64_t)c << (bf16 ? 1 : 2));
+  if (!bf16 && wide && c + 4 < D) {
+    asm volatile("ld.global.v8.b32 {%0,%1,%2,%3,%4,%5,%6,%7}, [%8];"
+                 : "=r"(r.a.x), "=r"(r.a.y), "=r"(r.a.z), "=r"(r.a.w), "=r"(r.b.x), "=r"(r.b.y), "=r"(r.b.z), "=r"(r.b.w)
+                 : "l"(p)
+                 : "memory");
+    return r;
+  }
   r.a = *reinterpret_cast<const uint4*>(p);
   r.b = make_uint4(0, 0, 0, 0);
   if (!bf16 && c + 4 < D) r.b = *reinterpret_cast<const uint4*>(p + 16);
@@ -63,10 +88,13 @@ __device__ __forceinline__ uint32_t two_bf16(float lo, float hi) {
   const __nv_bfloat162 v = __floats2bfloat162_rn(lo, hi);
   return *reinterpret_cast<const uint32_t*>(&v);
 }
-__device__ __forceinline__ void store8(char* row, int bf16, int c, int D, const float* f) {
+__device__ __forceinline__ void store8(char* row, int bf16, int wide, int c, int D, const float* f) {
   char* p = row + ((int64_t)c << (bf16 ? 1 : 2));
   if (bf16) {
     *reinterpret_cast<uint4*>(p) = make_uint4(two_bf16(f[0], f[1]), two_bf16(f[2], f[3]), two_bf16(f[4], f[5]), two_bf16(f[6], f[7]));
+  } else if (wide && c + 4 < D) {  // (16 bytes at a time would write every sector of L2 twice)
+    asm volatile("st.global.v8.f32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};" ::"l"(p), "f"(f[0]), "f"(f[1]), "f"(f[2]), "f"(f[3]), "f"(f[4]), "f"(f[5]), "f"(f[6]), "f"(f[7])
+                 : "memory");
   } else {
     *reinterpret_cast<float4*>(p) = make_float4(f[0], f[1], f[2], f[3]);
     if (c + 4 < D) *reinterpret_cast<float4*>(p + 16) = make_float4(f[4], f[5], f[6], f[7]);
@@ -78,6 +106,75 @@ __device__ __forceinline__ void load_gain(const float* g, int c, int D, float* f
   const float4 b = c + 4 < D ? __ldg(reinterpret_cast<const float4*>(g + c + 4)) : make_float4(0.f, 0.f, 0.f, 0.f);
   f[0] = a.x; f[1] = a.y; f[2] = a.z; f[3] = a.w;
   f[4] = b.x; f[5] = b.y; f[6] = b.z; f[7] = b.w;
+}
+
+// The same eight entries in pairs, for arithmetic on two at a time.
+struct Eight {
+  float2 v[4];
+};
+__device__ __forceinline__ float2 mul2(float2 a, float2 b) {
+  float2 d;
+  asm("{\n\t.reg .b64 ra, rb, rd;\n\tmov.b64 ra, {%2, %3};\n\tmov.b64 rb, {%4, %5};\n\tmul.rn.f32x2 rd, ra, rb;\n\tmov.b64 {%0, %1}, rd;\n\t}"
+      : "=f"(d.x), "=f"(d.y)
+      : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
+  return d;
+}
+__device__ __forceinline__ float2 both(float s) { return make_float2(s, s); }
+__device__ __forceinline__ Eight operator*(const Eight& a, const Eight& b) {
+  Eight r;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) r.v[i] = mul2(a.v[i], b.v[i]);
+  return r;
+}
+__device__ __forceinline__ Eight operator*(const Eight& a, float s) {
+  Eight r;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) r.v[i] = mul2(a.v[i], both(s));
+  return r;
+}
+__device__ __forceinline__ Eight fma8(const Eight& a, const Eight& b, const Eight& c) {
+  Eight r;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) r.v[i] = fma2(a.v[i], b.v[i], c.v[i]);
+  return r;
+}
+__device__ __forceinline__ Eight fma8(const Eight& a, float s, const Eight& c) {
+  Eight r;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) r.v[i] = fma2(a.v[i], both(s), c.v[i]);
+  return r;
+}
+__device__ __forceinline__ Eight eight_of(float s) {
+  Eight r;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) r.v[i] = both(s);
+  return r;
+}
+// sum + a . b, the two halves of the sum apart
+__device__ __forceinline__ float2 dot8(const Eight& a, const Eight& b, float2 sum) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i) sum = fma2(a.v[i], b.v[i], sum);
+  return sum;
+}
+__device__ __forceinline__ Eight unpack8(const Raw& r, int bf16) {
+  float f[8];
+  unpack(r, bf16, f);
+  Eight e;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) e.v[i] = make_float2(f[2 * i], f[2 * i + 1]);
+  return e;
+}
+__device__ __forceinline__ Eight gain8(const float* g, int c, int D) {
+  float f[8];
+  load_gain(g, c, D, f);
+  Eight e;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) e.v[i] = make_float2(f[2 * i], f[2 * i + 1]);
+  return e;
+}
+__device__ __forceinline__ void store8(char* row, int bf16, int wide, int c, int D, const Eight& e) {
+  const float f[8] = {e.v[0].x, e.v[0].y, e.v[1].x, e.v[1].y, e.v[2].x, e.v[2].y, e.v[3].x, e.v[3].y};
+  store8(row, bf16, wide, c, D, f);
 }
 
 // Sums over the W warps of a row, every thread's result bitwise the same.  `room`: W floats, not in use by the sum before.
@@ -111,9 +208,9 @@ __global__ void __launch_bounds__(Shape<W, V>::kThreads) block_forward_kernel(co
   for (int i = 0; i < V; ++i) {
     const int c = 8 * (in_row + 32 * W * i);
     if (c >= p.D) continue;
-    if (p.y) y[i] = load_raw(p.y + t * p.ld_y, p.y_bf16, c, p.D);
-    if (p.resid) x[i] = load_raw(p.resid + t * p.ld_resid, p.h_bf16, c, p.D);
-    if (p.gate_kind == SFFN_BLOCK_GATE_FULL) gate[i] = load_raw(p.gate + t * p.ld_gate, p.h_bf16, c, p.D);
+    if (p.y) y[i] = load_raw(p.y + t * p.ld_y, p.y_bf16, p.wide, c, p.D);
+    if (p.resid) x[i] = load_raw(p.resid + t * p.ld_resid, p.h_bf16, p.wide, c, p.D);
+    if (p.gate_kind == SFFN_BLOCK_GATE_FULL) gate[i] = load_raw(p.gate + t * p.ld_gate, p.h_bf16, p.wide, c, p.D);
   }
   float r = 1.f;
   if (post) {
@@ -159,7 +256,7 @@ __global__ void __launch_bounds__(Shape<W, V>::kThreads) block_forward_kernel(co
       }
 #pragma unroll
       for (int j = 0; j < 8; ++j) h[i][j] += f[j];
-      store8(p.h + t * p.ld_h, p.h_bf16, c, p.D, h[i]);
+      store8(p.h + t * p.ld_h, p.h_bf16, p.wide, c, p.D, h[i]);
     }
 #pragma unroll
     for (int j = 0; j < 8; ++j) hh = fmaf(h[i][j], h[i][j], hh);
@@ -175,7 +272,7 @@ __global__ void __launch_bounds__(Shape<W, V>::kThreads) block_forward_kernel(co
       load_gain(p.pre_gain, c, p.D, g);
 #pragma unroll
       for (int j = 0; j < 8; ++j) g[j] *= h[i][j] * rho;
-      store8(p.n + t * p.ld_n, p.n_bf16, c, p.D, g);
+      store8(p.n + t * p.ld_n, p.n_bf16, p.wide, c, p.D, g);
     }
   }
   if (p.stats && in_row == 0) {
@@ -184,36 +281,49 @@ __global__ void __launch_bounds__(Shape<W, V>::kThreads) block_forward_kernel(co
   }
 }
 
-// Four sums over the W warps of a row.  `room`: 4 W floats, not in use by the sums before.
+// ---- rows through shared memory ---------------------------------------------------------------------------------------
+
+// Four sums over the W warps of a row: six exchanges leave sum k in lanes 8 k to 8 k + 7.  `room`: 4 W floats, not in use by the sums before.
 template <int W>
 __device__ __forceinline__ void row_sums(float (&v)[4], float* room) {
+  const int lane = threadIdx.x & 31;
 #pragma unroll
-  for (int k = 0; k < 4; ++k) v[k] = warp_sum(v[k]);
+  for (int width = 2; width >= 1; width >>= 1) {
+    const bool upper = lane & (8 * width);
+#pragma unroll
+    for (int i = 0; i < width; ++i) {
+      const float send = upper ? v[i] : v[i + width], keep = upper ? v[i + width] : v[i];
+      v[i] = keep + __shfl_xor_sync(0xffffffffu, send, 8 * width);
+    }
+  }
+  float s = v[0];
+#pragma unroll
+  for (int o = 4; o >= 1; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
   if constexpr (W > 1) {
-    const int lane = threadIdx.x & 31;
-    if (lane == 0) *reinterpret_cast<float4*>(room + 4 * (threadIdx.x >> 5)) = make_float4(v[0], v[1], v[2], v[3]);
+    const int warp = (threadIdx.x >> 5) % W;
+    if ((lane & 7) == 0) room[4 * warp + (lane >> 3)] = s;
     __syncthreads();
-    float s = 0.f;  // lane l: sum l % 4, of every eighth warp
+    s = 0.f;  // lane l: sum l / 8, of every eighth warp
 #pragma unroll
     for (int w = 0; w < W; w += 8)
-      if (w + (lane >> 2) < W) s += room[4 * w + lane];
+      if (w + (lane & 7) < W) s += room[4 * (w + (lane & 7)) + (lane >> 3)];
 #pragma unroll
-    for (int o = 4; o < 32; o <<= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
-#pragma unroll
-    for (int k = 0; k < 4; ++k) v[k] = __shfl_sync(0xffffffffu, s, k);
+    for (int o = 1; o <= 4; o <<= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
   }
+#pragma unroll
+  for (int k = 0; k < 4; ++k) v[k] = __shfl_sync(0xffffffffu, s, 8 * k);
 }
 
-// Rows of up to 8192 entries: W warps, two pieces of eight entries a thread (one where W is 1: eight rows a CTA).  Wider ones: 32 warps of up
-// to four, whose sums of columns do not fit registers beside the rest.
+constexpr int kMostStages = 6;  // rows under way, at most
+
+// Rows of up to 8192 entries: W warps, one or two pieces of eight entries a thread (W 1: eight rows a CTA).  Wider ones: 32 warps of up to four
+// pieces, which have no room in shared memory and whose sums of columns do not fit registers beside the rest.
 template <int W, int V>
-struct BackShape {
+struct Ring {
   static constexpr int kRows = W == 1 ? 8 : 1, kThreads = 32 * W * kRows;
   static constexpr int kPerSm = kThreads >= 512 ? 1 : 512 / kThreads;
-  static constexpr bool kRing = W < 32;  // rows come through shared memory, which has no room for wider ones
+  static constexpr bool kShared = W < 32;
 };
-constexpr int kBackStages = 4;  // rows under way, at most
-
 __device__ __forceinline__ void copy16(uint32_t to, const char* from) {
   asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to), "l"(from) : "memory");
 }
@@ -222,210 +332,274 @@ __device__ __forceinline__ uint4 shared16(uint32_t from) {
   asm volatile("ld.shared.v4.b32 {%0,%1,%2,%3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(from) : "memory");
   return v;
 }
-
-// Every thread copies what it will read itself into shared memory, `stages` rows ahead: its own copies are all that it waits for.
-// ALL_BF16: y, h and n are bf16, else each is what the call says.
-template <int W, int V, bool ALL_BF16>
-__global__ void __launch_bounds__(BackShape<W, V>::kThreads, BackShape<W, V>::kPerSm)
-    block_backward_kernel(const __grid_constant__ BlockParams p, int stages) {
-  constexpr int kRows = BackShape<W, V>::kRows, kThreads = BackShape<W, V>::kThreads;
-  extern __shared__ __align__(16) uint8_t ring_raw[];
-  __shared__ __align__(16) float room[2][4 * W];
-  __shared__ float lines[W == 1 ? kRows : 1][W == 1 ? 256 * V : 1];
-  const int in_row = threadIdx.x % (32 * W);
-  const bool y_bf16 = ALL_BF16 || p.y_bf16, h_bf16 = ALL_BF16 || p.h_bf16, n_bf16 = ALL_BF16 || p.n_bf16;
-  const bool post = p.post_gain != nullptr, full = p.gate_kind == SFFN_BLOCK_GATE_FULL, channel = p.gate_kind == SFFN_BLOCK_GATE_CHANNEL;
-  const bool has_dh = p.dh != nullptr, has_n = p.dn != nullptr, has_y = p.y != nullptr;
-  // The ring: for every stage, array and piece (and half of an fp32 piece) a plane of 16 bytes a thread.
-  const int wide_h = h_bf16 ? 1 : 2, wide_n = n_bf16 ? 1 : 2, wide_y = y_bf16 ? 1 : 2;
-  struct Array {
-    const char* p;
-    int64_t ld;
-    int plane;
-    bool bf16;
-  };
-  const Array dh = {p.dh, p.ld_dh, 0, h_bf16}, dn = {p.dn, p.ld_dn, has_dh ? wide_h : 0, n_bf16}, h = {p.h, p.ld_h, dn.plane + (has_n ? wide_n : 0), h_bf16};
-  const Array y = {p.y, p.ld_y, h.plane + (has_n ? wide_h : 0), y_bf16}, gate = {p.gate, p.ld_gate, y.plane + (has_y ? wide_y : 0), h_bf16};
-  const int stage_bytes = (gate.plane + (full ? wide_h : 0)) * V * kThreads * 16;
-  const uint32_t ring = static_cast<uint32_t>(__cvta_generic_to_shared(ring_raw)) + threadIdx.x * 16;
-  auto plane = [&](int stage, const Array& a, int i) { return ring + stage * stage_bytes + (a.plane * V + (a.bf16 ? i : 2 * i)) * (kThreads * 16); };
-
-  pdl_launch_dependents();
-  pdl_wait();
-  auto copy_piece = [&](int stage, const Array& a, int t, int i, int c) {
+// Rows of a matrix; in a ring's stage, its first plane (16 bytes a thread and piece; two of an fp32 matrix).
+struct Array {
+  const char* p;
+  int64_t ld;
+  int plane;
+  bool bf16;
+};
+// Every warp copies what it will read itself, `stages` rows ahead, 512 consecutive bytes at a time: its own copies are all that it waits for.
+template <int W, int V>
+struct Rows {
+  static constexpr int kPlane = Ring<W, V>::kThreads * 16;
+  uint32_t ring;  // this thread's 16 bytes of the first plane
+  int D, T, wide, in_row, stages, stage_bytes;
+  __device__ __forceinline__ Rows(const BlockParams& p, const uint8_t* raw, int stages_, int planes)
+      : ring(static_cast<uint32_t>(__cvta_generic_to_shared(raw)) + threadIdx.x * 16), D(p.D), T(p.T), wide(p.wide), in_row(threadIdx.x % (32 * W)), stages(stages_),
+        stage_bytes(planes * V * kPlane) {}
+  __device__ __forceinline__ int column(int i) const { return 8 * (in_row + 32 * W * i); }
+  __device__ __forceinline__ uint32_t plane(int stage, const Array& a, int i) const {
+    return ring + stage * stage_bytes + (a.plane * V + (a.bf16 ? i : 2 * i)) * kPlane;
+  }
+  __device__ __forceinline__ void copy(int stage, const Array& a, int t, int i) const {
+    if (!a.p) return;
+    const int c = column(i);
     const uint32_t to = plane(stage, a, i);
-    const char* from = a.p + t * a.ld + ((int64_t)c << (a.bf16 ? 1 : 2));
-    copy16(to, from);
-    if (!a.bf16 && c + 4 < p.D) copy16(to + kThreads * 16, from + 16);
-  };
-  auto fetch = [&](int stage, int t) {
-    if constexpr (!BackShape<W, V>::kRing) return;
-    if (t < p.T) {
-#pragma unroll
-      for (int i = 0; i < V; ++i) {
-        const int c = 8 * (in_row + 32 * W * i);
-        if (c >= p.D) continue;
-        if (has_dh) copy_piece(stage, dh, t, i, c);
-        if (has_n) {
-          copy_piece(stage, dn, t, i, c);
-          copy_piece(stage, h, t, i, c);
-        }
-        if (has_y) copy_piece(stage, y, t, i, c);
-        if (full) copy_piece(stage, gate, t, i, c);
-      }
-    }
-    asm volatile("cp.async.commit_group;" ::: "memory");  // a group a row, empty or not
-  };
-  auto get = [&](int stage, const Array& a, int t, int i, int c, float* f) {
-    Raw r;
-    if constexpr (BackShape<W, V>::kRing) {
-      const uint32_t from = plane(stage, a, i);
-      r.a = shared16(from);
-      if (!a.bf16) r.b = c + 4 < p.D ? shared16(from + kThreads * 16) : make_uint4(0, 0, 0, 0);
-    } else {
-      r = load_raw(a.p + t * a.ld, a.bf16, c, p.D);
-    }
-    unpack(r, a.bf16, f);
-  };
-
-  const int first = blockIdx.x * kRows + threadIdx.x / (32 * W), step = gridDim.x * kRows;
-  for (int q = 0; q < stages; ++q) fetch(q, first + q * step);  // (not more than 2^30 rows and a grid's: no overflow)
-  // This thread's columns: n's gains, and what multiplies y's entries but for r and a gate of a token's or an entry's.
-  float pre[V][8], w[V][8], acc_pre[V][8], acc_c[V][8];
-#pragma unroll
-  for (int i = 0; i < V; ++i) {
-    const int c = 8 * (in_row + 32 * W * i);
-#pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      acc_pre[i][j] = acc_c[i][j] = pre[i][j] = 0.f;
-      w[i][j] = p.scale;
-    }
-    if (c >= p.D) continue;
-    if (has_n) load_gain(p.pre_gain, c, p.D, pre[i]);
-    float f[8];
-    if (post) {
-      load_gain(p.post_gain, c, p.D, f);
-#pragma unroll
-      for (int j = 0; j < 8; ++j) w[i][j] *= f[j];
-    }
-    if (channel) {
-      load_gain(reinterpret_cast<const float*>(p.gate), c, p.D, f);
-#pragma unroll
-      for (int j = 0; j < 8; ++j) w[i][j] *= f[j];
+    const char* const row = a.p + t * a.ld;
+    if (a.bf16) {
+      if (c < D) copy16(to, row + 2 * c);
+    } else {  // a warp's 256 columns: four of each lane, and four 128 further on
+      const int d = c - 4 * (int)(threadIdx.x & 31);
+      if (d < D) copy16(to, row + 4 * d);
+      if (d + 128 < D) copy16(to + kPlane, row + 4 * d + 512);
     }
   }
-  int turn = 0, stage = 0;
-  for (int t = first; t < p.T; t += step, turn ^= 1) {
-    if (stages >= 4) asm volatile("cp.async.wait_group 3;" ::: "memory");
-    else if (stages == 3) asm volatile("cp.async.wait_group 2;" ::: "memory");
-    else if (stages == 2) asm volatile("cp.async.wait_group 1;" ::: "memory");
-    else asm volatile("cp.async.wait_group 0;" ::: "memory");
-    const float r = post ? p.stats[t] : 1.f, rho = has_n ? p.stats[p.T + t] : 0.f;
-    const float token = p.gate_kind == SFFN_BLOCK_GATE_TOKEN ? reinterpret_cast<const float*>(p.gate)[t] : 1.f;
-    float sums[4] = {0.f, 0.f, 0.f, 0.f};  // of t h, w y dh, w y t, w y h
+  // A row of each array, one group of copies, empty or not.
+  template <typename... A>
+  __device__ __forceinline__ void fetch(int stage, int t, const A&... arrays) const {
+    if constexpr (Ring<W, V>::kShared) {
+      __syncwarp();  // all lanes have read what was there
+      if (t < T) {
+#pragma unroll
+        for (int i = 0; i < V; ++i) (copy(stage, arrays, t, i), ...);
+      }
+      asm volatile("cp.async.commit_group;" ::: "memory");
+    }
+  }
+  // The oldest row is there, all but `more` of the rows under way.
+  __device__ __forceinline__ void wait(int more) const {
+    if constexpr (Ring<W, V>::kShared) {
+      if (more >= 5) asm volatile("cp.async.wait_group 5;" ::: "memory");
+      else if (more == 4) asm volatile("cp.async.wait_group 4;" ::: "memory");
+      else if (more == 3) asm volatile("cp.async.wait_group 3;" ::: "memory");
+      else if (more == 2) asm volatile("cp.async.wait_group 2;" ::: "memory");
+      else if (more == 1) asm volatile("cp.async.wait_group 1;" ::: "memory");
+      else asm volatile("cp.async.wait_group 0;" ::: "memory");
+      __syncwarp();
+    }
+  }
+  __device__ __forceinline__ Eight get(int stage, const Array& a, int t, int i) const {
+    const int c = column(i);
+    Raw r;
+    if constexpr (Ring<W, V>::kShared) {
+      const uint32_t at = plane(stage, a, i);
+      if (a.bf16) {
+        r.a = shared16(at);
+      } else {  // lanes 0 to 15 have the first plane's 512 bytes, 32 each; their two reads in turn, so that eight lanes meet all banks
+        const int lane = threadIdx.x & 31;
+        const uint32_t own = at - 16 * lane + (lane >> 4) * kPlane + 32 * (lane & 15), swap = (lane & 4) << 2;
+        const uint4 u = shared16(own + swap), v = shared16(own + (16 ^ swap));
+        r.a = swap ? v : u;
+        r.b = c + 4 < D ? (swap ? u : v) : make_uint4(0, 0, 0, 0);
+      }
+    } else {
+      r = load_raw(a.p + t * a.ld, a.bf16, wide, c, D);
+    }
+    return unpack8(r, a.bf16);
+  }
+};
+// What multiplies y's entries in a thread's columns but for r and a gate of a token's or an entry's.
+template <int W, int V>
+__device__ __forceinline__ void weights_of(const BlockParams& p, const Rows<W, V>& rows, Eight (&w)[V]) {
+#pragma unroll
+  for (int i = 0; i < V; ++i) {
+    w[i] = eight_of(p.scale);
+    const int c = rows.column(i);
+    if (c >= p.D) continue;
+    if (p.post_gain) w[i] = w[i] * gain8(p.post_gain, c, p.D);
+    if (p.gate_kind == SFFN_BLOCK_GATE_CHANNEL) w[i] = w[i] * gain8(reinterpret_cast<const float*>(p.gate), c, p.D);
+  }
+}
+
+// The forward pass over many rows.  ALL_BF16: y, h and n are bf16, else each is what the call says.
+template <int W, int V, bool ALL_BF16>
+__global__ void __launch_bounds__(Ring<W, V>::kThreads, Ring<W, V>::kPerSm) block_forward_rows_kernel(const __grid_constant__ BlockParams p, int stages, int planes) {
+  extern __shared__ __align__(16) uint8_t ring_raw[];
+  __shared__ float room[2][32];
+  const bool y_bf16 = ALL_BF16 || p.y_bf16, h_bf16 = ALL_BF16 || p.h_bf16, n_bf16 = ALL_BF16 || p.n_bf16;
+  const bool post = p.post_gain != nullptr, pre = p.pre_gain != nullptr, full = p.gate_kind == SFFN_BLOCK_GATE_FULL;
+  const Rows<W, V> rows(p, ring_raw, stages, planes);
+  const Array y = {p.y, p.ld_y, 0, y_bf16}, x = {p.resid, p.ld_resid, p.y ? (y_bf16 ? 1 : 2) : 0, h_bf16};
+  const Array gate = {full ? p.gate : nullptr, p.ld_gate, x.plane + (p.resid ? (h_bf16 ? 1 : 2) : 0), h_bf16};
+  pdl_launch_dependents();
+  pdl_wait();
+  const int step = gridDim.x;
+  for (int q = 0; q < stages; ++q) rows.fetch(q, blockIdx.x + q * step, y, x, gate);
+  Eight w[V], gain[V];
+  weights_of(p, rows, w);
+#pragma unroll
+  for (int i = 0; i < V; ++i) {
+    gain[i] = eight_of(0.f);
+    if (pre && rows.column(i) < p.D) gain[i] = gain8(p.pre_gain, rows.column(i), p.D);
+  }
+  int stage = 0, turn = 0;
+  for (int t = blockIdx.x; t < p.T; t += step, turn ^= 1) {
+    rows.wait(stages - 1);
+    float r = 1.f;
+    if (post) {
+      float2 s = both(0.f);
+#pragma unroll
+      for (int i = 0; i < V; ++i) {
+        if (rows.column(i) >= p.D) continue;
+        const Eight f = rows.get(stage, y, t, i);
+        s = dot8(f, f, s);
+      }
+      r = rsqrtf(fmaf(row_sum<W>(s.x + s.y, room[0]), p.inv_d, p.eps));
+    }
+    const float factor = r * (p.gate_kind == SFFN_BLOCK_GATE_TOKEN ? reinterpret_cast<const float*>(p.gate)[t] : 1.f);
+    Eight h[V];
+    float2 s = both(0.f);
 #pragma unroll
     for (int i = 0; i < V; ++i) {
-      const int c = 8 * (in_row + 32 * W * i);
+      const int c = rows.column(i);
       if (c >= p.D) continue;
-      float a[8], b[8], e[8];
-      if (has_n) {
-        get(stage, dn, t, i, c, a);
-        get(stage, h, t, i, c, b);
+      h[i] = p.resid ? rows.get(stage, x, t, i) : eight_of(0.f);
+      if (p.y) {
+        Eight f = rows.get(stage, y, t, i) * factor;
+        if (full) f = f * rows.get(stage, gate, t, i);
+        h[i] = fma8(f, w[i], h[i]);
+        store8(p.h + t * p.ld_h, h_bf16, p.wide, c, p.D, h[i]);
+      }
+      s = dot8(h[i], h[i], s);
+    }
+    rows.fetch(stage, t + stages * step, y, x, gate);  // what was in this stage has been used
+    if (++stage == stages) stage = 0;
+    float rho = 0.f;
+    if (pre) {  // (a barrier lies between a sum and the one that takes its room)
+      rho = rsqrtf(fmaf(row_sum<W>(s.x + s.y, room[post ? 1 : turn]), p.inv_d, p.eps));
 #pragma unroll
-        for (int j = 0; j < 8; ++j) {
-          a[j] *= pre[i][j];
-          sums[0] = fmaf(a[j], b[j], sums[0]);
-        }
+      for (int i = 0; i < V; ++i)
+        if (rows.column(i) < p.D) store8(p.n + t * p.ld_n, n_bf16, p.wide, rows.column(i), p.D, h[i] * rho * gain[i]);
+    } else if (post) {
+      __syncthreads();
+    }
+    if (p.stats && threadIdx.x == 0) {
+      p.stats[t] = post ? r : 0.f;
+      p.stats[p.T + t] = rho;
+    }
+  }
+}
+
+// The backward pass.
+template <int W, int V, bool ALL_BF16>
+__global__ void __launch_bounds__(Ring<W, V>::kThreads, Ring<W, V>::kPerSm) block_backward_kernel(const __grid_constant__ BlockParams p, int stages, int planes) {
+  constexpr int kRows = Ring<W, V>::kRows, kThreads = Ring<W, V>::kThreads;
+  extern __shared__ __align__(16) uint8_t ring_raw[];
+  __shared__ float room[2][4 * W];
+  __shared__ __align__(8) float lines[W == 1 ? kRows : 1][W == 1 ? 256 * V : 1];
+  const bool y_bf16 = ALL_BF16 || p.y_bf16, h_bf16 = ALL_BF16 || p.h_bf16, n_bf16 = ALL_BF16 || p.n_bf16;
+  const bool post = p.post_gain != nullptr, full = p.gate_kind == SFFN_BLOCK_GATE_FULL;
+  const bool has_dh = p.dh != nullptr, has_n = p.dn != nullptr, has_y = p.y != nullptr;
+  const int wide_h = h_bf16 ? 1 : 2, wide_n = n_bf16 ? 1 : 2, wide_y = y_bf16 ? 1 : 2;
+  const Array dh = {p.dh, p.ld_dh, 0, h_bf16}, dn = {p.dn, p.ld_dn, has_dh ? wide_h : 0, n_bf16}, h = {has_n ? p.h : nullptr, p.ld_h, dn.plane + (has_n ? wide_n : 0), h_bf16};
+  const Array y = {p.y, p.ld_y, h.plane + (has_n ? wide_h : 0), y_bf16}, gate = {full ? p.gate : nullptr, p.ld_gate, y.plane + (has_y ? wide_y : 0), h_bf16};
+  const Rows<W, V> rows(p, ring_raw, stages, planes);
+  pdl_launch_dependents();
+  pdl_wait();
+  const int first = blockIdx.x * kRows + threadIdx.x / (32 * W), step = gridDim.x * kRows;
+  for (int q = 0; q < stages; ++q) rows.fetch(q, first + q * step, dh, dn, h, y, gate);  // (not more than 2^30 rows and a grid's: no overflow)
+  Eight pre[V], w[V], acc_pre[V], acc_c[V];
+  weights_of(p, rows, w);
+#pragma unroll
+  for (int i = 0; i < V; ++i) {
+    acc_pre[i] = acc_c[i] = pre[i] = eight_of(0.f);
+    if (has_n && rows.column(i) < p.D) pre[i] = gain8(p.pre_gain, rows.column(i), p.D);
+  }
+  // Statistics and a gate of tokens: for as many of its rows as it has threads, a row's warps bring them into shared memory at once.  (A load a
+  // row and thread, even one row ahead, costs a fifth: the wait for the ring's copies waits for it too.)
+  __shared__ float stat[kRows][3][32 * W];
+  float (*const own_stat)[32 * W] = stat[threadIdx.x / (32 * W)];
+  int turn = 0, stage = 0, at_stat = 0;
+  for (int t = first; t < p.T; t += step, turn ^= 1) {
+    if (at_stat == 0) {  // (what was there has been read: a sum's barrier lies between)
+      const int mine = t + rows.in_row * step;
+      if (rows.in_row < (p.T - t + step - 1) / step) {
+        own_stat[0][rows.in_row] = post ? p.stats[mine] : 1.f;
+        own_stat[1][rows.in_row] = has_n ? p.stats[p.T + mine] : 0.f;
+        own_stat[2][rows.in_row] = p.gate_kind == SFFN_BLOCK_GATE_TOKEN ? reinterpret_cast<const float*>(p.gate)[mine] : 1.f;
+      }
+      if constexpr (W == 1) __syncwarp();
+      else __syncthreads();
+    }
+    const float r = own_stat[0][at_stat], rho = own_stat[1][at_stat], token = own_stat[2][at_stat];
+    if (++at_stat == 32 * W) at_stat = 0;
+    rows.wait(stages - 1);
+    float2 s[4] = {both(0.f), both(0.f), both(0.f), both(0.f)};  // of t h, w y dh, w y t, w y h
+#pragma unroll
+    for (int i = 0; i < V; ++i) {
+      if (rows.column(i) >= p.D) continue;
+      Eight a, b;
+      if (has_n) {
+        a = rows.get(stage, dn, t, i) * pre[i];
+        b = rows.get(stage, h, t, i);
+        s[0] = dot8(a, b, s[0]);
       }
       if (has_y) {
-        get(stage, y, t, i, c, e);
-#pragma unroll
-        for (int j = 0; j < 8; ++j) e[j] *= w[i][j];
-        if (full) {
-          float f[8];
-          get(stage, gate, t, i, c, f);
-#pragma unroll
-          for (int j = 0; j < 8; ++j) e[j] *= f[j];
-        }
+        Eight e = rows.get(stage, y, t, i) * w[i];
+        if (full) e = e * rows.get(stage, gate, t, i);
         if (has_n) {
-#pragma unroll
-          for (int j = 0; j < 8; ++j) {
-            sums[2] = fmaf(e[j], a[j], sums[2]);
-            sums[3] = fmaf(e[j], b[j], sums[3]);
-          }
+          s[2] = dot8(e, a, s[2]);
+          s[3] = dot8(e, b, s[3]);
         }
-        if (has_dh) {
-          get(stage, dh, t, i, c, a);
-#pragma unroll
-          for (int j = 0; j < 8; ++j) sums[1] = fmaf(e[j], a[j], sums[1]);
-        }
+        if (has_dh) s[1] = dot8(e, rows.get(stage, dh, t, i), s[1]);
       }
     }
+    float sums[4];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) sums[k] = s[k].x + s[k].y;
     row_sums<W>(sums, room[turn]);
     const float k1 = rho * rho * rho * p.inv_d * sums[0];
     const float wyg = fmaf(rho, sums[2], sums[1]) - k1 * sums[3];
-    const float k2 = post ? r * r * r * p.inv_d * token * wyg : 0.f, up = r * token, own = p.scale * r * token;
-    if (p.dgate && p.gate_kind == SFFN_BLOCK_GATE_TOKEN && in_row == 0) reinterpret_cast<float*>(p.dgate)[t] = r * wyg;
+    const float k2 = post ? r * r * r * p.inv_d * token * wyg : 0.f, up = r * token, own = p.scale * up;
+    if (p.dgate && p.gate_kind == SFFN_BLOCK_GATE_TOKEN && rows.in_row == 0) reinterpret_cast<float*>(p.dgate)[t] = r * wyg;
 #pragma unroll
     for (int i = 0; i < V; ++i) {
-      const int c = 8 * (in_row + 32 * W * i);
+      const int c = rows.column(i);
       if (c >= p.D) continue;
-      float g[8], f[8], e[8];
-      if (has_dh) get(stage, dh, t, i, c, g);
-      else
-#pragma unroll
-        for (int j = 0; j < 8; ++j) g[j] = 0.f;
+      Eight g = has_dh ? rows.get(stage, dh, t, i) : eight_of(0.f);
       if (has_n) {
-        get(stage, dn, t, i, c, f);
-        get(stage, h, t, i, c, e);
-#pragma unroll
-        for (int j = 0; j < 8; ++j) {
-          f[j] *= rho;
-          g[j] = fmaf(-k1, e[j], fmaf(f[j], pre[i][j], g[j]));
-          acc_pre[i][j] = fmaf(f[j], e[j], acc_pre[i][j]);
-        }
+        const Eight f = rows.get(stage, dn, t, i) * rho, b = rows.get(stage, h, t, i);
+        g = fma8(b, -k1, fma8(f, pre[i], g));
+        acc_pre[i] = fma8(f, b, acc_pre[i]);
       }
-      if (p.dresid) store8(p.dresid + t * p.ld_dresid, h_bf16, c, p.D, g);
+      if (p.dresid) store8(p.dresid + t * p.ld_dresid, h_bf16, p.wide, c, p.D, g);
       if (has_y) {
-        get(stage, y, t, i, c, f);
+        const Eight f = rows.get(stage, y, t, i), ww = w[i] * up;
         if (full) {
-          get(stage, gate, t, i, c, e);
-          if (p.dgate) {
-            float d[8];
-#pragma unroll
-            for (int j = 0; j < 8; ++j) d[j] = up * w[i][j] * g[j] * f[j];
-            store8(p.dgate + t * p.ld_dgate, h_bf16, c, p.D, d);
-          }
-#pragma unroll
-          for (int j = 0; j < 8; ++j) g[j] *= e[j];
+          if (p.dgate) store8(p.dgate + t * p.ld_dgate, h_bf16, p.wide, c, p.D, ww * g * f);
+          g = g * rows.get(stage, gate, t, i);
         }
-#pragma unroll
-        for (int j = 0; j < 8; ++j) acc_c[i][j] = fmaf(own * g[j], f[j], acc_c[i][j]);
-        if (p.dy) {
-#pragma unroll
-          for (int j = 0; j < 8; ++j) f[j] = fmaf(up * w[i][j], g[j], -k2 * f[j]);
-          store8(p.dy + t * p.ld_dy, y_bf16, c, p.D, f);
-        }
+        acc_c[i] = fma8(g * own, f, acc_c[i]);
+        if (p.dy) store8(p.dy + t * p.ld_dy, y_bf16, p.wide, c, p.D, fma8(ww, g, f * -k2));
       }
     }
-    fetch(stage, t + stages * step);  // what was in this stage has been used
+    rows.fetch(stage, t + stages * step, dh, dn, h, y, gate);  // what was in this stage has been used
     if (++stage == stages) stage = 0;
   }
   // This CTA's line of column sums.
   float* const line = p.partial + (int64_t)blockIdx.x * p.D;
-  auto leave = [&](float* to, float (&acc)[V][8]) {
+  auto leave = [&](float* to, const Eight (&acc)[V]) {
     if constexpr (W > 1) {
 #pragma unroll
-      for (int i = 0; i < V; ++i) {
-        const int c = 8 * (in_row + 32 * W * i);
-        if (c < p.D) store8(reinterpret_cast<char*>(to), 0, c, p.D, acc[i]);
-      }
+      for (int i = 0; i < V; ++i)
+        if (rows.column(i) < p.D) store8(reinterpret_cast<char*>(to), 0, p.D % 8 == 0, rows.column(i), p.D, acc[i]);
     } else {  // of its warps' sums, in their order
       __syncthreads();
 #pragma unroll
       for (int i = 0; i < V; ++i)
 #pragma unroll
-        for (int j = 0; j < 8; ++j) lines[threadIdx.x >> 5][256 * i + 8 * in_row + j] = acc[i][j];
+        for (int j = 0; j < 4; ++j) *reinterpret_cast<float2*>(&lines[threadIdx.x >> 5][256 * i + 8 * rows.in_row + 2 * j]) = acc[i].v[j];
       __syncthreads();
       for (int c = threadIdx.x; c < p.D; c += kThreads) {
         float s = 0.f;
@@ -437,18 +611,27 @@ __global__ void __launch_bounds__(BackShape<W, V>::kThreads, BackShape<W, V>::kP
   };
   if (p.want_pre) leave(line, acc_pre);
   if (p.want_c) leave(line + (int64_t)p.lines * p.D, acc_c);
+  if (!p.together) return;
+  // The whole launch is one cluster: it adds up its lines itself.
+  asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
+  asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
+  for (int c = blockIdx.x * kThreads + threadIdx.x; c < 2 * p.D; c += gridDim.x * kThreads) {
+    const int which = c >= p.D, column = which ? c - p.D : c;
+    if (which ? !p.want_c : !p.want_pre) continue;
+    float s = 0.f;
+    for (int l = 0; l < gridDim.x; ++l) s += __ldcg(p.partial + ((int64_t)which * p.lines + l) * p.D + column);
+    column_out(p.sums, which, column, s);
+  }
 }
 
-// Column sums of `n` lines, added up in order: runs of lines, then the runs.  What the second array holds is sum g y (r, scale, and a
-// gate that is not one of the channels in it): times the channel gate it is the post gain's gradient, times the post gain the gate's.
+// Column sums of `n` lines, added up in order: runs of lines, then the runs.
 constexpr int kColumnRuns = 32;
-__global__ void __launch_bounds__(32 * kColumnRuns) block_columns_kernel(const float* partial, int n, int room, int D, const float* post_gain, const float* gate, float* dpre,
-                                                                        float* dpost, float* dgate) {
+__global__ void __launch_bounds__(32 * kColumnRuns) block_columns_kernel(const float* partial, int n, int room, int D, const ColumnSums out) {
   __shared__ float sums[kColumnRuns][32];
   pdl_launch_dependents();
   pdl_wait();
   const int c = blockIdx.x * 32 + (threadIdx.x & 31), run = threadIdx.x >> 5, which = blockIdx.y;
-  if (which == 0 ? !dpre : !dpost && !dgate) return;
+  if (which == 0 ? !out.dpre : !out.dpost && !out.dgate) return;
   float s = 0.f;
   if (c < D) {
     const float* from = partial + (int64_t)which * room * D + c;
@@ -462,13 +645,7 @@ __global__ void __launch_bounds__(32 * kColumnRuns) block_columns_kernel(const f
   s = 0.f;
 #pragma unroll
   for (int q = 0; q < kColumnRuns; ++q) s += sums[q][threadIdx.x];
-  if (which == 0) {
-    dpre[c] = s;
-  } else {
-    const float gain = post_gain ? post_gain[c] : 1.f, open = gate ? gate[c] : 1.f;
-    if (dpost) dpost[c] = s * open;
-    if (dgate) dgate[c] = s * gain;
-  }
+  column_out(out, which, c, s);
 }
 
 BlockParams params_of(const sffn_block_norm& b) {
@@ -485,7 +662,26 @@ BlockParams params_of(const sffn_block_norm& b) {
   p.h = static_cast<char*>(b.h); p.ld_h = bytes(b.h_dtype, b.ld_h);
   p.n = static_cast<char*>(b.n); p.ld_n = bytes(b.n_dtype, b.ld_n);
   p.stats = b.stats;
+  p.wide = 1;
+  auto look = [&](const void* at, int64_t ld, bool bf16) { p.wide = p.wide && (bf16 || !at || ((reinterpret_cast<uintptr_t>(at) | ld) & 31) == 0); };
+  look(p.y, p.ld_y, p.y_bf16);
+  look(p.resid, p.ld_resid, p.h_bf16);
+  look(p.h, p.ld_h, p.h_bf16);
+  look(p.n, p.ld_n, p.n_bf16);
+  if (p.gate_kind == SFFN_BLOCK_GATE_FULL) look(p.gate, p.ld_gate, p.h_bf16);
   return p;
+}
+
+constexpr int kManyRows = 8;           // rows an SM
+constexpr int kSmShared = 200 * 1024;  // of an SM, for the rings of the CTAs on it (up to eight, with up to 9 KB more each)
+// Stages of a ring of so many planes, and its bytes; at most five arrays of fp32, two pieces of 512 threads of an SM: 160 KB a stage.
+template <int W, int V>
+int stages_of(int planes, size_t* bytes) {
+  using S = Ring<W, V>;
+  const int stage = S::kShared ? planes * V * S::kThreads * 16 : 0, room = stage > 0 ? kSmShared / S::kPerSm / stage : 1;
+  const int stages = room > kMostStages ? kMostStages : room;
+  *bytes = (size_t)stages * stage;
+  return stages;
 }
 
 template <int W, int V>
@@ -493,24 +689,40 @@ cudaError_t forward(const BlockParams& p, cudaStream_t s) {
   using S = Shape<W, V>;
   return launch_pdl(block_forward_kernel<W, V>, dim3((p.T + S::kRows - 1) / S::kRows), dim3(S::kThreads), 0, s, p);
 }
-constexpr int kSmShared = 200 * 1024;  // of an SM, for the rings of the CTAs on it (up to eight, with up to 9 KB more each)
-
+template <int W, int V, bool ALL_BF16>
+cudaError_t forward_rows(const BlockParams& p, int stages, int planes, size_t bytes, int sm_count, cudaStream_t s) {
+  static unsigned long long configured = 0;
+  const cudaError_t e = allow_dynamic_smem(block_forward_rows_kernel<W, V, ALL_BF16>, kSmShared, configured);
+  if (e != cudaSuccess) return e;
+  const int room = Ring<W, V>::kPerSm * sm_count;
+  return launch_pdl(block_forward_rows_kernel<W, V, ALL_BF16>, dim3(p.T < room ? p.T : room), dim3(Ring<W, V>::kThreads), bytes, s, p, stages, planes);
+}
+template <int W, int V>
+cudaError_t forward_rows(const BlockParams& p, int sm_count, cudaStream_t s) {
+  const int h = p.h_bf16 ? 1 : 2, planes = (p.y ? (p.y_bf16 ? 1 : 2) : 0) + (p.resid ? h : 0) + (p.gate_kind == SFFN_BLOCK_GATE_FULL ? h : 0);
+  size_t bytes = 0;
+  const int stages = stages_of<W, V>(planes, &bytes);
+  return p.y_bf16 && p.h_bf16 && p.n_bf16 ? forward_rows<W, V, true>(p, stages, planes, bytes, sm_count, s)
+                                          : forward_rows<W, V, false>(p, stages, planes, bytes, sm_count, s);
+}
 template <int W, int V, bool ALL_BF16>
 cudaError_t backward(const BlockParams& p, int sm_count, int* lines, cudaStream_t s) {
-  using S = BackShape<W, V>;
+  using S = Ring<W, V>;
   static unsigned long long configured = 0;
   cudaError_t e = allow_dynamic_smem(block_backward_kernel<W, V, ALL_BF16>, kSmShared, configured);
   if (e != cudaSuccess) return e;
   const int h = p.h_bf16 ? 1 : 2, n = p.n_bf16 ? 1 : 2, y = p.y_bf16 ? 1 : 2;
   const int planes = (p.dh ? h : 0) + (p.dn ? n + h : 0) + (p.y ? y : 0) + (p.gate_kind == SFFN_BLOCK_GATE_FULL ? h : 0);
-  const int stage = S::kRing ? planes * V * S::kThreads * 16 : 0, rows = (p.T + S::kRows - 1) / S::kRows;
-  // At most five arrays of fp32, two pieces of 512 threads of an SM: 160 KB.
-  int stages = stage > 0 ? kSmShared / S::kPerSm / stage : 1;
-  stages = stages > kBackStages ? kBackStages : stages;
-  const int room = S::kPerSm * sm_count;
+  size_t bytes = 0;
+  const int stages = stages_of<W, V>(planes, &bytes), rows = (p.T + S::kRows - 1) / S::kRows, room = S::kPerSm * sm_count;
   *lines = rows < room ? rows : room;
   if (*lines > p.lines) *lines = p.lines;
-  return launch_pdl(block_backward_kernel<W, V, ALL_BF16>, dim3(*lines), dim3(S::kThreads), (size_t)stages * stage, s, p, stages);
+  // So few CTAs that they are a cluster (of eight at most): one launch less (64 tokens of 256: 15.8 / ? us).
+  BlockParams q = p;
+  q.together = *lines <= 8 && (p.want_pre || p.want_c);
+  const cudaError_t launched = launch_clusters(q.together ? *lines : 1, block_backward_kernel<W, V, ALL_BF16>, dim3(*lines), dim3(S::kThreads), bytes, s, q, stages, planes);
+  if (q.together) *lines = 0;
+  return launched;
 }
 template <int W, int V>
 cudaError_t backward(const BlockParams& p, int sm_count, int* lines, cudaStream_t s) {
@@ -519,16 +731,19 @@ cudaError_t backward(const BlockParams& p, int sm_count, int* lines, cudaStream_
 
 }  // namespace
 
-cudaError_t launch_block_forward(const sffn_block_norm& b, cudaStream_t s) {
+cudaError_t launch_block_forward(const sffn_block_norm& b, int sm_count, cudaStream_t s) {
   const BlockParams p = params_of(b);
-  const bool few = p.T <= 148;  // rows that do not fill the device: as many threads a row as it has pieces
+  // Rows that do not fill the device: as many threads a row as it has pieces.
+  const bool few = p.T <= sm_count;
+  // Enough of them for every CTA to have several: through rings.
+  const bool many = p.T >= kManyRows * sm_count;
   if (p.D <= 256) return forward<1, 1>(p, s);
   if (p.D <= 1024 && few) return forward<4, 1>(p, s);
   if (p.D <= 512) return forward<1, 2>(p, s);
   if (p.D <= 1024) return forward<1, 4>(p, s);
-  if (p.D <= 2048) return few ? forward<8, 1>(p, s) : forward<4, 2>(p, s);
-  if (p.D <= 4096) return few ? forward<16, 1>(p, s) : forward<8, 2>(p, s);
-  if (p.D <= 8192) return few ? forward<32, 1>(p, s) : forward<16, 2>(p, s);
+  if (p.D <= 2048) return few ? forward<8, 1>(p, s) : many ? forward_rows<4, 2>(p, sm_count, s) : forward<4, 2>(p, s);
+  if (p.D <= 4096) return few ? forward<16, 1>(p, s) : many ? forward_rows<8, 2>(p, sm_count, s) : forward<8, 2>(p, s);
+  if (p.D <= 8192) return few ? forward<32, 1>(p, s) : many ? forward_rows<16, 2>(p, sm_count, s) : forward<16, 2>(p, s);
   if (p.D <= 16384) return forward<32, 2>(p, s);
   return forward<32, 4>(p, s);
 }
@@ -542,24 +757,30 @@ cudaError_t launch_block_backward(const sffn_block_norm& b, const sffn_block_gra
   p.dresid = static_cast<char*>(g.dresid); p.ld_dresid = bytes(b.h_dtype, g.ld_dresid);
   p.dgate = p.gate_kind == SFFN_BLOCK_GATE_TOKEN || p.gate_kind == SFFN_BLOCK_GATE_FULL ? static_cast<char*>(g.dgate) : nullptr;
   p.ld_dgate = bytes(b.h_dtype, g.ld_dgate);
+  auto look = [&](const void* at, int64_t ld, bool bf16) { p.wide = p.wide && (bf16 || !at || ((reinterpret_cast<uintptr_t>(at) | ld) & 31) == 0); };
+  look(p.dh, p.ld_dh, p.h_bf16);
+  look(p.dn, p.ld_dn, p.n_bf16);
+  look(p.dy, p.ld_dy, p.y_bf16);
+  look(p.dresid, p.ld_dresid, p.h_bf16);
+  if (p.gate_kind == SFFN_BLOCK_GATE_FULL) look(p.dgate, p.ld_dgate, p.h_bf16);
   p.partial = partial;
   p.lines = block_lines(p.D);
-  float* const dchannel = p.gate_kind == SFFN_BLOCK_GATE_CHANNEL ? static_cast<float*>(g.dgate) : nullptr;
-  p.want_pre = g.dpre_gain != nullptr;
-  p.want_c = g.dpost_gain != nullptr || dchannel != nullptr;
+  p.sums = {p.post_gain, p.gate_kind == SFFN_BLOCK_GATE_CHANNEL ? reinterpret_cast<const float*>(p.gate) : nullptr, g.dpre_gain, g.dpost_gain,
+            p.gate_kind == SFFN_BLOCK_GATE_CHANNEL ? static_cast<float*>(g.dgate) : nullptr};
+  p.want_pre = p.sums.dpre != nullptr;
+  p.want_c = p.sums.dpost || p.sums.dgate;
   int lines = 0;
   cudaError_t e;
   if (p.D <= 256) e = backward<1, 1>(p, sm_count, &lines, s);
   else if (p.D <= 512) e = backward<2, 1>(p, sm_count, &lines, s);
-  else if (p.D <= 1024) e = backward<2, 2>(p, sm_count, &lines, s);
-  else if (p.D <= 2048) e = backward<4, 2>(p, sm_count, &lines, s);
-  else if (p.D <= 4096) e = backward<8, 2>(p, sm_count, &lines, s);
+  else if (p.D <= 1024) e = backward<4, 1>(p, sm_count, &lines, s);
+  else if (p.D <= 2048) e = backward<8, 1>(p, sm_count, &lines, s);
+  else if (p.D <= 4096) e = backward<16, 1>(p, sm_count, &lines, s);
   else if (p.D <= 8192) e = backward<16, 2>(p, sm_count, &lines, s);
   else if (p.D <= 16384) e = backward<32, 2>(p, sm_count, &lines, s);
   else e = backward<32, 4>(p, sm_count, &lines, s);
-  if (e != cudaSuccess || (!p.want_pre && !p.want_c)) return e;
-  return launch_pdl(block_columns_kernel, dim3((p.D + 31) / 32, 2), dim3(32 * kColumnRuns), 0, s, (const float*)partial, lines, p.lines, p.D, p.post_gain,
-                    p.gate_kind == SFFN_BLOCK_GATE_CHANNEL ? reinterpret_cast<const float*>(p.gate) : (const float*)nullptr, g.dpre_gain, g.dpost_gain, dchannel);
+  if (e != cudaSuccess || lines == 0 || (!p.want_pre && !p.want_c)) return e;
+  return launch_pdl(block_columns_kernel, dim3((p.D + 31) / 32, 2), dim3(32 * kColumnRuns), 0, s, (const float*)partial, lines, p.lines, p.D, p.sums);
 }
 
 }  // namespace sffn

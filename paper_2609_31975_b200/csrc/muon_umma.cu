@@ -228,11 +228,14 @@ __device__ __forceinline__ float factor(const Params& p, int batch, int which) {
 // What all chunks of a warp's row share.
 template <int KIND>
 struct Shared {
-  float d, f_m, f_n, f_k;  // this row's diagonal (kForm: of M; X M: none), and the first step's factors
-  __device__ __forceinline__ Shared(const Params& p, int batch, int m) : d(0.f), f_m(1.f), f_n(1.f), f_k(1.f) {
+  float d, d_n, f_m, f_n, f_k;  // this row's diagonal (kForm: of M, and of N; X M: none), and the first step's factors
+  __device__ __forceinline__ Shared(const Params& p, int batch, int m) : d(0.f), d_n(0.f), f_m(1.f), f_n(1.f), f_k(1.f) {
     const bool row = m < p.M;
     if constexpr (KIND == kForm) {
-      if (row) d = __ldcg(p.M_diag + batch * diag_ld(p.S) + m);
+      if (row) {
+        d = __ldcg(p.M_diag + batch * diag_ld(p.S) + m);
+        d_n = __ldcg(p.N_diag + batch * diag_ld(p.S) + m);
+      }
       if (p.first) {
         f_m = factor(p, batch, p.fm);
         f_n = factor(p, batch, p.fn);
@@ -464,8 +467,7 @@ __device__ __forceinline__ void finish(const Params& p, const Shared<KIND>& all,
         if constexpr (KIND == kGram) {
           p.out_diag[at] = own * p.dacc;
         } else {
-          const float d_n = __ldcg(p.N_diag + at);
-          p.out_diag[at] = p.dm * all.f_m * all.d + p.dn * all.f_n * d_n + p.dk * all.f_k * fmaf(own, p.dacc, all.d * d_n);
+          p.out_diag[at] = p.dm * all.f_m * all.d + p.dn * all.f_n * all.d_n + p.dk * all.f_k * fmaf(own, p.dacc, all.d * all.d_n);
         }
       }
     }
@@ -921,15 +923,21 @@ __global__ void __launch_bounds__(Small<TERMS>::kThreads, 2) muon_small_kernel(c
         if (!pieces && !wanted<KIND>(p, row0, n0)) break;
         float v[16];
         tmem_ld16(acc + 16 * c, v);
-        tmem_arrived(v);
         if constexpr (TERMS == 2) {  // the small products first
-          for (int run = 0; run * kRun < u1 - u0; ++run) {
-            float w[16];
+          float w[16];
+          tmem_ld16(acc + F::kCols + 16 * c, w);
+          tmem_arrived(v);
+          tmem_arrived(w);
+#pragma unroll
+          for (int i = 0; i < 16; ++i) v[i] += w[i];
+          for (int run = 1; run * kRun < u1 - u0; ++run) {
             tmem_ld16(acc + (1 + run) * F::kCols + 16 * c, w);
             tmem_arrived(w);
 #pragma unroll
             for (int i = 0; i < 16; ++i) v[i] += w[i];
           }
+        } else {
+          tmem_arrived(v);
         }
         if (pieces) put_piece(piece + 16 * c, v);
         else finish<KIND, TERMS>(p, all, at.batch, row0, n0, lane, v, more[0]);
