@@ -121,9 +121,9 @@ bool make_products(const sffn_newton_schulz& ns, int group, Products& out) {
 }
 
 // Steps at a time: one, two, three.  Where the longer side of X is longer than the shorter one, a step in the company of others is four products
-// of S x S instead of two, and saves a Gram matrix and a product with X: 14336 x 4096, bf16, one / two at a time ? / ? us.  Roundings in
-// between are not made good again by the next Gram matrix, and grow: in 16 bits two steps are as exact as one by one but for a factor of
-// two where singular values are far apart, three are not; with operands in two terms three are (2^-11 of the errors).
+// of S x S instead of two, and saves a Gram matrix and a product with X.  Roundings in between are not made good again by the next Gram
+// matrix, and grow: in 16 bits two steps are as exact as one by one but for a factor of two where singular values are far apart, three
+// are not; with operands in two terms three are (2^-11 of the errors).
 struct Plans {
   Products of[3];
 };
@@ -243,7 +243,14 @@ bool any_meet(std::vector<Range>& all) {
   return false;
 }
 
-int steps_at_a_time(const MuonBatch& b) { return 4 * (int64_t)b.L < 5 * (int64_t)b.S ? 1 : b.terms == 2 ? 3 : 2; }
+// What is small is a chain of launches, which company makes longer; what is nearly square gains little.  In us, one at a time / in company, bf16
+// and fp32: 1024 x 256 108 / 112, 159 / 178; 48 of them 338 / -, 466 / 377; 12 of 2048 x 512 418 / -, 665 / 469; 1280 x 1024 162 / 173, 324 / 343;
+// 2048 x 1024 191 / 192, 429 / 387; 4096 x 1024 318 / 270, 521 / 429; 2560 x 2048 506 / 444, 826 / 832; 5120 x 4096 1728 / 1627, 4467 / 4454;
+// 8192 x 2048 846 / 673, 1560 / 1145.
+int steps_at_a_time(const MuonBatch& b) {
+  const int64_t size = (int64_t)b.n * b.S * b.S, quarters = size < (1 << 22) ? 6 : 5;
+  return size < (1 << 19) || 4 * (int64_t)b.L < quarters * b.S ? 1 : b.terms == 2 ? 3 : 2;
+}
 
 int run(const std::vector<Matrix>& all, const Plans& plans, const MuonBatch& common, void* workspace, cudaStream_t s) {
   int sms = 0;

@@ -1035,7 +1035,7 @@ long long most_pieces(int rows, int cols, long long tiles, long long blocks) {
   return tiles < room && tiles * blocks < room ? tiles * blocks : room;
 }
 // Microseconds of the launch that joins `split` pieces of each of so many tiles.
-double join_time(double tiles, int split, int rows, int cols) { return 4.0 + 0.2 * split + tiles * (split + 1) * rows * cols * 4 / 3e6; }
+double join_time(double tiles, int split, int rows, int cols) { return 4.0 + 0.2 * split + tiles * (split + 1) * rows * cols * 4 / 2e6; }
 
 // Pairs' tiles: whole ones in rounds, the last, partly idle one cut along K into equal pieces where that is shorter (times in microseconds: of
 // a K block, of a tile's epilogue, of a piece's way to the workspace).
@@ -1079,7 +1079,7 @@ Plan plan_small(int kind, int M, int N, int K, int n, int sms) {
   for (int split = fewest; split <= blocks && (split == 1 || (long long)p.tiles * split <= room); ++split) {
     const long long ctas = (long long)p.tiles * split, rounds = (ctas + 2 * sms - 1) / (2 * sms);
     if (ctas > (1 << 30)) break;
-    const double block = (TERMS == 1 ? 0.35 : 0.7) * (ctas > sms ? 2 : 1);  // two CTAs share an SM's copies
+    const double block = (TERMS == 1 ? 0.3 : 0.65) * (ctas > sms ? 2 : 1);  // two CTAs share an SM's copies
     const double time = 3.0 + rounds * (2.0 + std::ceil((double)blocks / split) * block + (split > 1 ? 1.0 : 3.0)) +
                         (split > 1 ? join_time(p.tiles, split, F::kRows, F::kCols) : 0.0);
     if (time < p.time) {
