@@ -79,6 +79,7 @@ struct Params {
   int m_tiles, n_tiles, per, tiles, blocks;
   int whole, split;               // tiles dealt whole; pieces of each of the others
   int stages;                     // small tiles: of the ring
+  int together;                   // small tiles: the pieces of a tile are a cluster, which joins them itself
   int a_mn, b_mn;
   float* partial;
   int piece;                      // floats of a piece
@@ -785,7 +786,8 @@ __global__ void __launch_bounds__(Form<TERMS>::kThreads, 1) muon_umma_kernel(con
 
 // ---- small tiles -----------------------------------------------------------------------------------------------------
 // For products that do not fill the device with pairs' tiles: a CTA has one tile of 128 x 64 (or a piece of it along K).  A chain of
-// such launches is a chain of latencies (1024 x 256, fp32: 1.8 us from a launch's end to the next one's start, 1.3 to the first K block): the
+// such launches is a chain of latencies (1024 x 256, fp32: 1.8 us from a launch's end to the next one's start, 1.3 to the first K block): up to eight
+// pieces are a cluster that joins them through L2; the
 // eight warps of the epilogue read and multiply what is beside the accumulators while these are made, and where the launch leaves SMs
 // idle, all K blocks of a short K are under way at once.  With two terms, every run of K blocks has an accumulator of its own, so a piece is
 // at most three runs.
@@ -834,10 +836,11 @@ __global__ void __launch_bounds__(Small<TERMS>::kThreads, 2) muon_small_kernel(c
   fence_after();
   const uint32_t tmem = tmem_slot;
   const bool pieces = p.whole < p.tiles;
-  if (!(KIND == kLast && p.step && !pieces)) pdl_launch_dependents();
+  if (!(KIND == kLast && p.step && (!pieces || p.together))) pdl_launch_dependents();
   pdl_wait();
 
-  const int number = blockIdx.x, part = number / p.tiles, tile = number - part * p.tiles;
+  // pieces of one stretch of K together; a cluster's: of one tile
+  const int number = blockIdx.x, part = p.together ? number % p.split : number / p.tiles, tile = p.together ? number / p.split : number - part * p.tiles;
   const Place at = place_of<KIND, F>(p, tile);
   const int u0 = (int)((long long)p.blocks * part / p.split), u1 = (int)((long long)p.blocks * (part + 1) / p.split);
   auto wait_all = [&](uint32_t bar, uint32_t parity) { return __all_sync(0xffffffffu, mbar_wait(bar, parity, abort_flag, p.status, p.budget)) != 0; };
@@ -903,14 +906,20 @@ __global__ void __launch_bounds__(Small<TERMS>::kThreads, 2) muon_small_kernel(c
     const int quad = warp & 3, across = 32 * ((warp - 2) >> 2), n_base = at.n * F::kCols + across, row0 = at.m * F::kRows + 32 * quad;
     const bool rows = row0 < p.M;
     float more[2][16];
-    const Shared<KIND> all(p, at.batch, row0 + lane);
-    if (rows && !pieces) {
+    // what this warp finishes: 32 rows and 32 columns of its tile, or, of a cluster's sixteen parts of 32 x 16, one or none
+    const int own = (warp - 2) * p.split + part, own_r = 32 * (own >> 2), own_c = 16 * (own & 3);
+    const int joined_row = at.m * F::kRows + own_r, joined_n = at.n * F::kCols + own_c;
+    const bool joins = p.together && own < 16 && joined_row < p.M && wanted<KIND>(p, joined_row, joined_n);
+    const Shared<KIND> all(p, at.batch, (p.together ? joined_row : row0) + lane);
+    if (joins || (rows && !pieces)) {
 #pragma unroll
       for (int c = 0; c < 2; ++c) {
-        if (!wanted<KIND>(p, row0, n_base + 16 * c)) break;
+        const int n0 = p.together ? joined_n : n_base + 16 * c;
+        if (c == 1 && (p.together || !wanted<KIND>(p, row0, n0))) break;
+        if (c == 0 && !p.together && !wanted<KIND>(p, row0, n0)) break;
         Ahead<KIND, TERMS> a;
-        a.load(p, at.batch, row0 + lane, n_base + 16 * c);
-        beside<KIND, TERMS>(p, all, at.batch, n_base + 16 * c, a, more[c]);
+        a.load(p, at.batch, (p.together ? joined_row : row0) + lane, n0);
+        beside<KIND, TERMS>(p, all, at.batch, n0, a, more[c]);
       }
     }
     if (wait_all(acc_full, 0) && rows) {
@@ -939,13 +948,33 @@ __global__ void __launch_bounds__(Small<TERMS>::kThreads, 2) muon_small_kernel(c
         } else {
           tmem_arrived(v);
         }
-        if (pieces) put_piece(piece + 16 * c, v);
-        else finish<KIND, TERMS>(p, all, at.batch, row0, n0, lane, v, more[0]);
+        if (pieces) {
+          put_piece(piece + 16 * c, v);
+        } else {
+          finish<KIND, TERMS>(p, all, at.batch, row0, n0, lane, v, more[0]);
 #pragma unroll
-        for (int i = 0; i < 16; ++i) more[0][i] = more[1][i];
+          for (int i = 0; i < 16; ++i) more[0][i] = more[1][i];
+        }
+      }
+    }
+    if (p.together) {
+      cluster_sync();  // all pieces of the tile are there
+      if (joins) {
+        float v[16] = {};
+        const float* from = p.partial + (size_t)(number - part) * p.piece + (size_t)(own_r + lane) * F::kCols + own_c;
+#pragma unroll 4
+        for (int q = 0; q < p.split; ++q, from += p.piece) {
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const float4 f = __ldcg(reinterpret_cast<const float4*>(from) + i);
+            v[4 * i] += f.x; v[4 * i + 1] += f.y; v[4 * i + 2] += f.z; v[4 * i + 3] += f.w;
+          }
+        }
+        finish<KIND, TERMS>(p, all, at.batch, joined_row, joined_n, lane, v, more[0]);
       }
     }
   }
+  if (p.together && warp < 2) cluster_sync();  // (with the epilogue's warps, above)
   if (*abort_flag)  // (copies and MMAs that may still be in flight end within microseconds)
     for (int i = 0; i < 50; ++i) __nanosleep(1000);
   fence_before();
@@ -1024,8 +1053,9 @@ int tiles_of(int kind, int rows, int cols, int M, int N, int* m_tiles = nullptr,
   return m / 2 * (m / 2 + 1) + (m & 1 ? m / 2 + 1 : 0);
 }
 
+constexpr double kTogether = 4.5;  // microseconds of a cluster that joins its pieces
 struct Plan {
-  int per, m_tiles, n_tiles, tiles, whole, split, ctas, stages;
+  int per, m_tiles, n_tiles, tiles, whole, split, ctas, stages, together;
   double time;
 };
 // Floats of the pieces that the workspace has room for: 84 MB.
@@ -1076,20 +1106,29 @@ Plan plan_small(int kind, int M, int N, int K, int n, int sms) {
   const int blocks = (K + kDeep - 1) / kDeep, fewest = (blocks + F::kMostBlocks - 1) / F::kMostBlocks;
   const long long room = most_pieces(F::kRows, F::kCols, p.tiles, blocks);
   p.time = 1e30;
+  // A CTA with all stages fills an SM, half as many leave room for another.  Two, four or eight pieces are a cluster, which joins them itself: an
+  // SM each, clusters find about 128 places (those of eight two in a part of the device of 16 to 20 SMs).
+  const int alone = sms, clustered = sms * 7 / 8;
   for (int split = fewest; split <= blocks && (split == 1 || (long long)p.tiles * split <= room); ++split) {
-    const long long ctas = (long long)p.tiles * split, rounds = (ctas + 2 * sms - 1) / (2 * sms);
+    const bool together = split > 1 && split <= 8;
+    if (together && (split & (split - 1))) continue;
+    const long long ctas = (long long)p.tiles * split;
     if (ctas > (1 << 30)) break;
-    const double block = (TERMS == 1 ? 0.3 : 0.65) * (ctas > sms ? 2 : 1);  // two CTAs share an SM's copies
-    const double time = 3.0 + rounds * (2.0 + std::ceil((double)blocks / split) * block + (split > 1 ? 1.0 : 3.0)) +
-                        (split > 1 ? join_time(p.tiles, split, F::kRows, F::kCols) : 0.0);
+    const int places = together ? clustered : alone;
+    const bool full = ctas <= places;
+    const long long rounds = full ? 1 : (ctas + 2 * places - 1) / (2 * places);
+    const double block = (TERMS == 1 ? 0.3 : 0.65) * (full ? 1 : 2);  // two CTAs share an SM's copies
+    const double joined = split == 1 ? 0.0 : together ? kTogether : join_time(p.tiles, split, F::kRows, F::kCols);
+    const double time = 3.0 + rounds * (2.0 + std::ceil((double)blocks / split) * block + (split > 1 ? 1.0 : 3.0)) + joined;
     if (time < p.time) {
       p.time = time;
       p.split = split;
+      p.together = together;
+      p.stages = full ? F::kStages : F::kStages / 2;
     }
   }
   p.whole = p.split > 1 ? 0 : p.tiles;
   p.ctas = p.tiles * p.split;
-  p.stages = p.ctas > sms ? F::kStages / 2 : F::kStages;
   return p;
 }
 
@@ -1102,6 +1141,7 @@ template <typename F>
 void take_plan(Params& p, const Plan& plan) {
   p.m_tiles = plan.m_tiles; p.n_tiles = plan.n_tiles; p.per = plan.per; p.tiles = plan.tiles; p.whole = plan.whole; p.split = plan.split;
   p.stages = plan.stages;
+  p.together = plan.together;
   p.blocks = (p.K + kDeep - 1) / kDeep;
   p.piece = F::kRows * F::kCols;
 }
@@ -1129,8 +1169,8 @@ cudaError_t launch_small(Params& p, const Plan& plan, const Maps& maps, cudaStre
   static unsigned long long configured = 0;
   cudaError_t e = allow_dynamic_smem(muon_small_kernel<KIND, TERMS>, F::smem_bytes(F::kStages), configured);
   if (e != cudaSuccess) return e;
-  e = launch_pdl(muon_small_kernel<KIND, TERMS>, dim3(plan.ctas), dim3(F::kThreads), F::smem_bytes(plan.stages), s, p, maps);
-  return e != cudaSuccess || p.whole == p.tiles ? e : launch_join<KIND, TERMS, F>(p, s);
+  e = launch_clusters(plan.together ? plan.split : 1, muon_small_kernel<KIND, TERMS>, dim3(plan.ctas), dim3(F::kThreads), F::smem_bytes(plan.stages), s, p, maps);
+  return e != cudaSuccess || p.whole == p.tiles || p.together ? e : launch_join<KIND, TERMS, F>(p, s);
 }
 
 // What a product's operands are, and how they lie: `k`: rows are k.
