@@ -57,7 +57,7 @@ def build_calls(force: bool = False) -> Path | None:
            f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}", "-I", str(ROOT / "include")]
     for p in includes:
         cmd += ["-isystem", str(p)]
-    cmd += [str(src), "-o", str(tmp), "-L", str(at / "lib"), "-lc10", "-lc10_cuda", "-ltorch_cpu", "-ltorch_python"]
+    cmd += [str(src), "-o", str(tmp), "-L", str(at / "lib"), "-lc10", "-lc10_cuda", "-ltorch_cpu", "-ltorch_cuda", "-ltorch_python"]
     r = subprocess.run(cmd, capture_output=True, text=True)
     if r.returncode != 0:
         raise RuntimeError(f"{src.name}:\n{r.stdout}\n{r.stderr}")
