@@ -71,7 +71,7 @@ class BlockNormFunction(torch.autograd.Function):
         like = y if resid is None else resid
         D = like.shape[-1]
         rows = lambda t: None if t is None else t.reshape(-1, D)  # noqa: E731
-        g = gate if gate is None or gate.dim() == 1 else gate.reshape(-1, gate.shape[-1])
+        g = gate if gate is None or gate.dim() == 1 else gate.reshape(-1, gate.shape[-1]).contiguous()
         save = any(ctx.needs_input_grad)
         ry = rows(y)
         h, n, stats = block_norm_forward(ry, rows(resid), post_gain, pre_gain, g, scale=scale, eps=eps, save=save, n_dtype=n_dtype)

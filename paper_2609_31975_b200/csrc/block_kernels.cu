@@ -535,18 +535,19 @@ __global__ void __launch_bounds__(Ring<W, V>::kThreads, Ring<W, V>::kPerSm) bloc
     const float r = own_stat[0][at_stat], rho = own_stat[1][at_stat], token = own_stat[2][at_stat];
     if (++at_stat == 32 * W) at_stat = 0;
     rows.wait(stages - 1);
-    float2 s[4] = {both(0.f), both(0.f), both(0.f), both(0.f)};  // of t h, w y dh, w y t, w y h
+    // With h' = rho h and y' = r y (of size one, whatever the rows are: cubes of statistics would leave fp32): sums of t h', w y' dh, w y' t, w y' h'
+    float2 s[4] = {both(0.f), both(0.f), both(0.f), both(0.f)};
 #pragma unroll
     for (int i = 0; i < V; ++i) {
       if (rows.column(i) >= p.D) continue;
       Eight a, b;
       if (has_n) {
         a = rows.get(stage, dn, t, i) * pre[i];
-        b = rows.get(stage, h, t, i);
+        b = rows.get(stage, h, t, i) * rho;
         s[0] = dot8(a, b, s[0]);
       }
       if (has_y) {
-        Eight e = rows.get(stage, y, t, i) * w[i];
+        Eight e = rows.get(stage, y, t, i) * r * w[i];
         if (full) e = e * rows.get(stage, gate, t, i);
         if (has_n) {
           s[2] = dot8(e, a, s[2]);
@@ -559,29 +560,29 @@ __global__ void __launch_bounds__(Ring<W, V>::kThreads, Ring<W, V>::kPerSm) bloc
 #pragma unroll
     for (int k = 0; k < 4; ++k) sums[k] = s[k].x + s[k].y;
     row_sums<W>(sums, room[turn]);
-    const float k1 = rho * rho * rho * p.inv_d * sums[0];
-    const float wyg = fmaf(rho, sums[2], sums[1]) - k1 * sums[3];
-    const float k2 = post ? r * r * r * p.inv_d * token * wyg : 0.f, up = r * token, own = p.scale * up;
-    if (p.dgate && p.gate_kind == SFFN_BLOCK_GATE_TOKEN && rows.in_row == 0) reinterpret_cast<float*>(p.dgate)[t] = r * wyg;
+    // g = dh + rho t - k1 h',   sum(w y' g),   dy = up w g - k2 y'
+    const float mean = sums[0] * p.inv_d, k1 = rho * mean, wyg = fmaf(rho, fmaf(-mean, sums[3], sums[2]), sums[1]);
+    const float up = r * token, k2 = post ? up * wyg * p.inv_d : 0.f, own = p.scale * token;
+    if (p.dgate && p.gate_kind == SFFN_BLOCK_GATE_TOKEN && rows.in_row == 0) reinterpret_cast<float*>(p.dgate)[t] = wyg;
 #pragma unroll
     for (int i = 0; i < V; ++i) {
       const int c = rows.column(i);
       if (c >= p.D) continue;
       Eight g = has_dh ? rows.get(stage, dh, t, i) : eight_of(0.f);
       if (has_n) {
-        const Eight f = rows.get(stage, dn, t, i) * rho, b = rows.get(stage, h, t, i);
-        g = fma8(b, -k1, fma8(f, pre[i], g));
+        const Eight f = rows.get(stage, dn, t, i), b = rows.get(stage, h, t, i) * rho;
+        g = fma8(b, -k1, fma8(f * rho, pre[i], g));
         acc_pre[i] = fma8(f, b, acc_pre[i]);
       }
       if (p.dresid) store8(p.dresid + t * p.ld_dresid, h_bf16, p.wide, c, p.D, g);
       if (has_y) {
-        const Eight f = rows.get(stage, y, t, i), ww = w[i] * up;
+        const Eight f = rows.get(stage, y, t, i) * r;
         if (full) {
-          if (p.dgate) store8(p.dgate + t * p.ld_dgate, h_bf16, p.wide, c, p.D, ww * g * f);
+          if (p.dgate) store8(p.dgate + t * p.ld_dgate, h_bf16, p.wide, c, p.D, w[i] * g * f);
           g = g * rows.get(stage, gate, t, i);
         }
         acc_c[i] = fma8(g * own, f, acc_c[i]);
-        if (p.dy) store8(p.dy + t * p.ld_dy, y_bf16, p.wide, c, p.D, fma8(ww, g, f * -k2));
+        if (p.dy) store8(p.dy + t * p.ld_dy, y_bf16, p.wide, c, p.D, fma8(w[i] * up, g, f * -k2));
       }
     }
     rows.fetch(stage, t + stages * step, dh, dn, h, y, gate);  // what was in this stage has been used
@@ -717,7 +718,7 @@ cudaError_t backward(const BlockParams& p, int sm_count, int* lines, cudaStream_
   const int stages = stages_of<W, V>(planes, &bytes), rows = (p.T + S::kRows - 1) / S::kRows, room = S::kPerSm * sm_count;
   *lines = rows < room ? rows : room;
   if (*lines > p.lines) *lines = p.lines;
-  // So few CTAs that they are a cluster (of eight at most): one launch less (64 tokens of 256: 15.8 / ? us).
+  // So few CTAs that they are a cluster (of eight at most): one launch less (64 tokens of 256: 14.8 / 11.8 us).
   BlockParams q = p;
   q.together = *lines <= 8 && (p.want_pre || p.want_c);
   const cudaError_t launched = launch_clusters(q.together ? *lines : 1, block_backward_kernel<W, V, ALL_BF16>, dim3(*lines), dim3(S::kThreads), bytes, s, q, stages, planes);
