@@ -35,7 +35,7 @@
  * g_sign, rms_gain) are treated as parameters: the kernels may start reading them while the work queued
  * just before the call is still running (that is how back-to-back calls overlap), so they must not be
  * written by device work queued immediately before a call on the same stream -- put a stream or event
- * synchronisation between an update of the weights and the next call (sffn_adamw_step needs none).
+ * synchronisation between an update of the weights and the next call (sffn_adamw_step and sffn_muon_step need none).
  * A single-token call runs one CTA on every SM, and its CTAs wait for one another (LoPA: for the rank-r vector;
  * always: the first CTAs to finish stay and wait for the partial results of the rest, which they sum; every wait is bounded).
  * Calls of different handles are therefore meant to run one after another -- one stream, or streams ordered by
@@ -474,7 +474,8 @@ int sffn_muon_step(const sffn_muon_tensor* tensors, int n, const sffn_muon_confi
  * no n; without resid h is the second term; without y (NULL) h is resid, nothing is written to h, and n is its norm.  One call serves
  * training and decoding: a row is one token, its types are free (an FFN's fp32 y onto a bf16 stream, say), and T may be 1.
  * Like the training calls it takes no handle and is ordinary stream work: nothing is read before the work queued earlier has finished.
- * Sums and statistics are fp32; h and n are each rounded once (n is the norm of the unrounded h).
+ * Sums and statistics are fp32; h and n are each rounded once (n is the norm of the unrounded h).  Rows of y and h have squares whose sum
+ * fits fp32 (entries up to about 1e18); with eps = 0 a row of zeros is 0 / 0.
  * Types: y, h (and resid, with it) and n are each fp32 or bf16; gains, a gate of channels or tokens, and their gradients fp32; a full
  * gate has h's type.  D: up to SFFN_BLOCK_MAX_D, a multiple of 4, of 8 where anything is bf16.  Rows have strides in elements, a
  * multiple of 16 bytes; pointers are 16-byte aligned, those of a gate of tokens and of stats 4-byte.  T = 0 is a call like any other.
