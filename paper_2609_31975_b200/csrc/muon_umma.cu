@@ -64,7 +64,6 @@ struct Small {
   static constexpr int kStages = 8 / TERMS;                          // half of them where two CTAs share an SM
   static constexpr int kStageBytes = TERMS * (kBlockBytes + kBBytes);
   static constexpr int smem_bytes(int stages) { return stages * kStageBytes + 1024; }
-  static constexpr int kThreads = 64 + 256;
   static constexpr int kRuns = 3;                                    // two terms: runs that have an accumulator
   static constexpr int kTmem = TERMS == 1 ? kCols : (kRuns + 1) * kCols;
   static constexpr int kMostBlocks = TERMS == 1 ? 1 << 20 : kRuns * kRun;  // K blocks of a piece
@@ -787,10 +786,9 @@ __global__ void __launch_bounds__(Form<TERMS>::kThreads, 1) muon_umma_kernel(con
 // ---- small tiles -----------------------------------------------------------------------------------------------------
 // For products that do not fill the device with pairs' tiles: a CTA has one tile of 128 x 64 (or a piece of it along K).  A chain of
 // such launches is a chain of latencies (1024 x 256, fp32: 1.8 us from a launch's end to the next one's start, 1.3 to the first K block): up to eight
-// pieces are a cluster that joins them through L2; the
-// eight warps of the epilogue read and multiply what is beside the accumulators while these are made, and where the launch leaves SMs
-// idle, all K blocks of a short K are under way at once.  With two terms, every run of K blocks has an accumulator of its own, so a piece is
-// at most three runs.
+// pieces are a cluster that joins them through L2; the warps of the epilogue read and multiply what is beside the accumulators while these
+// are made, and where the launch leaves SMs idle, all K blocks of a short K are under way at once.  With two terms, every run of K blocks has
+// an accumulator of its own, so a piece is at most three runs.
 __device__ __forceinline__ void tma_tile_alone(uint32_t dst, const CUtensorMap* map, int c0, int c1, int c2, uint32_t bar) {
   asm volatile(
       "cp.async.bulk.tensor.3d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];" ::"r"(dst), "l"(map), "r"(c0), "r"(c1),
@@ -809,8 +807,11 @@ __device__ __forceinline__ void commit_alone(uint32_t bar) {
   asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
 }
 
-template <int KIND, int TERMS>
-__global__ void __launch_bounds__(Small<TERMS>::kThreads, 2) muon_small_kernel(const __grid_constant__ Params p, const __grid_constant__ Maps maps) {
+constexpr int small_threads(int warps) { return 64 + 32 * warps; }
+// WARPS: of the epilogue: sixteen where a CTA has an SM to itself, eight where two share one.  A whole orthogonalisation with sixteen and with
+// eight: fp32 1024 x 256 140 and 147 us, 1024 x 1024 231 and 250, 4096 x 1024 384 and 402; bf16 2048 x 512 132 and 129, 1024 x 1024 150 and 151.
+template <int KIND, int TERMS, int WARPS>
+__global__ void __launch_bounds__(small_threads(WARPS), 16 / WARPS) muon_small_kernel(const __grid_constant__ Params p, const __grid_constant__ Maps maps) {
   using F = Small<TERMS>;
   constexpr int kStages = F::kStages;
   extern __shared__ uint8_t smem_raw[];
@@ -903,17 +904,18 @@ __global__ void __launch_bounds__(Small<TERMS>::kThreads, 2) muon_small_kernel(c
       if (++s == p.stages) { s = 0; phase ^= 1; }
     }
   } else {
-    const int quad = warp & 3, across = 32 * ((warp - 2) >> 2), n_base = at.n * F::kCols + across, row0 = at.m * F::kRows + 32 * quad;
+    constexpr int kChunks = 16 / WARPS;  // of sixteen columns, of a warp
+    const int quad = warp & 3, across = 16 * kChunks * ((warp - 2) >> 2), n_base = at.n * F::kCols + across, row0 = at.m * F::kRows + 32 * quad;
     const bool rows = row0 < p.M;
-    float more[2][16];
-    // what this warp finishes: 32 rows and 32 columns of its tile, or, of a cluster's sixteen parts of 32 x 16, one or none
+    float more[kChunks][16];
+    // what this warp finishes: 32 rows and its columns of the tile, or, of a cluster's sixteen parts of 32 x 16, one or none
     const int own = (warp - 2) * p.split + part, own_r = 32 * (own >> 2), own_c = 16 * (own & 3);
     const int joined_row = at.m * F::kRows + own_r, joined_n = at.n * F::kCols + own_c;
     const bool joins = p.together && own < 16 && joined_row < p.M && wanted<KIND>(p, joined_row, joined_n);
     const Shared<KIND> all(p, at.batch, (p.together ? joined_row : row0) + lane);
     if (joins || (rows && !pieces)) {
 #pragma unroll
-      for (int c = 0; c < 2; ++c) {
+      for (int c = 0; c < kChunks; ++c) {
         const int n0 = p.together ? joined_n : n_base + 16 * c;
         if (c == 1 && (p.together || !wanted<KIND>(p, row0, n0))) break;
         if (c == 0 && !p.together && !wanted<KIND>(p, row0, n0)) break;
@@ -927,7 +929,7 @@ __global__ void __launch_bounds__(Small<TERMS>::kThreads, 2) muon_small_kernel(c
       const uint32_t acc = tmem + ((uint32_t)(32 * quad) << 16) + across;
       float* const piece = p.partial + (size_t)number * p.piece + (size_t)(32 * quad + lane) * F::kCols + across;
 #pragma unroll 1
-      for (int c = 0; c < 2; ++c) {
+      for (int c = 0; c < kChunks; ++c) {
         const int n0 = n_base + 16 * c;
         if (!pieces && !wanted<KIND>(p, row0, n0)) break;
         float v[16];
@@ -953,7 +955,7 @@ __global__ void __launch_bounds__(Small<TERMS>::kThreads, 2) muon_small_kernel(c
         } else {
           finish<KIND, TERMS>(p, all, at.batch, row0, n0, lane, v, more[0]);
 #pragma unroll
-          for (int i = 0; i < 16; ++i) more[0][i] = more[1][i];
+          for (int i = 0; i < 16; ++i) more[0][i] = more[kChunks - 1][i];
         }
       }
     }
@@ -1162,14 +1164,14 @@ cudaError_t launch_pairs(Params& p, const Plan& plan, const Maps& maps, cudaStre
   e = launch_clusters(2, muon_umma_kernel<KIND, TERMS>, dim3(plan.ctas), dim3(F::kThreads), F::kSmemBytes, s, p, maps);
   return e != cudaSuccess || p.whole == p.tiles ? e : launch_join<KIND, TERMS, F>(p, s);
 }
-template <int KIND, int TERMS>
+template <int KIND, int TERMS, int WARPS>
 cudaError_t launch_small(Params& p, const Plan& plan, const Maps& maps, cudaStream_t s) {
   using F = Small<TERMS>;
   take_plan<F>(p, plan);
   static unsigned long long configured = 0;
-  cudaError_t e = allow_dynamic_smem(muon_small_kernel<KIND, TERMS>, F::smem_bytes(F::kStages), configured);
+  cudaError_t e = allow_dynamic_smem(muon_small_kernel<KIND, TERMS, WARPS>, F::smem_bytes(F::kStages), configured);
   if (e != cudaSuccess) return e;
-  e = launch_clusters(plan.together ? plan.split : 1, muon_small_kernel<KIND, TERMS>, dim3(plan.ctas), dim3(F::kThreads), F::smem_bytes(plan.stages), s, p, maps);
+  e = launch_clusters(plan.together ? plan.split : 1, muon_small_kernel<KIND, TERMS, WARPS>, dim3(plan.ctas), dim3(small_threads(WARPS)), F::smem_bytes(plan.stages), s, p, maps);
   return e != cudaSuccess || p.whole == p.tiles || p.together ? e : launch_join<KIND, TERMS, F>(p, s);
 }
 
@@ -1193,7 +1195,8 @@ cudaError_t launch(const MuonBatch& b, Params& p, const Operand& x, const Operan
   if (TERMS == 1) maps.a[1] = maps.a[0], maps.b[1] = maps.b[0];
   p.a_mn = x.k;
   p.b_mn = y.k;
-  return few ? launch_small<KIND, TERMS>(p, alone, maps, s) : launch_pairs<KIND, TERMS>(p, pairs, maps, s);
+  if (!few) return launch_pairs<KIND, TERMS>(p, pairs, maps, s);
+  return alone.stages == Small<TERMS>::kStages ? launch_small<KIND, TERMS, 16>(p, alone, maps, s) : launch_small<KIND, TERMS, 8>(p, alone, maps, s);
 }
 
 }  // namespace
