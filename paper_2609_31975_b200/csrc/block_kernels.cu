@@ -14,6 +14,9 @@
 // sums: sum(w y g) is put together from sum(w y dh), sum(w y t) and sum(w y h), which do not wait for sum(t h).
 // Gradients of gains and of a channel gate are sums over the rows: a CTA's threads own columns and add up the rows that the CTA
 // meets in registers; one line of sums a CTA, which block_columns_kernel adds up in order.
+// Bound by memory.  Forward, 8192 x 8192, fp32 stream, bf16 y and n, a gate of channels: 131 us, 6.1 TB/s; 1000 x 4096 in bf16 10 us (33 MB, out of
+// L2), a row of 4096 4 us, both bound by the launch.  Backward, 4096 x 4096 in bf16: 48 us (201 MB, 4.2 TB/s; issue slots 55 %) and 7 to 9 for the sums
+// of columns; 5000 x 3840 with an fp32 stream and a gate of tokens: 76 us (346 MB, 4.6 TB/s).
 #include "block_kernels.cuh"
 
 #include "common.cuh"

@@ -9,7 +9,7 @@
 namespace sffn {
 
 constexpr int kMuonBatch = 64;     // matrices of a launch, at most
-constexpr int kMuonPartials = 256; // partial sums of a matrix's squares, at most
+constexpr int kMuonPartials = 1024; // partial sums of a matrix's squares, at most
 constexpr int kMuonPairs = 80;     // pairs of CTAs at most
 
 // A matrix as the caller has it.

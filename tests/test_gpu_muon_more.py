@@ -27,6 +27,15 @@ def test_batches(lib, shape, n, dtype):  # noqa: F811
         ref.close(o, ref.orthogonal(u), 32 if dtype == F32 else 16)
 
 
+@pytest.mark.parametrize("shape", [(200, 96), (90, 3001)], ids=str)
+@pytest.mark.parametrize("size", [2.0 ** -51.5, 2.0 ** 61])
+def test_squares_near_the_ends_of_32_bits(lib, size, shape):  # noqa: F811
+    """Eight squares are summed in 32 bits where they fit: sizes at which some eights of a matrix do and some do not."""
+    u = (torch.randn(shape, generator=gen(3), device=DEV, dtype=torch.float64) * size).float()
+    u[1::2, 8:24] = 0
+    ref.close(lib.orthogonalize(u, eps=0.0), ref.orthogonal(u, eps=0.0), 32)
+
+
 def test_two_streams_at_once(lib):  # noqa: F811
     """Calls that overlap have nothing in common but the status word."""
     sides = [torch.cuda.Stream() for _ in range(2)]
