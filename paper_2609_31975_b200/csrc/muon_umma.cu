@@ -78,7 +78,7 @@ struct Maps {
 };
 
 struct Params {
-  int kind, M, N, K, n;           // n: matrices
+  int M, N, K;
   int m_tiles, n_tiles, per, tiles, blocks;
   int whole, split;               // tiles dealt whole; pieces of each of the others
   int stages;                     // small tiles: of the ring
@@ -1221,8 +1221,6 @@ size_t muon_partial_floats(int S, int R, int C, int n, int terms) {
 
 cudaError_t launch_muon_product(const MuonBatch& b, const MuonProduct& q, int sm_count, cudaStream_t s) {
   Params p{};
-  p.kind = q.kind;
-  p.n = b.n;
   p.S = b.S;
   const bool sym = symmetric(q.kind);
   p.M = sym ? b.S : b.R;
