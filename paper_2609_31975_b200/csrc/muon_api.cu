@@ -68,7 +68,7 @@ bool make_products(const sffn_newton_schulz& ns, int group, Products& out) {
       return Held{which, exponent(m)};
     };
     auto push = [&](int kind, const Held& r, MuonTerm m, MuonTerm n, MuonTerm coefficient) {
-      out.push_back({kind, from, r.which, first, m, n, coefficient, ex, r.e});
+      out.push_back({kind, from, r.which, first, m, n, coefficient, ex, r.e, false});
     };
     for (int i = 0; i < kPoints; ++i) now[i] = x[i] * x[i];
     Held A = result(0, 1.0), B{}, R{};
@@ -115,6 +115,9 @@ bool make_products(const sffn_newton_schulz& ns, int group, Products& out) {
     k += steps;
     const bool last = k == ns.steps;
     push(last ? sffn::kLast : sffn::kApply, Held{0, last ? 0 : exponent(bound)}, with(R, 0, -1), none, only(q, factor(0)));
+    double growth = 1;
+    for (int i = k; i < ns.steps; ++i) growth *= std::fabs(ns.coefficients[3 * i]);
+    out.back().late = growth <= 4;
     if (!bounded || !(bound <= kLargestBound)) return false;
   }
   return true;
@@ -267,6 +270,10 @@ int run(const std::vector<Matrix>& all, const Plans& plans, const MuonBatch& com
   return SFFN_OK;
 }
 
+// Terms of the products' operands.  Roundings of a matrix of a few singular values do not average out (2 x 6 up to 8e-3 off in one term), and two
+// terms of so little cost no more than a tenth of the time.
+int terms_of(int bits, bool wide, const Matrix& m) { return bits == 32 || (bits == 0 && wide) || std::min(m.R, m.C) < 8 ? 2 : 1; }
+
 int matrices_of(const sffn_orthogonal* t, int n, const sffn_newton_schulz* ns, std::vector<Matrix>& out, bool pointers) {
   if (n < 0 || (n > 0 && !t)) return SFFN_ERR_INVALID_ARG;
   for (int i = 0; i < n; ++i) {
@@ -283,7 +290,7 @@ int matrices_of(const sffn_orthogonal* t, int n, const sffn_newton_schulz* ns, s
     m.item.out = a.o; m.item.ld_out = a.ld_o;
     m.R = a.rows; m.C = a.cols;
     m.src_bf16 = m.out_bf16 = a.dtype == SFFN_BF16;
-    m.terms = ns->bits == 32 || (ns->bits == 0 && a.dtype == SFFN_F32) ? 2 : 1;
+    m.terms = terms_of(ns->bits, a.dtype == SFFN_F32, m);
     out.push_back(m);
   }
   return SFFN_OK;
@@ -312,7 +319,7 @@ int matrices_of(const sffn_muon_tensor* t, int n, const sffn_newton_schulz* ns, 
     m.R = a.rows; m.C = a.cols;
     m.src_bf16 = a.g_dtype == SFFN_BF16;
     m.out_bf16 = a.p_dtype == SFFN_BF16;
-    m.terms = ns->bits == 32 || (ns->bits == 0 && (a.p_dtype == SFFN_F32 || a.master)) ? 2 : 1;
+    m.terms = terms_of(ns->bits, a.p_dtype == SFFN_F32 || a.master, m);
     out.push_back(m);
   }
   return SFFN_OK;

@@ -63,6 +63,7 @@ struct MuonProduct {
   bool first;           // factors are to be looked at
   MuonTerm m, n, k;
   int ex, e_out;        // exponents that X, and the result, are stored with
+  bool late;            // the steps to come multiply small singular values by four at most
 };
 
 cudaError_t launch_muon_product(const MuonBatch& b, const MuonProduct& p, int sm_count, cudaStream_t s);

@@ -11,6 +11,10 @@
 // of sixteen bits: singular values far below the largest grow by a in every step, 485 times in five, and with them the rounding of a X.
 // So X is held in two terms, hi + lo, and only the products take hi.  And every symmetric matrix is held as its diagonal, in fp32, and the
 // rest: diagonals are the largest entries by far, and what they contribute to a product is added in the epilogue.
+// What the diagonal of R contributes to R X takes both terms of X only in the last steps.  In R hi all is within the column space of R,
+// but with both terms for the diagonal alone what is wrong is (R - diag) lo, 2^-12 diag of it outside of every singular vector of X, to be
+// multiplied by a in each step to come: fine for X of full rank (five times as exact, R is near its diagonal then), but of rank 1 a matrix of
+// 4 x 19 came out 3.3e-2 off.  So: both where what is to come multiplies it by four at most (1.5e-3).
 // (64-bit model, 1344 x 384, error against exact, norm by norm, steps one by one / in pairs: Gaussian 6e-4 / 5e-4, of rank 16 1.2e-3 / 2.2e-3,
 // singular values dying away 3e-4 to 5e-4 / 6e-4 to 8e-4, half of them small 2e-3 / 3.6e-3; with a X from one term rank 16 2.9e-2, with bf16 operands 1.2e-2 and 0.24.)
 // Where results are wanted in 32 bits, every operand enters in two terms: hi hi in runs of eight K blocks, which are added up in registers
@@ -102,10 +106,10 @@ struct Params {
   float m, nn, k_m, k_n, k;
   float dm, dn, dk, dacc;         // the diagonal (as it is): dm d_M + dn d_N + dk (d_M d_N + dacc acc)
   int fm, fn, fk;                 // first step: which factor the terms in m, n, k take (-1: none)
-  // kApply, kLast: X' = (q + d) x_scale X + acc_scale acc
+  // kApply, kLast: X' = x_scale (q X + d X) + acc_scale acc, the second X without its second term unless `both` (1 or 0)
   const uint16_t* X;
   const float* diag;
-  float q, x_scale, acc_scale;
+  float q, x_scale, acc_scale, both;
   int fq;
   // kLast
   int step, out_bf16;
@@ -415,7 +419,7 @@ __device__ __forceinline__ void beside(const Params& p, const Shared<KIND>& all,
       }
     }
   } else if constexpr (!symmetric(KIND)) {
-    const float q = all.f_k + all.d;
+    const float q = all.f_k * p.x_scale;
     float d[16];
     if (p.tall) {
       columns16(p.diag + batch * diag_ld(p.S) + n0, d);
@@ -426,8 +430,8 @@ __device__ __forceinline__ void beside(const Params& p, const Shared<KIND>& all,
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
       const float2 hi = from_halves(a.t[0].w[i]), lo = from_halves(a.t[1].w[i]);
-      v[2 * i] = (q + d[2 * i]) * p.x_scale * (hi.x + lo.x);
-      v[2 * i + 1] = (q + d[2 * i + 1]) * p.x_scale * (hi.y + lo.y);
+      v[2 * i] = fmaf((all.d + d[2 * i]) * p.x_scale, fmaf(p.both, lo.x, hi.x), q * (hi.x + lo.x));
+      v[2 * i + 1] = fmaf((all.d + d[2 * i + 1]) * p.x_scale, fmaf(p.both, lo.y, hi.y), q * (hi.y + lo.y));
     }
   }
 }
@@ -1275,6 +1279,7 @@ cudaError_t launch_muon_product(const MuonBatch& b, const MuonProduct& q, int sm
   p.x_scale = two((last ? 0 : q.e_out) - q.ex);
   p.acc_scale = two((last ? 0 : q.e_out) - q.ex - q.m.e);
   p.diag = diag(q.m.which);
+  p.both = b.terms == 2 || q.late;
   p.X = X;
   if (!last) {
     p.out = b.x[q.from ^ 1];

@@ -36,6 +36,25 @@ def test_squares_near_the_ends_of_32_bits(lib, size, shape):  # noqa: F811
     ref.close(lib.orthogonalize(u, eps=0.0), ref.orthogonal(u, eps=0.0), 32)
 
 
+def test_of_few_singular_values(lib):  # noqa: F811
+    """Roundings of a few values do not average out: matrices as small as these take two terms whatever is asked for."""
+    for i, shape in enumerate([(1, 1), (1, 1), (2, 6), (2, 1), (6, 3), (5, 2), (13, 2), (2, 9), (2, 3), (1, 700), (7, 7), (5, 5000)] * 20):
+        u = normal(shape, gen(i))
+        ref.close(lib.orthogonalize(u, bits=16), ref.orthogonal(u), 32)
+        b = u.bfloat16()
+        ref.close(lib.orthogonalize(b), ref.orthogonal(b), 32)
+
+
+@pytest.mark.parametrize("steps", [5, 6])
+@pytest.mark.parametrize("rank", [1, 2, 5])
+@pytest.mark.parametrize("shape", [(4, 19), (7, 109), (145, 9), (2, 38), (21, 8), (300, 96), (1024, 256)], ids=str)
+def test_of_low_rank(lib, shape, rank, steps):  # noqa: F811
+    """What is not in the update's range stays small next to what is, in one matrix and in lists of them."""
+    us = [normal((shape[0], rank), gen(8 * i)) @ normal((rank, shape[1]), gen(8 * i + 1)) for i in range(12 if shape[1] == 256 else 1)]
+    for u, o in zip(us, lib.orthogonalize(us, bits=16, steps=steps)):
+        ref.close(o, ref.orthogonal(u, steps=steps), 16, steps)
+
+
 def test_two_streams_at_once(lib):  # noqa: F811
     """Calls that overlap have nothing in common but the status word."""
     sides = [torch.cuda.Stream() for _ in range(2)]
