@@ -36,7 +36,7 @@ def orthogonalize(update, out=None, *, steps=5, coefficients=MUON_COEFFICIENTS, 
 
     ``coefficients``: (a, b, c), or one such triple for every step.  ``bits`` of the products' operands: 16 (one fp16 term, O within
     about 1e-3 of its norm, 4e-3 where singular values are far apart), 32 (two terms, within 2e-5, three products for one; of a matrix
-    with a null space 1e-4), None: 16 for bf16, 32 for fp32.  ``out``: a tensor (a
+    with a null space 2e-4), None: 16 for bf16, 32 for fp32.  ``out``: a tensor (a
     list) to write to, which may be the update itself."""
     if stream is not None:
         with torch.cuda.stream(stream):
