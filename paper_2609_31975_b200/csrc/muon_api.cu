@@ -250,7 +250,9 @@ bool any_meet(std::vector<Range>& all) {
 // and fp32: 1024 x 256 108 / 112, 159 / 178; 48 of them 338 / -, 466 / 377; 12 of 2048 x 512 418 / -, 665 / 469; 1280 x 1024 162 / 173, 324 / 343;
 // 2048 x 1024 191 / 192, 429 / 387; 4096 x 1024 318 / 270, 521 / 429; 2560 x 2048 506 / 444, 826 / 832; 5120 x 4096 1728 / 1627, 4467 / 4454;
 // 8192 x 2048 846 / 673, 1560 / 1145.
+// In one term, what company leaves behind does not average out in small matrices: 33 of 145 x 2449, rank 20 to 60, 5.8e-3 off (one at a time 2e-3).
 int steps_at_a_time(const MuonBatch& b) {
+  if (b.terms == 1 && b.S < 256) return 1;
   const int64_t size = (int64_t)b.n * b.S * b.S, quarters = size < (1 << 22) ? 6 : 5;
   return size < (1 << 19) || 4 * (int64_t)b.L < quarters * b.S ? 1 : b.terms == 2 ? 3 : 2;
 }

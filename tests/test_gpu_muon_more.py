@@ -36,6 +36,14 @@ def test_squares_near_the_ends_of_32_bits(lib, size, shape):  # noqa: F811
     ref.close(lib.orthogonalize(u, eps=0.0), ref.orthogonal(u, eps=0.0), 32)
 
 
+def test_many_of_low_rank(lib):  # noqa: F811
+    """As many small matrices as are worth taking steps together."""
+    for shape, rank in (((145, 2449), 30), ((164, 1311), 50), ((338, 131), 40), ((300, 1200), 60)):
+        us = [normal((shape[0], rank), gen(2 * i)) @ normal((rank, shape[1]), gen(2 * i + 1)) for i in range(33)]
+        for u, o in zip(us, lib.orthogonalize(us, bits=16)):
+            ref.close(o, ref.orthogonal(u), 16)
+
+
 def test_of_few_singular_values(lib):  # noqa: F811
     """Roundings of a few values do not average out: matrices as small as these take two terms whatever is asked for."""
     for i, shape in enumerate([(1, 1), (1, 1), (2, 6), (2, 1), (6, 3), (5, 2), (13, 2), (2, 9), (2, 3), (1, 700), (7, 7), (5, 5000)] * 20):
