@@ -56,6 +56,7 @@ struct BlockParams {
   float* partial;                         // [2][lines][D], or NULL
   int lines, want_pre, want_c;
   int wide;                               // fp32 rows start on 32 bytes, all of them
+  int wide_lines;                         // lines of column sums, likewise
   int together;                           // the launch is one cluster
   ColumnSums sums;
 };
@@ -597,7 +598,7 @@ __global__ void __launch_bounds__(Ring<W, V>::kThreads, Ring<W, V>::kPerSm) bloc
     if constexpr (W > 1) {
 #pragma unroll
       for (int i = 0; i < V; ++i)
-        if (rows.column(i) < p.D) store8(reinterpret_cast<char*>(to), 0, p.D % 8 == 0, rows.column(i), p.D, acc[i]);
+        if (rows.column(i) < p.D) store8(reinterpret_cast<char*>(to), 0, p.wide_lines, rows.column(i), p.D, acc[i]);
     } else {  // of its warps' sums, in their order
       __syncthreads();
 #pragma unroll
@@ -769,6 +770,7 @@ cudaError_t launch_block_backward(const sffn_block_norm& b, const sffn_block_gra
   if (p.gate_kind == SFFN_BLOCK_GATE_FULL) look(p.dgate, p.ld_dgate, p.h_bf16);
   p.partial = partial;
   p.lines = block_lines(p.D);
+  p.wide_lines = p.D % 8 == 0 && (reinterpret_cast<uintptr_t>(partial) & 31) == 0;  // (a workspace starts on 16 bytes)
   p.sums = {p.post_gain, p.gate_kind == SFFN_BLOCK_GATE_CHANNEL ? reinterpret_cast<const float*>(p.gate) : nullptr, g.dpre_gain, g.dpost_gain,
             p.gate_kind == SFFN_BLOCK_GATE_CHANNEL ? static_cast<float*>(g.dgate) : nullptr};
   p.want_pre = p.sums.dpre != nullptr;
