@@ -520,7 +520,7 @@ typedef struct {
   float *dpost_gain, *dpre_gain;      /* [D] */
   void* dgate;                        /* as the gate */
   int64_t ld_dgate;
-  void* workspace;                    /* 16-byte aligned; needed where a gradient of a gain or of a gate of channels is wanted */
+  void* workspace;                    /* 16-byte aligned, over nothing else of the call; needed where a gradient of a gain or of a gate of channels is wanted */
   size_t workspace_bytes;
 } sffn_block_grads;
 int sffn_block_norm_workspace_bytes(int D, size_t* bytes);

@@ -118,9 +118,9 @@ int sffn_block_norm_backward(const sffn_block_norm* c, const sffn_block_grads* g
   const int64_t columns = 4ll * c->D;
   const Span dpost = whole(g->dpost_gain, columns), dpre = whole(g->dpre_gain, columns), dgate = gate_of(c, g->dgate, g->ld_dgate);
   const Span stats = whole(c->stats, 8ll * c->T), own = need ? whole(g->workspace, (int64_t)need) : none;
-  // each row of dresid is written when its row of dh has been read
-  if (outputs_meet({y, h, dn, stats, gate_of(c, c->gate, c->ld_gate), whole(c->post_gain, columns), whole(c->pre_gain, columns), own}, {dy, dresid, dpost, dpre, dgate}) ||
-      outputs_meet({dh}, {dy, dpost, dpre, dgate}) || (meet(dresid, dh) && !same(dresid, dh)))
+  // each row of dresid is written when its row of dh has been read; lines of column sums are written while other rows are still being read
+  if (outputs_meet({y, h, dn, stats, gate_of(c, c->gate, c->ld_gate), whole(c->post_gain, columns), whole(c->pre_gain, columns)}, {dy, dresid, dpost, dpre, dgate, own}) ||
+      outputs_meet({dh}, {dy, dpost, dpre, dgate, own}) || (meet(dresid, dh) && !same(dresid, dh)))
     return SFFN_ERR_INVALID_ARG;
   int sms = 0;
   const int count = sm_count(&sms);
