@@ -5,7 +5,9 @@
 //
 // The C entry points come in as addresses (`bind`), from the library that the binding has loaded.
 #include <ATen/ATen.h>
+#include <ATen/Context.h>
 #include <ATen/cuda/EmptyTensor.h>
+#include <c10/core/impl/LocalDispatchKeySet.h>
 #include <c10/cuda/CUDAGraphsC10Utils.h>
 #include <c10/cuda/CUDAGuard.h>
 #include <c10/cuda/CUDAStream.h>
@@ -93,8 +95,14 @@ int dtype_code(at::ScalarType t, const char* what) {
 void on_cuda(const Tensor& t) {
   if (!t.is_cuda()) type_error("tensors must be on a CUDA device");
 }
-// (Straight from torch's allocator: the way through its dispatcher takes longer than the allocation.)
-Tensor make(at::IntArrayRef shape, at::ScalarType dtype, const at::Device& dev) { return Tensor(at::detail::empty_cuda(shape, dtype, dev, std::nullopt)); }
+// Straight from torch's allocator, as the way through its dispatcher takes longer than the allocation: unless something looks on there (a
+// dispatch mode, a transform), or torch is to fill memory that nothing has written yet.
+Tensor make(at::IntArrayRef shape, at::ScalarType dtype, const at::Device& dev) {
+  const bool seen = !(c10::impl::tls_local_dispatch_key_set().included_ - c10::default_included_set).empty();
+  const auto& context = at::globalContext();
+  if (seen || (context.deterministicAlgorithms() && context.deterministicFillUninitializedMemory())) return at::empty(shape, at::TensorOptions().dtype(dtype).device(dev));
+  return Tensor(at::detail::empty_cuda(shape, dtype, dev, std::nullopt));
+}
 // [T, H] with rows a multiple of 16 bytes apart.
 Tensor make_hidden(int64_t T, int64_t H, at::ScalarType dtype, const at::Device& dev) {
   const int64_t ld = (H + 7) / 8 * 8;
