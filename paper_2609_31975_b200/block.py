@@ -39,12 +39,14 @@ def block_norm_forward(y, resid, post_gain=None, pre_gain=None, gate=None, *, sc
 def block_norm_backward(dh, dn, y, h, stats, post_gain=None, pre_gain=None, gate=None, *, scale=1.0, need=BLOCK_GRADS, out=None, stream=None):
     """Gradients of :func:`block_norm_forward` from dh (h's type) and dn (n's type; either may be None), y, and the h and stats that the
     forward pass left: a dict of those named in ``need`` that the call has (dy, dresid [T, D]; dpost_gain, dpre_gain [D] fp32; dgate as
-    the gate).  ``out``: a dict of tensors to write to; dresid may be dh, no other one may share memory with an input or another output."""
+    the gate).  ``out``: a dict of tensors to write to (those not in ``need`` are left alone); dresid may be dh, no other one may share
+    memory with an input or another output."""
     if stream is not None:
         with torch.cuda.stream(stream):
             return block_norm_backward(dh, dn, y, h, stats, post_gain, pre_gain, gate, scale=scale, need=need, out=out)
     bits = 31
     if need is not BLOCK_GRADS or out:
+        need = tuple(need)
         for name in (*need, *(out or ())):
             if name not in BLOCK_GRADS:
                 raise ValueError(f"no such gradient: {name!r}")
