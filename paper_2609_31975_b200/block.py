@@ -64,20 +64,34 @@ def block_norm_backward(dh, dn, y, h, stats, post_gain=None, pre_gain=None, gate
     return {name: t for name, t in zip(BLOCK_GRADS, got) if t is not None}
 
 
+def _readable(t):
+    """The rows t [T, D], or a copy of them where the calls do not take them as they lie: entries apart, or rows that start off 16 bytes."""
+    as_it_is = t.stride(1) == 1 and t.data_ptr() % 16 == 0
+    if t.shape[0] > 1:
+        as_it_is = as_it_is and t.shape[1] <= t.stride(0) <= 1 << 31 and t.stride(0) * t.element_size() % 16 == 0
+    return t if as_it_is else t.clone(memory_format=torch.contiguous_format)
+
+
 class BlockNormFunction(torch.autograd.Function):
     """The pair as a node of torch's graph: ``h, n = BlockNormFunction.apply(y, resid, post_gain, pre_gain, gate, scale, eps, n_dtype)``,
-    y and resid [..., D]; n is None without pre_gain.  First derivatives only."""
+    y and resid [..., D], at any strides, as gains and gate; n is None without pre_gain.  First derivatives only."""
 
     @staticmethod
     def forward(ctx, y, resid, post_gain=None, pre_gain=None, gate=None, scale=1.0, eps=1e-6, n_dtype=None):
         like = y if resid is None else resid
         D = like.shape[-1]
-        rows = lambda t: None if t is None else t.reshape(-1, D)  # noqa: E731
-        g = gate if gate is None or gate.dim() == 1 else gate.reshape(-1, gate.shape[-1]).contiguous()
+        rows = lambda t: None if t is None else _readable(t.reshape(-1, D))  # noqa: E731
+        vector = lambda t: t if t is None or t.is_contiguous() and t.data_ptr() % 16 == 0 else t.clone(memory_format=torch.contiguous_format)  # noqa: E731
+        post_gain, pre_gain = vector(post_gain), vector(pre_gain)
+        if gate is None or gate.dim() == 1:
+            g = vector(gate)
+        else:
+            g = gate.reshape(-1, gate.shape[-1])
+            g = g.contiguous() if g.shape[1] == 1 else _readable(g)
         save = any(ctx.needs_input_grad)
-        ry = rows(y)
-        h, n, stats = block_norm_forward(ry, rows(resid), post_gain, pre_gain, g, scale=scale, eps=eps, save=save, n_dtype=n_dtype)
-        if y is None:
+        ry, rx = rows(y), rows(resid)
+        h, n, stats = block_norm_forward(ry, rx, post_gain, pre_gain, g, scale=scale, eps=eps, save=save, n_dtype=n_dtype)
+        if y is None and h.data_ptr() == resid.data_ptr():
             h = h.clone()  # an output of a node is not its input
         if save:
             ctx.save_for_backward(ry, h, stats, post_gain, pre_gain, g)
@@ -92,12 +106,7 @@ class BlockNormFunction(torch.autograd.Function):
             return (None,) * 8
         y, h, stats, post_gain, pre_gain, gate = ctx.saved_tensors
 
-        def rows(t):
-            if t is None:
-                return None
-            t = t.reshape(h.shape).contiguous()
-            return t.clone() if t.data_ptr() % 16 else t
-
+        rows = lambda t: None if t is None else _readable(t.reshape(h.shape))  # noqa: E731
         wanted = dict(zip(("dy", "dresid", "dpost_gain", "dpre_gain", "dgate"), ctx.needs_input_grad))
         got = block_norm_backward(rows(dh), rows(dn), y, h, stats, post_gain, pre_gain, gate, scale=ctx.scale, need=[k for k, w in wanted.items() if w])
         for name, shape in (("dy", ctx.shape), ("dresid", ctx.shape), ("dgate", ctx.gate_shape)):
