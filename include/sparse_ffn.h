@@ -418,9 +418,11 @@ int sffn_adamw_state_values(const sffn_adamw_tensor* tensors, int n, float* cons
  *     X = U / (|U|_F + eps),   then for every step, with its coefficients a, b, c:   X = a X + (b P + c P^2) X,  P = X X^T
  * (on the shorter side: P = X^T X where rows > cols, from the right), O = X.  Singular values of U above about a^-steps of its norm come
  * out near 1 with the usual coefficients (3.4445, -4.7750, 2.0315), smaller ones are multiplied by a^steps.
- * `bits` of the products: 16: one fp16 term an operand (O within about 1e-3 of its norm, 4e-3 where singular values are far apart; two
- * terms all the same where a side is below 8); 32: two, three products for one (within 2e-5; where U has a null space, rounding in it is
- * multiplied by a^steps, 2e-4); 0: by what is written, 32 where that has 32 bits, else 16.  Sums are fp32, the norm 64-bit.  A NaN or infinity in U makes all of its O NaN; zeros give zeros; no rows or columns: nothing is done.
+ * `bits` of the products: 16: one fp16 term an operand (O within about 1e-3 of its norm, besides its own type's rounding, 3e-3 where a side
+ * is below 16, 5e-3 where singular values are few or far apart; two terms all the same where a side is below 8); 32: two, three products for
+ * one (within 2e-5 in five steps; where U has a null space, roundings in it are multiplied by as much as a^steps: of rank 1 or 2 up to 5e-4,
+ * as in fp32 products); 0: by what is written, 32 where that has 32 bits, else 16.  Sums are fp32, the norm 64-bit.  A NaN or infinity in U
+ * makes all of its O NaN; zeros give zeros; no rows or columns: nothing is done.
  * U and O: fp32 or bf16, rows at any stride >= cols, aligned as their type.  o may lie over its own u; other overlaps of an output with
  * anything of the call are SFFN_ERR_INVALID_ARG, as are coefficients under which singular values grow beyond 2^30.
  * Sides: up to 65536 and 2^22.  Matrices of one shape and type are multiplied together.  Results repeat bit for bit with the same list.

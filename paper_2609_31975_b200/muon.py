@@ -35,9 +35,9 @@ def orthogonalize(update, out=None, *, steps=5, coefficients=MUON_COEFFICIENTS, 
     X = a X + (b P + c P^2) X with P = X X^T on the shorter side.  fp32 or bf16; rows may be strided.
 
     ``coefficients``: (a, b, c), or one such triple for every step.  ``bits`` of the products' operands: 16 (one fp16 term, O within
-    about 1e-3 of its norm, 4e-3 where singular values are far apart), 32 (two terms, within 2e-5, three products for one; of a matrix
-    with a null space 2e-4), None: 16 for bf16, 32 for fp32.  ``out``: a tensor (a
-    list) to write to, which may be the update itself."""
+    about 1e-3 of its norm besides its own rounding, 3e-3 where a side is below 16, 5e-3 where singular values are few or far apart), 32
+    (two terms, within 2e-5, three products for one; of a matrix with a null space up to 5e-4, as fp32 products), None: 16 for bf16, 32
+    for fp32.  ``out``: a tensor (a list) to write to, which may be the update itself."""
     if stream is not None:
         with torch.cuda.stream(stream):
             return orthogonalize(update, out, steps=steps, coefficients=coefficients, eps=eps, bits=bits)
@@ -79,7 +79,7 @@ def muon_step(params, grads, states, *, lr, momentum=0.95, nesterov=True, weight
     params fp32 or bf16 matrices, grads fp32 or bf16, states as :func:`muon_state` makes them (updated).  ``lr``, ``weight_decay`` and
     ``scale``: one for all, or one for each; scale a number, "spectral" or "rms".  ``masters``: for bf16 parameters, fp32 copies that
     take the step (a list with None where there is none).  ``bits`` of the products: None: 32 where a parameter or its master is fp32,
-    else 16; 16 takes a third of the time, and is within 1e-3 of the update or little more.  ``grad_norm``, ``max_norm``: as for :func:`adamw_step`: a
+    else 16, which takes a third of the time (how far off either is: :func:`orthogonalize`).  ``grad_norm``, ``max_norm``: as for :func:`adamw_step`: a
     norm that is not finite leaves everything as it was.  Calls that read the parameters may follow on the same stream."""
     if max_norm is not None and grad_norm is None:
         raise ValueError("max_norm needs grad_norm")
