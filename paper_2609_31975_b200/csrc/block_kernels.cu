@@ -9,14 +9,17 @@
 //     dgain_pre = sum_t dn . h rho,   dgain_post = scale sum_t gate . g . y r,   dgate = scale g . gain_post . y r   (summed as the gate is
 //     broadcast)
 //
-// A row belongs to a warp or to a CTA, whose threads hold it in registers, eight consecutive entries each (or up to four such pieces):
-// every input is read once.  The forward pass needs two sums over a row, one after the other.  The backward pass needs one round of
+// A row belongs to a warp or to a CTA, whose threads hold it in registers, eight consecutive entries each (or up to four such pieces), or,
+// where there are many of them, in a ring in shared memory: every input is read from memory once up to 8192 columns.  Wider rows have no ring, and
+// the backward pass reads them twice, the second time out of L2 where they are still there.  The forward pass needs two sums over a row, one after the other.  The backward pass needs one round of
 // sums: sum(w y g) is put together from sum(w y dh), sum(w y t) and sum(w y h), which do not wait for sum(t h).
 // Gradients of gains and of a channel gate are sums over the rows: a CTA's threads own columns and add up the rows that the CTA
 // meets in registers; one line of sums a CTA, which block_columns_kernel adds up in order.
-// Bound by memory.  Forward, 8192 x 8192, fp32 stream, bf16 y and n, a gate of channels: 131 us, 6.1 TB/s; 1000 x 4096 in bf16 10 us (33 MB, out of
-// L2), a row of 4096 4 us, both bound by the launch.  Backward, 4096 x 4096 in bf16: 48 us (201 MB, 4.2 TB/s; issue slots 55 %) and 7 to 9 for the sums
-// of columns; 5000 x 3840 with an fp32 stream and a gate of tokens: 76 us (346 MB, 4.6 TB/s).
+// Forward, 8192 x 8192, fp32 stream, bf16 y and n, a gate of channels: 131 to 137 us, 5.9 to 6.1 TB/s, bound by memory; 1000 x 4096 in bf16 10 us (33 MB, out of
+// L2): 1000 CTAs, four an SM, are 1.7 rounds, each of which reads the gains and the gate again, issue slots 57 %; a row of 4096 3 us, bound by
+// the launch and two sums one after the other.  Backward, 4096 x 4096 in bf16: 44 us (201 MB, 4.6 TB/s; issue slots 55 %: each array is
+// unpacked twice a row) and 7 for the sums of columns; 5000 x 3840 with an fp32 stream and a gate of tokens: 76 us with them (346 MB, 4.6 TB/s).
+// Without a ring, 4096 x 16384 in bf16: forward 155 us (3.5 TB/s), backward 337 (2.4 TB/s; 64 registers a thread, the rest spilled).
 #include "block_kernels.cuh"
 
 #include "common.cuh"
@@ -318,7 +321,8 @@ __device__ __forceinline__ void row_sums(float (&v)[4], float* room) {
   for (int k = 0; k < 4; ++k) v[k] = __shfl_sync(0xffffffffu, s, 8 * k);
 }
 
-constexpr int kMostStages = 6;  // rows under way, at most
+constexpr int kMostStages = 6;         // rows under way, at most
+constexpr int kSmShared = 200 * 1024;  // of an SM's shared memory, for the rings of the CTAs on it
 
 // Rows of up to 8192 entries: W warps, one or two pieces of eight entries a thread (W 1: eight rows a CTA).  Wider ones: 32 warps of up to four
 // pieces, which have no room in shared memory and whose sums of columns do not fit registers beside the rest.
@@ -327,6 +331,11 @@ struct Ring {
   static constexpr int kRows = W == 1 ? 8 : 1, kThreads = 32 * W * kRows;
   static constexpr int kPerSm = kThreads >= 512 ? 1 : 512 / kThreads;
   static constexpr bool kShared = W < 32;
+  // Of the backward kernel, beside the ring: sums of a row, of its warps' columns (W 1), statistics of rows (11 KB where W is 1, 6.5 at most elsewhere
+  // with a ring).
+  static constexpr int kRoom = 2 * 4 * W, kLine = W == 1 ? 256 * V : 1, kStats = 32 * W;
+  static constexpr int kStatic = 4 * (kRoom + (W == 1 ? kRows * kLine : 2) + kRows * 3 * kStats);
+  static_assert(!kShared || kPerSm * (kSmShared / kPerSm + kStatic + 1024) <= 228 * 1024, "the CTAs of an SM, with the 1 KB that each takes of it by itself");
 };
 __device__ __forceinline__ void copy16(uint32_t to, const char* from) {
   asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to), "l"(from) : "memory");
@@ -500,8 +509,9 @@ template <int W, int V, bool ALL_BF16>
 __global__ void __launch_bounds__(Ring<W, V>::kThreads, Ring<W, V>::kPerSm) block_backward_kernel(const __grid_constant__ BlockParams p, int stages, int planes) {
   constexpr int kRows = Ring<W, V>::kRows, kThreads = Ring<W, V>::kThreads;
   extern __shared__ __align__(16) uint8_t ring_raw[];
-  __shared__ float room[2][4 * W];
-  __shared__ __align__(8) float lines[W == 1 ? kRows : 1][W == 1 ? 256 * V : 1];
+  using R = Ring<W, V>;
+  __shared__ float room[2][R::kRoom / 2];
+  __shared__ __align__(8) float lines[W == 1 ? kRows : 1][R::kLine];
   const bool y_bf16 = ALL_BF16 || p.y_bf16, h_bf16 = ALL_BF16 || p.h_bf16, n_bf16 = ALL_BF16 || p.n_bf16;
   const bool post = p.post_gain != nullptr, full = p.gate_kind == SFFN_BLOCK_GATE_FULL;
   const bool has_dh = p.dh != nullptr, has_n = p.dn != nullptr, has_y = p.y != nullptr;
@@ -522,7 +532,7 @@ __global__ void __launch_bounds__(Ring<W, V>::kThreads, Ring<W, V>::kPerSm) bloc
   }
   // Statistics and a gate of tokens: for as many of its rows as it has threads, a row's warps bring them into shared memory at once.  (A load a
   // row and thread, even one row ahead, costs a fifth: the wait for the ring's copies waits for it too.)
-  __shared__ float stat[kRows][3][32 * W];
+  __shared__ float stat[kRows][3][R::kStats];
   float (*const own_stat)[32 * W] = stat[threadIdx.x / (32 * W)];
   int turn = 0, stage = 0, at_stat = 0;
   for (int t = first; t < p.T; t += step, turn ^= 1) {
@@ -678,7 +688,6 @@ BlockParams params_of(const sffn_block_norm& b) {
 }
 
 constexpr int kManyRows = 8;           // rows an SM
-constexpr int kSmShared = 200 * 1024;  // of an SM, for the rings of the CTAs on it (up to eight, with up to 9 KB more each)
 // Stages of a ring of so many planes, and its bytes; at most five arrays of fp32, two pieces of 512 threads of an SM: 160 KB a stage.
 template <int W, int V>
 int stages_of(int planes, size_t* bytes) {

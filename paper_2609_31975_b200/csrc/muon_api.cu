@@ -247,9 +247,11 @@ bool any_meet(std::vector<Range>& all) {
 }
 
 // What is small is a chain of launches, which company makes longer; what is nearly square gains little.  In us, one at a time / in company, bf16
-// and fp32: 1024 x 256 108 / 112, 159 / 178; 48 of them 338 / -, 466 / 377; 12 of 2048 x 512 418 / -, 665 / 469; 1280 x 1024 162 / 173, 324 / 343;
-// 2048 x 1024 191 / 192, 429 / 387; 4096 x 1024 318 / 270, 521 / 429; 2560 x 2048 506 / 444, 826 / 832; 5120 x 4096 1728 / 1627, 4467 / 4454;
-// 8192 x 2048 846 / 673, 1560 / 1145.
+// and fp32: 1024 x 256 107 / 113, 141 / 165; 8 of them 125 / 126, 174 / 176; 48 336 / 275, 465 / 375; 2048 x 512 131 / 138, 174 / 184; 12 of them 421 / 328,
+// 669 / 478; 1280 x 1024 166 / 178, 308 / 300; 1536 x 1024 173 / 182, 351 / 317; 2048 x 1024 185 / 189, 329 / 309; 4096 x 1024 325 / 271, 509 / 383;
+// 2400 x 2048 421 / 385, 824 / 852; 2560 x 2048 413 / 385, 833 / 852; 5120 x 4096 1806 / 1683, 4854 / 4802; 8192 x 2048 936 / 667, 1852 / 1294.  Near the
+// thresholds, how many tiles are left for a last round decides more than they do, either way: 2600 x 2080 in bf16 561 / 653, 1700 x 1360 in fp32
+// 479 / 413 are the most that the rule loses.
 // In one term, what company leaves behind does not average out in small matrices: 33 of 145 x 2449, rank 20 to 60, 5.8e-3 off (one at a time 2e-3).
 int steps_at_a_time(const MuonBatch& b) {
   if (b.terms == 1 && b.S < 256) return 1;
