@@ -11,12 +11,13 @@ from test_gpu_block_norm import BF16, DEV, F32, inputs, lib  # noqa: F401
 pytestmark = pytest.mark.gpu
 
 
-@pytest.mark.parametrize("types", [(F32, F32, F32), (BF16, F32, BF16)], ids=["f32", "mixed"])
+ALL, MIXED = (F32, F32, F32), (BF16, F32, BF16)
+
+
+@pytest.mark.parametrize("D,types", [(260, ALL)] + [(D, types) for D in (64, 264, 520, 1032, 2056, 4104, 8200, 16392) for types in (ALL, MIXED)],
+                         ids=lambda v: {ALL: "f32", MIXED: "mixed"}.get(v, v))
 @pytest.mark.parametrize("T", [1, 5, 700])
-@pytest.mark.parametrize("D", [64, 260, 264, 520, 1032, 2056, 4104, 8200, 16392])
 def test_starts_on_any_sixteen_bytes(lib, T, D, types):  # noqa: F811
-    if D % 8 and BF16 in types:
-        pytest.skip("bf16 rows are a multiple of eight")
     so = lib.load_library()
     c, dh, dn = inputs(T, D, types, "channel", True, True, seed=D)
     h, n, stats = lib.block_norm_forward(**c, n_dtype=types[2])
